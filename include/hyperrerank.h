@@ -400,6 +400,134 @@ int hr_rerank_topk(const float* scores_dev, const int32_t* seg_dev, int32_t n_qu
 int hr_rerank_topk_host(const float* scores_dev, const int32_t* seg_offsets, int32_t n_queries, int32_t max_cands, int32_t k,
                         int32_t* topk_idx_dev, float* topk_scores_dev, void* stream);
 
+/* ---- operators of a layer, for models whose layers the caller runs ----
+ * hr_rerank_score runs the layers of one kind of decoder.  A model with other positions, masks or score functions can still
+ * keep its documents in a pool and run its own projections: these calls give it rotary positions (a pool's K is post-RoPE), the
+ * tables of a batch of pairs, built on the device, and the attention of the pairs' query tokens over their documents' pages.
+ * None of them allocates, waits on the host or keeps anything between calls; all may be recorded into a HIP graph. */
+
+/* Rotary positions.  The leading rotary_dim channels of every head are turned in rotary_dim / 2 pairs: pair i of a token at
+ * position p by the angle p * freqs[i]:  a' = a cos - b sin, b' = b cos + a sin; the other channels stay as they are.
+ *   HR_ROPE_HALF         pair i is channels i and i + rotary_dim / 2 (what hr_rerank_score and hr_doc_prefill apply)
+ *   HR_ROPE_INTERLEAVED  pair i is channels 2 i and 2 i + 1
+ * Frequencies f_i = base^(-2 i / rotary_dim), for contexts longer than the original_len a model was trained on:
+ *   HR_ROPE_SCALE_NONE    f_i
+ *   HR_ROPE_SCALE_LINEAR  f_i / factor
+ *   HR_ROPE_SCALE_BASE    with base * factor^(rotary_dim / (rotary_dim - 2)) in place of base (rotary_dim > 2)
+ *   HR_ROPE_SCALE_BANDS   by the pair's full turns over the original context, n_i = original_len f_i / 2 pi: f_i / factor up to
+ *                         `low` turns, f_i from `high` turns on, between them in proportion to n_i
+ *   HR_ROPE_SCALE_RAMP    in proportion to the index i instead, between the indices (rounded outwards, within the head) at
+ *                         which n_i passes `high` and `low` */
+typedef enum hr_rope_layout { HR_ROPE_HALF = 0, HR_ROPE_INTERLEAVED = 1 } hr_rope_layout;
+typedef enum hr_rope_scale {
+    HR_ROPE_SCALE_NONE = 0, HR_ROPE_SCALE_LINEAR = 1, HR_ROPE_SCALE_BASE = 2, HR_ROPE_SCALE_BANDS = 3, HR_ROPE_SCALE_RAMP = 4
+} hr_rope_scale;
+typedef struct hr_rope_cfg {
+    int32_t head_dim;      /* 2 .. 1024 */
+    int32_t rotary_dim;    /* even, 2 .. min(head_dim, 256) */
+    int32_t layout;        /* hr_rope_layout */
+    int32_t scaling;       /* hr_rope_scale */
+    float amplitude;       /* factor on the rotated channels, positive and finite; 1 unless the scaling wants another */
+    float base;            /* > 1 */
+    float factor;          /* >= 1; read by every scaling but NONE */
+    float original_len;    /* BANDS, RAMP: positive */
+    float low, high;       /* BANDS, RAMP: 0 < low < high */
+} hr_rope_cfg;
+/* The frequencies of cfg in radians per position, freqs_out[rotary_dim / 2] (host).  A caller may pass others of its own to
+ * hr_rope_apply. */
+int hr_rope_frequencies(const hr_rope_cfg* cfg, double* freqs_out);
+
+/* One tensor [n_tokens][n_heads][head_dim]: the channels of a head follow each other, strides are in elements.  out may be
+ * `in` itself (then with the same strides) and must not overlap it otherwise. */
+typedef struct hr_rope_tensor {
+    const void* in;        /* device */
+    void* out;             /* device */
+    int32_t n_heads;
+    int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;
+} hr_rope_tensor;
+/* Rotates up to two tensors (q and k) of n_tokens tokens in one launch.
+ *   freqs          host, [rotary_dim / 2], each in [0, 2 pi)
+ *   dtype          HR_F32 or HR_BF16; angles are reduced in 64 bits, products are fp32, rounded once
+ *   positions_dev  device int32 [n_tokens]; a token with a negative position is left out: its rows of `out` are not written.
+ *                  NULL: token t is at first_position + t % period (period 0: first_position + t), which may not pass 2^31 - 1
+ *   inverse        not 0: by the negative angles (takes the rotation back; amplitude multiplies again)
+ * HR_ERR_INVALID_ARG on null pointers, bad configurations, frequencies or strides; n_tokens = 0 is a no-op. */
+int hr_rope_apply(const hr_rope_cfg* cfg, const double* freqs, int dtype, int64_t n_tokens, const int32_t* positions_dev,
+                  int32_t first_position, int32_t period, const hr_rope_tensor* tensors, int32_t n_tensors, int inverse, void* stream);
+
+/* The documents a batch may ask for, in device memory: document i has doc_lens[i] tokens in the pages
+ * pages[page_cu[i]], pages[page_cu[i] + 1], .. */
+typedef struct hr_doc_list {
+    int32_t n_docs;
+    int32_t n_pages;             /* entries of pages */
+    const int32_t* doc_lens;     /* [n_docs] */
+    const int32_t* page_cu;      /* [n_docs + 1], ascending */
+    const int32_t* pages;        /* [n_pages] */
+} hr_doc_list;
+
+/* What a batch of pairs needs on the device; all arrays are the caller's device memory.  max_tokens: room for the pairs'
+ * query tokens (rows behind the last one belong to nobody). */
+typedef struct hr_pair_tables {
+    int32_t n_pairs, max_tokens, pt_stride;
+    int32_t n_q_heads;      /* of the model, a multiple of the pool's n_kv_heads */
+    int32_t* q_cu;          /* [n_pairs + 1]: pair p has the tokens q_cu[p] .. q_cu[p + 1] - 1 */
+    int32_t* doc_lens;      /* [n_pairs] */
+    int32_t* page_table;    /* [n_pairs][pt_stride]: -1 behind the document's last page */
+    int32_t* tok_pos;       /* [max_tokens]: position doc_lens[p] + i of token i of pair p; -1 behind the last token */
+    int32_t* tok_pair;      /* [max_tokens]: its pair; -1 likewise */
+    int32_t* order;         /* [n_pairs]: the pairs by document (those without one first), in their order among equals */
+    int32_t* report;        /* [4]: tokens, distinct documents (all pairs without one count as one), HR_TABLES_* bits, 0 */
+    void* sched;            /* hr_pair_tables_sched_bytes, 16-byte aligned: the attention's work list (private) */
+    size_t sched_bytes;
+} hr_pair_tables;
+#define HR_TABLES_BAD_DOC 1      /* a document id below -1 or >= n_docs: the pair has no document */
+#define HR_TABLES_BAD_LENGTH 2   /* a negative query length, counted as 0, or one cut because max_tokens was reached */
+#define HR_TABLES_CUT 4          /* a document longer than its entries of the page list or than pt_stride pages: cut to them */
+#define HR_TABLES_BAD_PAGE 8     /* a page id outside the pool: -1 in page_table; such a pair's attention is undefined */
+
+/* Bytes of hr_pair_tables.sched; 0 on invalid arguments. */
+size_t hr_pair_tables_sched_bytes(const hr_pool* pool, int32_t n_pairs, int32_t max_tokens, int32_t n_q_heads);
+/* Fills the tables from pair_doc_dev (device int32 [n_pairs]: a document, -1 for none) and query_lens_dev (device int32
+ * [n_pairs], 0 and more).  Nothing comes back to the host: what is wrong with the contents is mended as the bits above say and
+ * noted in report, and no table leads outside the pool, the page list or max_tokens.  Whether pages hold a document (hr_doc_kv_write)
+ * is not checked.  HR_ERR_INVALID_ARG on null pointers and bad sizes, HR_ERR_WORKSPACE_SMALL for sched_bytes;
+ * n_pairs = 0 is a no-op. */
+int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int32_t* pair_doc_dev, const int32_t* query_lens_dev,
+                         const hr_pair_tables* out, void* stream);
+
+/* Attention of a batch of pairs at one layer.  A query token i of a pair (position D + i behind its document of D tokens) and
+ * query head a have, for every key they see,
+ *   s = scale q . k;  cap > 0: s = cap tanh(s / cap);  slopes: s -= slopes[a] |distance of the positions|
+ * and out = sum softmax(s) v.  Keys are the document's, from the pool, and, with k and v, the pair's own: token j at position
+ * D + j is seen by token i if j <= i (causal) or j < prefix_lens[p] (the first tokens of a query, seen by all of it).  window
+ * w > 0: only keys less than w positions behind the query token.  A row that sees nothing is 0 (and its lse -infinity).  What is
+ * not seen does not count, whatever it holds.
+ * Pairs that share a document share one pass over its pages, whatever their order in the batch.
+ *   dtype         of q, k, v and out: HR_BF16 with 16-bit and fp8 pools, HR_F32 with fp32 pools (HR_ERR_MISMATCH otherwise).
+ *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them),
+ *                 or in fp32 where the head size is neither 64 nor 128; sums and the softmax are fp32
+ *   q, out        device [max_tokens][n_q_heads][head_dim]; k, v: [max_tokens][n_kv_heads][head_dim], both or neither; strides in
+ *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written
+ *   lse           NULL or device fp32 [max_tokens][n_q_heads]: natural logarithm of the row's sum of exp(s)
+ *   slopes        NULL or device fp32 [n_q_heads];  prefix_lens: NULL or device int32 [n_pairs] (cut to the query's length)
+ * tables come from hr_pair_tables_build with the same pool; n_q_heads is theirs. */
+typedef struct hr_attention_args {
+    int32_t dtype, layer;
+    float scale;            /* finite; 0: 1 / sqrt(head_dim) */
+    float cap;              /* 0 (none) or positive and finite */
+    int32_t window;         /* 0 (none) or the number of positions */
+    const void *q, *k, *v;
+    void* out;
+    float* lse;
+    const float* slopes;
+    const int32_t* prefix_lens;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, out_token_stride, out_head_stride;
+} hr_attention_args;
+/* Workspace of one call; may be 0.  It is private to the call until `stream` has drained. */
+size_t hr_pair_attention_workspace_bytes(const hr_pool* pool, const hr_pair_tables* tables);
+int hr_pair_attention(const hr_pool* pool, const hr_pair_tables* tables, const hr_attention_args* args, void* workspace_dev,
+                      size_t workspace_bytes, void* stream);
+
 /* ---- introspection for benchmarks ---- */
 
 /* Per-kernel timing for benchmarks.  While enabled, every kernel launch of a scoring call is

@@ -52,6 +52,34 @@ class hr_range_report(C.Structure):
         return {k: int(getattr(self, k)) for k in ("overflow", "underflow", "nonfinite_inputs", "fp8_nan_codes", "fp8_bad_scales")}
 
 
+class hr_rope_cfg(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32),
+                ("amplitude", C.c_float), ("base", C.c_float), ("factor", C.c_float), ("original_len", C.c_float),
+                ("low", C.c_float), ("high", C.c_float)]
+
+
+class hr_rope_tensor(C.Structure):
+    _fields_ = [("in_", C.c_void_p), ("out", C.c_void_p), ("n_heads", C.c_int32), ("in_token_stride", C.c_int64),
+                ("in_head_stride", C.c_int64), ("out_token_stride", C.c_int64), ("out_head_stride", C.c_int64)]
+
+
+class hr_doc_list(C.Structure):
+    _fields_ = [("n_docs", C.c_int32), ("n_pages", C.c_int32), ("doc_lens", C.c_void_p), ("page_cu", C.c_void_p), ("pages", C.c_void_p)]
+
+
+class hr_pair_tables(C.Structure):
+    _fields_ = [("n_pairs", C.c_int32), ("max_tokens", C.c_int32), ("pt_stride", C.c_int32), ("n_q_heads", C.c_int32),
+                ("q_cu", C.c_void_p), ("doc_lens", C.c_void_p), ("page_table", C.c_void_p), ("tok_pos", C.c_void_p),
+                ("tok_pair", C.c_void_p), ("order", C.c_void_p), ("report", C.c_void_p), ("sched", C.c_void_p), ("sched_bytes", C.c_size_t)]
+
+
+class hr_attention_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("layer", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("window", C.c_int32),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("slopes", C.c_void_p), ("prefix_lens", C.c_void_p)] + \
+               [(t + s, C.c_int64) for t in ("q", "k", "v", "out") for s in ("_token_stride", "_head_stride")]
+
+
 _PP = C.POINTER(C.c_void_p)
 
 
@@ -70,6 +98,7 @@ EXPORTS = [
     "hr_rerank_plan_destroy", "hr_model_set_precise_layers", "hr_model_precise_layers", "hr_rerank_set_streams", "hr_rerank_parts", "hr_rerank_validate",
     "hr_rerank_full_workspace_bytes", "hr_rerank_score_full", "hr_doc_prefill_workspace_bytes", "hr_doc_prefill", "hr_attention_path", "hr_gemm_path",
     "hr_rerank_topk", "hr_rerank_topk_host", "hr_model_range_report", "hr_kv_pool_range_report", "hr_probe_read_bandwidth", "hr_profile_enable", "hr_profile_select", "hr_profile_count", "hr_profile_name", "hr_profile_read",
+    "hr_rope_frequencies", "hr_rope_apply", "hr_pair_tables_sched_bytes", "hr_pair_tables_build", "hr_pair_attention_workspace_bytes", "hr_pair_attention",
 ]
 
 
@@ -140,6 +169,13 @@ def _load() -> C.CDLL:
         "hr_profile_count": (C.c_int, []),
         "hr_profile_name": (C.c_char_p, [C.c_int]),
         "hr_profile_read": (C.c_int, [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
+        "hr_rope_frequencies": (C.c_int, [C.POINTER(hr_rope_cfg), C.c_void_p]),
+        "hr_rope_apply": (C.c_int, [C.POINTER(hr_rope_cfg), C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int32, C.c_int32,
+                                    C.POINTER(hr_rope_tensor), C.c_int32, C.c_int, C.c_void_p]),
+        "hr_pair_tables_sched_bytes": (C.c_size_t, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32]),
+        "hr_pair_tables_build": (C.c_int, [C.c_void_p, C.POINTER(hr_doc_list), C.c_void_p, C.c_void_p, C.POINTER(hr_pair_tables), C.c_void_p]),
+        "hr_pair_attention_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(hr_pair_tables)]),
+        "hr_pair_attention": (C.c_int, [C.c_void_p, C.POINTER(hr_pair_tables), C.POINTER(hr_attention_args), C.c_void_p, C.c_size_t, C.c_void_p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -350,6 +386,194 @@ class KVPool:
             self.close()
         except Exception:
             pass
+
+
+# ----------------------------------------------------------------------------------------------
+# operators for models whose layers the caller runs
+# ----------------------------------------------------------------------------------------------
+ROPE_LAYOUT = {"half": 0, "interleaved": 1}
+ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
+TABLES_BAD_DOC, TABLES_BAD_LENGTH, TABLES_CUT, TABLES_BAD_PAGE = 1, 2, 4, 8
+_ACT_CODE: Dict[str, int] = {"torch.float32": HR_F32, "torch.bfloat16": HR_BF16}
+
+
+def _refuse(what: str):
+    raise HrError(HR_ERR_INVALID_ARG, what)
+
+
+def _rows(t, heads: Optional[int], d: int, device, dtype, what: str):
+    """Checks a tensor [tokens][heads][head_dim] whose channels follow each other."""
+    if t.dim() != 3 or t.shape[2] != d or (heads is not None and t.shape[1] != heads) or (d > 1 and t.numel() > 0 and t.stride(2) != 1):
+        _refuse(f"{what}: [tokens][{heads if heads is not None else 'heads'}][{d}] with adjacent channels expected, got {tuple(t.shape)}")
+    if t.device != device or t.dtype != dtype:
+        _refuse(f"{what}: a {dtype} tensor on {device} expected, got {t.dtype} on {t.device}")
+    return t
+
+
+def _ints(t, n: int, device, what: str):
+    import torch
+    if t.dtype != torch.int32 or t.device != device or t.numel() < n or not t.is_contiguous():
+        _refuse(f"{what}: {n} contiguous int32 on {device} expected, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+class _Current:
+    """The device that a call's tensors live on, made current for the call where it is not."""
+
+    def __init__(self, device):
+        import torch
+        self.guard = None
+        if device.type != "cuda":
+            _refuse(f"device tensors expected, got {device}")
+        if torch._C._cuda_getDevice() != device.index:
+            self.guard = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *e):
+        if self.guard is not None:
+            self.guard.__exit__(*e)
+
+
+class Rope:
+    """Rotary positions (hr_rope_apply).  rotary_dim: leading channels that are turned (None: all); scaling, factor, original_len,
+    low, high: see hr_rope_cfg; amplitude None: 1, and for "ramp" 0.1 ln(factor) + 1.  freqs: rotary_dim / 2 frequencies of the
+    caller's own, in radians per position, instead of those."""
+
+    def __init__(self, head_dim: int, base: float = 10000.0, rotary_dim: Optional[int] = None, layout: str = "half", scaling: str = "none",
+                 factor: float = 1.0, original_len: float = 0.0, low: float = 1.0, high: float = 4.0, amplitude: Optional[float] = None, freqs=None):
+        if layout not in ROPE_LAYOUT or scaling not in ROPE_SCALING:
+            _refuse(f"Rope: layout one of {sorted(ROPE_LAYOUT)}, scaling one of {sorted(ROPE_SCALING)}")
+        if amplitude is None:
+            amplitude = 0.1 * float(np.log(factor)) + 1.0 if scaling == "ramp" and factor >= 1.0 else 1.0
+        r = head_dim if rotary_dim is None else rotary_dim
+        self.cfg = hr_rope_cfg(head_dim, r, ROPE_LAYOUT[layout], ROPE_SCALING[scaling], amplitude, base, factor, original_len, low, high)
+        if freqs is None:
+            self.freqs = np.zeros(max(r // 2, 1), np.float64)
+            check(lib.hr_rope_frequencies(C.byref(self.cfg), self.freqs.ctypes.data), "hr_rope_frequencies")
+        else:
+            self.freqs = np.ascontiguousarray(freqs, np.float64)
+            if self.freqs.shape != (r // 2,):
+                _refuse(f"Rope: {r // 2} frequencies expected, got {self.freqs.shape}")
+        self._freqs = self.freqs.ctypes.data
+
+    def apply(self, positions, *tensors, out=None, period: int = 0, inverse: bool = False, stream=None):
+        """Turns one or two tensors [tokens][heads][head_dim] (bf16 or fp32; views with any token and head stride).  positions: int32
+        tensor [tokens] (tokens with a negative one are left out), or an int: token t is at positions + t % period (period 0: + t).
+        out: as many tensors, which may be `tensors` themselves (None: new ones).  Returns the list of outputs."""
+        import torch
+        d = self.cfg.head_dim
+        if not 1 <= len(tensors) <= 2:
+            _refuse("Rope.apply: one or two tensors")
+        x0 = tensors[0]
+        code, T, dev = _ACT_CODE.get(str(x0.dtype)), x0.shape[0] if x0.dim() == 3 else -1, x0.device
+        if code is None:
+            _refuse(f"Rope.apply: float32 or bfloat16, got {x0.dtype}")
+        with _Current(dev):
+            ptr = None
+            if not isinstance(positions, int):
+                ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
+            if out is None:
+                with torch.cuda.stream(stream):          # new tensors belong to the stream that writes them (None: the current one)
+                    out = [torch.empty(x.shape, dtype=x.dtype, device=dev) for x in tensors]
+            elif len(out) != len(tensors):
+                _refuse("Rope.apply: as many outputs as tensors")
+            sides = (hr_rope_tensor * len(tensors))()
+            for side, x, y in zip(sides, tensors, out):
+                _rows(x, None, d, dev, x0.dtype, "Rope.apply: input")
+                _rows(y, x.shape[1], d, dev, x0.dtype, "Rope.apply: output")
+                if x.shape[0] != T or y.shape[0] != T:
+                    _refuse("Rope.apply: as many tokens everywhere")
+                side.in_, side.out, side.n_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
+                side.in_token_stride, side.in_head_stride, _ = x.stride()
+                side.out_token_stride, side.out_head_stride, _ = y.stride()
+            if T > 0:
+                check(lib.hr_rope_apply(C.byref(self.cfg), self._freqs, code, T, ptr, positions, period, sides, len(tensors),
+                                        1 if inverse else 0, _stream_ptr(stream)), "hr_rope_apply")
+        return list(out)
+
+
+class DocList:
+    """The documents a batch may ask for: int32 device tensors doc_lens [n], page_cu [n + 1] and the page ids it points into."""
+
+    def __init__(self, doc_lens, page_cu, pages):
+        dev = doc_lens.device
+        n = doc_lens.numel()
+        self.tensors = (doc_lens, page_cu, pages)
+        self.device = dev
+        self.c = hr_doc_list(n, pages.numel(), _ints(doc_lens, n, dev, "DocList: doc_lens"), _ints(page_cu, n + 1, dev, "DocList: page_cu"),
+                             _ints(pages, 0, dev, "DocList: pages"))
+
+
+class PairTables:
+    """Device tables of a batch of n_pairs pairs with room for max_tokens query tokens and pt_stride pages a document (hr_pair_tables).
+    build() fills q_cu, doc_lens, page_table, tok_pos, tok_pair, order and report; n_q_heads is that of the attention that will read them."""
+
+    def __init__(self, pool: KVPool, n_pairs: int, max_tokens: int, pt_stride: int, n_q_heads: int):
+        import torch
+        self.pool, self.n_pairs, self.max_tokens, self.n_q_heads = pool, n_pairs, max_tokens, n_q_heads
+        self.device = pool.mem.device
+        nbytes = int(lib.hr_pair_tables_sched_bytes(pool.handle, n_pairs, max_tokens, n_q_heads))
+        if nbytes == 0 or pt_stride < 0:
+            raise HrError(HR_ERR_INVALID_ARG, "hr_pair_tables_sched_bytes")
+        with _Current(self.device):
+            new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=self.device)      # noqa: E731
+            self.q_cu, self.doc_lens, self.page_table = new(n_pairs + 1), new(n_pairs), new(n_pairs, pt_stride)
+            self.tok_pos, self.tok_pair, self.order, self.report = new(max_tokens), new(max_tokens), new(n_pairs), new(4)
+            self.sched = new(nbytes // 4)
+        self.c = hr_pair_tables(n_pairs, max_tokens, pt_stride, n_q_heads, *[t.data_ptr() for t in (
+            self.q_cu, self.doc_lens, self.page_table, self.tok_pos, self.tok_pair, self.order, self.report, self.sched)], nbytes)
+        self.workspace_bytes = int(lib.hr_pair_attention_workspace_bytes(pool.handle, C.byref(self.c)))
+
+    def build(self, docs: DocList, pair_doc, query_lens, stream=None) -> "PairTables":
+        """pair_doc, query_lens: int32 device tensors [n_pairs]; a pair without a document has -1."""
+        n, dev = self.n_pairs, self.device
+        if docs.device != dev:
+            _refuse(f"PairTables.build: documents on {dev} expected, got {docs.device}")
+        with _Current(dev):
+            check(lib.hr_pair_tables_build(self.pool.handle, C.byref(docs.c), _ints(pair_doc, n, dev, "PairTables.build: pair_doc"),
+                                           _ints(query_lens, n, dev, "PairTables.build: query_lens"), C.byref(self.c), _stream_ptr(stream)),
+                  "hr_pair_tables_build")
+        return self
+
+
+def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=None, out=None, scale: Optional[float] = None, cap: float = 0.0,
+                   slopes=None, window: int = 0, prefix_lens=None, with_lse: bool = False, stream=None):
+    """Attention of the pairs' query tokens over their documents' pages and, with k and v, their own keys (hr_pair_attention).
+    q [max_tokens][n_q_heads][d], k and v [max_tokens][n_kv_heads][d]: bf16 (16-bit and fp8 pools) or fp32 (fp32 pools), views with any
+    token and head stride; slopes: fp32 [n_q_heads]; prefix_lens: int32 [n_pairs].  Returns out (rows behind the last token are left as they
+    are, in a new tensor unset), with_lse: and the rows' log-sums [max_tokens][n_q_heads]."""
+    import torch
+    dev, n_q, T = tables.device, tables.n_q_heads, tables.max_tokens
+    _, n_kv, d = pool._dims
+    if pool.mem.device != dev:
+        _refuse("pair_attention: pool and tables on one device")
+    code = _ACT_CODE.get(str(q.dtype))
+    if code is None or (k is None) != (v is None):
+        _refuse("pair_attention: float32 or bfloat16, and both of k and v or neither")
+    with _Current(dev):
+        for name, t, heads in (("q", q, n_q), ("k", k, n_kv), ("v", v, n_kv), ("out", out, n_q)):
+            if t is not None and _rows(t, heads, d, dev, q.dtype, "pair_attention: " + name).shape[0] < T:
+                _refuse(f"pair_attention: {T} rows of {name} expected, got {t.shape[0]}")
+        if slopes is not None and (slopes.dtype != torch.float32 or slopes.device != dev or slopes.numel() != n_q or not slopes.is_contiguous()):
+            _refuse(f"pair_attention: slopes: {n_q} contiguous float32 on {dev} expected")
+        prefix = None if prefix_lens is None else _ints(prefix_lens, tables.n_pairs, dev, "pair_attention: prefix_lens")
+        with torch.cuda.stream(stream):                  # new tensors belong to the stream that writes them (None: the current one)
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            lse = torch.empty((T, n_q), dtype=torch.float32, device=dev) if with_lse else None
+            ws = torch.empty(tables.workspace_bytes, dtype=torch.uint8, device=dev) if tables.workspace_bytes else None
+        ks, vs = (k.stride(), v.stride()) if k is not None else ((0, 0), (0, 0))
+        qs, os_ = q.stride(), out.stride()
+        args = hr_attention_args(code, layer, 0.0 if scale is None else scale, cap, window, q.data_ptr(), None if k is None else k.data_ptr(),
+                                 None if v is None else v.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                 None if slopes is None else slopes.data_ptr(), prefix, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1])
+        if T > 0:
+            check(lib.hr_pair_attention(pool.handle, C.byref(tables.c), C.byref(args), None if ws is None else ws.data_ptr(),
+                                        tables.workspace_bytes, _stream_ptr(stream)), "hr_pair_attention")
+    return (out, lse) if with_lse else out
 
 
 _LAYER_KINDS = ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "norm1", "norm2")

@@ -76,9 +76,13 @@ constexpr size_t kSplitSlackBytes = (size_t)1 << 20;   // what two carvings of a
 
 thread_local char g_last_error[256] = "";
 
-void note_hip_error(hipError_t e, const char* what) {
+}  // namespace
+
+void hr::note_hip_error(hipError_t e, const char* what) {
     snprintf(g_last_error, sizeof(g_last_error), "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 #define HR_HIP(expr)                                   \
     do {                                               \

@@ -8,6 +8,8 @@
 
 namespace hr {
 
+void note_hip_error(hipError_t e, const char* what);      // the text behind HR_ERR_DEVICE (hr_last_error)
+
 // Per-layer view of the document-KV pool handed to attention kernels.
 struct PoolView {
     const char* data;      // pool base
@@ -189,6 +191,12 @@ hipError_t launch_segment_topk(const float* scores, const int32_t* seg, int n_se
 // the same with the offsets in host memory (they travel as kernel arguments)
 hipError_t launch_segment_topk_host(const float* scores, const int32_t* seg_host, int n_seg, int max_cands, int k, int32_t* idx,
                                     float* out_scores, hipStream_t st);
+// ---- operators for models whose layers the caller runs (hr_rope.hip, hr_tables.hip, hr_pair_attn*.hip); arguments have been checked
+hipError_t launch_rope_apply(const hr_rope_cfg& c, const double* freqs, int dtype, int64_t n_tokens, const int32_t* positions, int32_t first,
+                             int32_t period, const hr_rope_tensor* tensors, int32_t n_tensors, bool inverse, hipStream_t st);
+hipError_t launch_pair_tables(const hr_pool* pool, const hr_doc_list* docs, const int32_t* pair_doc, const int32_t* query_lens,
+                              const hr_pair_tables* t, hipStream_t st);
+hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* g, void* workspace, hipStream_t st);
 // copy whole pages (all kv heads) from the new-KV page buffer to pool pages of one layer:
 // pool page dst_table[i] <- new page src_first[doc(i)] + i  (16-bit pools: same arrangement on both sides)
 hipError_t launch_pages_to_pool(const char* kv_new, char* pool_layer_base, const int32_t* src_page, const int32_t* dst_page,

@@ -1,0 +1,61 @@
+// The operators for models whose layers the caller runs (hr_rope_apply, hr_pair_tables_build, hr_pair_attention): what their host
+// and device parts share.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include "hr_internal.h"
+#include "hr_layout.h"
+
+namespace hr {
+
+// ---- rotary positions
+constexpr int kMaxRotaryPairs = 128;
+int rope_check(const hr_rope_cfg* c);
+int rope_apply_check(const hr_rope_cfg* c, const double* freqs, int dtype, int64_t n_tokens, const int32_t* positions, int32_t first_position,
+                     int32_t period, const hr_rope_tensor* tensors, int32_t n_tensors);
+
+// How a wavefront's lanes are spread over a token's heads: a lane has `vec` pairs (or, behind the rotated channels, as many others as one of its
+// loads brings) of one head, `chunks` lanes have a head, `heads` heads and `tokens` tokens are taken at a time.
+struct RopeShape { int vec, chunks, heads, tokens; };
+RopeShape rope_shape(int head_dim, int rotary_dim, int layout, int esz, bool in_place, int n_heads);
+
+// ---- tables of a batch of pairs
+// The attention's work list, in int32 units from hr_pair_tables.sched.  "In order": the pairs by document, token behind token.
+// A group is the pairs of one document; its rows for a kv head are (token in order, query head of the group of heads), heads fastest.
+struct SchedLayout {
+    int64_t hdr = 0;           // SchedHdr
+    int64_t ord_first = 0;     // [n_pairs] place in order of a pair's first token
+    int64_t grp_pair = 0;      // [n_pairs + 1] a group's first place in `order`
+    int64_t grp_tok = 0;       // [n_pairs + 1] its first token's place
+    int64_t blk_cu = 0;        // [n_pairs + 1] blocks of kPairBlkRows rows before a group
+    int64_t tile_cu = 0;       // [n_pairs + 1] ... of kPairTileRows rows
+    int64_t key[2] = {0, 0}, idx = 0;      // [n_pairs] each: the sort
+    int64_t ord = 0;           // [max_tokens] int4: token's row, place of its pair's first token, pair, document length
+    int64_t blk = 0, tile = 0; // records of 8: a pair of the group, document length, group's first place, first row, rows of the group
+    int64_t total = 0;
+    int64_t cap_blk = 0, cap_tile = 0;
+};
+enum SchedHdr { SH_TOKENS = 0, SH_GROUPS = 1, SH_BLOCKS = 2, SH_TILES = 3 };
+constexpr int kPairBlkRows = 32, kPairTileRows = 128;
+constexpr int kSchedRec = 8;
+SchedLayout make_sched_layout(int64_t n_pairs, int64_t max_tokens, int g);
+int tables_check(const hr_pool* pool, const hr_pair_tables* t);       // sizes and pointers that building and reading have in common
+int tables_build_check(const hr_pool* pool, const hr_doc_list* docs, const int32_t* pair_doc, const int32_t* query_lens, const hr_pair_tables* t);
+
+// ---- attention
+int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* a);
+// Few rows and long documents: an item's keys are cut into up to `most` pieces, each a workgroup's, whose results are joined by a second
+// launch.  How many is decided on the device, which knows the items (pair_splits); `most` bounds grid and workspace.
+constexpr int kPairSplitMost = 64, kPairSplitKeys = 512;      // a piece has this many keys at least
+int pair_most_splits(int64_t max_tokens, int n_q, int n_kv, int64_t pt_stride);
+constexpr int kPairSplitWgs = 512;                            // workgroups that a launch wants
+HR_HD int pair_splits(int items, int most) {
+    const int s = kPairSplitWgs / (items > 0 ? items : 1);
+    return s < 1 ? 1 : s > most ? most : s;
+}
+struct PairWorkspace { size_t ml = 0, o = 0, total = 0; int most = 1; };
+PairWorkspace make_pair_workspace(int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
+
+}  // namespace hr

@@ -1,0 +1,138 @@
+// Device pieces that the kernels of hr_pair_attention share: their parameters, a block's rows and what they see, scores, softmax.
+//
+// A block is 32 rows of a group (the pairs of one document): (token in order, query head of the kv head's group of heads), heads fastest, so that
+// the rows of several short queries share a block.  Scores are computed transposed, S^T = K Q^T, in sub-tiles of 32 keys: lane l
+// of a wavefront owns row l & 31 and the keys 8 (r >> 2) + 4 (l >> 5) + (r & 3), r < 16, of a sub-tile; P is then in operand order for
+// O^T += V^T P^T, of which the lane holds channels 8 (r >> 2) + 4 (l >> 5) + (r & 3) of every 32.
+// What a row sees is two intervals: document keys [dlo, D) and, numbered by their place in order, own keys [olo, ohi).  So a mask is two
+// comparisons, and a sub-tile that all rows see whole needs none.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "hr_attn_common.h"
+#include "hr_device_types.h"
+#include "hr_pair.h"
+
+namespace hr {
+
+struct PairAttnArgs {
+    // what finds a workgroup's rows comes first: those words are in scalar registers when a wavefront starts
+    const int32_t* hdr;
+    const int4* rec;                  // records of the work list, two int4 each
+    const int4* ord;
+    const int32_t* page_table;
+    int32_t pt_stride, n_kv, g, most_splits;
+    int32_t num_pages, d, window, own_keys;
+    const int32_t *q_cu, *prefix;
+    const char* pool;                 // page 0 of the layer
+    const float* scales;              // fp8: of page 0 of the layer
+    const void *q, *k, *v;
+    void* out;
+    float* lse;
+    const float* slopes;
+    int64_t q_ts, q_hs, k_ts, k_hs, v_ts, v_hs, o_ts, o_hs;
+    float scale_log2;                 // scale times log2 e: scores are in log2 units
+    float cap_log2, cap_in;           // cap: s = cap_log2 tanh(s), where s is the scaled score times cap_in; 0: none
+    float* part_o;                    // pieces: [piece][token row][query head][d], unscaled
+    float2* part_ml;                  // ... and maximum and sum
+    int64_t part_rows;                // rows of a piece
+};
+
+constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ int rows_min(int v) {          // over the 32 rows of a wavefront
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int rows_max(int v) { return -rows_min(-v); }
+
+// Consecutive workgroups go to the 8 XCDs in turn: XCD x takes the x-th eighth of the items, so that the blocks and kv heads of a group, which
+// share pages, meet in one L2.
+__device__ __forceinline__ int item_of(int wg, int items) {
+    const int per = (items + 7) / 8, at = (wg & 7) * per + (wg >> 3);
+    return (wg >> 3) < per && at < items ? at : -1;
+}
+
+// A lane's row
+struct PairRow {
+    int token, head;                  // row of q, query head within the kv head's group
+    int place, start;                 // of its token and of its pair's first token, in order
+    int pos;                          // D + index within the query
+    int dlo, olo, ohi;                // see above
+    bool on;                          // the row exists (the others repeat the last one)
+    float slope;                      // slopes[a] log2 e, or 0
+};
+
+__device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, int4 rec, int rows, int row) {
+    PairRow r;
+    r.on = row < rows;
+    const int rc = min(row, rows - 1), t = rc / a.g;
+    r.head = rc - t * a.g;
+    r.place = rec.z + t;
+    const int4 o = a.ord[r.place];    // token row, start, pair, D
+    r.token = o.x;
+    r.start = o.y;
+    const int i = r.place - r.start;
+    r.pos = rec.y + i;
+    const int first = a.window > 0 ? r.pos - a.window + 1 : 0;      // the first position the row sees
+    r.dlo = min(max(first, 0), rec.y);
+    int all = 0;
+    if (a.prefix) all = min(max(a.prefix[o.z], 0), a.q_cu[o.z + 1] - a.q_cu[o.z]);
+    r.olo = r.start + min(max(first - rec.y, 0), i);
+    r.ohi = r.start + max(i + 1, all);
+    r.slope = a.slopes ? a.slopes[h * a.g + r.head] * kLog2e : 0.0f;
+    return r;
+}
+
+// The scaled scores of a sub-tile in log2 units: cap, then distance.  first: position (document) or place (own) of its first key as seen from
+// the row, i.e. minus the row's own
+__device__ __forceinline__ void pair_scores(floatx16& s, const PairAttnArgs& a, const PairRow& row, int first, int hh) {
+    if (a.cap_in != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            // tanh x = 1 - 2 / (e^2x + 1); 2 log2 e is in cap_in
+            const float e = __builtin_amdgcn_exp2f(s[r] * a.cap_in);
+            s[r] = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap_log2);
+        }
+    }
+    if (a.slopes) {
+        const float f = (float)(first + 4 * hh);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(-row.slope, fabsf(f + (float)(8 * (r >> 2) + (r & 3))), s[r]);
+    }
+}
+
+// Running softmax of a row over its keys (both lanes of the row hold the same)
+struct PairSoftmax {
+    float m = -INFINITY, l = 0.0f;    // maximum (log2 units), this lane's share of the sum
+};
+
+// s -> probabilities against the running maximum; the factor on what has been summed so far
+__device__ __forceinline__ float pair_softmax(PairSoftmax& sm, floatx16& s) {
+    float mx = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    mx = row_max2(mx);
+    // the maximum follows only scores that exceed it by kLazyMax: see hr_attn_mfma.hip
+    const float cand = fmaxf(sm.m, mx);
+    const bool move = cand > sm.m + kLazyMax;
+    const float m = move ? cand : sm.m;
+    const float alpha = !move ? 1.0f : sm.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm.m - m);
+    const float use = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        s[r] = __builtin_amdgcn_exp2f(s[r] - use);
+        sum += s[r];
+    }
+    sm.l = fmaf(sm.l, alpha, sum);
+    sm.m = m;
+    return alpha;
+}
+
+// Joins a row's pieces: what the results of one with maximum m count for under the common maximum
+__device__ __forceinline__ float piece_factor(float m, float all) { return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - all); }
+
+}  // namespace hr

@@ -1,0 +1,343 @@
+// hr_pair_attention in fp32 arithmetic: fp32 pools, and 16-bit and fp8 pools whose head size the half kernels do not take; and the join of
+// the pieces that long documents are cut into.
+//
+// A workgroup takes one block of 32 rows of one kv head, its four wavefronts every fourth sub-tile of 32 keys, each with a softmax of its own;
+// they are joined through LDS in a fixed order.  K, V and the rows go from memory straight into the operands of the fp32 matrix instruction (a page
+// holds them as a lane wants them: 8 channels of a key, 8 keys of a channel).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "hr_kernels.h"
+#include "hr_pair_attn.h"
+
+namespace hr {
+
+namespace {
+
+constexpr int kWaves = 4;
+
+typedef __attribute__((ext_vector_type(8))) float floatx8;
+
+template <typename T>
+__device__ __forceinline__ floatx8 load8(const T* p) {
+    const Loose<T, 8> x = *(const Loose<T, 8>*)p;
+    floatx8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = to_float<T>(x.w[e]);
+    return r;
+}
+template <>
+__device__ __forceinline__ floatx8 load8<uint8_t>(const uint8_t* p) {
+    const uint2 x = *(const uint2*)p;
+    floatx8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = e4m3_to_float((uint8_t)((e < 4 ? x.x : x.y) >> (8 * (e & 3))));
+    return r;
+}
+
+template <int MB, typename PT, typename QT>
+__global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs a) {
+    constexpr bool FP8 = sizeof(PT) == 1;
+    extern __shared__ __attribute__((aligned(16))) float smem[];
+    const int items = a.hdr[SH_BLOCKS] * a.n_kv;
+    const int item = item_of((int)blockIdx.x, items);
+    const int pieces = pair_splits(items, a.most_splits);
+    if (item < 0 || (int)blockIdx.y >= pieces) return;
+    const int blk = item / a.n_kv, h = item - blk * a.n_kv;
+    const int4 rec = a.rec[2 * blk];
+    const int rows = a.rec[2 * blk + 1].x, D = rec.y, d = a.d;
+    const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const PairRow row = pair_row(a, h, rec, rows, rec.w + ln);
+    const int32_t* pt = a.page_table + (int64_t)rec.x * a.pt_stride;
+    const int block = kPageTokens * d;                                  // elements of a K or V block
+    const PT* pool = (const PT*)a.pool + (int64_t)h * 2 * block;
+    const int64_t page_stride = (int64_t)a.n_kv * 2 * block;
+    const QT *kn = (const QT*)a.k + h * a.k_hs, *vn = (const QT*)a.v + h * a.v_hs;
+
+    // the sub-tiles that some row of the block sees, and this piece's share of them
+    const int dlo = rows_min(row.dlo), dlo_all = rows_max(row.dlo), olo = rows_min(row.olo), ohi = rows_max(row.ohi);
+    const int doc0 = dlo / 32, n_doc = max((D + 31) / 32 - doc0, 0), n_own = a.own_keys ? (ohi - olo + 31) / 32 : 0;
+    const int n_sub = n_doc + n_own, share = (n_sub + pieces - 1) / pieces;
+    const int j0 = (int)blockIdx.y * share, j1 = min(j0 + share, n_sub);
+
+    floatx8 qf[2 * MB];                                                 // lane: row ln, channels 16 m + 8 hh ..
+    {
+        const QT* qr = (const QT*)a.q + row.token * a.q_ts + (h * a.g + row.head) * a.q_hs;
+#pragma unroll
+        for (int m = 0; m < 2 * MB; ++m) {
+            if (16 * m < d) qf[m] = load8<QT>(qr + 16 * m + 8 * hh);
+            else qf[m] = floatx8{};
+        }
+    }
+    floatx16 o[MB];
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) o[mb] = floatx16{};
+    PairSoftmax sm;
+
+    for (int j = j0 + wave; j < j1; j += kWaves) {
+        const bool doc = j < n_doc;
+        const int key0 = doc ? (doc0 + j) * 32 : olo + (j - n_doc) * 32;
+        // K: lane = key ln of the sub-tile
+        floatx16 s = {};
+        float ks[2] = {1.0f, 1.0f}, vs[2] = {1.0f, 1.0f};
+        const PT* page[2] = {pool, pool};
+        const QT* kr = kn;
+        if (doc) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int at = min(key0 / kPageTokens + e, (D - 1) / kPageTokens);
+                const int id = min(max(pt[at], 0), a.num_pages - 1);
+                page[e] = pool + id * page_stride;
+                if (FP8) {
+                    const float2 sc = *(const float2*)(a.scales + ((int64_t)id * a.n_kv + h) * 2);
+                    ks[e] = sc.x;
+                    vs[e] = sc.y;
+                }
+            }
+        } else {
+            kr += (int64_t)a.ord[min(key0 + ln, ohi - 1)].x * a.k_ts;
+        }
+        const PT* kp = (ln >> 4) ? page[1] : page[0];
+#pragma unroll
+        for (int m = 0; m < 2 * MB; ++m) {
+            if (16 * m >= d) break;
+            const floatx8 kf = doc ? load8<PT>(kp + k_elem(ln & 15, 16 * m + 8 * hh, d, (int)sizeof(PT))) : load8<QT>(kr + 16 * m + 8 * hh);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[e], qf[m][e], s, 0, 0, 0);
+        }
+        const float c0 = a.scale_log2 * ks[0], c1 = a.scale_log2 * ks[1];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= r < 8 ? c0 : c1;
+        pair_scores(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        const bool whole = doc && key0 >= dlo_all && key0 + 32 <= D;
+        unsigned seen = 0xFFFFu;                                        // of the lane's 16 keys
+        if (!whole) {
+            const int lo = (doc ? row.dlo : row.olo) - key0 - 4 * hh, hi = (doc ? D : row.ohi) - key0 - 4 * hh;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int key = 8 * (r >> 2) + (r & 3);
+                const bool on = key >= lo && key < hi;
+                s[r] = on ? s[r] : -INFINITY;
+                seen = on ? seen : seen & ~(1u << r);
+            }
+        }
+        const float alpha = pair_softmax(sm, s);
+        if (__any(alpha != 1.0f)) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
+        }
+        // V: lane = channel ln of every 32, keys {0..3, 8..11} + 4 hh of a page
+        const int exist = min(doc ? D - key0 : ohi - key0, 32);         // keys of the sub-tile that there are
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            if (32 * mb >= d) break;
+            const int ch = min(32 * mb + ln, d - 1);
+            floatx8 vf[2];
+#pragma unroll
+            for (int e2 = 0; e2 < 2; ++e2) {
+                if (doc) {
+                    vf[e2] = load8<PT>(page[e2] + block + (hh * d + ch) * 8);
+                    if (FP8) vf[e2] *= vs[e2];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int x = min(key0 + 16 * e2 + (e & 3) + 2 * (e & 4) + 4 * hh, ohi - 1);
+                        vf[e2][e] = to_float<QT>(vn[(int64_t)a.ord[x].x * a.v_ts + ch]);
+                    }
+                }
+            }
+            if (whole) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[e >> 3][e & 7], s[e], o[mb], 0, 0, 0);
+                continue;
+            }
+            // Some row does not see some key: that key's V counts for nothing there, whatever it holds, and 0 times infinity is not nothing.
+            // Finite values go through the product; the others are counted where they are seen, as ones.
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int key = 8 * (e >> 2) + (e & 3) + 4 * hh;
+                const float v = key < exist ? vf[e >> 3][e & 7] : 0.0f;
+                vf[e >> 3][e & 7] = v;
+                odd = odd || !(fabsf(v) < INFINITY);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float v = vf[e >> 3][e & 7];
+                o[mb] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(v) < INFINITY ? v : 0.0f, s[e], o[mb], 0, 0, 0);
+            }
+            if (__any(odd)) {
+                floatx16 n[3] = {};                                     // infinities of either sign, NaN
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float v = vf[e >> 3][e & 7], p = seen >> e & 1 ? 1.0f : 0.0f;
+                    n[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v == INFINITY ? 1.0f : 0.0f, p, n[0], 0, 0, 0);
+                    n[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(v == -INFINITY ? 1.0f : 0.0f, p, n[1], 0, 0, 0);
+                    n[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(v != v ? 1.0f : 0.0f, p, n[2], 0, 0, 0);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (n[0][r] > 0.0f) o[mb][r] += INFINITY;
+                    if (n[1][r] > 0.0f) o[mb][r] -= INFINITY;
+                    if (n[2][r] > 0.0f) o[mb][r] += NAN;
+                }
+            }
+        }
+    }
+
+    // join the wavefronts: maxima first, then O rows in LDS, [wave][row][channels and 4 more, so that rows start at other banks]
+    const int ld = MB * 32 + 4;
+    float* ml = smem + kWaves * 32 * ld;                                // [wave][row][maximum, sum]
+    const float l = row_sum2(sm.l);
+    if (hh == 0) {
+        ml[(wave * 32 + ln) * 2] = sm.m;
+        ml[(wave * 32 + ln) * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *(float4*)(smem + (wave * 32 + ln) * ld + mb * 32 + 8 * (r >> 2) + 4 * hh) = make_float4(o[mb][r], o[mb][r + 1], o[mb][r + 2], o[mb][r + 3]);
+    // where the rows go
+    int2* where = (int2*)(ml + kWaves * 32 * 2);
+    if (wave == 0 && hh == 0) where[ln] = make_int2(row.on ? row.token : -1, row.head);
+    __syncthreads();
+    const int piece = d / 4;
+    for (int u = threadIdx.x; u < 32 * piece; u += kWaves * 64) {
+        const int rw = u / piece, c = (u - rw * piece) * 4;
+        const int2 to = where[rw];
+        if (to.x < 0) continue;
+        float m = -INFINITY, sum = 0.0f, f[kWaves];
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[(w * 32 + rw) * 2]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            f[w] = piece_factor(ml[(w * 32 + rw) * 2], m);
+            sum = fmaf(f[w], ml[(w * 32 + rw) * 2 + 1], sum);
+            const float4 x = *(const float4*)(smem + (w * 32 + rw) * ld + c);
+            if (f[w] == 0.0f) continue;                                 // nothing seen there
+            acc.x = fmaf(f[w], x.x, acc.x);
+            acc.y = fmaf(f[w], x.y, acc.y);
+            acc.z = fmaf(f[w], x.z, acc.z);
+            acc.w = fmaf(f[w], x.w, acc.w);
+        }
+        const int head = h * a.g + to.y;
+        if (pieces > 1) {
+            const int64_t at = (int64_t)blockIdx.y * a.part_rows + (int64_t)to.x * a.g * a.n_kv + head;
+            if (c == 0) a.part_ml[at] = make_float2(m, sum);
+            if (m != -INFINITY) *(float4*)(a.part_o + at * d + c) = acc;
+            continue;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        QT* out = (QT*)a.out + to.x * a.o_ts + head * a.o_hs + c;
+        using W = Loose<QT, 4>;
+        W y;
+        y.w[0] = from_float<QT>(acc.x * inv);
+        y.w[1] = from_float<QT>(acc.y * inv);
+        y.w[2] = from_float<QT>(acc.z * inv);
+        y.w[3] = from_float<QT>(acc.w * inv);
+        *(W*)out = y;
+        if (c == 0 && a.lse) a.lse[(int64_t)to.x * a.g * a.n_kv + head] = (m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2);
+    }
+}
+
+// A row's pieces, joined in their order: one wavefront per row
+template <typename QT>
+__global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a, int tile_items) {
+    const int items = a.hdr[tile_items ? SH_TILES : SH_BLOCKS] * a.n_kv, pieces = pair_splits(items, a.most_splits);
+    if (pieces == 1) return;                                            // the rows are there
+    const int n_q = a.g * a.n_kv;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (row >= (int64_t)a.hdr[SH_TOKENS] * n_q) return;
+    const int64_t token = row / n_q;
+    const int head = (int)(row - token * n_q);
+    float2 x = lane < pieces ? a.part_ml[lane * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
+    const float m = wave_max(x.x);
+    const float f = piece_factor(x.x, m), sum = wave_sum(f * x.y);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    for (int c = lane; c < a.d; c += 64) {
+        float acc = 0.0f;
+        for (int p = 0; p < pieces; ++p) {
+            const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), p));
+            if (fp != 0.0f) acc = fmaf(fp, a.part_o[(p * a.part_rows + row) * a.d + c], acc);
+        }
+        ((QT*)a.out)[token * a.o_ts + head * a.o_hs + c] = from_float<QT>(acc * inv);
+    }
+    if (lane == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+template <int MB, typename PT, typename QT>
+hipError_t f32_launch(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
+    const size_t lds = (size_t)kWaves * 32 * (MB * 32 + 4) * sizeof(float) + kWaves * 32 * 2 * sizeof(float) + 32 * sizeof(int2);
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)pair_attn_f32_kernel<MB, PT, QT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    pair_attn_f32_kernel<MB, PT, QT><<<grid, kWaves * 64, lds, st>>>(a);
+    return hipGetLastError();
+}
+template <typename PT, typename QT>
+hipError_t f32_by_size(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
+    if (a.d <= 32) return f32_launch<1, PT, QT>(a, grid, st);
+    if (a.d <= 64) return f32_launch<2, PT, QT>(a, grid, st);
+    if (a.d <= 128) return f32_launch<4, PT, QT>(a, grid, st);
+    return f32_launch<8, PT, QT>(a, grid, st);
+}
+
+}  // namespace
+
+hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, bool tile_items, hipStream_t st) {
+    const unsigned blocks = (unsigned)((max_tokens * a.g * a.n_kv + 3) / 4);
+    if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a, tile_items ? 1 : 0);
+    else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a, tile_items ? 1 : 0);
+    return hipGetLastError();
+}
+
+hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* g, void* workspace, hipStream_t st) {
+    const PoolLayout& lay = pool->lay;
+    const int heads = t->n_q_heads / lay.n_kv;
+    const SchedLayout s = make_sched_layout(t->n_pairs, t->max_tokens, heads);
+    const int32_t* S = (const int32_t*)t->sched;
+    PairAttnArgs a{};
+    a.hdr = S + s.hdr;
+    a.rec = (const int4*)(S + s.blk);
+    a.ord = (const int4*)(S + s.ord);
+    a.page_table = t->page_table;
+    a.pt_stride = t->pt_stride;
+    a.n_kv = lay.n_kv;
+    a.g = heads;
+    a.num_pages = lay.num_pages;
+    a.d = lay.d;
+    a.window = g->window;
+    a.own_keys = g->k != nullptr;
+    a.q_cu = t->q_cu;
+    a.prefix = g->prefix_lens;
+    a.pool = pool->base + (size_t)g->layer * lay.num_pages * lay.n_kv * 2 * lay.block_elems * lay.esz;
+    a.scales = lay.kv_dtype == HR_FP8_E4M3 ? (const float*)(pool->base + lay.data_bytes) + lay.scale_index(g->layer, 0, 0, 0) : nullptr;
+    a.q = g->q; a.k = g->k; a.v = g->v; a.out = g->out; a.lse = g->lse; a.slopes = g->slopes;
+    a.q_ts = g->q_token_stride; a.q_hs = g->q_head_stride; a.k_ts = g->k_token_stride; a.k_hs = g->k_head_stride;
+    a.v_ts = g->v_token_stride; a.v_hs = g->v_head_stride; a.o_ts = g->out_token_stride; a.o_hs = g->out_head_stride;
+    a.scale_log2 = (g->scale != 0.0f ? g->scale : 1.0f / sqrtf((float)lay.d)) * kLog2e;
+    if (g->cap > 0.0f) {
+        a.cap_log2 = g->cap * kLog2e;
+        a.cap_in = 2.0f / g->cap;                        // x = s / (cap log2 e); e^2x = 2^(2 log2 e x) = 2^(2 s / cap)
+    }
+    const PairWorkspace w = make_pair_workspace(t->max_tokens, t->n_q_heads, lay.n_kv, lay.d, t->pt_stride);
+    a.most_splits = w.most;
+    a.part_ml = (float2*)workspace;
+    a.part_o = (float*)((char*)workspace + w.o);
+    a.part_rows = (int64_t)t->max_tokens * t->n_q_heads;
+    const int64_t items = s.cap_blk * lay.n_kv;
+    const dim3 grid((unsigned)((items + 7) / 8 * 8), (unsigned)w.most);
+    hipError_t e;
+    if (lay.kv_dtype == HR_F32) e = f32_by_size<float, float>(a, grid, st);
+    else if (lay.kv_dtype == HR_BF16) e = f32_by_size<half_t, bf16_t>(a, grid, st);
+    else e = f32_by_size<uint8_t, bf16_t>(a, grid, st);
+    if (e != hipSuccess || w.most == 1) return e;
+    return launch_pair_join(g->dtype, a, t->max_tokens, false, st);
+}
+
+}  // namespace hr
