@@ -88,13 +88,28 @@ __device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, int4 r
 
 // The scaled scores of a sub-tile in log2 units: cap, then distance.  first: position (document) or place (own) of its first key as seen from
 // the row, i.e. minus the row's own
+// EXACT (fp32 operands): tanh of small arguments from its series, where the quotient's rounding, 2^-23 of one, is much of the value
+template <bool EXACT>
 __device__ __forceinline__ void pair_scores(floatx16& s, const PairAttnArgs& a, const PairRow& row, int first, int hh) {
     if (a.cap_in != 0.0f) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             // tanh x = 1 - 2 / (e^2x + 1); 2 log2 e is in cap_in
             const float e = __builtin_amdgcn_exp2f(s[r] * a.cap_in);
-            s[r] = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap_log2);
+            const float far = fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(e + 1.0f), a.cap_log2);
+            if constexpr (EXACT) {
+                // x - x^3 / 3 + 2 x^5 / 15 - ..: behind the seventh of these terms 10^-8 of the value is left at 1/2
+                const float x = s[r] * a.cap_in * (0.5f * kLn2), u = x * x;
+                float t = fmaf(u, 1.4558344e-3f, -3.5921280e-3f);
+                t = fmaf(u, t, 8.8632355e-3f);
+                t = fmaf(u, t, -2.1869489e-2f);
+                t = fmaf(u, t, 5.3968254e-2f);
+                t = fmaf(u, t, -1.3333333e-1f);
+                t = fmaf(u, t, 3.3333333e-1f);
+                s[r] = fabsf(x) < 0.5f ? a.cap_log2 * fmaf(-x * u, t, x) : far;
+            } else {
+                s[r] = far;
+            }
         }
     }
     if (a.slopes) {
@@ -134,5 +149,71 @@ __device__ __forceinline__ float pair_softmax(PairSoftmax& sm, floatx16& s) {
 
 // Joins a row's pieces: what the results of one with maximum m count for under the common maximum
 __device__ __forceinline__ float piece_factor(float m, float all) { return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - all); }
+
+// Joins what the NW wavefronts of a workgroup have of a block's rows, in the wavefronts' order, and writes the rows (or, of a call cut into
+// pieces, the piece's).  HD: channels that the accumulators hold, a.d or more.  smem: pair_join_bytes.
+constexpr size_t pair_join_bytes(int nw, int hd) {
+    return (size_t)nw * 32 * (hd + 4) * sizeof(float) + (size_t)nw * 32 * 2 * sizeof(float) + 32 * sizeof(int2);
+}
+template <int NW, int HD, typename QT>
+__device__ __forceinline__ void pair_join_waves(const PairAttnArgs& a, float* smem, const floatx16 (&o)[HD / 32], const PairSoftmax& sm,
+                                                const PairRow& row, int h, int pieces) {
+    constexpr int LD = HD + 4;
+    const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = threadIdx.x >> 6, d = a.d;
+    float* ml = smem + NW * 32 * LD;                                // [wave][row][maximum, sum]
+    const float l = row_sum2(sm.l);
+    if (hh == 0) {
+        ml[(wave * 32 + ln) * 2] = sm.m;
+        ml[(wave * 32 + ln) * 2 + 1] = l;
+    }
+#pragma unroll
+    for (int mb = 0; mb < HD / 32; ++mb)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            *(float4*)(smem + (wave * 32 + ln) * LD + mb * 32 + 8 * (r >> 2) + 4 * hh) = make_float4(o[mb][r], o[mb][r + 1], o[mb][r + 2], o[mb][r + 3]);
+    // where the rows go
+    int2* where = (int2*)(ml + NW * 32 * 2);
+    if (wave == 0 && hh == 0) where[ln] = make_int2(row.on ? row.token : -1, row.head);
+    __syncthreads();
+    const int piece = d / 4;
+    for (int u = threadIdx.x; u < 32 * piece; u += NW * 64) {
+        const int rw = u / piece, c = (u - rw * piece) * 4;
+        const int2 to = where[rw];
+        if (to.x < 0) continue;
+        float m = -INFINITY, sum = 0.0f, f[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[(w * 32 + rw) * 2]);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            f[w] = piece_factor(ml[(w * 32 + rw) * 2], m);
+            sum = fmaf(f[w], ml[(w * 32 + rw) * 2 + 1], sum);
+            const float4 x = *(const float4*)(smem + (w * 32 + rw) * LD + c);
+            if (f[w] == 0.0f) continue;                                 // nothing seen there
+            acc.x = fmaf(f[w], x.x, acc.x);
+            acc.y = fmaf(f[w], x.y, acc.y);
+            acc.z = fmaf(f[w], x.z, acc.z);
+            acc.w = fmaf(f[w], x.w, acc.w);
+        }
+        const int head = h * a.g + to.y;
+        if (pieces > 1) {
+            const int64_t at = (int64_t)blockIdx.y * a.part_rows + (int64_t)to.x * a.g * a.n_kv + head;
+            if (c == 0) a.part_ml[at] = make_float2(m, sum);
+            if (m != -INFINITY) *(float4*)(a.part_o + at * d + c) = acc;
+            continue;
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        QT* out = (QT*)a.out + to.x * a.o_ts + head * a.o_hs + c;
+        using W = Loose<QT, 4>;
+        W y;
+        y.w[0] = from_float<QT>(acc.x * inv);
+        y.w[1] = from_float<QT>(acc.y * inv);
+        y.w[2] = from_float<QT>(acc.z * inv);
+        y.w[3] = from_float<QT>(acc.w * inv);
+        *(W*)out = y;
+        if (c == 0 && a.lse) a.lse[(int64_t)to.x * a.g * a.n_kv + head] = (m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2);
+    }
+}
+
 
 }  // namespace hr

@@ -10,6 +10,7 @@
 
 #include "hr_kernels.h"
 #include "hr_pair_attn.h"
+#include "hr_pair_launch.h"
 
 namespace hr {
 
@@ -109,7 +110,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
         const float c0 = a.scale_log2 * ks[0], c1 = a.scale_log2 * ks[1];
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= r < 8 ? c0 : c1;
-        pair_scores(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        pair_scores<true>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
         const bool whole = doc && key0 >= dlo_all && key0 + 32 <= D;
         unsigned seen = 0xFFFFu;                                        // of the lane's 16 keys
         if (!whole) {
@@ -153,100 +154,43 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
                 continue;
             }
             // Some row does not see some key: that key's V counts for nothing there, whatever it holds, and 0 times infinity is not nothing.
-            // Finite values go through the product; the others are counted where they are seen, as ones.
+            // Values that are not finite are counted where they are seen, as ones, kind by kind; the product has zeros for them.
             bool odd = false;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int key = 8 * (e >> 2) + (e & 3) + 4 * hh;
-                const float v = key < exist ? vf[e >> 3][e & 7] : 0.0f;
+                const float v = 8 * (e >> 2) + (e & 3) + 4 * hh < exist ? vf[e >> 3][e & 7] : 0.0f;
                 vf[e >> 3][e & 7] = v;
                 odd = odd || !(fabsf(v) < INFINITY);
             }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float v = vf[e >> 3][e & 7];
-                o[mb] = __builtin_amdgcn_mfma_f32_32x32x2f32(fabsf(v) < INFINITY ? v : 0.0f, s[e], o[mb], 0, 0, 0);
-            }
             if (__any(odd)) {
-                floatx16 n[3] = {};                                     // infinities of either sign, NaN
+#pragma unroll 1
+                for (int kind = 0; kind < 3; ++kind) {                  // infinities of either sign, NaN
+                    floatx16 n = {};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float v = vf[e >> 3][e & 7], p = seen >> e & 1 ? 1.0f : 0.0f;
-                    n[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(v == INFINITY ? 1.0f : 0.0f, p, n[0], 0, 0, 0);
-                    n[1] = __builtin_amdgcn_mfma_f32_32x32x2f32(v == -INFINITY ? 1.0f : 0.0f, p, n[1], 0, 0, 0);
-                    n[2] = __builtin_amdgcn_mfma_f32_32x32x2f32(v != v ? 1.0f : 0.0f, p, n[2], 0, 0, 0);
+                    for (int e = 0; e < 16; ++e) {
+                        const float v = vf[e >> 3][e & 7];
+                        const bool is = kind == 2 ? v != v : v == (kind == 0 ? INFINITY : -INFINITY);
+                        n = __builtin_amdgcn_mfma_f32_32x32x2f32(is ? 1.0f : 0.0f, seen >> e & 1 ? 1.0f : 0.0f, n, 0, 0, 0);
+                    }
+                    const float add = kind == 2 ? NAN : kind == 0 ? INFINITY : -INFINITY;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[mb][r] += n[r] > 0.0f ? add : 0.0f;
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (n[0][r] > 0.0f) o[mb][r] += INFINITY;
-                    if (n[1][r] > 0.0f) o[mb][r] -= INFINITY;
-                    if (n[2][r] > 0.0f) o[mb][r] += NAN;
-                }
+                for (int e = 0; e < 16; ++e) vf[e >> 3][e & 7] = fabsf(vf[e >> 3][e & 7]) < INFINITY ? vf[e >> 3][e & 7] : 0.0f;
             }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[e >> 3][e & 7], s[e], o[mb], 0, 0, 0);
         }
     }
 
-    // join the wavefronts: maxima first, then O rows in LDS, [wave][row][channels and 4 more, so that rows start at other banks]
-    const int ld = MB * 32 + 4;
-    float* ml = smem + kWaves * 32 * ld;                                // [wave][row][maximum, sum]
-    const float l = row_sum2(sm.l);
-    if (hh == 0) {
-        ml[(wave * 32 + ln) * 2] = sm.m;
-        ml[(wave * 32 + ln) * 2 + 1] = l;
-    }
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-            *(float4*)(smem + (wave * 32 + ln) * ld + mb * 32 + 8 * (r >> 2) + 4 * hh) = make_float4(o[mb][r], o[mb][r + 1], o[mb][r + 2], o[mb][r + 3]);
-    // where the rows go
-    int2* where = (int2*)(ml + kWaves * 32 * 2);
-    if (wave == 0 && hh == 0) where[ln] = make_int2(row.on ? row.token : -1, row.head);
-    __syncthreads();
-    const int piece = d / 4;
-    for (int u = threadIdx.x; u < 32 * piece; u += kWaves * 64) {
-        const int rw = u / piece, c = (u - rw * piece) * 4;
-        const int2 to = where[rw];
-        if (to.x < 0) continue;
-        float m = -INFINITY, sum = 0.0f, f[kWaves];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, ml[(w * 32 + rw) * 2]);
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            f[w] = piece_factor(ml[(w * 32 + rw) * 2], m);
-            sum = fmaf(f[w], ml[(w * 32 + rw) * 2 + 1], sum);
-            const float4 x = *(const float4*)(smem + (w * 32 + rw) * ld + c);
-            if (f[w] == 0.0f) continue;                                 // nothing seen there
-            acc.x = fmaf(f[w], x.x, acc.x);
-            acc.y = fmaf(f[w], x.y, acc.y);
-            acc.z = fmaf(f[w], x.z, acc.z);
-            acc.w = fmaf(f[w], x.w, acc.w);
-        }
-        const int head = h * a.g + to.y;
-        if (pieces > 1) {
-            const int64_t at = (int64_t)blockIdx.y * a.part_rows + (int64_t)to.x * a.g * a.n_kv + head;
-            if (c == 0) a.part_ml[at] = make_float2(m, sum);
-            if (m != -INFINITY) *(float4*)(a.part_o + at * d + c) = acc;
-            continue;
-        }
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        QT* out = (QT*)a.out + to.x * a.o_ts + head * a.o_hs + c;
-        using W = Loose<QT, 4>;
-        W y;
-        y.w[0] = from_float<QT>(acc.x * inv);
-        y.w[1] = from_float<QT>(acc.y * inv);
-        y.w[2] = from_float<QT>(acc.z * inv);
-        y.w[3] = from_float<QT>(acc.w * inv);
-        *(W*)out = y;
-        if (c == 0 && a.lse) a.lse[(int64_t)to.x * a.g * a.n_kv + head] = (m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2);
-    }
+    pair_join_waves<kWaves, MB * 32, QT>(a, smem, o, sm, row, h, pieces);
 }
 
 // A row's pieces, joined in their order: one wavefront per row
 template <typename QT>
-__global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a, int tile_items) {
-    const int items = a.hdr[tile_items ? SH_TILES : SH_BLOCKS] * a.n_kv, pieces = pair_splits(items, a.most_splits);
+__global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
+    const int items = a.hdr[SH_BLOCKS] * a.n_kv, pieces = pair_splits(items, a.most_splits);
     if (pieces == 1) return;                                            // the rows are there
     const int n_q = a.g * a.n_kv;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -271,7 +215,7 @@ __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a, int tile
 
 template <int MB, typename PT, typename QT>
 hipError_t f32_launch(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
-    const size_t lds = (size_t)kWaves * 32 * (MB * 32 + 4) * sizeof(float) + kWaves * 32 * 2 * sizeof(float) + 32 * sizeof(int2);
+    const size_t lds = pair_join_bytes(kWaves, MB * 32);
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute((const void*)pair_attn_f32_kernel<MB, PT, QT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
@@ -289,10 +233,10 @@ hipError_t f32_by_size(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
 
 }  // namespace
 
-hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, bool tile_items, hipStream_t st) {
+static hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, hipStream_t st) {
     const unsigned blocks = (unsigned)((max_tokens * a.g * a.n_kv + 3) / 4);
-    if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a, tile_items ? 1 : 0);
-    else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a, tile_items ? 1 : 0);
+    if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a);
+    else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -333,11 +277,12 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
     const int64_t items = s.cap_blk * lay.n_kv;
     const dim3 grid((unsigned)((items + 7) / 8 * 8), (unsigned)w.most);
     hipError_t e;
-    if (lay.kv_dtype == HR_F32) e = f32_by_size<float, float>(a, grid, st);
+    if (lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 128)) e = launch_pair_rows(lay.kv_dtype == HR_FP8_E4M3, a, grid, st);
+    else if (lay.kv_dtype == HR_F32) e = f32_by_size<float, float>(a, grid, st);
     else if (lay.kv_dtype == HR_BF16) e = f32_by_size<half_t, bf16_t>(a, grid, st);
     else e = f32_by_size<uint8_t, bf16_t>(a, grid, st);
     if (e != hipSuccess || w.most == 1) return e;
-    return launch_pair_join(g->dtype, a, t->max_tokens, false, st);
+    return launch_pair_join(g->dtype, a, t->max_tokens, st);
 }
 
 }  // namespace hr
