@@ -48,14 +48,25 @@ int tables_build_check(const hr_pool* pool, const hr_doc_list* docs, const int32
 int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* a);
 // Few rows and long documents: an item's keys are cut into up to `most` pieces, each a workgroup's, whose results are joined by a second
 // launch.  How many is decided on the device, which knows the items (pair_splits); `most` bounds grid and workspace.
-constexpr int kPairSplitMost = 64, kPairSplitKeys = 512;      // a piece has this many keys at least
-int pair_most_splits(int64_t max_tokens, int n_q, int n_kv, int64_t pt_stride);
+// The join costs about 3 us: 16 blocks of 304 keys 8.5 us whole and 11.5 in two pieces, 16 of 2049 17.9 and 13.7 in eight.
+constexpr int kPairSplitMost = 128, kPairSplitKeys = 256, kPairSplitLeast = 1024;      // keys of a piece, of documents that are cut, at least
+int pair_most_splits(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
 constexpr int kPairSplitWgs = 512;                            // workgroups that a launch wants
-HR_HD int pair_splits(int items, int most) {
-    const int s = kPairSplitWgs / (items > 0 ? items : 1);
-    return s < 1 ? 1 : s > most ? most : s;
+// Whether an attention's work items are blocks of 32 rows, each streaming its keys for itself, or tiles of four, which share a stream (see
+// hr_pair_attn_mfma.hip), and their pieces.  blocks, tiles: of all kv heads.  Tiles read and expand keys once for up to four blocks, blocks fill
+// the chip sooner: tiles pay where they are more than half full and the blocks more than the chip takes at once.  Blocks / tiles, in us: 64 channels,
+// 280 blocks of 544 keys 11.7 / 16.4, 320 of 2064 26.3 / 32.4, 1120 of 544 24.7 / 22.7, 4480 of 544 78 / 50; 128 channels, 128 blocks of 4112 43.5 / 39.4,
+// 288 of 8200 136 / 87, 640 of 288 26.7 / 18.4; one block a tile, 800 of 2049 (fp8) 101 / 190, 3200 of 520 188 / 197.
+HR_HD int pair_tile_blocks(int d) { return d == 64 ? 768 : 256; }
+struct PairChoice { bool tiles; int pieces; };
+HR_HD PairChoice pair_choice(int blocks, int tiles, int d, int most) {
+    PairChoice c;
+    c.tiles = blocks > pair_tile_blocks(d) && 2 * (int64_t)blocks > 3 * (int64_t)tiles;
+    const int items = c.tiles ? tiles : blocks, s = kPairSplitWgs / (items > 0 ? items : 1);
+    c.pieces = s < 1 ? 1 : s > most ? most : s;
+    return c;
 }
 struct PairWorkspace { size_t ml = 0, o = 0, total = 0; int most = 1; };
-PairWorkspace make_pair_workspace(int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
+PairWorkspace make_pair_workspace(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
 
 }  // namespace hr

@@ -19,7 +19,7 @@ namespace hr {
 struct PairAttnArgs {
     // what finds a workgroup's rows comes first: those words are in scalar registers when a wavefront starts
     const int32_t* hdr;
-    const int4* rec;                  // records of the work list, two int4 each
+    const int4 *rec, *rec_tiles;      // records of the work list, two int4 each: blocks, tiles
     const int4* ord;
     const int32_t* page_table;
     int32_t pt_stride, n_kv, g, most_splits;
@@ -37,7 +37,11 @@ struct PairAttnArgs {
     float* part_o;                    // pieces: [piece][token row][query head][d], unscaled
     float2* part_ml;                  // ... and maximum and sum
     int64_t part_rows;                // rows of a piece
+    int32_t blocks_only;              // work items are blocks (kernels that know no tiles)
 };
+
+// Scores need more than a positive factor before they are compared: the kernels' EXTRA form
+inline bool pair_extra(const PairAttnArgs& a) { return a.cap_in != 0.0f || a.slopes || a.scale_log2 < 0.0f; }
 
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
 
@@ -122,6 +126,17 @@ __device__ __forceinline__ void pair_scores(floatx16& s, const PairAttnArgs& a, 
 // Running softmax of a row over its keys (both lanes of the row hold the same)
 struct PairSoftmax {
     float m = -INFINITY, l = 0.0f;    // maximum (log2 units), this lane's share of the sum
+
+    // takes in the row's largest new score; the factor on what has been summed so far.  The maximum follows only scores that exceed it by
+    // kLazyMax: see hr_attn_mfma.hip
+    __device__ __forceinline__ float follow(float mx) {
+        const float cand = fmaxf(m, mx);
+        if (!(cand > m + kLazyMax)) return 1.0f;
+        const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - cand);
+        m = cand;
+        return alpha;
+    }
+    __device__ __forceinline__ float used() const { return m == -INFINITY ? 0.0f : m; }      // a row that has seen nothing keeps p = 0
 };
 
 // s -> probabilities against the running maximum; the factor on what has been summed so far
@@ -129,13 +144,7 @@ __device__ __forceinline__ float pair_softmax(PairSoftmax& sm, floatx16& s) {
     float mx = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-    mx = row_max2(mx);
-    // the maximum follows only scores that exceed it by kLazyMax: see hr_attn_mfma.hip
-    const float cand = fmaxf(sm.m, mx);
-    const bool move = cand > sm.m + kLazyMax;
-    const float m = move ? cand : sm.m;
-    const float alpha = !move ? 1.0f : sm.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm.m - m);
-    const float use = m == -INFINITY ? 0.0f : m;
+    const float alpha = sm.follow(row_max2(mx)), use = sm.used();
     float sum = 0.0f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -143,7 +152,6 @@ __device__ __forceinline__ float pair_softmax(PairSoftmax& sm, floatx16& s) {
         sum += s[r];
     }
     sm.l = fmaf(sm.l, alpha, sum);
-    sm.m = m;
     return alpha;
 }
 

@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
     extern __shared__ __attribute__((aligned(16))) float smem[];
     const int items = a.hdr[SH_BLOCKS] * a.n_kv;
     const int item = item_of((int)blockIdx.x, items);
-    const int pieces = pair_splits(items, a.most_splits);
+    const int pieces = pair_choice(items, items, a.d, a.most_splits).pieces;
     if (item < 0 || (int)blockIdx.y >= pieces) return;
     const int blk = item / a.n_kv, h = item - blk * a.n_kv;
     const int4 rec = a.rec[2 * blk];
@@ -187,30 +187,47 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
     pair_join_waves<kWaves, MB * 32, QT>(a, smem, o, sm, row, h, pieces);
 }
 
-// A row's pieces, joined in their order: one wavefront per row
+// A row's pieces, joined: one workgroup per row, every wavefront a quarter of the pieces, in a fixed order
 template <typename QT>
 __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
-    const int items = a.hdr[SH_BLOCKS] * a.n_kv, pieces = pair_splits(items, a.most_splits);
+    __shared__ float part[4][256], piece_m[kPairSplitMost], piece_l[kPairSplitMost];
+    const int blocks = a.hdr[SH_BLOCKS] * a.n_kv, tiles = a.blocks_only ? blocks : a.hdr[SH_TILES] * a.n_kv;
+    const int pieces = pair_choice(blocks, tiles, a.d, a.most_splits).pieces;
     if (pieces == 1) return;                                            // the rows are there
-    const int n_q = a.g * a.n_kv;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
+    const int n_q = a.g * a.n_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = blockIdx.x;
     if (row >= (int64_t)a.hdr[SH_TOKENS] * n_q) return;
+    if (threadIdx.x < kPairSplitMost) {
+        const float2 x = (int)threadIdx.x < pieces ? a.part_ml[threadIdx.x * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
+        piece_m[threadIdx.x] = x.x;
+        piece_l[threadIdx.x] = x.y;
+    }
+    __syncthreads();
+    static_assert(kPairSplitMost == 128, "two pieces a lane");
+    const float m0 = piece_m[lane], m1 = piece_m[lane + 64], m = wave_max(fmaxf(m0, m1));
+    const float sum = wave_sum(fmaf(piece_factor(m0, m), piece_l[lane], piece_factor(m1, m) * piece_l[lane + 64]));
+    for (int c = lane; c < a.d; c += 64) {
+        constexpr int AHEAD = 8;
+        float acc = 0.0f;
+        for (int p0 = wave; p0 < pieces; p0 += 4 * AHEAD) {
+            float x[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) x[u] = a.part_o[(min(p0 + 4 * u, pieces - 1) * a.part_rows + row) * a.d + c];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const float f = p0 + 4 * u < pieces ? piece_factor(piece_m[min(p0 + 4 * u, pieces - 1)], m) : 0.0f;
+                acc = f != 0.0f ? fmaf(f, x[u], acc) : acc;             // nothing is written of a piece that sees nothing
+            }
+        }
+        part[wave][c] = acc;
+    }
+    __syncthreads();
     const int64_t token = row / n_q;
     const int head = (int)(row - token * n_q);
-    float2 x = lane < pieces ? a.part_ml[lane * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
-    const float m = wave_max(x.x);
-    const float f = piece_factor(x.x, m), sum = wave_sum(f * x.y);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    for (int c = lane; c < a.d; c += 64) {
-        float acc = 0.0f;
-        for (int p = 0; p < pieces; ++p) {
-            const float fp = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), p));
-            if (fp != 0.0f) acc = fmaf(fp, a.part_o[(p * a.part_rows + row) * a.d + c], acc);
-        }
-        ((QT*)a.out)[token * a.o_ts + head * a.o_hs + c] = from_float<QT>(acc * inv);
-    }
-    if (lane == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    const int c = threadIdx.x;
+    if (c < a.d) ((QT*)a.out)[token * a.o_ts + head * a.o_hs + c] = from_float<QT>((part[0][c] + part[1][c] + part[2][c] + part[3][c]) * inv);
+    if (c == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 template <int MB, typename PT, typename QT>
@@ -234,7 +251,7 @@ hipError_t f32_by_size(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
 }  // namespace
 
 static hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, hipStream_t st) {
-    const unsigned blocks = (unsigned)((max_tokens * a.g * a.n_kv + 3) / 4);
+    const unsigned blocks = (unsigned)(max_tokens * a.g * a.n_kv);
     if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a);
     else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a);
     return hipGetLastError();
@@ -269,7 +286,7 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
         a.cap_log2 = g->cap * kLog2e;
         a.cap_in = 2.0f / g->cap;                        // x = s / (cap log2 e); e^2x = 2^(2 log2 e x) = 2^(2 s / cap)
     }
-    const PairWorkspace w = make_pair_workspace(t->max_tokens, t->n_q_heads, lay.n_kv, lay.d, t->pt_stride);
+    const PairWorkspace w = make_pair_workspace(t->n_pairs, t->max_tokens, t->n_q_heads, lay.n_kv, lay.d, t->pt_stride);
     a.most_splits = w.most;
     a.part_ml = (float2*)workspace;
     a.part_o = (float*)((char*)workspace + w.o);
@@ -277,7 +294,10 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
     const int64_t items = s.cap_blk * lay.n_kv;
     const dim3 grid((unsigned)((items + 7) / 8 * 8), (unsigned)w.most);
     hipError_t e;
-    if (lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 128)) e = launch_pair_rows(lay.kv_dtype == HR_FP8_E4M3, a, grid, st);
+    a.rec_tiles = (const int4*)(S + s.tile);
+    const bool half = lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 128);
+    a.blocks_only = !half;
+    if (half) e = launch_pair_half(lay.kv_dtype == HR_FP8_E4M3, a, grid, st);
     else if (lay.kv_dtype == HR_F32) e = f32_by_size<float, float>(a, grid, st);
     else if (lay.kv_dtype == HR_BF16) e = f32_by_size<half_t, bf16_t>(a, grid, st);
     else e = f32_by_size<uint8_t, bf16_t>(a, grid, st);

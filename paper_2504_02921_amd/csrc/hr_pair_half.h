@@ -1,0 +1,80 @@
+// Device pieces that the half-precision kernels of hr_pair_attention share.
+#pragma once
+
+#include "hr_pair_attn.h"
+
+namespace hr {
+
+typedef const __attribute__((address_space(4))) int32_t* const_int_t;       // read through the scalar cache: uniform, written by an earlier launch
+typedef const __attribute__((address_space(4))) float* const_float_t;
+
+template <int HD, bool FP8>
+struct PairGeo {
+    static constexpr int KC = HD / 16, MB = HD / 32;
+    static constexpr int ESZ = FP8 ? 1 : 2;
+    static constexpr int BLOCK = kPageTokens * HD * ESZ;      // bytes of a K or V block
+    using Piece = std::conditional_t<FP8, uint2, halfx8>;     // 8 elements of a page
+};
+
+__device__ __forceinline__ halfx8 bf16x8_to_half(const bf16_t* p) {
+    const Loose<bf16_t, 8> x = *(const Loose<bf16_t, 8>*)p;
+    halfx8 r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = (half_t)(float)x.w[e];       // beyond the half range: infinity
+    return r;
+}
+
+// the lane's 16 probabilities as the B operands of two products over 16 keys each
+__device__ __forceinline__ void pack_p(const floatx16& s, halfx8 (&pf)[2], float f0, float f1) {
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const halfx2 x = __builtin_convertvector(floatx2{s[e] * f0, s[e + 1] * f0}, halfx2);
+        const halfx2 y = __builtin_convertvector(floatx2{s[8 + e] * f1, s[9 + e] * f1}, halfx2);
+        pf[0][e] = x[0]; pf[0][e + 1] = x[1];
+        pf[1][e] = y[0]; pf[1][e + 1] = y[1];
+    }
+}
+
+// Hides the keys of a sub-tile outside [lo, hi), relative to the lane's first
+__device__ __forceinline__ void hide_keys(floatx16& s, int lo, int hi) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int key = 8 * (r >> 2) + (r & 3);
+        s[r] = key >= lo && key < hi ? s[r] : -INFINITY;
+    }
+}
+
+// O^T += V^T P^T over a sub-tile that not every row sees whole.  A hidden key's V counts for nothing, whatever it holds, and 0 times infinity is
+// not nothing: the product has zeros for what is not finite and for keys from `exist` on, and what is not finite is added (rarely, value by value)
+// to the rows that see it.  frag(mb, e): the lane's V operand; value(key, ch): one value of the sub-tile; [lo, hi): the keys that the row sees.
+template <int MB, typename Frag, typename Value>
+__device__ __forceinline__ void add_pv_masked(floatx16 (&o)[MB], const halfx8 (&pf)[2], int lo, int hi, int exist, int hh, Frag frag, Value value) {
+    bool odd = false;
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            halfx8 v = frag(mb, e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool there = 16 * e + 8 * (i >> 2) + (i & 3) + 4 * hh < exist, fine = __builtin_fabsf16(v[i]) < (half_t)INFINITY;
+                odd = odd || (there && !fine);
+                v[i] = there && fine ? v[i] : (half_t)0.0f;
+            }
+            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[e], o[mb], 0, 0, 0);
+        }
+    }
+    if (!__any(odd)) return;
+#pragma unroll 1
+    for (int key = 0; key < exist; ++key) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float v = (float)value(key, mb * 32 + 8 * (r >> 2) + 4 * hh + (r & 3));
+                o[mb][r] += key >= lo && key < hi && !(fabsf(v) < INFINITY) ? v : 0.0f;
+            }
+    }
+}
+
+}  // namespace hr

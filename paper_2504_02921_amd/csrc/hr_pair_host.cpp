@@ -138,16 +138,22 @@ int tables_build_check(const hr_pool* pool, const hr_doc_list* docs, const int32
     return HR_OK;
 }
 
-int pair_most_splits(int64_t max_tokens, int n_q, int n_kv, int64_t pt_stride) {
-    const int64_t fewest = (max_tokens * (n_q / n_kv) + kPairBlkRows - 1) / kPairBlkRows * n_kv;      // all pairs in one group
-    const int64_t pieces = (pt_stride * kPageTokens + kPairSplitKeys - 1) / kPairSplitKeys;
-    const int64_t s = std::min<int64_t>(kPairSplitWgs / std::max<int64_t>(fewest, 1), std::min<int64_t>(pieces, kPairSplitMost));
+int pair_most_splits(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride) {
+    const int64_t keys = pt_stride * kPageTokens, rows = max_tokens * (n_q / n_kv);
+    if (keys < kPairSplitLeast) return 1;
+    // items of a full batch: blocks are fewest with all pairs in one group and most with a group each; tiles hold at most four blocks, and
+    // are taken from a number of blocks on
+    const int64_t blocks = (rows + kPairBlkRows - 1) / kPairBlkRows * n_kv, most_blocks = (rows / kPairBlkRows + std::min(n_pairs, max_tokens)) * n_kv;
+    int64_t s = kPairSplitWgs / std::max<int64_t>(blocks, 1);
+    const int64_t from = pair_tile_blocks(d);
+    if (most_blocks > from) s = std::max<int64_t>(s, kPairSplitWgs / std::max((blocks + 3) / 4, (from + 3) / 4));
+    s = std::min<int64_t>(s, std::min<int64_t>((keys + kPairSplitKeys - 1) / kPairSplitKeys, kPairSplitMost));
     return (int)std::max<int64_t>(s, 1);
 }
 
-PairWorkspace make_pair_workspace(int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride) {
+PairWorkspace make_pair_workspace(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride) {
     PairWorkspace w;
-    w.most = pair_most_splits(max_tokens, n_q, n_kv, pt_stride);
+    w.most = pair_most_splits(n_pairs, max_tokens, n_q, n_kv, d, pt_stride);
     if (w.most == 1) return w;
     const size_t rows = (size_t)w.most * (size_t)max_tokens * n_q;
     w.o = align_up(rows * 2 * sizeof(float));
@@ -218,7 +224,7 @@ size_t hr_pair_tables_sched_bytes(const hr_pool* pool, int32_t n_pairs, int32_t 
 
 size_t hr_pair_attention_workspace_bytes(const hr_pool* pool, const hr_pair_tables* t) {
     if (hr::tables_check(pool, t) != HR_OK || t->n_pairs == 0) return 0;
-    return hr::make_pair_workspace(t->max_tokens, t->n_q_heads, pool->cfg.n_kv_heads, pool->cfg.head_dim, t->pt_stride).total;
+    return hr::make_pair_workspace(t->n_pairs, t->max_tokens, t->n_q_heads, pool->cfg.n_kv_heads, pool->cfg.head_dim, t->pt_stride).total;
 }
 
 }  // extern "C"
