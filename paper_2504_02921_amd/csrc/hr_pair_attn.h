@@ -16,6 +16,9 @@
 
 namespace hr {
 
+typedef const __attribute__((address_space(4))) int32_t* const_int_t;       // read through the scalar cache: uniform, written by an earlier launch
+typedef const __attribute__((address_space(4))) float* const_float_t;
+
 struct PairAttnArgs {
     // what finds a workgroup's rows comes first: those words are in scalar registers when a wavefront starts
     const int32_t* hdr;
@@ -24,6 +27,8 @@ struct PairAttnArgs {
     const int32_t* page_table;
     int32_t pt_stride, n_kv, g, most_splits;
     int32_t num_pages, d, window, own_keys;
+    int32_t n_pairs, max_tokens;
+    int64_t cap_blk, cap_tile;        // records of the work list
     const int32_t *q_cu, *prefix;
     const char* pool;                 // page 0 of the layer
     const float* scales;              // fp8: of page 0 of the layer
@@ -59,6 +64,27 @@ __device__ __forceinline__ int item_of(int wg, int items) {
     return (wg >> 3) < per && at < items ? at : -1;
 }
 
+// What the work list says.  Tables that were not built, or not for this call, are taken for what they can at most be: every index below stays inside
+// its array and every loop ends, whatever they hold.
+struct PairItem {
+    int pair, D;                      // a pair of the group, and its document's length
+    int tok, row, rows;               // place of the group's first token, the item's first row, rows of the group
+};
+__device__ __forceinline__ int list_items(const PairAttnArgs& a, bool tiles) {
+    const const_int_t hdr = (const_int_t)a.hdr;
+    return (int)min((int64_t)hdr[tiles ? SH_TILES : SH_BLOCKS], tiles ? a.cap_tile : a.cap_blk) * a.n_kv;
+}
+__device__ __forceinline__ PairItem list_item(const PairAttnArgs& a, bool tiles, int at) {
+    const const_int_t r = (const_int_t)((tiles ? a.rec_tiles : a.rec) + 2 * (int64_t)at);
+    PairItem it;
+    it.pair = min(max(r[0], 0), a.n_pairs - 1);
+    it.D = (int)min((int64_t)max(r[1], 0), (int64_t)a.pt_stride * kPageTokens);
+    it.tok = min(max(r[2], 0), a.max_tokens - 1);
+    it.row = max(r[3], 0);
+    it.rows = min(max(r[4], it.row + 1), a.max_tokens * a.g);
+    return it;
+}
+
 // A lane's row
 struct PairRow {
     int token, head;                  // row of q, query head within the kv head's group
@@ -69,26 +95,28 @@ struct PairRow {
     float slope;                      // slopes[a] log2 e, or 0
 };
 
-__device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, int4 rec, int rows, int row) {
+__device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, const PairItem& it, int row) {
     PairRow r;
-    r.on = row < rows;
-    const int rc = min(row, rows - 1), t = rc / a.g;
+    r.on = row < it.rows;
+    const int rc = min(row, it.rows - 1), t = rc / a.g;
     r.head = rc - t * a.g;
-    r.place = rec.z + t;
+    r.place = min(it.tok + t, a.max_tokens - 1);
     const int4 o = a.ord[r.place];    // token row, start, pair, D
-    r.token = o.x;
-    r.start = o.y;
-    const int i = r.place - r.start;
-    r.pos = rec.y + i;
+    r.token = min(max(o.x, 0), a.max_tokens - 1);
+    r.start = min(max(o.y, 0), r.place);
+    const int i = r.place - r.start, pair = min(max(o.z, 0), a.n_pairs - 1);
+    r.pos = it.D + i;
     const int first = a.window > 0 ? r.pos - a.window + 1 : 0;      // the first position the row sees
-    r.dlo = min(max(first, 0), rec.y);
+    r.dlo = min(max(first, 0), it.D);
     int all = 0;
-    if (a.prefix) all = min(max(a.prefix[o.z], 0), a.q_cu[o.z + 1] - a.q_cu[o.z]);
-    r.olo = r.start + min(max(first - rec.y, 0), i);
-    r.ohi = r.start + max(i + 1, all);
+    if (a.prefix) all = min(max(a.prefix[pair], 0), a.q_cu[pair + 1] - a.q_cu[pair]);
+    r.olo = r.start + min(max(first - it.D, 0), i);
+    r.ohi = min(r.start + max(i + 1, all), a.max_tokens);
     r.slope = a.slopes ? a.slopes[h * a.g + r.head] * kLog2e : 0.0f;
     return r;
 }
+// A lane's own key: its place's token row
+__device__ __forceinline__ int64_t own_token(const PairAttnArgs& a, int place) { return min(max(a.ord[place].x, 0), a.max_tokens - 1); }
 
 // The scaled scores of a sub-tile in log2 units: cap, then distance.  first: position (document) or place (own) of its first key as seen from
 // the row, i.e. minus the row's own

@@ -41,16 +41,16 @@ template <int MB, typename PT, typename QT>
 __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs a) {
     constexpr bool FP8 = sizeof(PT) == 1;
     extern __shared__ __attribute__((aligned(16))) float smem[];
-    const int items = a.hdr[SH_BLOCKS] * a.n_kv;
+    const int items = list_items(a, false);
     const int item = item_of((int)blockIdx.x, items);
     const int pieces = pair_choice(items, items, a.d, a.most_splits).pieces;
     if (item < 0 || (int)blockIdx.y >= pieces) return;
     const int blk = item / a.n_kv, h = item - blk * a.n_kv;
-    const int4 rec = a.rec[2 * blk];
-    const int rows = a.rec[2 * blk + 1].x, D = rec.y, d = a.d;
+    const PairItem it = list_item(a, false, blk);
+    const int D = it.D, d = a.d;
     const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const PairRow row = pair_row(a, h, rec, rows, rec.w + ln);
-    const int32_t* pt = a.page_table + (int64_t)rec.x * a.pt_stride;
+    const PairRow row = pair_row(a, h, it, it.row + ln);
+    const int32_t* pt = a.page_table + (int64_t)it.pair * a.pt_stride;
     const int block = kPageTokens * d;                                  // elements of a K or V block
     const PT* pool = (const PT*)a.pool + (int64_t)h * 2 * block;
     const int64_t page_stride = (int64_t)a.n_kv * 2 * block;
@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
                 }
             }
         } else {
-            kr += (int64_t)a.ord[min(key0 + ln, ohi - 1)].x * a.k_ts;
+            kr += own_token(a, min(key0 + ln, ohi - 1)) * a.k_ts;
         }
         const PT* kp = (ln >> 4) ? page[1] : page[0];
 #pragma unroll
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int x = min(key0 + 16 * e2 + (e & 3) + 2 * (e & 4) + 4 * hh, ohi - 1);
-                        vf[e2][e] = to_float<QT>(vn[(int64_t)a.ord[x].x * a.v_ts + ch]);
+                        vf[e2][e] = to_float<QT>(vn[own_token(a, x) * a.v_ts + ch]);
                     }
                 }
             }
@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
 template <typename QT>
 __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
     __shared__ float part[4][256], piece_m[kPairSplitMost], piece_l[kPairSplitMost];
-    const int blocks = a.hdr[SH_BLOCKS] * a.n_kv, tiles = a.blocks_only ? blocks : a.hdr[SH_TILES] * a.n_kv;
+    const int blocks = list_items(a, false), tiles = a.blocks_only ? blocks : list_items(a, true);
     const int pieces = pair_choice(blocks, tiles, a.d, a.most_splits).pieces;
     if (pieces == 1) return;                                            // the rows are there
     const int n_q = a.g * a.n_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -274,6 +274,10 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
     a.d = lay.d;
     a.window = g->window;
     a.own_keys = g->k != nullptr;
+    a.n_pairs = t->n_pairs;
+    a.max_tokens = t->max_tokens;
+    a.cap_blk = s.cap_blk;
+    a.cap_tile = s.cap_tile;
     a.q_cu = t->q_cu;
     a.prefix = g->prefix_lens;
     a.pool = pool->base + (size_t)g->layer * lay.num_pages * lay.n_kv * 2 * lay.block_elems * lay.esz;

@@ -20,13 +20,14 @@ namespace hr {
 namespace {
 
 constexpr int kPairWaves = 4;
-constexpr int kStageKeys = 64, kStagePages = kStageKeys / kPageTokens;
 
+// The ring of sub-tiles that tiles read: four slots of 32 keys, as half
 template <int HD>
 struct TileGeo {
-    static constexpr int HBLOCK = kPageTokens * HD * 2, HPAGE = 2 * HBLOCK, STAGE = kStagePages * HPAGE;      // bytes, as half
+    static constexpr int HBLOCK = kPageTokens * HD * 2, SLOT = 4 * HBLOCK;      // bytes
+    static constexpr int LOADS = HBLOCK / 1024;   // of a wavefront for a block
     static constexpr int TURN = HD * 2 + 16;      // bytes between the rows of a block on its way out: they start at other banks
-    static constexpr int LDS = std::max(2 * STAGE, kPairWaves * 32 * TURN);
+    static constexpr int LDS = std::max(4 * SLOT, kPairWaves * 32 * TURN);
 };
 
 // What rows of a group see together (row, row + 1, .. last of them), without asking each
@@ -35,7 +36,7 @@ struct PairSpan {
     int olo, ohi;                     // own keys that some row sees, by place
 };
 // mine: the rows of this wavefront, one per lane of a half
-__device__ __forceinline__ PairSpan pair_span(const PairAttnArgs& a, const PairRow& mine, int4 rec, int first, int last) {
+__device__ __forceinline__ PairSpan pair_span(const PairAttnArgs& a, const PairRow& mine, const PairItem& it, int first, int last) {
     PairSpan s;
     if (a.window > 0) {
         s.dlo = rows_min(mine.dlo);
@@ -45,14 +46,14 @@ __device__ __forceinline__ PairSpan pair_span(const PairAttnArgs& a, const PairR
         return s;
     }
     // without a window: the first row's query from its first token, the last row's as far as that row sees
-    const int t0 = rec.z + first / a.g, t1 = rec.z + last / a.g;
+    const int t0 = min(it.tok + first / a.g, a.max_tokens - 1), t1 = min(it.tok + last / a.g, a.max_tokens - 1);
     const const_int_t f = (const_int_t)(a.ord + t0), l = (const_int_t)(a.ord + t1);
     s.dlo = s.dlo_all = 0;
-    s.olo = f[1];
+    s.olo = min(max(f[1], 0), t0);
     s.ohi = t1 + 1;
     if (a.prefix) {
-        const int pair = l[2], n = ((const_int_t)a.q_cu)[pair + 1] - ((const_int_t)a.q_cu)[pair];
-        s.ohi = max(s.ohi, l[1] + min(((const_int_t)a.prefix)[pair], n));
+        const int pair = min(max(l[2], 0), a.n_pairs - 1), n = ((const_int_t)a.q_cu)[pair + 1] - ((const_int_t)a.q_cu)[pair];
+        s.ohi = min(max(s.ohi, min(max(l[1], 0), t1) + min(((const_int_t)a.prefix)[pair], n)), a.max_tokens);
     }
     return s;
 }
@@ -70,20 +71,20 @@ __device__ __forceinline__ void load_q(const PairAttnArgs& a, const PairRow& row
 
 // ---- few rows
 template <int HD, bool FP8, bool EXTRA>
-__device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, int4 rec, int rows, int h, int pieces) {
+__device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, const PairItem& it, int h, int pieces) {
     using G = PairGeo<HD, FP8>;
     using Piece = typename G::Piece;
     constexpr int KC = G::KC, MB = G::MB, NW = kPairWaves;
-    const int D = rec.y;
+    const int D = it.D;
     const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const PairRow row = pair_row(a, h, rec, rows, rec.w + ln);
-    const const_int_t pt = (const_int_t)(a.page_table + (int64_t)rec.x * a.pt_stride);
+    const PairRow row = pair_row(a, h, it, it.row + ln);
+    const const_int_t pt = (const_int_t)(a.page_table + (int64_t)it.pair * a.pt_stride);
     const char* pool = a.pool + (int64_t)h * 2 * G::BLOCK;
     const int64_t page_stride = (int64_t)a.n_kv * 2 * G::BLOCK;
 
     // The sub-tiles that some row of the block sees: document sub-tiles that all rows see whole, then those at an edge (the window's, the
     // document's end), then the pairs' own keys; and this piece's share of them
-    const PairSpan span = pair_span(a, row, rec, rec.w, min(rec.w + 32, rows) - 1);
+    const PairSpan span = pair_span(a, row, it, it.row, min(it.row + 32, it.rows) - 1);
     const int dlo = span.dlo, dlo_all = span.dlo_all, olo = span.olo, ohi = span.ohi;
     const int doc0 = dlo / 32, doc1 = (D + 31) / 32, whole0 = (dlo_all + 31) / 32, whole1 = max(D / 32, whole0);
     const int n_whole = whole1 - whole0, n_doc = max(doc1 - doc0, 0), n_own = a.own_keys ? (ohi - olo + 31) / 32 : 0;
@@ -199,7 +200,7 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, in
         } else {
             key0 = olo + (j - n_doc) * 32;
             exist = min(ohi - key0, 32);
-            const int64_t token = a.ord[min(key0 + ln, ohi - 1)].x;
+            const int64_t token = own_token(a, min(key0 + ln, ohi - 1));
             const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs;
             halfx8 x[KC];
 #pragma unroll
@@ -232,110 +233,95 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, in
 
 // ---- many rows
 template <int HD, bool FP8, bool EXTRA>
-__device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, int4 rec, int rows, int h, int pieces) {
+__device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, const PairItem& it, int h, int pieces) {
     using G = PairGeo<HD, FP8>;
     using T = TileGeo<HD>;
     constexpr int KC = G::KC, MB = G::MB, NW = kPairWaves;
-    const int D = rec.y;
+    const int D = it.D;
     const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const const_int_t pt = (const_int_t)(a.page_table + (int64_t)rec.x * a.pt_stride);
-    const char* pool = a.pool + (int64_t)h * 2 * G::BLOCK;
+    const const_int_t pt = (const_int_t)(a.page_table + (int64_t)it.pair * a.pt_stride);
     const int64_t page_stride = (int64_t)a.n_kv * 2 * G::BLOCK;
-    const int last_page = (D - 1) / kPageTokens, last_row = min(rec.w + kPairTileRows, rows) - 1;
+    const int last_page = (D - 1) / kPageTokens, last_row = min(it.row + kPairTileRows, it.rows) - 1;
 
     // ---- the wavefront's block; without rows of its own it only brings pages
-    const int first = rec.w + wave * 32;
+    const int first = it.row + wave * 32;
     const bool active = first <= last_row;
-    const PairRow row = pair_row(a, h, rec, rows, first + ln);
-    const PairSpan mine = pair_span(a, row, rec, min(first, last_row), min(first + 31, last_row));
-    PairSpan wg = pair_span(a, row, rec, rec.w, last_row);
+    const PairRow row = pair_row(a, h, it, first + ln);
+    const PairSpan mine = pair_span(a, row, it, min(first, last_row), min(first + 31, last_row));
+    PairSpan wg = pair_span(a, row, it, it.row, last_row);
     if (a.window > 0) {                                                 // the wavefronts' together
         int* range = (int*)smem;
         if (lane == 0) {
             range[wave] = mine.dlo;
-            range[NW + wave] = mine.olo;
-            range[2 * NW + wave] = mine.ohi;
+            range[NW + wave] = mine.dlo_all;
+            range[2 * NW + wave] = mine.olo;
+            range[3 * NW + wave] = mine.ohi;
         }
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
             wg.dlo = min(wg.dlo, range[w]);
-            wg.olo = min(wg.olo, range[NW + w]);
-            wg.ohi = max(wg.ohi, range[2 * NW + w]);
+            wg.dlo_all = max(wg.dlo_all, range[NW + w]);
+            wg.olo = min(wg.olo, range[2 * NW + w]);
+            wg.ohi = max(wg.ohi, range[3 * NW + w]);
         }
         wg.dlo = __builtin_amdgcn_readfirstlane(wg.dlo);
+        wg.dlo_all = __builtin_amdgcn_readfirstlane(wg.dlo_all);
         wg.olo = __builtin_amdgcn_readfirstlane(wg.olo);
         wg.ohi = __builtin_amdgcn_readfirstlane(wg.ohi);
         __syncthreads();
     }
-    // this piece's stages: the document's, then the own keys'
-    const int doc0 = wg.dlo / kStageKeys, n_doc = wg.dlo < D ? (D + kStageKeys - 1) / kStageKeys - doc0 : 0;
-    const int n_own = a.own_keys ? (wg.ohi - wg.olo + kStageKeys - 1) / kStageKeys : 0;
-    const int share = (n_doc + n_own + pieces - 1) / pieces, u0 = (int)blockIdx.y * share, u1 = min(u0 + share, n_doc + n_own);
-    const int j0 = doc0 + u0, j1 = doc0 + min(u1, n_doc);               // document stages
+    // this piece's sub-tiles, in the order of pair_rows
+    const int doc0 = wg.dlo / 32, doc1 = (D + 31) / 32, whole0 = (wg.dlo_all + 31) / 32, whole1 = max(D / 32, whole0);
+    const int n_whole = whole1 - whole0, n_doc = max(doc1 - doc0, 0), n_own = a.own_keys ? (wg.ohi - wg.olo + 31) / 32 : 0;
+    const int n_sub = n_doc + n_own, share = (n_sub + pieces - 1) / pieces;
+    const int u0 = (int)blockIdx.y * share, u1 = min(u0 + share, n_sub);
+    const int i0 = whole0 + min(u0, n_whole), i1 = whole0 + min(u1, n_whole);      // whole ones
 
-    // ---- a stage's K and V blocks, page after page, K first: a wavefront brings one page
-    auto id_at = [&](int at) { return min(max(pt[min(at, last_page)], 0), a.num_pages - 1); };
-    auto request = [&](int id, int buf) {                               // a half page, verbatim
-        const char* src = pool + id * page_stride + lane * 16;
-        char* dst = smem + buf * T::STAGE + wave * T::HPAGE;
+    // ---- a sub-tile in the ring: K of its two pages, V of its two pages; wavefront w brings page w & 1's K (w < 2) or V
+    const int my_page = wave & 1;
+    const char* block0 = a.pool + ((int64_t)h * 2 + (wave >> 1)) * G::BLOCK;
+    char* const my_part = smem + (wave >> 1) * 2 * T::HBLOCK + my_page * T::HBLOCK;
+    auto id_of = [&](int sub, int page) { return min(max(pt[min(2 * sub + page, last_page)], 0), a.num_pages - 1); };
+    auto request = [&](int id, int slot) {                              // a half block, verbatim
+        const char* src = block0 + id * page_stride + lane * 16;
+        char* dst = my_part + slot * T::SLOT;
 #pragma unroll
-        for (int e = 0; e < T::HPAGE / 1024; ++e)
+        for (int e = 0; e < T::LOADS; ++e)
             __builtin_amdgcn_global_load_lds((gbl_ptr_t)(src + e * 1024), (lds_ptr_t)(dst + e * 1024), 16, 0, 0);
     };
-    constexpr int RAW = FP8 ? 2 * G::BLOCK / 512 : 1;                   // fp8: 8-byte words of a page that a lane has
-    uint2 raw[RAW];
-    auto fetch = [&](int id) {
-        const char* src = pool + id * page_stride + lane * 8;
+    struct Raw { uint2 w[FP8 ? G::BLOCK / 512 : 1]; };                  // fp8: a block as it lies there
+    auto fetch = [&](int id, Raw& r) {
+        const char* src = block0 + id * page_stride + lane * 8;
 #pragma unroll
-        for (int e = 0; e < RAW; ++e) raw[e] = *(const uint2*)(src + e * 512);
+        for (int e = 0; e < G::BLOCK / 512; ++e) r.w[e] = *(const uint2*)(src + e * 512);
     };
-    auto expand = [&](int buf, float v_scale) {
-        char* dst = smem + buf * T::STAGE + wave * T::HPAGE;
+    auto expand = [&](const Raw& r, int slot, float v_scale) {
+        char* dst = my_part + slot * T::SLOT;
+        const halfx2 f = fp8_expand_factor(wave < 2 ? 1.0f : v_scale);      // K's scale goes into the scores
 #pragma unroll
-        for (int e = 0; e < RAW; ++e) {
-            const int w = (e % (RAW / 2)) * 64 + lane, t = w / (HD / 8), c8 = (w % (HD / 8)) ^ k_swizzle(t, HD, 1);
-            if (e < RAW / 2) *(halfx8*)(dst + (t * HD + ((c8 ^ k_swizzle(t, HD, 2)) << 3)) * 2) = fp8x8_to_half(raw[e], fp8_expand_factor(1.0f));
-            else *(halfx8*)(dst + T::HBLOCK + w * 16) = fp8x8_to_half(raw[e], fp8_expand_factor(v_scale));
+        for (int e = 0; e < G::BLOCK / 512; ++e) {
+            const int w = e * 64 + lane, t = w / (HD / 8), c8 = (w % (HD / 8)) ^ k_swizzle(t, HD, 1);
+            *(halfx8*)(dst + (wave < 2 ? (t * HD + ((c8 ^ k_swizzle(t, HD, 2)) << 3)) * 2 : w * 16)) = fp8x8_to_half(r.w[e], f);
         }
     };
-    // What is needed of a stage's pages, asked for ahead of it: ids (the wavefront's own, fp8: all), and, fp8, the factors of its scores, and of its
-    // probabilities what the expansion leaves of the V scales
-    struct Ids { int own, all[FP8 ? kStagePages : 1]; };
-    auto ids_of = [&](int stage) {
-        Ids r;
-        stage = min(stage, j1 - 1);                                     // behind the last stage its pages again, which nobody reads
-        if constexpr (FP8) {
-#pragma unroll
-            for (int e = 0; e < kStagePages; ++e) r.all[e] = id_at(kStagePages * stage + e);
-            r.own = pick(wave >= 2, pick(wave == 1, r.all[0], r.all[1]), pick(wave == 3, r.all[2], r.all[3]));
-        } else {
-            r.own = id_at(kStagePages * stage + wave);
-        }
-        return r;
-    };
-    struct Scales { float k[kStagePages], v[kStagePages]; };
-    auto scales_of = [&](const Ids& ids) {
+    // fp8: scales of a sub-tile's two pages
+    struct Scales { float k0 = 1.0f, k1 = 1.0f, v0 = 1.0f, v1 = 1.0f; };      // half pages: one
+    auto scales_of = [&](int id0, int id1) {
         Scales r;
-#pragma unroll
-        for (int e = 0; e < kStagePages; ++e) {
-            r.k[e] = r.v[e] = 1.0f;
-            if constexpr (FP8) {
-                const const_float_t sc = (const_float_t)(a.scales + ((int64_t)ids.all[e] * a.n_kv + h) * 2);
-                r.k[e] = sc[0];
-                r.v[e] = sc[1];
-            }
+        if constexpr (FP8) {
+            const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
+            r.k0 = s0[0], r.k1 = s1[0], r.v0 = s0[1], r.v1 = s1[1];
         }
         return r;
     };
-    auto own_scale = [&](const Scales& s) { return pick(wave >= 2, pick(wave == 1, s.v[0], s.v[1]), pick(wave == 3, s.v[2], s.v[3])); };
-    // own keys from place key0 on: a thread has one key and its wavefront's share of the channels
-    auto own_stage = [&](int key0, int buf) {
-        constexpr int CH = HD / NW;
-        const int64_t token = a.ord[min(key0 + lane, wg.ohi - 1)].x;
-        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs + wave * CH, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs + wave * CH;
-        char* page = smem + buf * T::STAGE + (lane >> 4) * T::HPAGE;
-        const int t = lane & 15;
+    // 32 own keys from place key0 on: eight threads have a key, each its share of the channels
+    auto own_keys = [&](int key0, int slot) {
+        constexpr int CH = HD / 8;
+        const int key = threadIdx.x & 31, c0 = (threadIdx.x >> 5) * CH, t = key & 15;
+        const int64_t token = own_token(a, min(key0 + key, wg.ohi - 1));
+        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs + c0, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs + c0;
+        half_t* dst = (half_t*)(smem + slot * T::SLOT + (key >> 4) * T::HBLOCK);
         halfx8 kx[CH / 8], vx[CH / 8];
 #pragma unroll
         for (int e = 0; e < CH / 8; ++e) {
@@ -344,23 +330,42 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, int
         }
 #pragma unroll
         for (int e = 0; e < CH / 8; ++e) {
-            const int c = wave * CH + e * 8;
-            *(halfx8*)(page + k_elem(t, c, HD, 2) * 2) = kx[e];
+            *(halfx8*)(dst + k_elem(t, c0 + e * 8, HD, 2)) = kx[e];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *(half_t*)(page + T::HBLOCK + v_elem(t, c + i, HD) * 2) = vx[e][i];
+            for (int i = 0; i < 8; ++i) dst[T::HBLOCK + v_elem(t, c0 + e * 8 + i, HD)] = vx[e][i];      // V two blocks on
         }
     };
+    auto k_frag = [&](int slot, int kk) {
+        const int t = ln & 15;
+        return *(const halfx8*)(smem + slot * T::SLOT + (ln >> 4) * T::HBLOCK + (t * HD + (((2 * kk + hh) ^ k_swizzle(t, HD, 2)) << 3)) * 2);
+    };
+    auto v_frag = [&](int slot, int mb, int e) { return *(const halfx8*)(smem + slot * T::SLOT + (2 + e) * T::HBLOCK + (hh * HD + mb * 32 + ln) * 16); };
 
-    // the first pages are on their way while the rows are read
-    Ids ids;                          // of the stage that is asked for next
-    Scales sc_now, sc_next;           // of this stage and the one behind it
-    if (j0 < j1) {
-        ids = ids_of(j0);
-        if constexpr (FP8) fetch(ids.own);
-        else request(ids.own, 0);
-        sc_now = scales_of(ids);
-        ids = ids_of(j0 + 1);
-        sc_next = scales_of(ids);
+    // ---- the first sub-tiles are on their way while the rows are read.  Behind the last one that one's again, which nobody reads: what is asked for
+    // does not hang on a branch.
+    Raw raw[2];
+    int ids[2][2] = {};                                                 // pages of the next sub-tiles that are asked for
+    Scales sc[4];                                                       // fp8: of this sub-tile and those behind it
+    auto ids_of = [&](int sub, int (&r)[2]) {
+        sub = min(sub, i1 - 1);
+        r[0] = id_of(sub, 0);
+        r[1] = id_of(sub, 1);
+    };
+    if (i0 < i1) {
+        if constexpr (FP8) {
+            int r[2];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                ids_of(i0 + e, r);
+                if (e < 2) fetch(my_page ? +r[1] : +r[0], raw[e]);
+                sc[e] = scales_of(r[0], r[1]);
+                if (e >= 2) ids[e - 2][0] = r[0], ids[e - 2][1] = r[1];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 3; ++e) request(id_of(min(i0 + e, i1 - 1), my_page), e);
+            ids[0][0] = id_of(min(i0 + 3, i1 - 1), my_page);
+        }
     }
     halfx8 q[KC];
     load_q<HD>(a, row, h, hh, q);
@@ -368,139 +373,140 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, int
 #pragma unroll
     for (int mb = 0; mb < MB; ++mb) o[mb] = floatx16{};
     PairSoftmax sm;
-
-    // ---- sub: the first of a sub-tile's two pages in LDS
-    auto k_frag = [&](const char* sub, int kk) {
-        const int t = ln & 15;
-        return *(const halfx8*)(sub + (ln >> 4) * T::HPAGE + (t * HD + (((2 * kk + hh) ^ k_swizzle(t, HD, 2)) << 3)) * 2);
-    };
-    auto v_frag = [&](const char* sub, int mb, int e) { return *(const halfx8*)(sub + e * T::HPAGE + T::HBLOCK + (hh * HD + mb * 32 + ln) * 16); };
     auto rescale = [&](float alpha) {
         if (__any(alpha != 1.0f)) {
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) o[mb] *= alpha;
         }
     };
-    constexpr bool SCALED = EXTRA || FP8;      // scores are scaled before they are compared
-    constexpr int SUBS = HD == 64 || FP8 ? 1 : 2;     // sub-tiles at a time: at 64 channels a second one's scores would cost the fourth wavefront of a SIMD
 
-    // SUBS sub-tiles that the wavefront's rows see whole, the stage's first-th and on
-    auto whole = [&](const char* buf, int first, int key0, const Scales& sc) {
-        floatx16 s[SUBS];
-#pragma unroll
-        for (int st = 0; st < SUBS; ++st) {
-            const char* sub = buf + (first + st) * 2 * T::HPAGE;
-            s[st] = floatx16{};
-            halfx8 k[KC];
-#pragma unroll
-            for (int kk = 0; kk < KC; ++kk) k[kk] = k_frag(sub, kk);
-#pragma unroll
-            for (int kk = 0; kk < KC; ++kk) s[st] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[kk], q[kk], s[st], 0, 0, 0);
-        }
-        float mx = -INFINITY;
-#pragma unroll
-        for (int st = 0; st < SUBS; ++st) {
-            const bool behind = first + st > 0;
-            if (SCALED) {
-                const float c0 = a.scale_log2 * pick(behind, sc.k[0], sc.k[2]), c1 = a.scale_log2 * pick(behind, sc.k[1], sc.k[3]);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[st][r] *= r < 8 ? c0 : c1;
+    // ---- sub-tiles at an edge and own keys, in the ring's last slot
+    for (int u = max(u0, n_whole); u < u1; ++u) {
+        const bool doc = u < n_doc;
+        const int sub = u - n_whole < whole0 - doc0 ? doc0 + u - n_whole : doc0 + u;
+        const int key0 = doc ? 32 * sub : wg.olo + (u - n_doc) * 32, end = doc ? D : wg.ohi;
+        Scales se;
+        __syncthreads();                                                // everyone is past the one before
+        if (doc) {
+            const int id0 = id_of(sub, 0), id1 = id_of(sub, 1);
+            se = scales_of(id0, id1);
+            if constexpr (FP8) {
+                Raw r;
+                fetch(my_page ? id1 : id0, r);
+                expand(r, 3, my_page ? +se.v1 : +se.v0);
+            } else {
+                request(my_page ? id1 : id0, 3);
+                __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0)
             }
-            if (EXTRA) pair_scores<false>(s[st], a, row, key0 + 32 * (first + st) - row.pos, hh);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[st][r]);
+        } else {
+            own_keys(key0, 3);
         }
-        const float c = SCALED ? 1.0f : a.scale_log2;
-        const float alpha = sm.follow(row_max2(mx) * c), use = sm.used();
-        rescale(alpha);
-        float sum = 0.0f;
-        halfx8 p[SUBS][2];
-#pragma unroll
-        for (int st = 0; st < SUBS; ++st) {
-            const bool behind = first + st > 0;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[st][r] = __builtin_amdgcn_exp2f(fmaf(s[st][r], c, -use));
-                sum += s[st][r];
-            }
-            pack_p(s[st], p[st], FP8 ? fp8_scale_mantissa(pick(behind, sc.v[0], sc.v[2])) : 1.0f, FP8 ? fp8_scale_mantissa(pick(behind, sc.v[1], sc.v[3])) : 1.0f);
-        }
-        sm.l = fmaf(sm.l, alpha, sum);
-#pragma unroll
-        for (int st = 0; st < SUBS; ++st)
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(buf + (first + st) * 2 * T::HPAGE, mb, e), p[st][e], o[mb], 0, 0, 0);
-    };
-    // 32 keys at an edge: document keys from key0 on, or own keys from place key0 on; end: behind the last key there is
-    auto edge = [&](const char* sub, bool doc, int key0, int end, float ks0, float ks1, float vs0, float vs1) {
-        if (doc ? key0 + 32 <= mine.dlo : key0 + 32 <= mine.olo || key0 >= mine.ohi) return;      // seen by none of the rows
+        __syncthreads();
+        if (!active || (doc ? key0 + 32 <= mine.dlo : key0 + 32 <= mine.olo || key0 >= mine.ohi)) continue;      // seen by none of the rows
         floatx16 s = {};
 #pragma unroll
-        for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(sub, kk), q[kk], s, 0, 0, 0);
+        for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(3, kk), q[kk], s, 0, 0, 0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.scale_log2 * (r < 8 ? ks0 : ks1);
+        for (int r = 0; r < 16; ++r) s[r] *= a.scale_log2 * (r < 8 ? se.k0 : se.k1);
         if (EXTRA) pair_scores<false>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
         const int lo = (doc ? row.dlo : row.olo) - key0, hi = (doc ? D : row.ohi) - key0;
         hide_keys(s, lo - 4 * hh, hi - 4 * hh);
         rescale(pair_softmax(sm, s));
         halfx8 pf[2];
-        pack_p(s, pf, FP8 ? fp8_scale_mantissa(vs0) : 1.0f, FP8 ? fp8_scale_mantissa(vs1) : 1.0f);
-        add_pv_masked<MB>(o, pf, lo, hi, min(end - key0, 32), hh, [&](int mb, int e) { return v_frag(sub, mb, e); },
-                          [&](int key, int ch) { return ((const half_t*)(sub + (key >> 4) * T::HPAGE + T::HBLOCK))[v_elem(key & 15, ch, HD)]; });
-    };
+        pack_p(s, pf, FP8 ? fp8_scale_mantissa(se.v0) : 1.0f, FP8 ? fp8_scale_mantissa(se.v1) : 1.0f);
+        add_pv_masked<MB>(o, pf, lo, hi, min(end - key0, 32), hh, [&](int mb, int e) { return v_frag(3, mb, e); },
+                          [&](int key, int ch) { return ((const half_t*)(smem + 3 * T::SLOT + (2 + (key >> 4)) * T::HBLOCK))[v_elem(key & 15, ch, HD)]; });
+    }
 
-    // ---- own keys, in the second buffer, while the document's first pages come
-    for (int u = max(u0, n_doc); u < u1; ++u) {
-        const int key0 = wg.olo + (u - n_doc) * kStageKeys;
-        own_stage(key0, 1);
+    // ---- whole sub-tiles.  S of one is computed next to the exponentials of the one before, and its maxima next to that one's V P: a wavefront issues in
+    // order, and without the other's arithmetic between them it would wait 32 cycles for each of its matrix instructions
+    if (i0 < i1) {
+        floatx16 s = {};
+        float mx = 0.0f;
+        // the largest of a lane's raw scores, scaled where they are scaled later; EXTRA: scaled, capped and biased in place
+        auto largest = [&](floatx16& x, int key0, const Scales& c) {
+            if (EXTRA) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) x[r] *= a.scale_log2 * (r < 8 ? c.k0 : c.k1);
+                pair_scores<false>(x, a, row, key0 - row.pos, hh);
+            }
+            float m0 = x[0], m1 = x[8];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) {
+                m0 = fmaxf(m0, x[r]);
+                m1 = fmaxf(m1, x[8 + r]);
+            }
+            return EXTRA ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
+        };
+        auto step = [&](int i, Raw& r, int (&next)[2]) {
+            const int at = i - i0;
+            // everyone has the next sub-tile, and is past the one before: its slot is free
+            if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
+            __syncthreads();
+            if constexpr (FP8) {
+                expand(r, (at + 2) & 3, my_page ? +sc[2].v1 : +sc[2].v0);
+                fetch(my_page ? +next[1] : +next[0], r);
+            } else {
+                request(next[0], (at + 3) & 3);
+                next[0] = id_of(min(i + 4, i1 - 1), my_page);
+            }
+            if (active) {
+                const int ks = (at + 1) & 3, vs = at & 3;
+                const float alpha = sm.follow(row_max2(mx)), use = sm.used();
+                rescale(alpha);
+                floatx16 sn = {};
+#pragma unroll
+                for (int kk = 0; kk < KC; ++kk) sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(ks, kk), q[kk], sn, 0, 0, 0);
+                const float c0 = EXTRA ? 1.0f : a.scale_log2 * sc[0].k0, c1 = EXTRA ? 1.0f : a.scale_log2 * sc[0].k1;
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], FP8 ? (e < 8 ? c0 : c1) : EXTRA ? 1.0f : a.scale_log2, -use));
+                    sum += s[e];
+                }
+                sm.l = fmaf(sm.l, alpha, sum);
+                halfx8 p[2];
+                pack_p(s, p, FP8 ? fp8_scale_mantissa(sc[0].v0) : 1.0f, FP8 ? fp8_scale_mantissa(sc[0].v1) : 1.0f);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(vs, mb, e), p[e], o[mb], 0, 0, 0);
+                mx = largest(sn, 32 * (i + 1), sc[1]);
+                s = sn;
+            }
+            if constexpr (FP8) {
+                sc[0] = sc[1];
+                sc[1] = sc[2];
+                sc[2] = sc[3];
+                sc[3] = scales_of(next[0], next[1]);
+                ids_of(i + 6, next);
+            }
+        };
+        if constexpr (FP8) {
+            expand(raw[0], 0, my_page ? +sc[0].v1 : +sc[0].v0);
+            expand(raw[1], 1, my_page ? +sc[1].v1 : +sc[1].v0);
+            fetch(my_page ? +ids[0][1] : +ids[0][0], raw[0]);
+            fetch(my_page ? +ids[1][1] : +ids[1][0], raw[1]);
+            ids_of(i0 + 4, ids[0]);
+            ids_of(i0 + 5, ids[1]);
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * T::LOADS));
+        }
         __syncthreads();
         if (active) {
-#pragma unroll 1
-            for (int st = 0; st < 2; ++st) edge(smem + T::STAGE + st * 2 * T::HPAGE, false, key0 + 32 * st, wg.ohi, 1.0f, 1.0f, 1.0f, 1.0f);
+#pragma unroll
+            for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(0, kk), q[kk], s, 0, 0, 0);
+            mx = largest(s, 32 * i0, sc[0]);
         }
-        __syncthreads();
-    }
-    // ---- the document
-    if (j0 < j1) {
+        int i = i0;
         if constexpr (FP8) {
-            expand(0, own_scale(sc_now));
-            fetch(ids.own);
-            ids = ids_of(j0 + 2);
-        }
-        for (int j = j0; j < j1; ++j) {
-            const int buf = (j - j0) & 1;
-            const char* at = smem + buf * T::STAGE;
-            if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70);     // this wavefront's page has landed
-            __syncthreads();                                            // everyone's has; and everyone is past the stage before
-            Scales sc_after;
-            if constexpr (FP8) {
-                expand(buf ^ 1, own_scale(sc_next));
-                fetch(ids.own);
-                sc_after = scales_of(ids);
-                ids = ids_of(j + 3);
-            } else {
-                request(ids.own, buf ^ 1);
-                sc_after = sc_now;
-                ids = ids_of(j + 2);
+            for (; i + 1 < i1; i += 2) {
+                step(i, raw[0], ids[0]);
+                step(i + 1, raw[1], ids[1]);
             }
-            const int key0 = j * kStageKeys;
-            if (active) {
-                if (key0 >= mine.dlo_all && key0 + kStageKeys <= D) {
-#pragma unroll 1
-                    for (int st = 0; st < 2; st += SUBS) whole(at, st, key0, sc_now);
-                } else {
-#pragma unroll 1
-                    for (int st = 0; st < 2; ++st)
-                        if (key0 + 32 * st < D)
-                            edge(at + st * 2 * T::HPAGE, true, key0 + 32 * st, D, pick(st, sc_now.k[0], sc_now.k[2]), pick(st, sc_now.k[1], sc_now.k[3]),
-                                 pick(st, sc_now.v[0], sc_now.v[2]), pick(st, sc_now.v[1], sc_now.v[3]));
-                }
-            }
-            sc_now = sc_next;
-            sc_next = sc_after;
+            if (i < i1) step(i, raw[0], ids[0]);
+        } else {
+            for (; i < i1; ++i) step(i, raw[0], ids[0]);
         }
     }
     // ---- out
@@ -552,15 +558,14 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, int
 template <int HD, bool FP8, bool EXTRA>
 __global__ void __launch_bounds__(kPairWaves * 64) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2, 8))) pair_attn_half_kernel(PairAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    const const_int_t hdr = (const_int_t)a.hdr;
-    const PairChoice ch = pair_choice(hdr[SH_BLOCKS] * a.n_kv, hdr[SH_TILES] * a.n_kv, HD, a.most_splits);
-    const int item = item_of((int)blockIdx.x, (ch.tiles ? hdr[SH_TILES] : hdr[SH_BLOCKS]) * a.n_kv);
+    const int blocks = list_items(a, false), tiles = list_items(a, true);
+    const PairChoice ch = pair_choice(blocks, tiles, HD, a.most_splits);
+    const int item = item_of((int)blockIdx.x, ch.tiles ? tiles : blocks);
     if (item < 0 || (int)blockIdx.y >= ch.pieces) return;
     const int at = item / a.n_kv, h = item - at * a.n_kv;
-    const const_int_t rp = (const_int_t)((ch.tiles ? a.rec_tiles : a.rec) + 2 * at);
-    const int4 rec = make_int4(rp[0], rp[1], rp[2], rp[3]);
-    if (ch.tiles) pair_tile<HD, FP8, EXTRA>(a, smem, rec, rp[4], h, ch.pieces);
-    else pair_rows<HD, FP8, EXTRA>(a, (float*)smem, rec, rp[4], h, ch.pieces);
+    const PairItem it = list_item(a, ch.tiles, at);
+    if (ch.tiles) pair_tile<HD, FP8, EXTRA>(a, smem, it, h, ch.pieces);
+    else pair_rows<HD, FP8, EXTRA>(a, (float*)smem, it, h, ch.pieces);
 }
 
 template <int HD, bool FP8, bool EXTRA>

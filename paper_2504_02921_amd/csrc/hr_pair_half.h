@@ -5,9 +5,6 @@
 
 namespace hr {
 
-typedef const __attribute__((address_space(4))) int32_t* const_int_t;       // read through the scalar cache: uniform, written by an earlier launch
-typedef const __attribute__((address_space(4))) float* const_float_t;
-
 template <int HD, bool FP8>
 struct PairGeo {
     static constexpr int KC = HD / 16, MB = HD / 32;

@@ -270,13 +270,16 @@ def test_attention_is_the_reference(kv, n_q, n_kv, d):
 
 
 @pytest.mark.parametrize("kv,n_q,n_kv,d", [("bf16", 14, 2, 64), ("fp8", 32, 8, 128), ("bf16", 8, 1, 128), ("f32", 4, 4, 64)])
-@pytest.mark.parametrize("pairs,doc,query", [(1, 3000, 1), (2, 5000, 3), (40, 200, 1), (30, 70, 40)])
+@pytest.mark.parametrize("pairs,doc,query", [(1, 3000, 1), (2, 5000, 3), (40, 200, 1), (30, 70, 40), (70, 500, 37)])
 def test_attention_of_few_and_of_many_rows(kv, n_q, n_kv, d, pairs, doc, query):
     """Few rows behind long documents (their keys in pieces), single tokens, many rows."""
     T = torch()
     rng = np.random.default_rng(pairs)
     b = Batch(kv, n_q, n_kv, d, rng.integers(doc // 2, doc + 1, pairs), rng.permutation(pairs), np.full(pairs, query), seed=3, layers=1, layer=0)
     b.check(what="plain")
+    b.check(cap=20.0, what="cap")
+    b.check(slopes=T.full((n_q,), 0.002, device=DEV), what="slopes")
+    b.check(cap=30.0, slopes=T.full((n_q,), 0.01, device=DEV), scale=-0.1, own=False, what="cap and slopes")
     b.check(window=doc // 3, cap=20.0, slopes=T.full((n_q,), 0.01, device=DEV), what="edges inside a piece")
     b.check(own=False, window=2, what="pieces that see nothing")
 
@@ -284,7 +287,9 @@ def test_attention_of_few_and_of_many_rows(kv, n_q, n_kv, d, pairs, doc, query):
 @pytest.mark.parametrize("kv,d", [("bf16", 64), ("fp8", 128), ("f32", 64)])
 def test_attention_of_one_document_for_all(kv, d):
     b = Batch(kv, 8, 2, d, [1500, 40], [0] * 60 + [1] * 3 + [0] * 9, np.random.default_rng(1).integers(0, 12, 72), seed=9)
+    slopes = torch().full((8,), 0.003, device=DEV)
     b.check()
+    b.check(cap=10.0, slopes=slopes, prefix_lens=dev_i32(np.arange(72) % 9))
     b.check(window=700)
 
 
