@@ -307,11 +307,39 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     };
     // fp8: scales of a sub-tile's two pages
     struct Scales { float k0 = 1.0f, k1 = 1.0f, v0 = 1.0f, v1 = 1.0f; };      // half pages: one
-    auto scales_of = [&](int id0, int id1) {
+    // The pages of the whole sub-tiles, 32 sub-tiles at a time: a lane has the id and the scales of one page.  Lane reads cost the loop no wait; requests
+    // through the scalar cache would share the counter of the LDS reads, and out of order, so that each of those waited for all.
+    struct Pages { int id; float k, v; };
+    auto pages_of = [&](int block) {
+        Pages r;
+        const int sub = min(i0 + 32 * block + (lane >> 1), i1 - 1);     // behind the last one that one's again
+        r.id = min(max(a.page_table[(int64_t)it.pair * a.pt_stride + min(2 * sub + (lane & 1), last_page)], 0), a.num_pages - 1);
+        return r;
+    };
+    auto scale_pages = [&](Pages& r) {
+        if constexpr (FP8) {
+            const float2 x = *(const float2*)(a.scales + ((int64_t)r.id * a.n_kv + h) * 2);
+            r.k = x.x;
+            r.v = x.y;
+        }
+    };
+    Pages now, ahead;                                                   // of this block of 32 and of the one behind it
+    auto lane_int = [&](int block, int c, int n, int l) {
+        const int x = __builtin_amdgcn_readlane(c, l), y = __builtin_amdgcn_readlane(n, l);
+        return block ? y : x;
+    };
+    auto lane_float = [&](int block, float c, float n, int l) { return __int_as_float(lane_int(block, __float_as_int(c), __float_as_int(n), l)); };
+    // of the sub-tile `on` behind the at-th one
+    auto page_of = [&](int at, int on) { return lane_int((at & 31) + on >> 5, now.id, ahead.id, (2 * (at + on) + my_page) & 63); };
+    auto v_scale_of = [&](int at, int on) { return FP8 ? lane_float((at & 31) + on >> 5, now.v, ahead.v, (2 * (at + on) + my_page) & 63) : 1.0f; };
+    auto scales_at = [&](int at, int on) {
         Scales r;
         if constexpr (FP8) {
-            const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
-            r.k0 = s0[0], r.k1 = s1[0], r.v0 = s0[1], r.v1 = s1[1];
+            const int b = (at & 31) + on >> 5, l = 2 * (at + on) & 63;
+            r.k0 = lane_float(b, now.k, ahead.k, l);
+            r.k1 = lane_float(b, now.k, ahead.k, l + 1);
+            r.v0 = lane_float(b, now.v, ahead.v, l);
+            r.v1 = lane_float(b, now.v, ahead.v, l + 1);
         }
         return r;
     };
@@ -344,28 +372,18 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     // ---- the first sub-tiles are on their way while the rows are read.  Behind the last one that one's again, which nobody reads: what is asked for
     // does not hang on a branch.
     Raw raw[2];
-    int ids[2][2] = {};                                                 // pages of the next sub-tiles that are asked for
-    Scales sc[4];                                                       // fp8: of this sub-tile and those behind it
-    auto ids_of = [&](int sub, int (&r)[2]) {
-        sub = min(sub, i1 - 1);
-        r[0] = id_of(sub, 0);
-        r[1] = id_of(sub, 1);
-    };
     if (i0 < i1) {
+        now = pages_of(0);
+        scale_pages(now);
         if constexpr (FP8) {
-            int r[2];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                ids_of(i0 + e, r);
-                if (e < 2) fetch(my_page ? +r[1] : +r[0], raw[e]);
-                sc[e] = scales_of(r[0], r[1]);
-                if (e >= 2) ids[e - 2][0] = r[0], ids[e - 2][1] = r[1];
-            }
+            fetch(page_of(0, 0), raw[0]);
+            fetch(page_of(0, 1), raw[1]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e) request(id_of(min(i0 + e, i1 - 1), my_page), e);
-            ids[0][0] = id_of(min(i0 + 3, i1 - 1), my_page);
+            for (int e = 0; e < 3; ++e) request(page_of(0, e), e);
         }
+        ahead = pages_of(1);
+        scale_pages(ahead);
     }
     halfx8 q[KC];
     load_q<HD>(a, row, h, hh, q);
@@ -389,11 +407,14 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         __syncthreads();                                                // everyone is past the one before
         if (doc) {
             const int id0 = id_of(sub, 0), id1 = id_of(sub, 1);
-            se = scales_of(id0, id1);
+            if constexpr (FP8) {
+                const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
+                se.k0 = s0[0], se.k1 = s1[0], se.v0 = s0[1], se.v1 = s1[1];
+            }
             if constexpr (FP8) {
                 Raw r;
                 fetch(my_page ? id1 : id0, r);
-                expand(r, 3, my_page ? +se.v1 : +se.v0);
+                expand(r, 3, pick(my_page, se.v0, se.v1));
             } else {
                 request(my_page ? id1 : id0, 3);
                 __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0)
@@ -438,75 +459,70 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             }
             return EXTRA ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
         };
-        auto step = [&](int i, Raw& r, int (&next)[2]) {
+        auto step = [&](int i, Raw& r) {
             const int at = i - i0;
             // everyone has the next sub-tile, and is past the one before: its slot is free
             if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
             __syncthreads();
+            if ((at & 31) == 0 && at > 0) {
+                now = ahead;
+                ahead = pages_of((at >> 5) + 1);
+                scale_pages(ahead);
+            }
             if constexpr (FP8) {
-                expand(r, (at + 2) & 3, my_page ? +sc[2].v1 : +sc[2].v0);
-                fetch(my_page ? +next[1] : +next[0], r);
+                expand(r, (at + 2) & 3, v_scale_of(at, 2));
+                fetch(page_of(at, 4), r);
             } else {
-                request(next[0], (at + 3) & 3);
-                next[0] = id_of(min(i + 4, i1 - 1), my_page);
+                request(page_of(at, 3), (at + 3) & 3);
             }
-            if (active) {
-                const int ks = (at + 1) & 3, vs = at & 3;
-                const float alpha = sm.follow(row_max2(mx)), use = sm.used();
-                rescale(alpha);
-                floatx16 sn = {};
+            if (!active) return;
+            const int ks = (at + 1) & 3, vs = at & 3;
+            const Scales c = scales_at(at, 0), cn = scales_at(at, 1);
+            const float alpha = sm.follow(row_max2(mx)), use = sm.used();
+            rescale(alpha);
+            floatx16 sn = {};
 #pragma unroll
-                for (int kk = 0; kk < KC; ++kk) sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(ks, kk), q[kk], sn, 0, 0, 0);
-                const float c0 = EXTRA ? 1.0f : a.scale_log2 * sc[0].k0, c1 = EXTRA ? 1.0f : a.scale_log2 * sc[0].k1;
-                float sum = 0.0f;
+            for (int kk = 0; kk < KC; ++kk) sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(ks, kk), q[kk], sn, 0, 0, 0);
+            const float c0 = EXTRA ? 1.0f : a.scale_log2 * c.k0, c1 = EXTRA ? 1.0f : a.scale_log2 * c.k1;
+            float sum = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], FP8 ? (e < 8 ? c0 : c1) : EXTRA ? 1.0f : a.scale_log2, -use));
-                    sum += s[e];
-                }
-                sm.l = fmaf(sm.l, alpha, sum);
-                halfx8 p[2];
-                pack_p(s, p, FP8 ? fp8_scale_mantissa(sc[0].v0) : 1.0f, FP8 ? fp8_scale_mantissa(sc[0].v1) : 1.0f);
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(vs, mb, e), p[e], o[mb], 0, 0, 0);
-                mx = largest(sn, 32 * (i + 1), sc[1]);
-                s = sn;
+            for (int e = 0; e < 16; ++e) {
+                s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], e < 8 ? c0 : c1, -use));
+                sum += s[e];
             }
-            if constexpr (FP8) {
-                sc[0] = sc[1];
-                sc[1] = sc[2];
-                sc[2] = sc[3];
-                sc[3] = scales_of(next[0], next[1]);
-                ids_of(i + 6, next);
-            }
+            sm.l = fmaf(sm.l, alpha, sum);
+            halfx8 p[2];
+            pack_p(s, p, FP8 ? fp8_scale_mantissa(c.v0) : 1.0f, FP8 ? fp8_scale_mantissa(c.v1) : 1.0f);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(vs, mb, e), p[e], o[mb], 0, 0, 0);
+            mx = largest(sn, 32 * (i + 1), cn);
+            s = sn;
         };
         if constexpr (FP8) {
-            expand(raw[0], 0, my_page ? +sc[0].v1 : +sc[0].v0);
-            expand(raw[1], 1, my_page ? +sc[1].v1 : +sc[1].v0);
-            fetch(my_page ? +ids[0][1] : +ids[0][0], raw[0]);
-            fetch(my_page ? +ids[1][1] : +ids[1][0], raw[1]);
-            ids_of(i0 + 4, ids[0]);
-            ids_of(i0 + 5, ids[1]);
+            expand(raw[0], 0, v_scale_of(0, 0));
+            expand(raw[1], 1, v_scale_of(0, 1));
+            fetch(page_of(0, 2), raw[0]);
+            fetch(page_of(0, 3), raw[1]);
         } else {
-            __builtin_amdgcn_s_waitcnt(0x0F70 | (2 * T::LOADS));
+            __builtin_amdgcn_s_waitcnt(0x0F70);                         // the pages' numbers came behind the first blocks
         }
         __syncthreads();
         if (active) {
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(0, kk), q[kk], s, 0, 0, 0);
-            mx = largest(s, 32 * i0, sc[0]);
+            mx = largest(s, 32 * i0, scales_at(0, 0));
         }
         int i = i0;
         if constexpr (FP8) {
             for (; i + 1 < i1; i += 2) {
-                step(i, raw[0], ids[0]);
-                step(i + 1, raw[1], ids[1]);
+                step(i, raw[0]);
+                step(i + 1, raw[1]);
             }
-            if (i < i1) step(i, raw[0], ids[0]);
+            if (i < i1) step(i, raw[0]);
         } else {
-            for (; i < i1; ++i) step(i, raw[0], ids[0]);
+            for (; i < i1; ++i) step(i, raw[0]);
         }
     }
     // ---- out
