@@ -27,7 +27,7 @@ struct PairAttnArgs {
     const int32_t* page_table;
     int32_t pt_stride, n_kv, g, most_splits;
     int32_t num_pages, d, window, own_keys;
-    int32_t n_pairs, max_tokens;
+    int32_t n_pairs, max_tokens, chunk;
     int64_t cap_blk, cap_tile;        // records of the work list
     const int32_t *q_cu, *prefix;
     const char* pool;                 // page 0 of the layer
@@ -57,11 +57,11 @@ __device__ __forceinline__ int rows_min(int v) {          // over the 32 rows of
 }
 __device__ __forceinline__ int rows_max(int v) { return -rows_min(-v); }
 
-// Consecutive workgroups go to the 8 XCDs in turn: XCD x takes the x-th eighth of the items, so that the blocks and kv heads of a group, which
-// share pages, meet in one L2.
-__device__ __forceinline__ int item_of(int wg, int items) {
-    const int per = (items + 7) / 8, at = (wg & 7) * per + (wg >> 3);
-    return (wg >> 3) < per && at < items ? at : -1;
+// Consecutive workgroups go to the 8 XCDs in turn: of every 8 << c items XCD x takes 1 << c that follow each other, so that the kv heads and
+// the neighbouring tiles of a group, which share pages, meet in one L2.  (Eighths of all items would take a look at their number first.)
+// chunk = c; 0 where keys are cut into pieces: few items, that are to be spread.
+__device__ __forceinline__ int item_of(int wg, int chunk) {
+    return (wg >> (3 + chunk) << (3 + chunk)) + ((wg & 7) << chunk) + (wg >> 3 & ((1 << chunk) - 1));
 }
 
 // What the work list says.  Tables that were not built, or not for this call, are taken for what they can at most be: every index below stays inside
@@ -75,7 +75,7 @@ __device__ __forceinline__ int list_items(const PairAttnArgs& a, bool tiles) {
     return (int)min((int64_t)hdr[tiles ? SH_TILES : SH_BLOCKS], tiles ? a.cap_tile : a.cap_blk) * a.n_kv;
 }
 __device__ __forceinline__ PairItem list_item(const PairAttnArgs& a, bool tiles, int at) {
-    const const_int_t r = (const_int_t)((tiles ? a.rec_tiles : a.rec) + 2 * (int64_t)at);
+    const const_int_t r = (const_int_t)((tiles ? a.rec_tiles : a.rec) + 2 * min((int64_t)at, (tiles ? a.cap_tile : a.cap_blk) - 1));
     PairItem it;
     it.pair = min(max(r[0], 0), a.n_pairs - 1);
     it.D = (int)min((int64_t)max(r[1], 0), (int64_t)a.pt_stride * kPageTokens);

@@ -42,9 +42,9 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
     constexpr bool FP8 = sizeof(PT) == 1;
     extern __shared__ __attribute__((aligned(16))) float smem[];
     const int items = list_items(a, false);
-    const int item = item_of((int)blockIdx.x, items);
+    const int item = item_of((int)blockIdx.x, a.chunk);
     const int pieces = pair_choice(items, items, a.d, a.most_splits).pieces;
-    if (item < 0 || (int)blockIdx.y >= pieces) return;
+    if (item >= items || (int)blockIdx.y >= pieces) return;
     const int blk = item / a.n_kv, h = item - blk * a.n_kv;
     const PairItem it = list_item(a, false, blk);
     const int D = it.D, d = a.d;
@@ -296,7 +296,9 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
     a.part_o = (float*)((char*)workspace + w.o);
     a.part_rows = (int64_t)t->max_tokens * t->n_q_heads;
     const int64_t items = s.cap_blk * lay.n_kv;
-    const dim3 grid((unsigned)((items + 7) / 8 * 8), (unsigned)w.most);
+    while (w.most == 1 && a.chunk < 5 && 1 << a.chunk < 2 * lay.n_kv) ++a.chunk;
+    const int64_t round = 8 << a.chunk;
+    const dim3 grid((unsigned)((items + round - 1) / round * round), (unsigned)w.most);
     hipError_t e;
     a.rec_tiles = (const int4*)(S + s.tile);
     const bool half = lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 128);

@@ -239,7 +239,6 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     constexpr int KC = G::KC, MB = G::MB, NW = kPairWaves;
     const int D = it.D;
     const int lane = threadIdx.x & 63, ln = lane & 31, hh = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const const_int_t pt = (const_int_t)(a.page_table + (int64_t)it.pair * a.pt_stride);
     const int64_t page_stride = (int64_t)a.n_kv * 2 * G::BLOCK;
     const int last_page = (D - 1) / kPageTokens, last_row = min(it.row + kPairTileRows, it.rows) - 1;
 
@@ -271,18 +270,20 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         wg.ohi = __builtin_amdgcn_readfirstlane(wg.ohi);
         __syncthreads();
     }
-    // this piece's sub-tiles, in the order of pair_rows
+    // this piece's sub-tiles, in the order of pair_rows: whole ones, those at the window's edge, the document's last if it is not whole, own keys
     const int doc0 = wg.dlo / 32, doc1 = (D + 31) / 32, whole0 = (wg.dlo_all + 31) / 32, whole1 = max(D / 32, whole0);
     const int n_whole = whole1 - whole0, n_doc = max(doc1 - doc0, 0), n_own = a.own_keys ? (wg.ohi - wg.olo + 31) / 32 : 0;
-    const int n_sub = n_doc + n_own, share = (n_sub + pieces - 1) / pieces;
-    const int u0 = (int)blockIdx.y * share, u1 = min(u0 + share, n_sub);
+    const int share = (n_doc + n_own + pieces - 1) / pieces, u0 = (int)blockIdx.y * share, u1 = min(u0 + share, n_doc + n_own);
     const int i0 = whole0 + min(u0, n_whole), i1 = whole0 + min(u1, n_whole);      // whole ones
+    const int own0 = max(u0, n_doc);
+    // the last one follows the whole ones through the ring
+    const bool tail = i0 < i1 && i1 == whole1 && whole1 < doc1 && u1 >= n_doc;
+    const int i_last = i1 - 1 + (tail ? 1 : 0);
 
     // ---- a sub-tile in the ring: K of its two pages, V of its two pages; wavefront w brings page w & 1's K (w < 2) or V
     const int my_page = wave & 1;
     const char* block0 = a.pool + ((int64_t)h * 2 + (wave >> 1)) * G::BLOCK;
     char* const my_part = smem + (wave >> 1) * 2 * T::HBLOCK + my_page * T::HBLOCK;
-    auto id_of = [&](int sub, int page) { return min(max(pt[min(2 * sub + page, last_page)], 0), a.num_pages - 1); };
     auto request = [&](int id, int slot) {                              // a half block, verbatim
         const char* src = block0 + id * page_stride + lane * 16;
         char* dst = my_part + slot * T::SLOT;
@@ -307,12 +308,12 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     };
     // fp8: scales of a sub-tile's two pages
     struct Scales { float k0 = 1.0f, k1 = 1.0f, v0 = 1.0f, v1 = 1.0f; };      // half pages: one
-    // The pages of the whole sub-tiles, 32 sub-tiles at a time: a lane has the id and the scales of one page.  Lane reads cost the loop no wait; requests
+    // The pages of the sub-tiles, 32 sub-tiles at a time: a lane has the id and the scales of one page.  Lane reads cost the loop no wait; requests
     // through the scalar cache would share the counter of the LDS reads, and out of order, so that each of those waited for all.
     struct Pages { int id; float k, v; };
     auto pages_of = [&](int block) {
         Pages r;
-        const int sub = min(i0 + 32 * block + (lane >> 1), i1 - 1);     // behind the last one that one's again
+        const int sub = min(i0 + 32 * block + (lane >> 1), i_last);      // behind the last one that one's again
         r.id = min(max(a.page_table[(int64_t)it.pair * a.pt_stride + min(2 * sub + (lane & 1), last_page)], 0), a.num_pages - 1);
         return r;
     };
@@ -344,23 +345,27 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         return r;
     };
     // 32 own keys from place key0 on: eight threads have a key, each its share of the channels
-    auto own_keys = [&](int key0, int slot) {
-        constexpr int CH = HD / 8;
-        const int key = threadIdx.x & 31, c0 = (threadIdx.x >> 5) * CH, t = key & 15;
-        const int64_t token = own_token(a, min(key0 + key, wg.ohi - 1));
-        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs + c0, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs + c0;
-        half_t* dst = (half_t*)(smem + slot * T::SLOT + (key >> 4) * T::HBLOCK);
-        halfx8 kx[CH / 8], vx[CH / 8];
+    constexpr int CH = HD / 8;
+    const int own_key = threadIdx.x & 31, own_c = (threadIdx.x >> 5) * CH;
+    struct Own { VecN<bf16_t, 8> k[CH / 8], v[CH / 8]; };
+    auto load_own = [&](int key0, Own& x) {
+        const int64_t token = own_token(a, min(key0 + own_key, wg.ohi - 1));
+        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs + own_c, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs + own_c;
 #pragma unroll
         for (int e = 0; e < CH / 8; ++e) {
-            kx[e] = bf16x8_to_half(kp + e * 8);
-            vx[e] = bf16x8_to_half(vp + e * 8);
+            x.k[e] = ((const Loose<bf16_t, 8>*)(kp + e * 8))->w;
+            x.v[e] = ((const Loose<bf16_t, 8>*)(vp + e * 8))->w;
         }
+    };
+    auto store_own = [&](const Own& x, int slot) {
+        const int t = own_key & 15;
+        half_t* dst = (half_t*)(smem + slot * T::SLOT + (own_key >> 4) * T::HBLOCK);
 #pragma unroll
         for (int e = 0; e < CH / 8; ++e) {
-            *(halfx8*)(dst + k_elem(t, c0 + e * 8, HD, 2)) = kx[e];
+            *(halfx8*)(dst + k_elem(t, own_c + e * 8, HD, 2)) = to_half8(x.k[e]);
+            const halfx8 v = to_half8(x.v[e]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[T::HBLOCK + v_elem(t, c0 + e * 8 + i, HD)] = vx[e][i];      // V two blocks on
+            for (int i = 0; i < 8; ++i) dst[T::HBLOCK + v_elem(t, own_c + e * 8 + i, HD)] = v[i];      // V two blocks on
         }
     };
     auto k_frag = [&](int slot, int kk) {
@@ -385,6 +390,8 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         ahead = pages_of(1);
         scale_pages(ahead);
     }
+    Own own;                                                            // needed behind the document
+    if (own0 < u1) load_own(wg.olo + 32 * (own0 - n_doc), own);
     halfx8 q[KC];
     load_q<HD>(a, row, h, hh, q);
     floatx16 o[MB];
@@ -398,48 +405,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         }
     };
 
-    // ---- sub-tiles at an edge and own keys, in the ring's last slot
-    for (int u = max(u0, n_whole); u < u1; ++u) {
-        const bool doc = u < n_doc;
-        const int sub = u - n_whole < whole0 - doc0 ? doc0 + u - n_whole : doc0 + u;
-        const int key0 = doc ? 32 * sub : wg.olo + (u - n_doc) * 32, end = doc ? D : wg.ohi;
-        Scales se;
-        __syncthreads();                                                // everyone is past the one before
-        if (doc) {
-            const int id0 = id_of(sub, 0), id1 = id_of(sub, 1);
-            if constexpr (FP8) {
-                const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
-                se.k0 = s0[0], se.k1 = s1[0], se.v0 = s0[1], se.v1 = s1[1];
-            }
-            if constexpr (FP8) {
-                Raw r;
-                fetch(my_page ? id1 : id0, r);
-                expand(r, 3, pick(my_page, se.v0, se.v1));
-            } else {
-                request(my_page ? id1 : id0, 3);
-                __builtin_amdgcn_s_waitcnt(0x0F70);                     // vmcnt(0)
-            }
-        } else {
-            own_keys(key0, 3);
-        }
-        __syncthreads();
-        if (!active || (doc ? key0 + 32 <= mine.dlo : key0 + 32 <= mine.olo || key0 >= mine.ohi)) continue;      // seen by none of the rows
-        floatx16 s = {};
-#pragma unroll
-        for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(3, kk), q[kk], s, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= a.scale_log2 * (r < 8 ? se.k0 : se.k1);
-        if (EXTRA) pair_scores<false>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
-        const int lo = (doc ? row.dlo : row.olo) - key0, hi = (doc ? D : row.ohi) - key0;
-        hide_keys(s, lo - 4 * hh, hi - 4 * hh);
-        rescale(pair_softmax(sm, s));
-        halfx8 pf[2];
-        pack_p(s, pf, FP8 ? fp8_scale_mantissa(se.v0) : 1.0f, FP8 ? fp8_scale_mantissa(se.v1) : 1.0f);
-        add_pv_masked<MB>(o, pf, lo, hi, min(end - key0, 32), hh, [&](int mb, int e) { return v_frag(3, mb, e); },
-                          [&](int key, int ch) { return ((const half_t*)(smem + 3 * T::SLOT + (2 + (key >> 4)) * T::HBLOCK))[v_elem(key & 15, ch, HD)]; });
-    }
-
-    // ---- whole sub-tiles.  S of one is computed next to the exponentials of the one before, and its maxima next to that one's V P: a wavefront issues in
+    // ---- the document.  S of one sub-tile is computed next to the exponentials of the one before, and its maxima next to that one's V P: a wavefront issues in
     // order, and without the other's arithmetic between them it would wait 32 cycles for each of its matrix instructions
     if (i0 < i1) {
         floatx16 s = {};
@@ -480,10 +446,10 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             const Scales c = scales_at(at, 0), cn = scales_at(at, 1);
             const float alpha = sm.follow(row_max2(mx)), use = sm.used();
             rescale(alpha);
+            const float c0 = EXTRA ? 1.0f : a.scale_log2 * c.k0, c1 = EXTRA ? 1.0f : a.scale_log2 * c.k1;
             floatx16 sn = {};
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk) sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(ks, kk), q[kk], sn, 0, 0, 0);
-            const float c0 = EXTRA ? 1.0f : a.scale_log2 * c.k0, c1 = EXTRA ? 1.0f : a.scale_log2 * c.k1;
             float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -524,6 +490,52 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         } else {
             for (; i < i1; ++i) step(i, raw[0]);
         }
+    }
+    // ---- sub-tiles at an edge, and own keys
+#pragma unroll 1
+    for (int u = max(u0, n_whole); u < u1; ++u) {
+        const bool doc = u < n_doc, in_ring = tail && u == n_doc - 1;
+        const int sub = u - n_whole < whole0 - doc0 ? doc0 + u - n_whole : doc0 + u;
+        const int key0 = doc ? 32 * sub : wg.olo + (u - n_doc) * 32, end = doc ? D : wg.ohi;
+        const int slot = in_ring ? (i1 - i0) & 3 : (i1 - i0 + 1) & 3;
+        Scales c;
+        __builtin_amdgcn_s_waitcnt(0x0F70);                             // nothing is on its way into LDS
+        __syncthreads();                                                // everyone is past the sub-tile before
+        if (doc) {
+            const const_int_t pt = (const_int_t)(a.page_table + (int64_t)it.pair * a.pt_stride);
+            const int id0 = min(max(pt[min(2 * sub, last_page)], 0), a.num_pages - 1), id1 = min(max(pt[min(2 * sub + 1, last_page)], 0), a.num_pages - 1);
+            if constexpr (FP8) {
+                const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
+                c.k0 = s0[0], c.k1 = s1[0], c.v0 = s0[1], c.v1 = s1[1];
+            }
+            if (!in_ring) {
+                if constexpr (FP8) {
+                    fetch(pick(my_page, id0, id1), raw[0]);
+                    expand(raw[0], slot, pick(my_page, c.v0, c.v1));
+                } else {
+                    request(pick(my_page, id0, id1), slot);
+                    __builtin_amdgcn_s_waitcnt(0x0F70);
+                }
+            }
+        } else {
+            store_own(own, slot);
+            if (u + 1 < u1) load_own(key0 + 32, own);
+        }
+        __syncthreads();
+        if (!active || (doc ? key0 + 32 <= mine.dlo : key0 + 32 <= mine.olo || key0 >= mine.ohi)) continue;      // seen by none of the rows
+        floatx16 s = {};
+#pragma unroll
+        for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(slot, kk), q[kk], s, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= a.scale_log2 * (r < 8 ? c.k0 : c.k1);
+        if (EXTRA) pair_scores<false>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        const int lo = (doc ? row.dlo : row.olo) - key0, hi = (doc ? D : row.ohi) - key0;
+        hide_keys(s, lo - 4 * hh, hi - 4 * hh);
+        rescale(pair_softmax(sm, s));
+        halfx8 p[2];
+        pack_p(s, p, FP8 ? fp8_scale_mantissa(c.v0) : 1.0f, FP8 ? fp8_scale_mantissa(c.v1) : 1.0f);
+        add_pv_masked<MB>(o, p, lo, hi, min(end - key0, 32), hh, [&](int mb, int e) { return v_frag(slot, mb, e); },
+                          [&](int key, int ch) { return ((const half_t*)(smem + slot * T::SLOT + (2 + (key >> 4)) * T::HBLOCK))[v_elem(key & 15, ch, HD)]; });
     }
     // ---- out
     __builtin_amdgcn_s_waitcnt(0x0F70);                                 // nothing is on its way into LDS
@@ -574,12 +586,13 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
 template <int HD, bool FP8, bool EXTRA>
 __global__ void __launch_bounds__(kPairWaves * 64) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2, 8))) pair_attn_half_kernel(PairAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    // the item's record as either kind is asked for together with the counts that say which kind it is
+    const int item = item_of((int)blockIdx.x, a.chunk), at = item / a.n_kv, h = item - at * a.n_kv;
+    const PairItem block = list_item(a, false, at), tile = list_item(a, true, at);
     const int blocks = list_items(a, false), tiles = list_items(a, true);
     const PairChoice ch = pair_choice(blocks, tiles, HD, a.most_splits);
-    const int item = item_of((int)blockIdx.x, ch.tiles ? tiles : blocks);
-    if (item < 0 || (int)blockIdx.y >= ch.pieces) return;
-    const int at = item / a.n_kv, h = item - at * a.n_kv;
-    const PairItem it = list_item(a, ch.tiles, at);
+    if (item >= (ch.tiles ? tiles : blocks) || (int)blockIdx.y >= ch.pieces) return;
+    const PairItem it = ch.tiles ? tile : block;
     if (ch.tiles) pair_tile<HD, FP8, EXTRA>(a, smem, it, h, ch.pieces);
     else pair_rows<HD, FP8, EXTRA>(a, (float*)smem, it, h, ch.pieces);
 }

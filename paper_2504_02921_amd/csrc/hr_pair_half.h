@@ -13,13 +13,13 @@ struct PairGeo {
     using Piece = std::conditional_t<FP8, uint2, halfx8>;     // 8 elements of a page
 };
 
-__device__ __forceinline__ halfx8 bf16x8_to_half(const bf16_t* p) {
-    const Loose<bf16_t, 8> x = *(const Loose<bf16_t, 8>*)p;
+__device__ __forceinline__ halfx8 to_half8(VecN<bf16_t, 8> x) {
     halfx8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (half_t)(float)x.w[e];       // beyond the half range: infinity
+    for (int e = 0; e < 8; ++e) r[e] = (half_t)(float)x[e];         // beyond the half range: infinity
     return r;
 }
+__device__ __forceinline__ halfx8 bf16x8_to_half(const bf16_t* p) { return to_half8(((const Loose<bf16_t, 8>*)p)->w); }
 
 // the lane's 16 probabilities as the B operands of two products over 16 keys each
 __device__ __forceinline__ void pack_p(const floatx16& s, halfx8 (&pf)[2], float f0, float f1) {
