@@ -274,11 +274,13 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     const int doc0 = wg.dlo / 32, doc1 = (D + 31) / 32, whole0 = (wg.dlo_all + 31) / 32, whole1 = max(D / 32, whole0);
     const int n_whole = whole1 - whole0, n_doc = max(doc1 - doc0, 0), n_own = a.own_keys ? (wg.ohi - wg.olo + 31) / 32 : 0;
     const int share = (n_doc + n_own + pieces - 1) / pieces, u0 = (int)blockIdx.y * share, u1 = min(u0 + share, n_doc + n_own);
-    const int i0 = whole0 + min(u0, n_whole), i1 = whole0 + min(u1, n_whole);      // whole ones
     const int own0 = max(u0, n_doc);
-    // the last one follows the whole ones through the ring
-    const bool tail = i0 < i1 && i1 == whole1 && whole1 < doc1 && u1 >= n_doc;
-    const int i_last = i1 - 1 + (tail ? 1 : 0);
+    // those of the document go through the ring: n_ring of them, whole ones first
+    const int n_ring = max(min(u1, n_doc) - u0, 0), n_ring_whole = max(min(u1, n_whole) - u0, 0);
+    auto sub_of = [&](int at) {
+        const int u = u0 + at;
+        return u < n_whole ? whole0 + u : u - n_whole < whole0 - doc0 ? doc0 + u - n_whole : doc0 + u;
+    };
 
     // ---- a sub-tile in the ring: K of its two pages, V of its two pages; wavefront w brings page w & 1's K (w < 2) or V
     const int my_page = wave & 1;
@@ -313,7 +315,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     struct Pages { int id; float k, v; };
     auto pages_of = [&](int block) {
         Pages r;
-        const int sub = min(i0 + 32 * block + (lane >> 1), i_last);      // behind the last one that one's again
+        const int sub = sub_of(min(32 * block + (lane >> 1), n_ring - 1));      // behind the last one that one's again
         r.id = min(max(a.page_table[(int64_t)it.pair * a.pt_stride + min(2 * sub + (lane & 1), last_page)], 0), a.num_pages - 1);
         return r;
     };
@@ -377,7 +379,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     // ---- the first sub-tiles are on their way while the rows are read.  Behind the last one that one's again, which nobody reads: what is asked for
     // does not hang on a branch.
     Raw raw[2];
-    if (i0 < i1) {
+    if (n_ring > 0) {
         now = pages_of(0);
         scale_pages(now);
         if constexpr (FP8) {
@@ -405,9 +407,36 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         }
     };
 
-    // ---- the document.  S of one sub-tile is computed next to the exponentials of the one before, and its maxima next to that one's V P: a wavefront issues in
+    // At the at-th sub-tile: everyone has the next one, and is past the one before, whose slot is free
+    auto advance = [&](int at, Raw& r) {
+        if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
+        __syncthreads();
+        if ((at & 31) == 0 && at > 0) {
+            now = ahead;
+            ahead = pages_of((at >> 5) + 1);
+            scale_pages(ahead);
+        }
+        if constexpr (FP8) {
+            expand(r, (at + 2) & 3, v_scale_of(at, 2));
+            fetch(page_of(at, 4), r);
+        } else {
+            request(page_of(at, 3), (at + 3) & 3);
+        }
+    };
+    if (n_ring > 0) {
+        if constexpr (FP8) {
+            expand(raw[0], 0, v_scale_of(0, 0));
+            expand(raw[1], 1, v_scale_of(0, 1));
+            fetch(page_of(0, 2), raw[0]);
+            fetch(page_of(0, 3), raw[1]);
+        } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                         // the pages' numbers came behind the first blocks
+        }
+        __syncthreads();
+    }
+    // ---- whole sub-tiles.  S of one is computed next to the exponentials of the one before, and its maxima next to that one's V P: a wavefront issues in
     // order, and without the other's arithmetic between them it would wait 32 cycles for each of its matrix instructions
-    if (i0 < i1) {
+    if (n_ring_whole > 0) {
         floatx16 s = {};
         float mx = 0.0f;
         // the largest of a lane's raw scores, scaled where they are scaled later; EXTRA: scaled, capped and biased in place
@@ -425,22 +454,8 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             }
             return EXTRA ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
         };
-        auto step = [&](int i, Raw& r) {
-            const int at = i - i0;
-            // everyone has the next sub-tile, and is past the one before: its slot is free
-            if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
-            __syncthreads();
-            if ((at & 31) == 0 && at > 0) {
-                now = ahead;
-                ahead = pages_of((at >> 5) + 1);
-                scale_pages(ahead);
-            }
-            if constexpr (FP8) {
-                expand(r, (at + 2) & 3, v_scale_of(at, 2));
-                fetch(page_of(at, 4), r);
-            } else {
-                request(page_of(at, 3), (at + 3) & 3);
-            }
+        auto step = [&](int at, Raw& r) {
+            advance(at, r);
             if (!active) return;
             const int ks = (at + 1) & 3, vs = at & 3;
             const Scales c = scales_at(at, 0), cn = scales_at(at, 1);
@@ -463,65 +478,43 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(vs, mb, e), p[e], o[mb], 0, 0, 0);
-            mx = largest(sn, 32 * (i + 1), cn);
+            mx = largest(sn, 32 * (whole0 + u0 + at + 1), cn);
             s = sn;
         };
-        if constexpr (FP8) {
-            expand(raw[0], 0, v_scale_of(0, 0));
-            expand(raw[1], 1, v_scale_of(0, 1));
-            fetch(page_of(0, 2), raw[0]);
-            fetch(page_of(0, 3), raw[1]);
-        } else {
-            __builtin_amdgcn_s_waitcnt(0x0F70);                         // the pages' numbers came behind the first blocks
-        }
-        __syncthreads();
         if (active) {
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(0, kk), q[kk], s, 0, 0, 0);
-            mx = largest(s, 32 * i0, scales_at(0, 0));
+            mx = largest(s, 32 * (whole0 + u0), scales_at(0, 0));
         }
-        int i = i0;
+        int at = 0;
         if constexpr (FP8) {
-            for (; i + 1 < i1; i += 2) {
-                step(i, raw[0]);
-                step(i + 1, raw[1]);
+            for (; at + 1 < n_ring_whole; at += 2) {
+                step(at, raw[0]);
+                step(at + 1, raw[1]);
             }
-            if (i < i1) step(i, raw[0]);
+            if (at < n_ring_whole) step(at, raw[0]);
         } else {
-            for (; i < i1; ++i) step(i, raw[0]);
+            for (; at < n_ring_whole; ++at) step(at, raw[0]);
         }
     }
     // ---- sub-tiles at an edge, and own keys
 #pragma unroll 1
-    for (int u = max(u0, n_whole); u < u1; ++u) {
-        const bool doc = u < n_doc, in_ring = tail && u == n_doc - 1;
-        const int sub = u - n_whole < whole0 - doc0 ? doc0 + u - n_whole : doc0 + u;
-        const int key0 = doc ? 32 * sub : wg.olo + (u - n_doc) * 32, end = doc ? D : wg.ohi;
-        const int slot = in_ring ? (i1 - i0) & 3 : (i1 - i0 + 1) & 3;
+    for (int u = u0 + n_ring_whole; u < u1; ++u) {
+        const bool doc = u < n_doc;
+        const int at = u - u0, slot = doc ? at & 3 : 0;
+        const int key0 = 32 * (doc ? sub_of(at) : u - n_doc) + (doc ? 0 : wg.olo), end = doc ? D : wg.ohi;
         Scales c;
-        __builtin_amdgcn_s_waitcnt(0x0F70);                             // nothing is on its way into LDS
-        __syncthreads();                                                // everyone is past the sub-tile before
         if (doc) {
-            const const_int_t pt = (const_int_t)(a.page_table + (int64_t)it.pair * a.pt_stride);
-            const int id0 = min(max(pt[min(2 * sub, last_page)], 0), a.num_pages - 1), id1 = min(max(pt[min(2 * sub + 1, last_page)], 0), a.num_pages - 1);
-            if constexpr (FP8) {
-                const const_float_t s0 = (const_float_t)(a.scales + ((int64_t)id0 * a.n_kv + h) * 2), s1 = (const_float_t)(a.scales + ((int64_t)id1 * a.n_kv + h) * 2);
-                c.k0 = s0[0], c.k1 = s1[0], c.v0 = s0[1], c.v1 = s1[1];
-            }
-            if (!in_ring) {
-                if constexpr (FP8) {
-                    fetch(pick(my_page, id0, id1), raw[0]);
-                    expand(raw[0], slot, pick(my_page, c.v0, c.v1));
-                } else {
-                    request(pick(my_page, id0, id1), slot);
-                    __builtin_amdgcn_s_waitcnt(0x0F70);
-                }
-            }
+            if (FP8 && (at & 1)) advance(at, raw[1]);
+            else advance(at, raw[0]);
+            c = scales_at(at, 0);
         } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                         // nothing is on its way into LDS
+            __syncthreads();                                            // everyone is past the sub-tile before
             store_own(own, slot);
             if (u + 1 < u1) load_own(key0 + 32, own);
+            __syncthreads();
         }
-        __syncthreads();
         if (!active || (doc ? key0 + 32 <= mine.dlo : key0 + 32 <= mine.olo || key0 >= mine.ohi)) continue;      // seen by none of the rows
         floatx16 s = {};
 #pragma unroll

@@ -34,34 +34,39 @@ __device__ __forceinline__ void pack_p(const floatx16& s, halfx8 (&pf)[2], float
 
 // Hides the keys of a sub-tile outside [lo, hi), relative to the lane's first
 __device__ __forceinline__ void hide_keys(floatx16& s, int lo, int hi) {
+    const unsigned n = (unsigned)max(hi - lo, 0);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int key = 8 * (r >> 2) + (r & 3);
-        s[r] = key >= lo && key < hi ? s[r] : -INFINITY;
-    }
+    for (int r = 0; r < 16; ++r) s[r] = (unsigned)(8 * (r >> 2) + (r & 3) - lo) < n ? s[r] : -INFINITY;
 }
 
 // O^T += V^T P^T over a sub-tile that not every row sees whole.  A hidden key's V counts for nothing, whatever it holds, and 0 times infinity is
-// not nothing: the product has zeros for what is not finite and for keys from `exist` on, and what is not finite is added (rarely, value by value)
-// to the rows that see it.  frag(mb, e): the lane's V operand; value(key, ch): one value of the sub-tile; [lo, hi): the keys that the row sees.
+// not nothing: where a value is not finite (rarely: 0 times all of them is summed, and is NaN then) the product has zeros for those, and they are added
+// value by value to the rows that see them, [lo, hi) of the first `exist` keys.  frag(mb, e): the lane's V operand; value(key, ch): one value.
 template <int MB, typename Frag, typename Value>
 __device__ __forceinline__ void add_pv_masked(floatx16 (&o)[MB], const halfx8 (&pf)[2], int lo, int hi, int exist, int hh, Frag frag, Value value) {
-    bool odd = false;
+    halfx2 none[4] = {};
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
+    for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const halfx8 v = frag(mb, e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) none[i] = __builtin_elementwise_fma(halfx2{v[2 * i], v[2 * i + 1]}, halfx2{}, none[i]);
+        }
+    const halfx2 odd = (none[0] + none[1]) + (none[2] + none[3]);
+    const bool fix = __any(odd[0] != odd[0] || odd[1] != odd[1]);
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             halfx8 v = frag(mb, e);
+            if (fix) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool there = 16 * e + 8 * (i >> 2) + (i & 3) + 4 * hh < exist, fine = __builtin_fabsf16(v[i]) < (half_t)INFINITY;
-                odd = odd || (there && !fine);
-                v[i] = there && fine ? v[i] : (half_t)0.0f;
+                for (int i = 0; i < 8; ++i) v[i] = __builtin_fabsf16(v[i]) < (half_t)INFINITY ? v[i] : (half_t)0.0f;
             }
             o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, pf[e], o[mb], 0, 0, 0);
         }
-    }
-    if (!__any(odd)) return;
+    if (!fix) return;
 #pragma unroll 1
     for (int key = 0; key < exist; ++key) {
 #pragma unroll
