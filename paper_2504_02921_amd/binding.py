@@ -394,20 +394,28 @@ class KVPool:
 ROPE_LAYOUT = {"half": 0, "interleaved": 1}
 ROPE_SCALING = {"none": 0, "linear": 1, "base": 2, "bands": 3, "ramp": 4}
 TABLES_BAD_DOC, TABLES_BAD_LENGTH, TABLES_CUT, TABLES_BAD_PAGE = 1, 2, 4, 8
-_ACT_CODE: Dict[str, int] = {"torch.float32": HR_F32, "torch.bfloat16": HR_BF16}
+_ACT_CODE: Dict = {}      # torch.dtype -> hr_dtype of activations
+
+
+def _act_code(dtype) -> Optional[int]:
+    if not _ACT_CODE:
+        import torch
+        _ACT_CODE.update({torch.float32: HR_F32, torch.bfloat16: HR_BF16})
+    return _ACT_CODE.get(dtype)
 
 
 def _refuse(what: str):
     raise HrError(HR_ERR_INVALID_ARG, what)
 
 
-def _rows(t, heads: Optional[int], d: int, device, dtype, what: str):
-    """Checks a tensor [tokens][heads][head_dim] whose channels follow each other."""
-    if t.dim() != 3 or t.shape[2] != d or (heads is not None and t.shape[1] != heads) or (d > 1 and t.numel() > 0 and t.stride(2) != 1):
-        _refuse(f"{what}: [tokens][{heads if heads is not None else 'heads'}][{d}] with adjacent channels expected, got {tuple(t.shape)}")
-    if t.device != device or t.dtype != dtype:
-        _refuse(f"{what}: a {dtype} tensor on {device} expected, got {t.dtype} on {t.device}")
-    return t
+def _strides(t, rows: int, heads: Optional[int], d: int, like, what: str):
+    """(heads, token stride, head stride) of a tensor [rows or more][heads][d] of the type and on the device of `like`, channels adjacent."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != d or shape[0] < rows or (heads is not None and shape[1] != heads) or (d > 1 and shape[0] and stride[2] != 1) \
+            or t.dtype != like.dtype or t.device != like.device:
+        _refuse(f"{what}: [{rows}][{heads if heads is not None else 'heads'}][{d}] with adjacent channels, {like.dtype} on {like.device} expected; "
+                f"got {tuple(shape)}, strides {tuple(stride)}, {t.dtype} on {t.device}")
+    return shape[1], stride[0], stride[1]
 
 
 def _ints(t, n: int, device, what: str):
@@ -417,24 +425,21 @@ def _ints(t, n: int, device, what: str):
     return t.data_ptr()
 
 
-class _Current:
-    """The device that a call's tensors live on, made current for the call where it is not."""
+def _elsewhere(device) -> bool:
+    """Whether another device than `device` is the current one."""
+    import torch
+    if device.type != "cuda":
+        _refuse(f"device tensors expected, got {device}")
+    return torch._C._cuda_getDevice() != device.index
 
-    def __init__(self, device):
-        import torch
-        self.guard = None
-        if device.type != "cuda":
-            _refuse(f"device tensors expected, got {device}")
-        if torch._C._cuda_getDevice() != device.index:
-            self.guard = torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *e):
-        if self.guard is not None:
-            self.guard.__exit__(*e)
+def _new(shape, dtype, device, stream):
+    """A tensor that belongs to the stream that will write it (None: the current one)."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 class Rope:
@@ -463,35 +468,35 @@ class Rope:
         """Turns one or two tensors [tokens][heads][head_dim] (bf16 or fp32; views with any token and head stride).  positions: int32
         tensor [tokens] (tokens with a negative one are left out), or an int: token t is at positions + t % period (period 0: + t).
         out: as many tensors, which may be `tensors` themselves (None: new ones).  Returns the list of outputs."""
-        import torch
         d = self.cfg.head_dim
         if not 1 <= len(tensors) <= 2:
             _refuse("Rope.apply: one or two tensors")
         x0 = tensors[0]
-        code, T, dev = _ACT_CODE.get(str(x0.dtype)), x0.shape[0] if x0.dim() == 3 else -1, x0.device
-        if code is None:
-            _refuse(f"Rope.apply: float32 or bfloat16, got {x0.dtype}")
-        with _Current(dev):
-            ptr = None
-            if not isinstance(positions, int):
-                ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
-            if out is None:
-                with torch.cuda.stream(stream):          # new tensors belong to the stream that writes them (None: the current one)
-                    out = [torch.empty(x.shape, dtype=x.dtype, device=dev) for x in tensors]
-            elif len(out) != len(tensors):
-                _refuse("Rope.apply: as many outputs as tensors")
-            sides = (hr_rope_tensor * len(tensors))()
-            for side, x, y in zip(sides, tensors, out):
-                _rows(x, None, d, dev, x0.dtype, "Rope.apply: input")
-                _rows(y, x.shape[1], d, dev, x0.dtype, "Rope.apply: output")
-                if x.shape[0] != T or y.shape[0] != T:
-                    _refuse("Rope.apply: as many tokens everywhere")
-                side.in_, side.out, side.n_heads = x.data_ptr(), y.data_ptr(), x.shape[1]
-                side.in_token_stride, side.in_head_stride, _ = x.stride()
-                side.out_token_stride, side.out_head_stride, _ = y.stride()
-            if T > 0:
-                check(lib.hr_rope_apply(C.byref(self.cfg), self._freqs, code, T, ptr, positions, period, sides, len(tensors),
-                                        1 if inverse else 0, _stream_ptr(stream)), "hr_rope_apply")
+        code, dev = _act_code(x0.dtype), x0.device
+        if code is None or x0.dim() != 3:
+            _refuse(f"Rope.apply: [tokens][heads][{d}] in float32 or bfloat16, got {tuple(x0.shape)} {x0.dtype}")
+        if _elsewhere(dev):
+            import torch
+            with torch.cuda.device(dev):
+                return self.apply(positions, *tensors, out=out, period=period, inverse=inverse, stream=stream)
+        T = x0.shape[0]
+        ptr = None
+        if not isinstance(positions, int):
+            ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
+        if out is None:
+            out = [_new(x.shape, x.dtype, dev, stream) for x in tensors]
+        elif len(out) != len(tensors):
+            _refuse("Rope.apply: as many outputs as tensors")
+        sides = (hr_rope_tensor * len(tensors))()
+        for side, x, y in zip(sides, tensors, out):
+            heads, xt, xh = _strides(x, T, None, d, x0, "Rope.apply: input")
+            _, yt, yh = _strides(y, T, heads, d, x0, "Rope.apply: output")
+            if x.shape[0] != T or y.shape[0] != T:
+                _refuse("Rope.apply: as many tokens everywhere")
+            side.__init__(x.data_ptr(), y.data_ptr(), heads, xt, xh, yt, yh)
+        if T > 0:
+            check(lib.hr_rope_apply(C.byref(self.cfg), self._freqs, code, T, ptr, positions, period, sides, len(sides),
+                                    1 if inverse else 0, _stream_ptr(stream)), "hr_rope_apply")
         return list(out)
 
 
@@ -518,11 +523,10 @@ class PairTables:
         nbytes = int(lib.hr_pair_tables_sched_bytes(pool.handle, n_pairs, max_tokens, n_q_heads))
         if nbytes == 0 or pt_stride < 0:
             raise HrError(HR_ERR_INVALID_ARG, "hr_pair_tables_sched_bytes")
-        with _Current(self.device):
-            new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=self.device)      # noqa: E731
-            self.q_cu, self.doc_lens, self.page_table = new(n_pairs + 1), new(n_pairs), new(n_pairs, pt_stride)
-            self.tok_pos, self.tok_pair, self.order, self.report = new(max_tokens), new(max_tokens), new(n_pairs), new(4)
-            self.sched = new(nbytes // 4)
+        new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=self.device)      # noqa: E731
+        self.q_cu, self.doc_lens, self.page_table = new(n_pairs + 1), new(n_pairs), new(n_pairs, pt_stride)
+        self.tok_pos, self.tok_pair, self.order, self.report = new(max_tokens), new(max_tokens), new(n_pairs), new(4)
+        self.sched = new(nbytes // 4)
         self.c = hr_pair_tables(n_pairs, max_tokens, pt_stride, n_q_heads, *[t.data_ptr() for t in (
             self.q_cu, self.doc_lens, self.page_table, self.tok_pos, self.tok_pair, self.order, self.report, self.sched)], nbytes)
         self.workspace_bytes = int(lib.hr_pair_attention_workspace_bytes(pool.handle, C.byref(self.c)))
@@ -532,10 +536,13 @@ class PairTables:
         n, dev = self.n_pairs, self.device
         if docs.device != dev:
             _refuse(f"PairTables.build: documents on {dev} expected, got {docs.device}")
-        with _Current(dev):
-            check(lib.hr_pair_tables_build(self.pool.handle, C.byref(docs.c), _ints(pair_doc, n, dev, "PairTables.build: pair_doc"),
-                                           _ints(query_lens, n, dev, "PairTables.build: query_lens"), C.byref(self.c), _stream_ptr(stream)),
-                  "hr_pair_tables_build")
+        if _elsewhere(dev):
+            import torch
+            with torch.cuda.device(dev):
+                return self.build(docs, pair_doc, query_lens, stream)
+        check(lib.hr_pair_tables_build(self.pool.handle, C.byref(docs.c), _ints(pair_doc, n, dev, "PairTables.build: pair_doc"),
+                                       _ints(query_lens, n, dev, "PairTables.build: query_lens"), C.byref(self.c), _stream_ptr(stream)),
+              "hr_pair_tables_build")
         return self
 
 
@@ -547,32 +554,36 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
     are, in a new tensor unset), with_lse: and the rows' log-sums [max_tokens][n_q_heads]."""
     import torch
     dev, n_q, T = tables.device, tables.n_q_heads, tables.max_tokens
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return pair_attention(pool, layer, tables, q, k, v, out, scale, cap, slopes, window, prefix_lens, with_lse, stream)
     _, n_kv, d = pool._dims
-    if pool.mem.device != dev:
-        _refuse("pair_attention: pool and tables on one device")
-    code = _ACT_CODE.get(str(q.dtype))
+    code = _act_code(q.dtype)
+    if pool.mem.device != dev or q.device != dev:
+        _refuse(f"pair_attention: pool, tables and tensors on one device expected, got {pool.mem.device}, {dev} and {q.device}")
     if code is None or (k is None) != (v is None):
         _refuse("pair_attention: float32 or bfloat16, and both of k and v or neither")
-    with _Current(dev):
-        for name, t, heads in (("q", q, n_q), ("k", k, n_kv), ("v", v, n_kv), ("out", out, n_q)):
-            if t is not None and _rows(t, heads, d, dev, q.dtype, "pair_attention: " + name).shape[0] < T:
-                _refuse(f"pair_attention: {T} rows of {name} expected, got {t.shape[0]}")
-        if slopes is not None and (slopes.dtype != torch.float32 or slopes.device != dev or slopes.numel() != n_q or not slopes.is_contiguous()):
-            _refuse(f"pair_attention: slopes: {n_q} contiguous float32 on {dev} expected")
-        prefix = None if prefix_lens is None else _ints(prefix_lens, tables.n_pairs, dev, "pair_attention: prefix_lens")
-        with torch.cuda.stream(stream):                  # new tensors belong to the stream that writes them (None: the current one)
-            if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-            lse = torch.empty((T, n_q), dtype=torch.float32, device=dev) if with_lse else None
-            ws = torch.empty(tables.workspace_bytes, dtype=torch.uint8, device=dev) if tables.workspace_bytes else None
-        ks, vs = (k.stride(), v.stride()) if k is not None else ((0, 0), (0, 0))
-        qs, os_ = q.stride(), out.stride()
-        args = hr_attention_args(code, layer, 0.0 if scale is None else scale, cap, window, q.data_ptr(), None if k is None else k.data_ptr(),
-                                 None if v is None else v.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
-                                 None if slopes is None else slopes.data_ptr(), prefix, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1])
-        if T > 0:
-            check(lib.hr_pair_attention(pool.handle, C.byref(tables.c), C.byref(args), None if ws is None else ws.data_ptr(),
-                                        tables.workspace_bytes, _stream_ptr(stream)), "hr_pair_attention")
+    _, q_t, q_h = _strides(q, T, n_q, d, q, "pair_attention: q")
+    k_p = v_p = None
+    k_t = k_h = v_t = v_h = 0
+    if k is not None:
+        _, k_t, k_h = _strides(k, T, n_kv, d, q, "pair_attention: k")
+        _, v_t, v_h = _strides(v, T, n_kv, d, q, "pair_attention: v")
+        k_p, v_p = k.data_ptr(), v.data_ptr()
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.device != dev or slopes.numel() != n_q or not slopes.is_contiguous()):
+        _refuse(f"pair_attention: slopes: {n_q} contiguous float32 on {dev} expected")
+    prefix = None if prefix_lens is None else _ints(prefix_lens, tables.n_pairs, dev, "pair_attention: prefix_lens")
+    if out is None:
+        out = _new(q.shape, q.dtype, dev, stream)
+    _, o_t, o_h = _strides(out, T, n_q, d, q, "pair_attention: out")
+    lse = _new((T, n_q), torch.float32, dev, stream) if with_lse else None
+    ws = _new((tables.workspace_bytes,), torch.uint8, dev, stream) if tables.workspace_bytes else None
+    args = hr_attention_args(code, layer, 0.0 if scale is None else scale, cap, window, q.data_ptr(), k_p, v_p, out.data_ptr(),
+                             None if lse is None else lse.data_ptr(), None if slopes is None else slopes.data_ptr(), prefix,
+                             q_t, q_h, k_t, k_h, v_t, v_h, o_t, o_h)
+    if T > 0:
+        check(lib.hr_pair_attention(pool.handle, C.byref(tables.c), C.byref(args), None if ws is None else ws.data_ptr(),
+                                    tables.workspace_bytes, _stream_ptr(stream)), "hr_pair_attention")
     return (out, lse) if with_lse else out
 
 
