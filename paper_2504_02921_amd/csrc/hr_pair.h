@@ -26,7 +26,7 @@ RopeShape rope_shape(int head_dim, int rotary_dim, int layout, int esz, bool in_
 // A group is the pairs of one document; its rows for a kv head are (token in order, query head of the group of heads), heads fastest.
 struct SchedLayout {
     int64_t hdr = 0;           // SchedHdr
-    int64_t ord_first = 0;     // [n_pairs] place in order of a pair's first token
+    int64_t ord_first = 0;     // [n_pairs] place of the first token of every pair, pairs in order
     int64_t grp_pair = 0;      // [n_pairs + 1] a group's first place in `order`
     int64_t grp_tok = 0;       // [n_pairs + 1] its first token's place
     int64_t blk_cu = 0;        // [n_pairs + 1] blocks of kPairBlkRows rows before a group

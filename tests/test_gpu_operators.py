@@ -147,6 +147,32 @@ def test_tables_are_the_references(n_pairs, n_docs, q_hi, spare):
     built(pool, len(pages), lens, cu, pages, rng.integers(-1, n_docs, n_pairs), q_lens, int(q_lens.sum()) + spare, 7)
 
 
+@pytest.mark.parametrize("n_pairs,n_docs", [(256, 40), (257, 40), (2048, 3), (32768, 500), (32769, 500), (300, 140000), (70000, 66000)])
+def test_tables_of_batches_on_either_side_of_a_choice(n_pairs, n_docs):
+    rng = np.random.default_rng(n_pairs)
+    lens = rng.integers(0, 40, n_docs)
+    cu, pages = corpus(rng, lens)
+    pool = hb().KVPool(1, 2, 16, len(pages), "bf16", DEV)
+    q_lens = rng.integers(0, 4, n_pairs)
+    built(pool, len(pages), lens, cu, pages, rng.integers(-1, n_docs, n_pairs), q_lens, int(q_lens.sum()) + 2, 3)
+
+
+def test_work_lists_do_not_depend_on_the_way_they_are_built():
+    """One small workgroup, a sort in LDS and a sort in memory: the attention of the same pairs is the same, bit for bit."""
+    T, H = torch(), hb()
+    rng = np.random.default_rng(8)
+    b = Batch("bf16", 14, 2, 64, [100, 0, 33, 300], rng.integers(-1, 4, 40), rng.integers(0, 9, 40), seed=8)
+    want, log = b.check()
+    for more, pairs in ((0, 260), (1 << 17, 0)):            # empty pairs behind them, documents that nobody asks for
+        lens = np.concatenate([b.doc_lens, np.zeros(more, np.int64)])
+        cu, pages = corpus(np.random.default_rng(8), lens)
+        t = H.PairTables(b.pool, 40 + pairs, b.tokens, 19, n_q_heads=14)
+        t.build(H.DocList(dev_i32(lens), dev_i32(cu), b.list.tensors[2]), dev_i32(np.concatenate([b.pair_doc, np.full(pairs, -1)])),
+                dev_i32(np.concatenate([b.q_lens, np.zeros(pairs, np.int64)])))
+        out, log2 = H.pair_attention(b.pool, b.layer, t, b.q, b.k, b.v, with_lse=True)
+        assert T.equal(out[:b.tokens], want[:b.tokens]) and T.equal(log2[:b.tokens], log[:b.tokens])
+
+
 def test_tables_of_pairs_that_are_in_order_already():
     rng = np.random.default_rng(4)
     lens = rng.integers(1, 200, 50)
