@@ -187,47 +187,85 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
     pair_join_waves<kWaves, MB * 32, QT>(a, smem, o, sm, row, h, pieces);
 }
 
-// A row's pieces, joined: one workgroup per row, every wavefront a quarter of the pieces, in a fixed order
+// A row's pieces, joined in a fixed order: few pieces by one wavefront, many by the four of a workgroup, a quarter each.
+constexpr int kJoinAlone = 16;      // pieces that one wavefront joins: two rounds of loads
+
+template <typename QT>
+__device__ __forceinline__ void join_store(const PairAttnArgs& a, int64_t row, int c, float v) {
+    const int n_q = a.g * a.n_kv;
+    const int64_t token = row / n_q;
+    ((QT*)a.out)[token * a.o_ts + (row - token * n_q) * a.o_hs + c] = from_float<QT>(v);
+}
+
 template <typename QT>
 __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
     __shared__ float part[4][256], piece_m[kPairSplitMost], piece_l[kPairSplitMost];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int blocks = list_items(a, false), tiles = a.blocks_only ? blocks : list_items(a, true);
     const int pieces = pair_choice(blocks, tiles, a.d, a.most_splits).pieces;
     if (pieces == 1) return;                                            // the rows are there
-    const int n_q = a.g * a.n_kv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x;
-    if (row >= (int64_t)a.hdr[SH_TOKENS] * n_q) return;
-    if (threadIdx.x < kPairSplitMost) {
-        const float2 x = (int)threadIdx.x < pieces ? a.part_ml[threadIdx.x * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
-        piece_m[threadIdx.x] = x.x;
-        piece_l[threadIdx.x] = x.y;
-    }
-    __syncthreads();
-    static_assert(kPairSplitMost == 128, "two pieces a lane");
-    const float m0 = piece_m[lane], m1 = piece_m[lane + 64], m = wave_max(fmaxf(m0, m1));
-    const float sum = wave_sum(fmaf(piece_factor(m0, m), piece_l[lane], piece_factor(m1, m) * piece_l[lane + 64]));
-    for (int c = lane; c < a.d; c += 64) {
-        constexpr int AHEAD = 8;
-        float acc = 0.0f;
-        for (int p0 = wave; p0 < pieces; p0 += 4 * AHEAD) {
-            float x[AHEAD];
+    const int64_t rows = (int64_t)a.hdr[SH_TOKENS] * a.g * a.n_kv;
+    constexpr int AHEAD = 8;
+    if (pieces <= kJoinAlone) {
+        const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+        if (row >= rows) return;
+        const float2 x = lane < pieces ? a.part_ml[lane * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
+        const float m = wave_max(x.x), f = piece_factor(x.x, m), sum = wave_sum(f * x.y), inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        for (int c = lane; c < a.d; c += 128) {
+            const int c2 = min(c + 64, a.d - 1);
+            float acc = 0.0f, acc2 = 0.0f;
+            for (int p0 = 0; p0 < pieces; p0 += AHEAD) {
+                float v[AHEAD], v2[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) x[u] = a.part_o[(min(p0 + 4 * u, pieces - 1) * a.part_rows + row) * a.d + c];
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float* o = a.part_o + (min(p0 + u, pieces - 1) * a.part_rows + row) * a.d;
+                    v[u] = o[c];
+                    v2[u] = o[c2];
+                }
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const float f = p0 + 4 * u < pieces ? piece_factor(piece_m[min(p0 + 4 * u, pieces - 1)], m) : 0.0f;
-                acc = f != 0.0f ? fmaf(f, x[u], acc) : acc;             // nothing is written of a piece that sees nothing
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float fu = p0 + u < pieces ? __shfl(f, p0 + u, 64) : 0.0f;
+                    acc = fu != 0.0f ? fmaf(fu, v[u], acc) : acc;       // nothing is written of a piece that sees nothing
+                    acc2 = fu != 0.0f ? fmaf(fu, v2[u], acc2) : acc2;
+                }
             }
+            join_store<QT>(a, row, c, acc * inv);
+            if (c + 64 < a.d) join_store<QT>(a, row, c + 64, acc2 * inv);
         }
-        part[wave][c] = acc;
+        if (lane == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        return;
     }
-    __syncthreads();
-    const int64_t token = row / n_q;
-    const int head = (int)(row - token * n_q);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    const int c = threadIdx.x;
-    if (c < a.d) ((QT*)a.out)[token * a.o_ts + head * a.o_hs + c] = from_float<QT>((part[0][c] + part[1][c] + part[2][c] + part[3][c]) * inv);
-    if (c == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        if (threadIdx.x < kPairSplitMost) {
+            const float2 x = (int)threadIdx.x < pieces ? a.part_ml[threadIdx.x * a.part_rows + row] : make_float2(-INFINITY, 0.0f);
+            piece_m[threadIdx.x] = x.x;
+            piece_l[threadIdx.x] = x.y;
+        }
+        __syncthreads();
+        static_assert(kPairSplitMost == 128, "two pieces a lane");
+        const float m0 = piece_m[lane], m1 = piece_m[lane + 64], m = wave_max(fmaxf(m0, m1));
+        const float sum = wave_sum(fmaf(piece_factor(m0, m), piece_l[lane], piece_factor(m1, m) * piece_l[lane + 64]));
+        for (int c = lane; c < a.d; c += 64) {
+            float acc = 0.0f;
+            for (int p0 = wave; p0 < pieces; p0 += 4 * AHEAD) {
+                float x[AHEAD];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) x[u] = a.part_o[(min(p0 + 4 * u, pieces - 1) * a.part_rows + row) * a.d + c];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float f = p0 + 4 * u < pieces ? piece_factor(piece_m[min(p0 + 4 * u, pieces - 1)], m) : 0.0f;
+                    acc = f != 0.0f ? fmaf(f, x[u], acc) : acc;
+                }
+            }
+            part[wave][c] = acc;
+        }
+        __syncthreads();
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int c = threadIdx.x;
+        if (c < a.d) join_store<QT>(a, row, c, (part[0][c] + part[1][c] + part[2][c] + part[3][c]) * inv);
+        if (c == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        __syncthreads();                                                // the next row writes where this one reads
+    }
 }
 
 template <int MB, typename PT, typename QT>
@@ -251,7 +289,8 @@ hipError_t f32_by_size(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
 }  // namespace
 
 static hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, hipStream_t st) {
-    const unsigned blocks = (unsigned)(max_tokens * a.g * a.n_kv);
+    const int64_t rows = max_tokens * a.g * a.n_kv;
+    const unsigned blocks = (unsigned)std::max<int64_t>((rows + 3) / 4, std::min<int64_t>(rows, kPairSplitWgs));
     if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a);
     else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a);
     return hipGetLastError();
