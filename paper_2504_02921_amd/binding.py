@@ -433,13 +433,15 @@ def _elsewhere(device) -> bool:
     return torch._C._cuda_getDevice() != device.index
 
 
-def _new(shape, dtype, device, stream):
-    """A tensor that belongs to the stream that will write it (None: the current one)."""
+def _new(like, stream, shape=None, dtype=None):
+    """A contiguous tensor like `like`, of the shape and type given, that belongs to the stream that will write it (None: the current one)."""
     import torch
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if shape is None:
+            return torch.empty_like(like, memory_format=torch.contiguous_format)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _new(like, None, shape, dtype)
 
 
 class Rope:
@@ -483,21 +485,25 @@ class Rope:
         ptr = None
         if not isinstance(positions, int):
             ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
-        if out is None:
-            out = [_new(x.shape, x.dtype, dev, stream) for x in tensors]
-        elif len(out) != len(tensors):
-            _refuse("Rope.apply: as many outputs as tensors")
         sides = (hr_rope_tensor * len(tensors))()
-        for side, x, y in zip(sides, tensors, out):
+        if out is not None and len(out) != len(tensors):
+            _refuse("Rope.apply: as many outputs as tensors")
+        outs = []
+        for i, x in enumerate(tensors):
             heads, xt, xh = _strides(x, T, None, d, x0, "Rope.apply: input")
-            _, yt, yh = _strides(y, T, heads, d, x0, "Rope.apply: output")
+            if out is None:
+                y, yt, yh = _new(x, stream), heads * d, d
+            else:
+                y = out[i]
+                _, yt, yh = _strides(y, T, heads, d, x0, "Rope.apply: output")
             if x.shape[0] != T or y.shape[0] != T:
                 _refuse("Rope.apply: as many tokens everywhere")
-            side.__init__(x.data_ptr(), y.data_ptr(), heads, xt, xh, yt, yh)
+            outs.append(y)
+            sides[i].__init__(x.data_ptr(), y.data_ptr(), heads, xt, xh, yt, yh)
         if T > 0:
             check(lib.hr_rope_apply(C.byref(self.cfg), self._freqs, code, T, ptr, positions, period, sides, len(sides),
                                     1 if inverse else 0, _stream_ptr(stream)), "hr_rope_apply")
-        return list(out)
+        return outs
 
 
 class DocList:
@@ -574,10 +580,10 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
         _refuse(f"pair_attention: slopes: {n_q} contiguous float32 on {dev} expected")
     prefix = None if prefix_lens is None else _ints(prefix_lens, tables.n_pairs, dev, "pair_attention: prefix_lens")
     if out is None:
-        out = _new(q.shape, q.dtype, dev, stream)
+        out = _new(q, stream)
     _, o_t, o_h = _strides(out, T, n_q, d, q, "pair_attention: out")
-    lse = _new((T, n_q), torch.float32, dev, stream) if with_lse else None
-    ws = _new((tables.workspace_bytes,), torch.uint8, dev, stream) if tables.workspace_bytes else None
+    lse = _new(q, stream, (T, n_q), torch.float32) if with_lse else None
+    ws = _new(q, stream, (tables.workspace_bytes,), torch.uint8) if tables.workspace_bytes else None
     args = hr_attention_args(code, layer, 0.0 if scale is None else scale, cap, window, q.data_ptr(), k_p, v_p, out.data_ptr(),
                              None if lse is None else lse.data_ptr(), None if slopes is None else slopes.data_ptr(), prefix,
                              q_t, q_h, k_t, k_h, v_t, v_h, o_t, o_h)
