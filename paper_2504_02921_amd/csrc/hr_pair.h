@@ -48,16 +48,17 @@ int tables_build_check(const hr_pool* pool, const hr_doc_list* docs, const int32
 int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* a);
 // Few rows and long documents: an item's keys are cut into up to `most` pieces, each a workgroup's, whose results are joined by a second
 // launch.  How many is decided on the device, which knows the items (pair_splits); `most` bounds grid and workspace.
-// The join costs about 3 us: 16 blocks of 304 keys 8.5 us whole and 11.5 in two pieces, 16 of 2049 17.9 and 13.7 in eight.
-constexpr int kPairSplitMost = 128, kPairSplitKeys = 256, kPairSplitLeast = 1024;      // keys of a piece, of documents that are cut, at least
+// Whole / in pieces, with the join: 16 blocks of 304 keys 10.6 / 11.8 us, of 544 12.7 / 12.4, of 1025 18.1 / 12.5, of 2049 28.7 / 12.7.
+constexpr int kPairSplitMost = 128, kPairSplitKeys = 256, kPairSplitLeast = 768;      // keys of a piece, of documents that are cut, at least
 int pair_most_splits(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
 constexpr int kPairSplitWgs = 512;                            // workgroups that a launch wants
 // Whether an attention's work items are blocks of 32 rows, each streaming its keys for itself, or tiles of four, which share a stream (see
 // hr_pair_attn_mfma.hip), and their pieces.  blocks, tiles: of all kv heads.  Tiles read and expand keys once for up to four blocks, blocks fill
-// the chip sooner: tiles pay where they are more than half full and the blocks more than the chip takes at once.  Blocks / tiles, in us: 64 channels,
-// 280 blocks of 544 keys 11.7 / 16.4, 320 of 2064 26.3 / 32.4, 1120 of 544 24.7 / 22.7, 4480 of 544 78 / 50; 128 channels, 128 blocks of 4112 43.5 / 39.4,
-// 288 of 8200 136 / 87, 640 of 288 26.7 / 18.4; one block a tile, 800 of 2049 (fp8) 101 / 190, 3200 of 520 188 / 197.
-HR_HD int pair_tile_blocks(int d) { return d == 64 ? 768 : 256; }
+// the chip sooner: tiles pay where they are more than a third full and the blocks more than the chip takes at once.  Blocks / tiles, in us:
+// 64 channels, 280 blocks of 544 keys 11.2 / 15.3, 320 of 2064 24.6 / 41.0, 700 of 544 17.9 / 15.9, 1120 of 544 27.7 / 21.2, 4480 of 544 84.8 / 44.4, two
+// a tile 2560 of 520 51.3 / 41.9; 128 channels, 128 blocks of 4112 33.3 / 44.2, 256 of 4128 45.7 / 45.3, 312 of 8200 95.0 / 75.2, 640 of 288 24.7 / 17.3;
+// one block a tile, 1280 of 516 (64 channels) 37.0 / 37.1, 3200 of 520 183 / 190, 800 of 2049 (fp8) 101 / 159.
+HR_HD int pair_tile_blocks(int d) { return d == 64 ? 512 : 256; }
 struct PairChoice { bool tiles; int pieces; };
 HR_HD PairChoice pair_choice(int blocks, int tiles, int d, int most) {
     PairChoice c;
