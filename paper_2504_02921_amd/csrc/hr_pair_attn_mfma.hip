@@ -108,7 +108,7 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, co
             page[e] = pool + id * page_stride;
             if constexpr (FP8) {
                 const const_float_t sc = (const_float_t)(a.scales + ((int64_t)id * a.n_kv + h) * 2);
-                k_scale[e] = sc[0];
+                k_scale[e] = sc[0] * kFp8Low;
                 v_scale[e] = sc[1];
             }
         }
@@ -131,11 +131,11 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, co
         }
     };
     auto half_k = [&](const Piece& x) {
-        if constexpr (FP8) return fp8x8_to_half(x, fp8_expand_factor(1.0f));
+        if constexpr (FP8) return fp8x8_low(x);
         else return x;
     };
     auto half_v = [&](const Piece& x, float scale) {
-        if constexpr (FP8) return fp8x8_to_half(x, fp8_expand_factor(scale));
+        if constexpr (FP8) return fp8x8_times(x, fp8_expand_factor(scale));
         else return x;
     };
 
@@ -301,48 +301,44 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     };
     auto expand = [&](const Raw& r, int slot, float v_scale) {
         char* dst = my_part + slot * T::SLOT;
-        const halfx2 f = fp8_expand_factor(wave < 2 ? 1.0f : v_scale);      // K's scale goes into the scores
+        const halfx2 f = fp8_expand_factor(v_scale);                        // K's scale goes into the scores
 #pragma unroll
         for (int e = 0; e < G::BLOCK / 512; ++e) {
             const int w = e * 64 + lane, t = w / (HD / 8), c8 = (w % (HD / 8)) ^ k_swizzle(t, HD, 1);
-            *(halfx8*)(dst + (wave < 2 ? (t * HD + ((c8 ^ k_swizzle(t, HD, 2)) << 3)) * 2 : w * 16)) = fp8x8_to_half(r.w[e], f);
+            if (wave < 2) *(halfx8*)(dst + (t * HD + ((c8 ^ k_swizzle(t, HD, 2)) << 3)) * 2) = fp8x8_low(r.w[e]);
+            else *(halfx8*)(dst + w * 16) = fp8x8_times(r.w[e], f);
         }
     };
     // fp8: scales of a sub-tile's two pages
     struct Scales { float k0 = 1.0f, k1 = 1.0f, v0 = 1.0f, v1 = 1.0f; };      // half pages: one
-    // The pages of the sub-tiles, 32 sub-tiles at a time: a lane has the id and the scales of one page.  Lane reads cost the loop no wait; requests
-    // through the scalar cache would share the counter of the LDS reads, and out of order, so that each of those waited for all.
+    // The pages of the sub-tiles, a window of 32 sub-tiles that moves on by 16: a lane has the id and the scales of one page.  Lane reads cost the loop
+    // no wait; requests through the scalar cache would share the counter of the LDS reads, and out of order, so that each of those waited for all.
     struct Pages { int id; float k, v; };
-    auto pages_of = [&](int block) {
+    const int lane_sub = lane >> 1;
+    auto pages_of = [&](int at) {
         Pages r;
-        const int sub = sub_of(min(32 * block + (lane >> 1), n_ring - 1));      // behind the last one that one's again
+        const int sub = sub_of(min(at, n_ring - 1));                    // behind the last one that one's again
         r.id = min(max(a.page_table[(int64_t)it.pair * a.pt_stride + min(2 * sub + (lane & 1), last_page)], 0), a.num_pages - 1);
         return r;
     };
     auto scale_pages = [&](Pages& r) {
         if constexpr (FP8) {
             const float2 x = *(const float2*)(a.scales + ((int64_t)r.id * a.n_kv + h) * 2);
-            r.k = x.x;
+            r.k = x.x * kFp8Low;
             r.v = x.y;
         }
     };
-    Pages now, ahead;                                                   // of this block of 32 and of the one behind it
-    auto lane_int = [&](int block, int c, int n, int l) {
-        const int x = __builtin_amdgcn_readlane(c, l), y = __builtin_amdgcn_readlane(n, l);
-        return block ? y : x;
-    };
-    auto lane_float = [&](int block, float c, float n, int l) { return __int_as_float(lane_int(block, __float_as_int(c), __float_as_int(n), l)); };
-    // of the sub-tile `on` behind the at-th one
-    auto page_of = [&](int at, int on) { return lane_int((at & 31) + on >> 5, now.id, ahead.id, (2 * (at + on) + my_page) & 63); };
-    auto v_scale_of = [&](int at, int on) { return FP8 ? lane_float((at & 31) + on >> 5, now.v, ahead.v, (2 * (at + on) + my_page) & 63) : 1.0f; };
-    auto scales_at = [&](int at, int on) {
+    Pages pages, later;                                                 // the window, and what half of it becomes next
+    auto lane_float = [&](float x, int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), l & 63)); };
+    auto page_of = [&](int at) { return __builtin_amdgcn_readlane(pages.id, 2 * at + my_page & 63); };
+    auto v_scale_of = [&](int at) { return FP8 ? lane_float(pages.v, 2 * at + my_page) : 1.0f; };
+    auto scales_at = [&](int at) {
         Scales r;
         if constexpr (FP8) {
-            const int b = (at & 31) + on >> 5, l = 2 * (at + on) & 63;
-            r.k0 = lane_float(b, now.k, ahead.k, l);
-            r.k1 = lane_float(b, now.k, ahead.k, l + 1);
-            r.v0 = lane_float(b, now.v, ahead.v, l);
-            r.v1 = lane_float(b, now.v, ahead.v, l + 1);
+            r.k0 = lane_float(pages.k, 2 * at);
+            r.k1 = lane_float(pages.k, 2 * at + 1);
+            r.v0 = lane_float(pages.v, 2 * at);
+            r.v1 = lane_float(pages.v, 2 * at + 1);
         }
         return r;
     };
@@ -380,17 +376,17 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     // does not hang on a branch.
     Raw raw[2];
     if (n_ring > 0) {
-        now = pages_of(0);
-        scale_pages(now);
+        pages = pages_of(lane_sub);
+        scale_pages(pages);
         if constexpr (FP8) {
-            fetch(page_of(0, 0), raw[0]);
-            fetch(page_of(0, 1), raw[1]);
+            fetch(page_of(0), raw[0]);
+            fetch(page_of(1), raw[1]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e) request(page_of(0, e), e);
+            for (int e = 0; e < 3; ++e) request(page_of(e), e);
         }
-        ahead = pages_of(1);
-        scale_pages(ahead);
+        later = pages_of(32 + (lane_sub & 15));
+        scale_pages(later);
     }
     Own own;                                                            // needed behind the document
     if (own0 < u1) load_own(wg.olo + 32 * (own0 - n_doc), own);
@@ -411,24 +407,29 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     auto advance = [&](int at, Raw& r) {
         if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
         __syncthreads();
-        if ((at & 31) == 0 && at > 0) {
-            now = ahead;
-            ahead = pages_of((at >> 5) + 1);
-            scale_pages(ahead);
+        if ((at & 15) == 0 && at > 0) {                                 // the half that is past
+            const bool mine = lane_sub >> 4 == (at - 16 >> 4 & 1);
+            pages.id = mine ? later.id : pages.id;
+            if constexpr (FP8) {
+                pages.k = mine ? later.k : pages.k;
+                pages.v = mine ? later.v : pages.v;
+            }
+            later = pages_of(at + 32 + (lane_sub & 15));
         }
+        if (FP8 && (at & 15) == 8 && at > 8) scale_pages(later);        // their ids are there
         if constexpr (FP8) {
-            expand(r, (at + 2) & 3, v_scale_of(at, 2));
-            fetch(page_of(at, 4), r);
+            expand(r, (at + 2) & 3, v_scale_of(at + 2));
+            fetch(page_of(at + 4), r);
         } else {
-            request(page_of(at, 3), (at + 3) & 3);
+            request(page_of(at + 3), (at + 3) & 3);
         }
     };
     if (n_ring > 0) {
         if constexpr (FP8) {
-            expand(raw[0], 0, v_scale_of(0, 0));
-            expand(raw[1], 1, v_scale_of(0, 1));
-            fetch(page_of(0, 2), raw[0]);
-            fetch(page_of(0, 3), raw[1]);
+            expand(raw[0], 0, v_scale_of(0));
+            expand(raw[1], 1, v_scale_of(1));
+            fetch(page_of(2), raw[0]);
+            fetch(page_of(3), raw[1]);
         } else {
             __builtin_amdgcn_s_waitcnt(0x0F70);                         // the pages' numbers came behind the first blocks
         }
@@ -439,6 +440,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     if (n_ring_whole > 0) {
         floatx16 s = {};
         float mx = 0.0f;
+        Scales c = scales_at(0);
         // the largest of a lane's raw scores, scaled where they are scaled later; EXTRA: scaled, capped and biased in place
         auto largest = [&](floatx16& x, int key0, const Scales& c) {
             if (EXTRA) {
@@ -458,7 +460,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             advance(at, r);
             if (!active) return;
             const int ks = (at + 1) & 3, vs = at & 3;
-            const Scales c = scales_at(at, 0), cn = scales_at(at, 1);
+            const Scales cn = scales_at(at + 1);
             const float alpha = sm.follow(row_max2(mx)), use = sm.used();
             rescale(alpha);
             const float c0 = EXTRA ? 1.0f : a.scale_log2 * c.k0, c1 = EXTRA ? 1.0f : a.scale_log2 * c.k1;
@@ -480,11 +482,12 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
                 for (int e = 0; e < 2; ++e) o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v_frag(vs, mb, e), p[e], o[mb], 0, 0, 0);
             mx = largest(sn, 32 * (whole0 + u0 + at + 1), cn);
             s = sn;
+            c = cn;
         };
         if (active) {
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(0, kk), q[kk], s, 0, 0, 0);
-            mx = largest(s, 32 * (whole0 + u0), scales_at(0, 0));
+            mx = largest(s, 32 * (whole0 + u0), c);
         }
         int at = 0;
         if constexpr (FP8) {
@@ -507,7 +510,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         if (doc) {
             if (FP8 && (at & 1)) advance(at, raw[1]);
             else advance(at, raw[0]);
-            c = scales_at(at, 0);
+            c = scales_at(at);
         } else {
             __builtin_amdgcn_s_waitcnt(0x0F70);                         // nothing is on its way into LDS
             __syncthreads();                                            // everyone is past the sub-tile before

@@ -13,6 +13,23 @@ struct PairGeo {
     using Piece = std::conditional_t<FP8, uint2, halfx8>;     // 8 elements of a page
 };
 
+// 8 consecutive E4M3 codes as halves of 2^-8 of their values, exactly (fp8x8_to_half without its factor): a code in the upper byte of a half,
+// shifted down by one with its sign kept, has exponent and mantissa in a half's fields, and between them and the sign a copy of the sign to clear.
+// K's factor goes into the scores' scale.  Three instructions for two codes: tiles of fp8 pools are bound by what is issued.
+__device__ __forceinline__ halfx8 fp8x8_low(uint2 w) {
+    typedef __attribute__((ext_vector_type(2))) short shortx2;
+    auto pair = [&](unsigned x, unsigned sel) {
+        return __builtin_bit_cast(unsigned, __builtin_bit_cast(shortx2, __builtin_amdgcn_perm(x, 0u, sel)) >> 1) & 0xBFFFBFFFu;
+    };
+    const uint4 r = make_uint4(pair(w.x, 0x050c040cu), pair(w.x, 0x070c060cu), pair(w.y, 0x050c040cu), pair(w.y, 0x070c060cu));
+    return __builtin_bit_cast(halfx8, r);
+}
+// ... times a power of two and 2^8 (fp8_expand_factor)
+__device__ __forceinline__ halfx8 fp8x8_times(uint2 w, halfx2 f) {
+    return fp8x8_low(w) * __builtin_shufflevector(f, f, 0, 1, 0, 1, 0, 1, 0, 1);
+}
+constexpr float kFp8Low = 256.0f;      // what fp8x8_low leaves for the scores
+
 __device__ __forceinline__ halfx8 to_half8(VecN<bf16_t, 8> x) {
     halfx8 r;
 #pragma unroll

@@ -386,6 +386,28 @@ def test_attention_gives_the_same_bits_again_and_on_other_streams():
             assert T.equal(x[0], y[0]) and T.equal(x[1], y[1])
 
 
+@pytest.mark.parametrize("n_q,n_kv,d,q_len", [(14, 2, 64, 40), (32, 8, 128, 300), (14, 2, 64, 1200)])
+def test_attention_of_fp8_keys_below_the_normal_range(n_q, n_kv, d, q_len):
+    """Codes without an exponent count for what they are, in blocks and in tiles: 2^-9 steps beside a channel of 448 that the queries do not look at."""
+    T = torch()
+    D = 100
+    b = Batch("fp8", n_q, n_kv, d, [D], [0], [q_len], seed=6)
+    rng = np.random.default_rng(6)
+    (_, _), (vc, vs) = [ofp8.quantize_doc_kv(rng.standard_normal((2, D, n_kv, d))) for _ in range(2)]
+    kc = (rng.integers(0, 8, (2, D, n_kv, d)) | rng.integers(0, 2, (2, D, n_kv, d)) << 7).astype(np.uint8)
+    kc[..., 0] = 0x7E
+    ks = np.ones_like(vs)
+    ids = b.list.tensors[2].cpu().numpy()
+    b.pool.free(ids)
+    b.pool.write(D, ids, *[T.from_numpy(np.ascontiguousarray(x)).to(DEV) for x in (kc, vc, ks.astype(np.float32), vs.astype(np.float32))])
+    per = np.arange(D) // R.PAGE
+    b.docs[0] = tuple(ofp8.e4m3_decode(c)[b.layer] * s.astype(np.float32)[b.layer][per][:, :, None] for c, s in ((kc, ks), (vc, vs)))
+    q = b.q * 256.0
+    q[..., 0] = 0.0
+    b.check(False, q=q)
+    b.check(False, q=q, cap=5.0)
+
+
 def test_attention_of_bad_tables_stays_in_the_pool():
     """Page ids outside the pool are -1 in the table; such a pair's rows are undefined, the others are as ever."""
     T, H = torch(), hb()
