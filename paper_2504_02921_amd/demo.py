@@ -1,8 +1,38 @@
 """End-to-end walk through the library on one GPU: prefill a few documents into a paged pool, score every (query,
-document) pair with only the query tokens run through the layers, pick each query's best candidates, move a document
-to pinned host memory and back (16-bit records, then 4-bit ones).  Random weights and token ids; run as `python -m paper_2504_02921_amd.demo`."""
+document) pair with only the query tokens run through the layers, pick each query's best candidates, run one layer's
+rotary positions and attention over the same pool, move a document to pinned host memory and back (16-bit records, then 4-bit ones).  Random weights and token ids; run as `python -m paper_2504_02921_amd.demo`."""
 
 import numpy as np
+
+
+def layer_of_the_callers(pool, cfg, docs, doc_pages, query_lens, window: int = 64):
+    """One layer as a caller runs it whose model hr_rerank_score does not cover: rotary positions, tables built on the device, attention with a
+    window over the documents' pages (layer 0).  Every document gets one query.  Returns the largest difference from plain torch operations."""
+    import torch
+
+    from . import binding as hb
+
+    dev, n, tokens = pool.mem.device, len(docs), int(sum(query_lens))
+    i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(dev)      # noqa: E731
+    n_pages = [len(p) for p in doc_pages]
+    listed = hb.DocList(i32([len(d) for d in docs]), i32(np.concatenate([[0], np.cumsum(n_pages)])), i32(np.concatenate(doc_pages)))
+    tables = hb.PairTables(pool, n, tokens, max(n_pages), n_q_heads=cfg.n_q_heads)
+    tables.build(listed, i32(np.arange(n)), i32(query_lens))
+    gen = torch.Generator(device=dev).manual_seed(0)
+    q, k, v = (torch.randn((tokens, heads, cfg.head_dim), generator=gen, device=dev, dtype=torch.bfloat16) for heads in (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))
+    q, k = hb.Rope(cfg.head_dim, cfg.rope_base).apply(tables.tok_pos, q, k)
+    out = hb.pair_attention(pool, 0, tables, q, k, v, window=window)
+
+    gap, t0 = 0.0, 0
+    for doc, pages, m in zip(docs, doc_pages, query_lens):
+        kd, vd = (x[0].float() for x in pool.read(len(doc), pages))
+        keys, values = (torch.cat([d, own[t0:t0 + m].float()]).repeat_interleave(cfg.group, 1) for d, own in ((kd, k), (vd, v)))
+        s = torch.einsum("ihd,jhd->hij", q[t0:t0 + m].float(), keys) * cfg.head_dim ** -0.5
+        behind = (len(doc) + torch.arange(m, device=dev))[:, None] - torch.arange(len(doc) + m, device=dev)[None]
+        s = s.masked_fill((behind < 0) | (behind >= window), float("-inf"))
+        gap = max(gap, float((torch.einsum("hij,jhd->ihd", s.softmax(-1), values) - out[t0:t0 + m].float()).abs().max()))
+        t0 += m
+    return gap
 
 
 def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int = 24, top_k: int = 2, verbose: bool = True):
@@ -41,6 +71,8 @@ def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int
     torch.cuda.synchronize()
     gap = float((scores - full).abs().max())
 
+    layer_gap = layer_of_the_callers(pool, cfg, docs, doc_pages, [query_len] * n_docs)
+
     # host tier: evict document 0 to pinned host memory, free its pages, bring it back at other pages
     rec = torch.empty(pages_per_doc * pool.page_record_bytes, dtype=torch.uint8, pin_memory=True)
     pool.pages_out(doc_pages[0], rec)
@@ -71,6 +103,7 @@ def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int
             print(f"query {q}: best documents {best[q].tolist()}  scores {[round(float(scores[q * n_docs + int(d)]), 4) for d in best[q]]}")
         print(f"max |reuse - full recompute| = {gap:.2e}; scores after the host-tier round trip identical: {same}; "
               f"after a round trip of one document in 4 bits they move by at most {change4:.2e}")
+        print(f"a layer of the caller's own (rotary positions, windowed attention over the pool) differs from plain operations by at most {layer_gap:.2e}")
     model.close()
     pool.close()
     return scores.cpu().numpy(), best.cpu().numpy(), gap, same
