@@ -3,7 +3,8 @@
 //
 // A workgroup takes one block of 32 rows of one kv head, its four wavefronts every fourth sub-tile of 32 keys, each with a softmax of its own;
 // they are joined through LDS in a fixed order.  K, V and the rows go from memory straight into the operands of the fp32 matrix instruction (a page
-// holds them as a lane wants them: 8 channels of a key, 8 keys of a channel).
+// holds them as a lane wants them: 8 channels of a key, 8 keys of a channel).  What bounds small calls is the chain of loads: work list, rows and
+// page numbers, keys, own keys (8 queries of 16 tokens, documents of 128, 4 heads of 64: 14 us, of which the products are 4).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -187,7 +188,8 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
     pair_join_waves<kWaves, MB * 32, QT>(a, smem, o, sm, row, h, pieces);
 }
 
-// A row's pieces, joined in a fixed order: few pieces by one wavefront, many by the four of a workgroup, a quarter each.
+// A row's pieces, joined in a fixed order: few pieces by one wavefront, many by the four of a workgroup, a quarter each.  Bound by reading them:
+// 9824 rows of 6 pieces of 128 channels, 30 MB, 8.4 us (a workgroup for each row took 29); 14 rows of 128 pieces 5.7 us.
 constexpr int kJoinAlone = 16;      // pieces that one wavefront joins: two rounds of loads
 
 template <typename QT>

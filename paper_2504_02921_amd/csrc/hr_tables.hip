@@ -1,12 +1,15 @@
 // The tables of a batch of pairs, built on the device from the pairs' documents and query lengths (hr_pair_tables_build).
 //
-// Three ways.  A small batch is one workgroup's, a thread a pair, with everything that one step hands to the next in LDS: what it costs is the
-// loads that depend on each other (document, its place in the list, its pages).  Else two launches.  What goes over all pairs in turn (offsets,
-// the stable order by document, groups, their row blocks) is a few passes of scans of one workgroup, which are short (a pair is 8 bytes), while a
-// launch of many would wait at a grid barrier for each of them; what is written per pair, token and block goes to the whole chip.  The order is a
-// radix sort of up to 8 bits a pass, least first, each wavefront with a run of its own: equal documents keep the pairs' order, and no result depends on
-// which wavefront is first.  It runs in registers and LDS where key and place share a word, else through memory, whose scattered stores take a
-// cache line each.
+// Three ways; no result depends on which wavefront is first.
+//   small    one workgroup, a thread a pair, everything that one step hands to the next in LDS: what it costs is the loads that depend on each other
+//            (document, its place in the list, its pages).  20 pairs 6 us on the device, 200 of 4 tokens 18.0 (256, the second way: 20.0).
+//   sorted   one workgroup goes over the pairs in turn (offsets, a stable radix sort by document of up to 8 bits a pass, least first, each wavefront
+//            with a run of its own, groups, row blocks): passes of scans, which are short (a pair is 8 bytes), while a launch of many would wait
+//            at a grid barrier for each.  What is written per pair, token and block goes to the whole chip in a second launch.
+//   counted  many pairs: that workgroup only counts the pairs and tokens of every document, kWindow of them at a time in LDS, which gives groups and
+//            row blocks; the order of the pairs, most of the sort's time, is found by many workgroups (tables_place_kernel).
+// Sorted / counted, in us: 4096 pairs over 1000 documents 33.9 / 34.4, 8192 over 1000 43.6 / 36.7, 25600 over 8192 129 / 65 (counts 30, places 18,
+// what is written, 21 MB, 17); windows cost a look at the pairs each: 4096 over 30000 37 / 55, 16384 over 40000 94 / 77, 60000 over 200000 337 / 372.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -21,10 +24,11 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kDigits = 256;
-constexpr int kChipWaves = 8192;                          // wavefronts that the chip holds; more pairs than that share them, four at a time
-constexpr int kSmallPairs = 256, kSmallWork = 16384;      // of a batch that one workgroup builds; work: entries written
-constexpr int kPlaceBits = 15, kKeyBits = 32 - kPlaceBits;      // of a word of the sort in LDS
-constexpr int kLdsPairs = 1 << kPlaceBits;
+constexpr int kChipWaves = 8192;                          // wavefronts that the chip holds; more pairs than that share them, four at a time (25600: 19.7 to 17 us)
+constexpr int kSmallPairs = 256, kSmallWork = 16384;      // of a small batch; work: entries written
+constexpr int kWindow = 16384, kWindowPairs = 5000;       // documents that are counted in LDS at a time, and the pairs for which that pays
+constexpr int kCountPairs = 65535;                        // pairs and groups share a word there
+constexpr int kPlacePairs = 128;                          // pairs whose groups begin in a workgroup's share of the order
 
 struct TablesArgs {
     const int32_t *pair_doc, *query_lens;
@@ -39,8 +43,7 @@ struct TablesArgs {
 };
 
 struct Shared {
-    unsigned scan[2][kWaves];
-    unsigned carry[2];
+    unsigned scan[4][kWaves];
     int unsorted, bits;
     unsigned count[kWaves][kDigits];
 };
@@ -59,32 +62,42 @@ __device__ __forceinline__ unsigned wave_scan(unsigned v, unsigned cap) {
     return min(v + (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false), cap);
 }
 
-// exclusive sums over the workgroup of PER values a thread, saturating at `cap` (at most 2^30 + 2^30 meets before the cap is applied); total: of
-// all.  A wavefront's 64 PER values stand together, 64 beside each other, so that what they come from is read in whole lines.
-template <int PER>
-__device__ __forceinline__ void block_scan(const unsigned (&v)[PER], unsigned (&ex)[PER], unsigned cap, unsigned* s, unsigned& total) {
+// exclusive sums over the workgroup of PER values a thread, of NV kinds, saturating at `cap` (at most 2^30 + 2^30 meets before the cap is applied);
+// total: of all.  A wavefront's 64 PER values stand together, 64 beside each other, so that what they come from is read in whole lines.
+template <int NV, int PER>
+__device__ __forceinline__ void block_scan(const unsigned (&v)[NV][PER], unsigned (&ex)[NV][PER], unsigned cap, unsigned (*s)[kWaves],
+                                           unsigned (&total)[NV]) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    unsigned carry = 0;
+    unsigned carry[NV] = {};
 #pragma unroll
-    for (int e = 0; e < PER; ++e) {
-        const unsigned inc = wave_scan(v[e], cap);
-        ex[e] = min(carry + (unsigned)lane_before((int)inc, 0), cap);
-        carry = min(carry + (unsigned)lane_last((int)inc), cap);
-    }
+    for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const unsigned inc = wave_scan(v[n][e], cap);
+            ex[n][e] = min(carry[n] + (unsigned)lane_before((int)inc, 0), cap);
+            carry[n] = min(carry[n] + (unsigned)lane_last((int)inc), cap);
+        }
     __syncthreads();                                      // the last scan's sums have been read
-    if (lane == 0) s[wave] = carry;
-    __syncthreads();
-    const unsigned inc = wave_scan(lane < kWaves ? s[lane] : 0u, cap);
-    const unsigned before = wave == 0 ? 0u : (unsigned)__builtin_amdgcn_readlane((int)inc, wave - 1);
-    total = (unsigned)lane_last((int)inc);
+    if (lane == 0) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) ex[e] = min(before + ex[e], cap);
+        for (int n = 0; n < NV; ++n) s[n][wave] = carry[n];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        const unsigned inc = wave_scan(lane < kWaves ? s[n][lane] : 0u, cap);
+        const unsigned before = wave == 0 ? 0u : (unsigned)__builtin_amdgcn_readlane((int)inc, wave - 1);
+        total[n] = (unsigned)lane_last((int)inc);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) ex[n][e] = min(before + ex[n][e], cap);
+    }
 }
-__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned cap, unsigned* s, unsigned& total) {
-    const unsigned one[1] = {v};
-    unsigned ex[1];
-    block_scan(one, ex, cap, s, total);
-    return ex[0];
+__device__ __forceinline__ unsigned block_scan(unsigned v, unsigned cap, unsigned (*s)[kWaves], unsigned& total) {
+    const unsigned one[1][1] = {{v}};
+    unsigned ex[1][1], all[1];
+    block_scan(one, ex, cap, s, all);
+    total = all[0];
+    return ex[0][0];
 }
 
 __device__ __forceinline__ int key_of(const TablesArgs& a, int doc) { return doc < 0 || doc >= a.n_docs ? 0 : doc + 1; }
@@ -132,7 +145,7 @@ __device__ __forceinline__ void digit_places(Shared& sh) {
         c[e] = sh.count[i % kWaves][i / kWaves];
         sum += c[e];
     }
-    unsigned total, at = block_scan(sum, 0xFFFFFFFFu, sh.scan[0], total);
+    unsigned total, at = block_scan(sum, 0xFFFFFFFFu, sh.scan, total);
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         const int i = threadIdx.x * PER + e;
@@ -173,49 +186,7 @@ __device__ __forceinline__ void stream(int first, int step, int n, Get get, Put 
     }
 }
 
-// The pairs in the documents' order, words [key | pair] in LDS.  A pass deals out from memory what the one before left in LDS.
-__device__ void sort_lds(const TablesArgs& a, Shared& sh, unsigned* word) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs;
-    int32_t* copy = a.sched + a.lay.idx;
-    stream(tid, kThreads, n, [&](int p) { return a.pair_doc[p]; }, [&](int p, int doc) {
-        word[p] = (unsigned)key_of(a, doc) << kPlaceBits | (unsigned)p;
-        copy[p] = (int)word[p];
-    });
-    if (!sh.unsorted) {
-        __syncthreads();
-        return;
-    }
-    const int run = (n + kThreads - 1) / kThreads * 64, lo = min(wave * run, n), hi = min(lo + run, n);      // a wavefront's pairs
-    constexpr int AHEAD = 8;
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = kPlaceBits + a.bits * pass;
-        const unsigned mask = (1u << a.bits) - 1;
-        clear_counts(sh);
-        stream(lo + lane, 64, hi, [&](int i) { return word[i]; }, [&](int, unsigned w) {
-            atomicAdd(&sh.count[wave][(w >> shift) & mask], 1u);      // a count: the order of the additions does not show
-        });
-        __syncthreads();
-        digit_places(sh);
-        for (int i0 = lo + lane; i0 - lane < hi; i0 += 64 * AHEAD) {
-            unsigned w[AHEAD];                            // clamped places: loads without a branch between them
-#pragma unroll
-            for (int e = 0; e < AHEAD; ++e) w[e] = (unsigned)copy[min(i0 + 64 * e, n - 1)];
-#pragma unroll
-            for (int e = 0; e < AHEAD; ++e) {
-                if (i0 - lane + 64 * e >= hi) break;
-                const bool on = i0 + 64 * e < hi;
-                const unsigned at = take_place(sh.count[wave], (w[e] >> shift) & mask, a.bits, on);
-                if (on) word[at] = w[e];
-            }
-        }
-        __syncthreads();
-        if (pass + 1 < a.passes) {
-            stream(tid, kThreads, n, [&](int p) { return word[p]; }, [&](int p, unsigned w) { copy[p] = (int)w; });
-        }
-    }
-}
-
-// The same through memory: keys in key[0], pairs in `order`
+// The pairs in the documents' order: keys in key[0], pairs in `order`
 __device__ void sort_memory(const TablesArgs& a, Shared& sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs;
     int32_t *key = a.sched + a.lay.key[0], *key2 = a.sched + a.lay.key[1], *idx = a.sched + a.lay.idx;
@@ -256,142 +227,314 @@ __device__ void sort_memory(const TablesArgs& a, Shared& sh) {
     }
 }
 
-// Everything that goes over the pairs in turn.  One workgroup.
-template <bool LDS>
-__device__ void tables_scan(const TablesArgs& a, Shared& sh, unsigned* word) {
+// Offsets of the queries; the tokens.  unsorted: whether the pairs are not in the documents' order as they stand
+__device__ int tables_offsets(const TablesArgs& a, Shared& sh) {
+    constexpr int PER = 2 * kPer;                         // fewer rounds of loads
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs;
-    int32_t* const S = a.sched;
     if (tid == 0) {
         sh.unsorted = 0;
         sh.bits = 0;
         a.q_cu[0] = 0;
     }
-    // offsets of the queries; are the pairs in the documents' order as they stand?
     unsigned carry = 0;
     int bits = 0, unsorted = 0;
     const unsigned cap = (unsigned)a.max_tokens + 1;      // the first sum past max_tokens is told from the last that fits
-    for (int base = 0; base < n; base += kThreads * kPer) {
-        unsigned q[kPer], at[kPer], total;
-        const int p0 = base + wave * 64 * kPer + lane;
-        int len[kPer], doc[kPer];                         // clamped places: loads without a branch between them
+    for (int base = 0; base < n; base += kThreads * PER) {
+        unsigned q[1][PER], at[1][PER], total[1];
+        const int p0 = base + wave * 64 * PER + lane;
+        int len[PER], doc[PER];                         // clamped places: loads without a branch between them
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
+        for (int e = 0; e < PER; ++e) {
             len[e] = a.query_lens[min(p0 + 64 * e, n - 1)];
             doc[e] = a.pair_doc[min(p0 + 64 * e, n - 1)];
         }
         int k0 = key_of(a, a.pair_doc[min(max(p0 - 1, 0), n - 1)]);      // of the pair before, in a run's first lane
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
+        for (int e = 0; e < PER; ++e) {
             const bool on = p0 + 64 * e < n;
             const int k = key_of(a, doc[e]), up = lane_before(k, k0);
-            q[e] = on ? (unsigned)min(max(len[e], 0), a.max_tokens + 1) : 0u;
+            q[0][e] = on ? (unsigned)min(max(len[e], 0), a.max_tokens + 1) : 0u;
             if (on && len[e] < 0) bits |= HR_TABLES_BAD_LENGTH;
             unsorted |= on && k < up;
             k0 = lane_last(k);
         }
-        block_scan(q, at, cap, sh.scan[0], total);
+        block_scan(q, at, cap, sh.scan, total);
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const unsigned end = min(min(carry + at[e], cap) + q[e], cap);
+        for (int e = 0; e < PER; ++e) {
+            const unsigned end = min(min(carry + at[0][e], cap) + q[0][e], cap);
             if (end == cap) bits |= HR_TABLES_BAD_LENGTH;
             if (p0 + 64 * e < n) a.q_cu[p0 + 64 * e + 1] = (int)min(end, (unsigned)a.max_tokens);
         }
-        carry = min(carry + total, cap);
+        carry = min(carry + total[0], cap);
     }
     if (bits) atomicOr(&sh.bits, bits);
     if (unsorted) atomicOr(&sh.unsorted, 1);
     __syncthreads();
-    const int tokens = (int)min(carry, (unsigned)a.max_tokens);
+    return (int)min(carry, (unsigned)a.max_tokens);
+}
 
-    if constexpr (LDS) {
-        sort_lds(a, sh, word);
-        stream(tid, kThreads, n, [&](int i) { return word[i]; }, [&](int i, unsigned w) { a.order[i] = (int)(w & (kLdsPairs - 1)); });
-    } else {
-        sort_memory(a, sh);
-    }
+__device__ __forceinline__ int blocks_of(int rows) { return (rows + kPairBlkRows - 1) / kPairBlkRows; }
+__device__ __forceinline__ int tiles_of(int rows) { return (rows + kPairTileRows - 1) / kPairTileRows; }
+
+// What is written once: the lists' ends, header and report
+__device__ __forceinline__ void tables_close(const TablesArgs& a, int bits, int tokens, int groups, int blocks, int tiles) {
+    int32_t* const S = a.sched;
+    S[a.lay.grp_pair + groups] = a.n_pairs;
+    S[a.lay.grp_tok + groups] = tokens;
+    S[a.lay.blk_cu + groups] = blocks;
+    S[a.lay.tile_cu + groups] = tiles;
+    int32_t* hdr = S + a.lay.hdr;
+    hdr[SH_TOKENS] = tokens;
+    hdr[SH_GROUPS] = groups;
+    hdr[SH_BLOCKS] = blocks;
+    hdr[SH_TILES] = tiles;
+    a.report[0] = tokens;
+    a.report[1] = groups;
+    a.report[2] = bits;
+    a.report[3] = 0;
+}
+
+// Offsets, the pairs sorted, groups and their row blocks.  One workgroup.
+__global__ void __launch_bounds__(kThreads) tables_sort_kernel(TablesArgs a) {
+    __shared__ Shared sh;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs;
+    int32_t* const S = a.sched;
+    const int tokens = tables_offsets(a, sh);
+    sort_memory(a, sh);
     const int32_t* key = S + a.lay.key[0];
-    auto pair_at = [&](int i) { return LDS ? (int)(word[i] & (kLdsPairs - 1)) : a.order[i]; };
-    auto key_at = [&](int i) { return LDS ? (int)(word[max(i, 0)] >> kPlaceBits) : key[max(i, 0)]; };
-
     // groups: pairs of one document
     unsigned tok_carry = 0, grp_carry = 0;
     for (int base = 0; base < n; base += kThreads * kPer) {
         const int i0 = base + wave * 64 * kPer + lane;
-        unsigned q[kPer], head[kPer], t[kPer], g[kPer], q_all, g_all;
+        unsigned v[2][kPer], ex[2][kPer], all[2];         // tokens, heads of groups
         Ends ends[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const int i = min(i0 + 64 * e, n - 1);
-            ends[e] = *(const Ends*)(a.q_cu + pair_at(i));
-            head[e] = (i == 0) | (key_at(i) != key_at(i - 1)) ? 1u : 0u;
+            ends[e] = *(const Ends*)(a.q_cu + a.order[i]);
+            v[1][e] = (i == 0) | (key[i] != key[max(i - 1, 0)]) ? 1u : 0u;
         }
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const bool on = i0 + 64 * e < n;
-            q[e] = on ? (unsigned)(ends[e].hi - ends[e].lo) : 0u;
-            head[e] = on ? head[e] : 0u;
+            v[0][e] = on ? (unsigned)(ends[e].hi - ends[e].lo) : 0u;
+            v[1][e] = on ? v[1][e] : 0u;
         }
-        block_scan(q, t, 0xFFFFFFFFu, sh.scan[0], q_all);
-        block_scan(head, g, 0xFFFFFFFFu, sh.scan[1], g_all);
+        block_scan(v, ex, 0xFFFFFFFFu, sh.scan, all);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const int i = i0 + 64 * e;
             if (i >= n) break;
-            S[a.lay.ord_first + i] = (int)(tok_carry + t[e]);
-            if (head[e]) {
-                S[a.lay.grp_pair + grp_carry + g[e]] = i;
-                S[a.lay.grp_tok + grp_carry + g[e]] = (int)(tok_carry + t[e]);
+            S[a.lay.ord_first + i] = (int)(tok_carry + ex[0][e]);
+            if (v[1][e]) {
+                S[a.lay.grp_pair + grp_carry + ex[1][e]] = i;
+                S[a.lay.grp_tok + grp_carry + ex[1][e]] = (int)(tok_carry + ex[0][e]);
             }
         }
-        tok_carry += q_all;
-        grp_carry += g_all;
+        tok_carry += all[0];
+        grp_carry += all[1];
     }
     const int groups = (int)grp_carry;
-    if (tid == 0) {
-        S[a.lay.grp_pair + groups] = n;
-        S[a.lay.grp_tok + groups] = tokens;
-    }
+    if (tid == 0) S[a.lay.grp_tok + groups] = tokens;
     __syncthreads();
-
     // row blocks of the groups
     unsigned b_carry = 0, t_carry = 0;
     for (int base = 0; base < groups; base += kThreads * kPer) {
         const int g0 = base + wave * 64 * kPer + lane;
-        unsigned b[kPer], t[kPer], bo[kPer], to[kPer], b_all, t_all;
+        unsigned v[2][kPer], ex[2][kPer], all[2];
         Ends ends[kPer];
 #pragma unroll
         for (int e = 0; e < kPer; ++e) ends[e] = *(const Ends*)(S + a.lay.grp_tok + min(g0 + 64 * e, groups - 1));
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             const int rows = g0 + 64 * e < groups ? (ends[e].hi - ends[e].lo) * a.g : 0;
-            b[e] = (unsigned)(rows + kPairBlkRows - 1) / kPairBlkRows;
-            t[e] = (unsigned)(rows + kPairTileRows - 1) / kPairTileRows;
+            v[0][e] = (unsigned)blocks_of(rows);
+            v[1][e] = (unsigned)tiles_of(rows);
         }
-        block_scan(b, bo, 0xFFFFFFFFu, sh.scan[0], b_all);
-        block_scan(t, to, 0xFFFFFFFFu, sh.scan[1], t_all);
+        block_scan(v, ex, 0xFFFFFFFFu, sh.scan, all);
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
             if (g0 + 64 * e >= groups) break;
-            S[a.lay.blk_cu + g0 + 64 * e] = (int)(b_carry + bo[e]);
-            S[a.lay.tile_cu + g0 + 64 * e] = (int)(t_carry + to[e]);
+            S[a.lay.blk_cu + g0 + 64 * e] = (int)(b_carry + ex[0][e]);
+            S[a.lay.tile_cu + g0 + 64 * e] = (int)(t_carry + ex[1][e]);
         }
-        b_carry += b_all;
-        t_carry += t_all;
+        b_carry += all[0];
+        t_carry += all[1];
     }
-    if (tid == 0) {
-        S[a.lay.blk_cu + groups] = (int)b_carry;
-        S[a.lay.tile_cu + groups] = (int)t_carry;
-        int32_t* hdr = S + a.lay.hdr;
-        hdr[SH_TOKENS] = tokens;
-        hdr[SH_GROUPS] = groups;
-        hdr[SH_BLOCKS] = (int)b_carry;
-        hdr[SH_TILES] = (int)t_carry;
-        a.report[0] = tokens;
-        a.report[1] = groups;
-        a.report[2] = sh.bits;
-        a.report[3] = 0;
+    if (tid == 0) tables_close(a, sh.bits, tokens, groups, (int)b_carry, (int)t_carry);
+}
+
+// The same from counts: pairs and tokens of every document, kWindow documents at a time in LDS, give groups and row blocks without an order of the
+// pairs, which many workgroups then find (tables_place_kernel).  One workgroup.
+__global__ void __launch_bounds__(kThreads) tables_count_kernel(TablesArgs a) {
+    __shared__ Shared sh;
+    extern __shared__ unsigned counts[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs, n_keys = a.n_docs + 1, width = min(n_keys, kWindow);
+    unsigned *pairs = counts, *toks = counts + width;
+    int32_t* const S = a.sched;
+    const int tokens = tables_offsets(a, sh);
+    unsigned pair_carry = 0, tok_carry = 0, b_carry = 0, t_carry = 0;      // pair_carry: groups in the upper half
+    if (tid == 0) S[a.lay.idx] = 0;
+    for (int first = 0; first < n_keys; first += kWindow) {
+        for (int i = tid; i < width; i += kThreads) pairs[i] = toks[i] = 0;
+        __syncthreads();
+        struct Pair { int doc; Ends ends; };
+        stream(tid, kThreads, n, [&](int p) { return Pair{a.pair_doc[p], *(const Ends*)(a.q_cu + p)}; }, [&](int, const Pair& x) {
+            const int k = key_of(a, x.doc) - first;
+            if (k < 0 || k >= width) return;
+            atomicAdd(&pairs[k], 1u);                     // counts: the order of the additions does not show
+            atomicAdd(&toks[k], (unsigned)(x.ends.hi - x.ends.lo));
+        });
+        __syncthreads();
+        for (int base = 0; base < width; base += kThreads * kPer) {
+            const int k0 = base + wave * 64 * kPer + lane;
+            unsigned v[4][kPer], ex[4][kPer], all[4];     // pairs and groups, tokens, blocks, tiles
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const int k = min(k0 + 64 * e, width - 1);
+                const bool on = k0 + 64 * e < width && first + k < n_keys;
+                const unsigned c = on ? pairs[k] : 0u, t = on ? toks[k] : 0u;
+                v[0][e] = c | (c ? 1u << 16 : 0u);
+                v[1][e] = t;
+                v[2][e] = (unsigned)blocks_of((int)t * a.g);
+                v[3][e] = (unsigned)tiles_of((int)t * a.g);
+            }
+            block_scan(v, ex, 0xFFFFFFFFu, sh.scan, all);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const int c = (int)(v[0][e] & 0xFFFFu);
+                if (c == 0) continue;
+                const unsigned both = pair_carry + ex[0][e];
+                const int g = (int)(both >> 16), p = (int)(both & 0xFFFFu);
+                S[a.lay.grp_pair + g] = p;
+                S[a.lay.grp_tok + g] = (int)(tok_carry + ex[1][e]);
+                S[a.lay.blk_cu + g] = (int)(b_carry + ex[2][e]);
+                S[a.lay.tile_cu + g] = (int)(t_carry + ex[3][e]);
+                S[a.lay.key[0] + g] = first + k0 + 64 * e;
+                for (int m = p / kPlacePairs + 1; m <= (p + c) / kPlacePairs; ++m) S[a.lay.idx + m] = g + 1;      // the first group from there on
+            }
+            pair_carry += all[0];
+            tok_carry += all[1];
+            b_carry += all[2];
+            t_carry += all[3];
+        }
+        __syncthreads();                                  // counts have been read
+    }
+    if (tid == 0) tables_close(a, sh.bits, tokens, (int)(pair_carry >> 16), (int)b_carry, (int)t_carry);
+}
+
+// The pairs' places in the order, and their first tokens': a workgroup has the groups that begin in its kPlacePairs places and looks through all pairs
+// for theirs.  They are ranked by counting.  If the last of these groups, the only one that may be long, is longer than kPlacePairs, its pairs are taken
+// one behind the other instead, in a second look: they are of one document.
+__global__ void __launch_bounds__(kThreads) tables_place_kernel(TablesArgs a) {
+    constexpr int MOST = 2 * kPlacePairs, AHEAD = 16, EACH = kThreads / MOST;
+    __shared__ int list_key[kWaves][MOST], list_pair[kWaves][MOST], list_len[kWaves][MOST];
+    __shared__ int key[MOST], pair[MOST], len[MOST];
+    __shared__ int wave_few[kWaves], wave_last[kWaves], wave_tok[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.n_pairs, w = blockIdx.x;
+    int32_t* const S = a.sched;
+    const int groups = S[a.lay.hdr + SH_GROUPS];
+    const int g0 = min(S[a.lay.idx + w], groups), g1 = (int64_t)(w + 1) * kPlacePairs > n ? groups : min(S[a.lay.idx + w + 1], groups);
+    if (g0 >= g1) return;
+    const int key_lo = S[a.lay.key[0] + g0], key_last = S[a.lay.key[0] + g1 - 1];
+    const int place0 = S[a.lay.grp_pair + g0], place_last = S[a.lay.grp_pair + g1 - 1], place1 = S[a.lay.grp_pair + g1];
+    const int tok0 = S[a.lay.grp_tok + g0], tok_last = S[a.lay.grp_tok + g1 - 1];
+    const bool is_long = place1 - place_last > kPlacePairs;
+    const int key_hi = key_last + (is_long ? 0 : 1);      // keys that are ranked: below it
+    const int run = (n + kThreads - 1) / kThreads * 64, lo = min(wave * run, n), hi = min(lo + run, n);      // a wavefront's pairs
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    int few = 0, last = 0, toks = 0;
+    auto look = [&](auto each) {                          // each(pair, key or -1, tokens), for 64 pairs beside each other
+        for (int i0 = lo; i0 < hi; i0 += 64 * AHEAD) {
+            int doc[AHEAD];
+            Ends ends[AHEAD];
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int i = min(i0 + 64 * e + lane, n - 1);
+                doc[e] = a.pair_doc[i];
+                ends[e] = *(const Ends*)(a.q_cu + i);
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int i = i0 + 64 * e + lane;
+                each(i, i < hi ? key_of(a, doc[e]) : -1, ends[e].hi - ends[e].lo);
+            }
+        }
+    };
+    look([&](int i, int k, int tokens) {
+        const bool is_few = k >= key_lo && k < key_hi;
+        const uint64_t f = __ballot(is_few);
+        if (f) {
+            const int at = few + (int)__popcll(f & below);
+            if (is_few && at < MOST) {
+                list_key[wave][at] = k;
+                list_pair[wave][at] = i;
+                list_len[wave][at] = tokens;
+            }
+            few += (int)__popcll(f);
+        }
+        if (is_long) {
+            const uint64_t l = __ballot(k == key_last);
+            last += (int)__popcll(l);
+            if (l) toks += lane_last((int)wave_scan(k == key_last ? (unsigned)tokens : 0u, 0xFFFFFFFFu));
+        }
+    });
+    if (lane == 0) {
+        wave_few[wave] = min(few, MOST);
+        wave_last[wave] = last;
+        wave_tok[wave] = toks;
     }
     __syncthreads();
+    int at0 = 0, m = 0;
+    last = place_last;
+    toks = tok_last;
+    for (int v = 0; v < kWaves; ++v) {
+        if (v < wave) {
+            at0 += wave_few[v];
+            last += wave_last[v];
+            toks += wave_tok[v];
+        }
+        m += wave_few[v];
+    }
+    m = min(m, MOST);
+    for (int i = lane; i < wave_few[wave] && at0 + i < MOST; i += 64) {
+        key[at0 + i] = list_key[wave][i];
+        pair[at0 + i] = list_pair[wave][i];
+        len[at0 + i] = list_len[wave][i];
+    }
+    __syncthreads();
+    const int mine = tid / EACH;
+    int before = 0, tok = 0;
+    if (mine < m) {
+        const int k = key[mine];
+        for (int j = tid % EACH; j < m; j += EACH) {
+            const bool is = key[j] < k || (key[j] == k && j < mine);
+            before += is ? 1 : 0;
+            tok += is ? len[j] : 0;
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < EACH; o <<= 1) {
+        before += __shfl_xor(before, o, 64);
+        tok += __shfl_xor(tok, o, 64);
+    }
+    if (mine < m && tid % EACH == 0 && place0 + before < n) {
+        a.order[place0 + before] = pair[mine];
+        S[a.lay.ord_first + place0 + before] = tok0 + tok;
+    }
+    if (!is_long) return;
+    look([&](int i, int k, int tokens) {
+        const bool is_last = k == key_last;
+        const uint64_t l = __ballot(is_last);
+        if (!l) return;
+        const int inc = (int)wave_scan(is_last ? (unsigned)tokens : 0u, 0xFFFFFFFFu), at = last + (int)__popcll(l & below);
+        if (is_last && at < n) {
+            a.order[at] = i;
+            S[a.lay.ord_first + at] = toks + inc - tokens;
+        }
+        last += (int)__popcll(l);
+        toks += lane_last(inc);
+    });
 }
 
 // What the parts that write pairs, tokens and blocks take from the part before them, from memory or LDS
@@ -455,12 +598,6 @@ __device__ __forceinline__ int tables_fill(const TablesArgs& a, const Found& f, 
     return bits;
 }
 
-template <bool LDS>
-__global__ void __launch_bounds__(kThreads) tables_scan_kernel(TablesArgs a) {
-    __shared__ Shared sh;
-    extern __shared__ unsigned word[];
-    tables_scan<LDS>(a, sh, word);
-}
 __global__ void __launch_bounds__(256) tables_fill_kernel(TablesArgs a) {
     const int32_t* S = a.sched;
     const int32_t* hdr = S + a.lay.hdr;
@@ -494,7 +631,7 @@ __global__ void __launch_bounds__(kThreads) tables_small_kernel(TablesArgs a) {
     if (tid < n) s.key[tid] = key_of(a, a.pair_doc[tid]);
     const unsigned q = (unsigned)min(max(len, 0), a.max_tokens + 1);
     unsigned total;
-    const unsigned end = min(block_scan(q, cap, s.scan[0], total) + q, cap);
+    const unsigned end = min(block_scan(q, cap, s.scan, total) + q, cap);
     if (len < 0 || end == cap) bits |= HR_TABLES_BAD_LENGTH;
     if (tid < n) a.q_cu[tid + 1] = s.q_cu[tid + 1] = (int)min(end, (unsigned)a.max_tokens);
     const int tokens = (int)min(total, (unsigned)a.max_tokens), pair = tid >> 2;
@@ -520,7 +657,7 @@ __global__ void __launch_bounds__(kThreads) tables_small_kernel(TablesArgs a) {
         head = tid == 0 || s.key[p] != s.key[s.order[tid - 1]];
         mine = (unsigned)(s.q_cu[p + 1] - s.q_cu[p]) << 12 | (head ? 1u : 0u);
     }
-    const unsigned at = block_scan(mine, 0xFFFFFFFFu, s.scan[1], total);
+    const unsigned at = block_scan(mine, 0xFFFFFFFFu, s.scan, total);
     const int groups = (int)(total & 0xFFFu);
     if (tid < n) {
         s.ord_first[tid] = (int)(at >> 12);
@@ -536,9 +673,10 @@ __global__ void __launch_bounds__(kThreads) tables_small_kernel(TablesArgs a) {
     __syncthreads();
     // row blocks of the groups
     const int rows = tid < groups ? (s.grp_tok[tid + 1] - s.grp_tok[tid]) * a.g : 0;
-    unsigned blocks, tiles;
-    const unsigned b0 = block_scan((unsigned)(rows + kPairBlkRows - 1) / kPairBlkRows, 0xFFFFFFFFu, s.scan[0], blocks);
-    const unsigned t0 = block_scan((unsigned)(rows + kPairTileRows - 1) / kPairTileRows, 0xFFFFFFFFu, s.scan[1], tiles);
+    const unsigned both[2][1] = {{(unsigned)blocks_of(rows)}, {(unsigned)tiles_of(rows)}};
+    unsigned ex[2][1], all[2];
+    block_scan(both, ex, 0xFFFFFFFFu, s.scan, all);
+    const unsigned b0 = ex[0][0], t0 = ex[1][0], blocks = all[0], tiles = all[1];
     if (tid < groups) {
         s.blk_cu[tid] = (int)b0;
         s.tile_cu[tid] = (int)t0;
@@ -594,21 +732,21 @@ hipError_t launch_pair_tables(const hr_pool* pool, const hr_doc_list* docs, cons
     a.passes = (key_bits + 7) / 8;                        // digits of one width: the last one is as cheap as the others
     a.bits = (key_bits + a.passes - 1) / a.passes;
     a.wide = t->n_pairs > kChipWaves ? 4 : 6;
-    // entries written; one workgroup writes a few thousand in the time of a launch
     const int64_t work = (int64_t)t->n_pairs * (t->pt_stride + 64) + t->max_tokens;
     if (t->n_pairs <= kSmallPairs && work <= kSmallWork) {
         tables_small_kernel<<<1, kThreads, 0, st>>>(a);
         return hipGetLastError();
     }
-    if (t->n_pairs <= kLdsPairs && docs->n_docs < 1 << kKeyBits) {
-        const size_t lds = (size_t)t->n_pairs * sizeof(unsigned);
+    if (t->n_pairs <= kCountPairs && docs->n_docs < kWindow * (t->n_pairs / kWindowPairs)) {
+        const size_t lds = (size_t)std::min(docs->n_docs + 1, kWindow) * 2 * sizeof(unsigned);
         if (lds + sizeof(Shared) > 65536) {
-            const hipError_t e = hipFuncSetAttribute((const void*)tables_scan_kernel<true>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            const hipError_t e = hipFuncSetAttribute((const void*)tables_count_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
         }
-        tables_scan_kernel<true><<<1, kThreads, lds, st>>>(a);
+        tables_count_kernel<<<1, kThreads, lds, st>>>(a);
+        tables_place_kernel<<<(unsigned)((t->n_pairs + kPlacePairs - 1) / kPlacePairs), kThreads, 0, st>>>(a);
     } else {
-        tables_scan_kernel<false><<<1, kThreads, 0, st>>>(a);
+        tables_sort_kernel<<<1, kThreads, 0, st>>>(a);
     }
     const int64_t blocks = std::min<int64_t>((std::max<int64_t>((int64_t)t->n_pairs << a.wide, t->max_tokens) + 255) / 256, kChipWaves / 4);
     tables_fill_kernel<<<(unsigned)blocks, 256, 0, st>>>(a);

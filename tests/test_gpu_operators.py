@@ -147,7 +147,7 @@ def test_tables_are_the_references(n_pairs, n_docs, q_hi, spare):
     built(pool, len(pages), lens, cu, pages, rng.integers(-1, n_docs, n_pairs), q_lens, int(q_lens.sum()) + spare, 7)
 
 
-@pytest.mark.parametrize("n_pairs,n_docs", [(256, 40), (257, 40), (2048, 3), (32768, 500), (32769, 500), (300, 140000), (70000, 66000)])
+@pytest.mark.parametrize("n_pairs,n_docs", [(256, 40), (257, 40), (2048, 3), (4999, 40), (5000, 40), (16000, 40000), (16000, 60000), (65535, 500), (65536, 500), (300, 140000)])
 def test_tables_of_batches_on_either_side_of_a_choice(n_pairs, n_docs):
     rng = np.random.default_rng(n_pairs)
     lens = rng.integers(0, 40, n_docs)
@@ -157,13 +157,26 @@ def test_tables_of_batches_on_either_side_of_a_choice(n_pairs, n_docs):
     built(pool, len(pages), lens, cu, pages, rng.integers(-1, n_docs, n_pairs), q_lens, int(q_lens.sum()) + 2, 3)
 
 
+@pytest.mark.parametrize("docs", ["one", "two", "a long one between short ones", "all different", "none", "the last ones"])
+def test_tables_of_pairs_spread_unevenly(docs):
+    n, n_docs = 11000, 20000
+    rng = np.random.default_rng(12)
+    pair_doc = {"one": np.full(n, 7), "two": rng.integers(3, 5, n), "none": np.full(n, -1), "all different": rng.permutation(n), "the last ones": n_docs - 1 - rng.integers(0, 2, n),
+                "a long one between short ones": np.where(rng.random(n) < 0.6, 500, rng.integers(400, 600, n))}[docs]
+    lens = rng.integers(0, 40, n_docs)
+    cu, pages = corpus(rng, lens)
+    pool = hb().KVPool(1, 2, 16, len(pages), "bf16", DEV)
+    q_lens = rng.integers(0, 4, n)
+    built(pool, len(pages), lens, cu, pages, pair_doc, q_lens, int(q_lens.sum()) - 5, 3)
+
+
 def test_work_lists_do_not_depend_on_the_way_they_are_built():
-    """One small workgroup, a sort in LDS and a sort in memory: the attention of the same pairs is the same, bit for bit."""
+    """In one small workgroup, sorted and counted: the attention of the same pairs is the same, bit for bit."""
     T, H = torch(), hb()
     rng = np.random.default_rng(8)
     b = Batch("bf16", 14, 2, 64, [100, 0, 33, 300], rng.integers(-1, 4, 40), rng.integers(0, 9, 40), seed=8)
     want, log = b.check()
-    for more, pairs in ((0, 260), (1 << 17, 0)):            # empty pairs behind them, documents that nobody asks for
+    for more, pairs in ((0, 260), (0, 6000), (30000, 11000)):      # empty pairs behind them, documents that nobody asks for
         lens = np.concatenate([b.doc_lens, np.zeros(more, np.int64)])
         cu, pages = corpus(np.random.default_rng(8), lens)
         t = H.PairTables(b.pool, 40 + pairs, b.tokens, 19, n_q_heads=14)
