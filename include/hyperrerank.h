@@ -451,7 +451,9 @@ typedef struct hr_rope_tensor {
  *   positions_dev  device int32 [n_tokens]; a token with a negative position is left out: its rows of `out` are not written.
  *                  NULL: token t is at first_position + t % period (period 0: first_position + t), which may not pass 2^31 - 1
  *   inverse        not 0: by the negative angles (takes the rotation back; amplitude multiplies again)
- * HR_ERR_INVALID_ARG on null pointers, bad configurations, frequencies or strides; n_tokens = 0 is a no-op. */
+ * HR_ERR_INVALID_ARG on null pointers, bad configurations, frequencies or strides, and if one tensor's `out` is the other's `in` or
+ * `out`; HR_ERR_LEN_RANGE beyond 2^30 tokens or what a launch can hold (2^24 workgroups of four wavefronts, each with the tokens whose
+ * heads fill its lanes); n_tokens = 0 is a no-op. */
 int hr_rope_apply(const hr_rope_cfg* cfg, const double* freqs, int dtype, int64_t n_tokens, const int32_t* positions_dev,
                   int32_t first_position, int32_t period, const hr_rope_tensor* tensors, int32_t n_tensors, int inverse, void* stream);
 
@@ -507,10 +509,12 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
  *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them),
  *                 or in fp32 where the head size is neither 64 nor 128; sums and the softmax are fp32
  *   q, out        device [max_tokens][n_q_heads][head_dim]; k, v: [max_tokens][n_kv_heads][head_dim], both or neither; strides in
- *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written
+ *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written.  out overlaps
+ *                 none of the inputs
  *   lse           NULL or device fp32 [max_tokens][n_q_heads]: natural logarithm of the row's sum of exp(s)
  *   slopes        NULL or device fp32 [n_q_heads];  prefix_lens: NULL or device int32 [n_pairs] (cut to the query's length)
- * tables come from hr_pair_tables_build with the same pool; n_q_heads is theirs. */
+ * tables come from hr_pair_tables_build with the same pool; n_q_heads is theirs.  HR_ERR_LEN_RANGE if the work list has room for more
+ * than some 2^24 blocks of 32 rows (max_tokens x heads of a kv head / 32, and a block for every pair, times the kv heads). */
 typedef struct hr_attention_args {
     int32_t dtype, layer;
     float scale;            /* finite; 0: 1 / sqrt(head_dim) */

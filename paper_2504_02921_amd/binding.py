@@ -9,6 +9,7 @@ raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -425,6 +426,14 @@ def _ints(t, n: int, device, what: str):
     return t.data_ptr()
 
 
+def _int32(x, what: str) -> int:
+    """A number that the C side takes as int32 (ctypes would wrap it around)."""
+    x = operator.index(x)
+    if not 0 <= x < 1 << 31:
+        _refuse(f"{what}: 0 .. 2^31 - 1 expected, got {x}")
+    return x
+
+
 def _elsewhere(device) -> bool:
     """Whether another device than `device` is the current one."""
     import torch
@@ -483,8 +492,10 @@ class Rope:
                 return self.apply(positions, *tensors, out=out, period=period, inverse=inverse, stream=stream)
         T = x0.shape[0]
         ptr = None
-        if not isinstance(positions, int):
+        if hasattr(positions, "data_ptr"):
             ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
+        else:
+            positions, period = _int32(positions, "Rope.apply: positions"), _int32(period, "Rope.apply: period")
         sides = (hr_rope_tensor * len(tensors))()
         if out is not None and len(out) != len(tensors):
             _refuse("Rope.apply: as many outputs as tensors")
@@ -526,8 +537,10 @@ class PairTables:
         import torch
         self.pool, self.n_pairs, self.max_tokens, self.n_q_heads = pool, n_pairs, max_tokens, n_q_heads
         self.device = pool.mem.device
+        for what, x in (("n_pairs", n_pairs), ("max_tokens", max_tokens), ("pt_stride", pt_stride), ("n_q_heads", n_q_heads)):
+            _int32(x, f"PairTables: {what}")
         nbytes = int(lib.hr_pair_tables_sched_bytes(pool.handle, n_pairs, max_tokens, n_q_heads))
-        if nbytes == 0 or pt_stride < 0:
+        if nbytes == 0:
             raise HrError(HR_ERR_INVALID_ARG, "hr_pair_tables_sched_bytes")
         new = lambda *shape: torch.empty(shape, dtype=torch.int32, device=self.device)      # noqa: E731
         self.q_cu, self.doc_lens, self.page_table = new(n_pairs + 1), new(n_pairs), new(n_pairs, pt_stride)
@@ -565,8 +578,11 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
             return pair_attention(pool, layer, tables, q, k, v, out, scale, cap, slopes, window, prefix_lens, with_lse, stream)
     _, n_kv, d = pool._dims
     code = _act_code(q.dtype)
-    if pool.mem.device != dev or q.device != dev:
-        _refuse(f"pair_attention: pool, tables and tensors on one device expected, got {pool.mem.device}, {dev} and {q.device}")
+    if pool is not tables.pool or q.device != dev:
+        _refuse(f"pair_attention: the tables' own pool and tensors on {dev} expected, got {q.device}")
+    if scale == 0.0:
+        _refuse("pair_attention: scale: None (1 / sqrt(head_dim)) or a number that is not 0")
+    layer, window = _int32(layer, "pair_attention: layer"), _int32(window, "pair_attention: window")
     if code is None or (k is None) != (v is None):
         _refuse("pair_attention: float32 or bfloat16, and both of k and v or neither")
     _, q_t, q_h = _strides(q, T, n_q, d, q, "pair_attention: q")

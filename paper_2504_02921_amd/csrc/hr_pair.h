@@ -11,7 +11,7 @@
 namespace hr {
 
 // ---- rotary positions
-constexpr int kMaxRotaryPairs = 128;
+constexpr int kMaxRotaryPairs = 128, kRopeWaves = 4;
 int rope_check(const hr_rope_cfg* c);
 int rope_apply_check(const hr_rope_cfg* c, const double* freqs, int dtype, int64_t n_tokens, const int32_t* positions, int32_t first_position,
                      int32_t period, const hr_rope_tensor* tensors, int32_t n_tensors);

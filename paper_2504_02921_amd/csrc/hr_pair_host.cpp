@@ -10,6 +10,7 @@ namespace hr {
 namespace {
 
 constexpr int32_t kMaxTokens = 1 << 30, kMaxStride = 1 << 26;
+constexpr int64_t kMaxGroups = (1 << 24) - 512;      // workgroups of 256 threads in a launch, of which items are rounded up to 256
 
 bool finite_positive(float v) { return v > 0.0f && std::isfinite(v); }
 
@@ -62,6 +63,10 @@ int rope_apply_check(const hr_rope_cfg* c, const double* freqs, int dtype, int64
         if ((uintptr_t)t.in % esz != 0 || (uintptr_t)t.out % esz != 0) return HR_ERR_INVALID_ARG;
         heads += t.n_heads;
     }
+    // what one tensor's rows are turned into, nothing else is read or written
+    if (n_tensors == 2 && (tensors[0].out == tensors[1].out || tensors[0].out == tensors[1].in || tensors[1].out == tensors[0].in)) return HR_ERR_INVALID_ARG;
+    const RopeShape s = rope_shape(c->head_dim, c->rotary_dim, c->layout, (int)dtype_size(dtype), false, (int)heads);
+    if (n_tokens / ((int64_t)s.tokens * kRopeWaves) > kMaxGroups) return HR_ERR_LEN_RANGE;
     return HR_OK;
 }
 
@@ -181,6 +186,7 @@ int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_atten
                  !strides_fit(t->max_tokens, n_kv, a->v_token_stride, a->v_head_stride)))
         return HR_ERR_INVALID_ARG;
     if (!rows_apart(t->max_tokens, n_q, a->out_token_stride, a->out_head_stride, d)) return HR_ERR_INVALID_ARG;
+    if (make_sched_layout(t->n_pairs, t->max_tokens, n_q / n_kv).cap_blk * n_kv > kMaxGroups) return HR_ERR_LEN_RANGE;
     return HR_OK;
 }
 

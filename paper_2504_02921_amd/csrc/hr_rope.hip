@@ -17,7 +17,6 @@ namespace hr {
 
 namespace {
 
-constexpr int kRopeWaves = 4;
 constexpr int kHeadsAhead = 4;      // heads whose loads are in flight together
 
 struct RopeSide {

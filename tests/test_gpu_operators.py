@@ -186,6 +186,33 @@ def test_work_lists_do_not_depend_on_the_way_they_are_built():
         assert T.equal(out[:b.tokens], want[:b.tokens]) and T.equal(log2[:b.tokens], log[:b.tokens])
 
 
+@pytest.mark.parametrize("n_pairs,n_docs", [(20, 50), (3000, 400), (12000, 9000)])
+def test_tables_recorded_and_replayed(n_pairs, n_docs):
+    """Built in one small workgroup, sorted and counted: replays with other documents and lengths, eager work between."""
+    T, H = torch(), hb()
+    rng = np.random.default_rng(n_pairs)
+    lens = rng.integers(0, 60, n_docs)
+    cu, pages = corpus(rng, lens)
+    pool = H.KVPool(1, 2, 16, len(pages), "bf16", DEV)
+    room = 6 * n_pairs
+    listed, doc, q = H.DocList(dev_i32(lens), dev_i32(cu), dev_i32(pages)), dev_i32(np.zeros(n_pairs)), dev_i32(np.zeros(n_pairs))
+    t, side, graph = H.PairTables(pool, n_pairs, room, 4, n_q_heads=14), T.cuda.Stream(), T.cuda.CUDAGraph()
+    T.cuda.synchronize()
+    with T.cuda.stream(side):
+        t.build(listed, doc, q)
+    side.synchronize()
+    with T.cuda.graph(graph):
+        t.build(listed, doc, q)
+    for _ in range(4):
+        pair_doc, q_lens = rng.integers(-1, n_docs, n_pairs), rng.integers(0, 7, n_pairs)
+        doc.copy_(dev_i32(pair_doc))
+        q.copy_(dev_i32(q_lens))
+        graph.replay()
+        T.cuda.synchronize()
+        for name, w in R.tables(lens, cu, pages, len(pages), pair_doc, q_lens, room, 4).items():
+            np.testing.assert_array_equal(getattr(t, name).cpu().numpy(), w, err_msg=name)
+
+
 def test_tables_of_pairs_that_are_in_order_already():
     rng = np.random.default_rng(4)
     lens = rng.integers(1, 200, 50)
@@ -481,6 +508,26 @@ def test_a_layer_of_rotary_positions_pool_tables_and_attention_is_the_oracles(kv
                                            orr.rope(y[:, n_q:n_q + n_kv], pos, 10000.0), y[:, n_q + n_kv:])
         assert np.abs(out[t:t + n] - want).max() <= tol
         t += n
+
+
+def test_calls_that_would_be_taken_for_others_are_refused():
+    T, H = torch(), hb()
+    b = Batch("bf16", 14, 2, 64, [40], [0], [3])
+    other = H.KVPool(2, 2, 64, 8, "bf16", DEV)
+    with pytest.raises(H.HrError):
+        H.pair_attention(other, 0, b.tables, b.q, b.k, b.v)
+    for a in (dict(scale=0.0), dict(window=(1 << 32) + 1), dict(window=-1)):
+        with pytest.raises(H.HrError):
+            b.run(**a)
+    rope = H.Rope(64)
+    for pos, a in ((1 << 32, {}), (-1, {}), (0, dict(period=(1 << 32) + 1))):
+        with pytest.raises(H.HrError):
+            rope.apply(pos, b.q, **a)
+    with pytest.raises(H.HrError):
+        rope.apply(0, b.q, b.q, out=[b.q, b.q])
+    y, = rope.apply(np.int64(5), b.q)
+    z, = rope.apply(5, b.q)
+    assert T.equal(y, z)
 
 
 def test_a_recorded_layer_replays_with_new_lengths_and_values():

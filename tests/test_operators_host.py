@@ -159,3 +159,37 @@ def test_the_work_list_has_room_for_every_distribution_of_the_tokens():
             most = max(most, int((-(-split * g // 32)).sum()))
         assert max_tokens * g // 32 + min(n_pairs, max_tokens) >= most
         assert ints >= most * 8 + max_tokens * 4 + 6 * n_pairs
+
+
+def test_one_tensors_output_is_not_the_others():
+    cfg = hb.hr_rope_cfg(64, 64, 0, 0, 1.0, 10000.0, 1.0, 0.0, 1.0, 4.0)
+    freqs = np.full(32, 0.5)
+
+    def call(a, b, tokens=1):
+        t = (hb.hr_rope_tensor * 2)(*[hb.hr_rope_tensor(x, y, 2, 128, 64, 128, 64) for x, y in (a, b)])
+        return hb.lib.hr_rope_apply(C.byref(cfg), freqs.ctypes.data, hb.HR_BF16, tokens, FAKE, 0, 0, t, 2, 0, None)
+
+    w, x, y, z = (FAKE + 4096 * i for i in range(4))
+    for a, b in (((w, z), (x, z)), ((w, x), (x, y)), ((x, y), (w, x)), ((w, w), (w, w))):
+        assert call(a, b) == hb.HR_ERR_INVALID_ARG
+    assert call((w, w), (x, x), tokens=0) == hb.HR_OK
+
+
+def test_calls_that_no_launch_can_hold_are_refused():
+    # 64 heads of 1024 channels: a wavefront has one token
+    wide = hb.hr_rope_cfg(1024, 256, 0, 0, 1.0, 10000.0, 1.0, 0.0, 1.0, 4.0)
+    assert rope_call(cfg=wide, tokens=1 << 27, n_heads=1, in_token_stride=1024, in_head_stride=1024, out_token_stride=1024, out_head_stride=1024) == hb.HR_ERR_LEN_RANGE
+    pool = pool_handle(n_kv=8)
+    assert attend(pool, tables(pool, n_pairs=1 << 21, max_tokens=1 << 21, n_q=32), q_token_stride=2048, out_token_stride=2048) == hb.HR_ERR_LEN_RANGE
+
+
+def test_numbers_that_would_wrap_around_are_refused():
+    for x in (-1, 1 << 31, (1 << 32) + 5):
+        with pytest.raises(hb.HrError):
+            hb._int32(x, "x")
+    assert hb._int32((1 << 31) - 1, "x") == (1 << 31) - 1
+    class Pool:                                             # noqa: E306
+        mem = type("M", (), {"device": "cpu"})
+    for change in (dict(n_pairs=1 << 32), dict(max_tokens=(1 << 32) + 4), dict(pt_stride=-1), dict(n_q_heads=1 << 31)):
+        with pytest.raises(hb.HrError):
+            hb.PairTables(Pool(), **{**dict(n_pairs=1, max_tokens=1, pt_stride=1, n_q_heads=1), **change})
