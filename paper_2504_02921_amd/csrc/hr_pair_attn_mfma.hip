@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "hr_kernels.h"
 #include "hr_pair_half.h"
@@ -408,7 +409,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     };
 
     // At the at-th sub-tile: everyone has the next one, and is past the one before, whose slot is free
-    auto advance = [&](int at, Raw& r) {
+    auto advance = [&](int at, int slot, Raw& r) {
         if constexpr (!FP8) __builtin_amdgcn_s_waitcnt(0x0F70 | T::LOADS);
         __syncthreads();
         if ((at & 15) == 0 && at > 0) {                                 // the half that is past
@@ -422,10 +423,10 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         }
         if (FP8 && (at & 15) == 8 && at > 8) scale_pages(later);        // their ids are there
         if constexpr (FP8) {
-            expand(r, (at + 2) & 3, v_scale_of(at + 2));
+            expand(r, (slot + 2) & 3, v_scale_of(at + 2));
             fetch(page_of(at + 4), r);
         } else {
-            request(page_of(at + 3), (at + 3) & 3);
+            request(page_of(at + 3), (slot + 3) & 3);
         }
     };
     if (n_ring > 0) {
@@ -460,10 +461,11 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             }
             return EXTRA ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
         };
-        auto step = [&](int at, Raw& r) {
-            advance(at, r);
+        // by = at & 3: known where it is called, so that a slot's place is part of the LDS instructions
+        auto step = [&](int at, auto by, Raw& r) {
+            constexpr int vs = decltype(by)::value, ks = (vs + 1) & 3;
+            advance(at, vs, r);
             if (!active) return;
-            const int ks = (at + 1) & 3, vs = at & 3;
             const Scales cn = scales_at(at + 1);
             const float alpha = sm.follow(row_max2(mx)), use = sm.used();
             rescale(alpha);
@@ -493,16 +495,21 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(0, kk), q[kk], s, 0, 0, 0);
             mx = largest(s, 32 * (whole0 + u0), c);
         }
+        constexpr std::integral_constant<int, 0> s0{};
+        constexpr std::integral_constant<int, 1> s1{};
+        constexpr std::integral_constant<int, 2> s2{};
+        constexpr std::integral_constant<int, 3> s3{};
+        constexpr int odd = FP8 ? 1 : 0;
         int at = 0;
-        if constexpr (FP8) {
-            for (; at + 1 < n_ring_whole; at += 2) {
-                step(at, raw[0]);
-                step(at + 1, raw[1]);
-            }
-            if (at < n_ring_whole) step(at, raw[0]);
-        } else {
-            for (; at < n_ring_whole; ++at) step(at, raw[0]);
+        for (; at + 3 < n_ring_whole; at += 4) {
+            step(at, s0, raw[0]);
+            step(at + 1, s1, raw[odd]);
+            step(at + 2, s2, raw[0]);
+            step(at + 3, s3, raw[odd]);
         }
+        if (at < n_ring_whole) step(at, s0, raw[0]);
+        if (at + 1 < n_ring_whole) step(at + 1, s1, raw[odd]);
+        if (at + 2 < n_ring_whole) step(at + 2, s2, raw[0]);
     }
     // ---- sub-tiles at an edge, and own keys
 #pragma unroll 1
@@ -512,8 +519,8 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         const int key0 = 32 * (doc ? sub_of(at) : u - n_doc) + (doc ? 0 : wg.olo), end = doc ? D : wg.ohi;
         Scales c;
         if (doc) {
-            if (FP8 && (at & 1)) advance(at, raw[1]);
-            else advance(at, raw[0]);
+            if (FP8 && (at & 1)) advance(at, slot, raw[1]);
+            else advance(at, slot, raw[0]);
             c = scales_at(at);
         } else {
             __builtin_amdgcn_s_waitcnt(0x0F70);                         // nothing is on its way into LDS
