@@ -507,7 +507,7 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
  * Pairs that share a document share one pass over its pages, whatever their order in the batch.
  *   dtype         of q, k, v and out: HR_BF16 with 16-bit and fp8 pools, HR_F32 with fp32 pools (HR_ERR_MISMATCH otherwise).
  *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them),
- *                 or in fp32 where the head size is neither 64 nor 128; sums and the softmax are fp32
+ *                 or in fp32 where the head size is none of 64, 96 and 128; sums and the softmax are fp32
  *   q, out        device [max_tokens][n_q_heads][head_dim]; k, v: [max_tokens][n_kv_heads][head_dim], both or neither; strides in
  *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written.  out overlaps
  *                 none of the inputs

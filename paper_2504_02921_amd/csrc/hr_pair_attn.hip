@@ -342,7 +342,7 @@ hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, c
     const dim3 grid((unsigned)((items + round - 1) / round * round), (unsigned)w.most);
     hipError_t e;
     a.rec_tiles = (const int4*)(S + s.tile);
-    const bool half = lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 128);
+    const bool half = lay.kv_dtype != HR_F32 && (lay.d == 64 || lay.d == 96 || lay.d == 128);
     a.blocks_only = !half;
     if (half) e = launch_pair_half(lay.kv_dtype == HR_FP8_E4M3, a, grid, st);
     else if (lay.kv_dtype == HR_F32) e = f32_by_size<float, float>(a, grid, st);

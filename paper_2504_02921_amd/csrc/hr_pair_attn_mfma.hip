@@ -1,4 +1,4 @@
-// hr_pair_attention on the half matrix instructions: 16-bit and fp8 pools with heads of 64 or 128 channels.
+// hr_pair_attention on the half matrix instructions: 16-bit and fp8 pools with heads of 64, 96 or 128 channels.
 //
 // A workgroup of four wavefronts goes about its work item in one of two ways; the device, which knows the items, chooses (pair_choice):
 //   few rows   the item is one block of 32 rows, a wavefront has every fourth sub-tile of 32 keys and a softmax of its own, and they are joined
@@ -347,28 +347,31 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         }
         return r;
     };
-    // 32 own keys from place key0 on: eight threads have a key, each its share of the channels
-    constexpr int CH = HD / 8;
-    const int own_key = threadIdx.x & 31, own_c = (threadIdx.x >> 5) * CH;
-    struct Own { VecN<bf16_t, 8> k[CH / 8], v[CH / 8]; };
+    // 32 own keys from place key0 on: eight threads have a key, every eighth chunk of eight channels each
+    constexpr int CHUNKS = HD / 8, MINE = (CHUNKS + 7) / 8;
+    const int own_key = threadIdx.x & 31, own_c = threadIdx.x >> 5;
+    struct Own { VecN<bf16_t, 8> k[MINE], v[MINE]; };
     auto load_own = [&](int key0, Own& x) {
         const int64_t token = own_token(a, min(key0 + own_key, wg.ohi - 1));
-        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs + own_c, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs + own_c;
+        const bf16_t *kp = (const bf16_t*)a.k + token * a.k_ts + h * a.k_hs, *vp = (const bf16_t*)a.v + token * a.v_ts + h * a.v_hs;
 #pragma unroll
-        for (int e = 0; e < CH / 8; ++e) {
-            x.k[e] = ((const Loose<bf16_t, 8>*)(kp + e * 8))->w;
-            x.v[e] = ((const Loose<bf16_t, 8>*)(vp + e * 8))->w;
+        for (int e = 0; e < MINE; ++e) {
+            const int c = min(own_c + 8 * e, CHUNKS - 1) * 8;
+            x.k[e] = ((const Loose<bf16_t, 8>*)(kp + c))->w;
+            x.v[e] = ((const Loose<bf16_t, 8>*)(vp + c))->w;
         }
     };
     auto store_own = [&](const Own& x, int slot) {
         const int t = own_key & 15;
         half_t* dst = (half_t*)(smem + slot * T::SLOT + (own_key >> 4) * T::HBLOCK);
 #pragma unroll
-        for (int e = 0; e < CH / 8; ++e) {
-            *(halfx8*)(dst + k_elem(t, own_c + e * 8, HD, 2)) = to_half8(x.k[e]);
+        for (int e = 0; e < MINE; ++e) {
+            const int c = (own_c + 8 * e) * 8;
+            if (c >= HD) break;
+            *(halfx8*)(dst + k_elem(t, c, HD, 2)) = to_half8(x.k[e]);
             const halfx8 v = to_half8(x.v[e]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[T::HBLOCK + v_elem(t, own_c + e * 8 + i, HD)] = v[i];      // V two blocks on
+            for (int i = 0; i < 8; ++i) dst[T::HBLOCK + v_elem(t, c + i, HD)] = v[i];      // V two blocks on
         }
     };
     auto k_frag = [&](int slot, int kk) {
@@ -623,6 +626,7 @@ hipError_t half_launch(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
 
 hipError_t launch_pair_half(bool fp8, const PairAttnArgs& a, dim3 grid, hipStream_t st) {
     if (a.d == 64) return fp8 ? half_launch<64, true>(a, grid, st) : half_launch<64, false>(a, grid, st);
+    if (a.d == 96) return fp8 ? half_launch<96, true>(a, grid, st) : half_launch<96, false>(a, grid, st);
     return fp8 ? half_launch<128, true>(a, grid, st) : half_launch<128, false>(a, grid, st);
 }
 

@@ -5,7 +5,7 @@
 
 namespace hr {
 
-// 16-bit and fp8 pools with heads of 64 or 128 channels; grid: (work items of either kind, pieces)
+// 16-bit and fp8 pools with heads of 64, 96 or 128 channels; grid: (work items of either kind, pieces)
 hipError_t launch_pair_half(bool fp8, const PairAttnArgs& a, dim3 grid, hipStream_t st);
 
 }  // namespace hr

@@ -396,6 +396,16 @@ def test_what_is_not_seen_does_not_count(kv, d):
     c.check(what="document cut")
 
 
+@pytest.mark.parametrize("kv,n_q,n_kv", [("bf16", 12, 4), ("fp8", 6, 2)])
+def test_attention_of_96_channels(kv, n_q, n_kv):
+    """A head size whose rows are not a power of two: every shape and mask of the tests above."""
+    test_attention_is_the_reference(kv, n_q, n_kv, 96)
+    for pairs, doc, query in ((1, 3000, 1), (2, 5000, 3), (40, 200, 1), (30, 70, 40), (70, 500, 37)):
+        test_attention_of_few_and_of_many_rows(kv, n_q, n_kv, 96, pairs, doc, query)
+    test_attention_of_one_document_for_all(kv, 96)
+    test_what_is_not_seen_does_not_count(kv, 96)
+
+
 def test_attention_takes_views_and_leaves_other_rows_alone():
     T, H = torch(), hb()
     for kv, d in (("bf16", 64), ("bf16", 128), ("f32", 64)):
