@@ -56,7 +56,7 @@ constexpr int kPairSplitWgs = 512;                            // workgroups that
 // hr_pair_attn_mfma.hip), and their pieces.  blocks, tiles: of all kv heads.  Tiles read and expand keys once for up to four blocks, blocks fill
 // the chip sooner: tiles pay where they are more than a third full and the blocks more than the chip takes at once.  Blocks / tiles, in us:
 // 64 channels, 280 blocks of 544 keys 11.2 / 15.3, 320 of 2064 24.6 / 41.0, 700 of 544 17.9 / 15.9, 1120 of 544 27.7 / 21.2, 4480 of 544 84.8 / 44.4, two
-// a tile 2560 of 520 51.3 / 41.9; 128 channels, 128 blocks of 4112 33.3 / 44.2, 256 of 4128 45.7 / 45.3, 312 of 8200 95.0 / 75.2, 640 of 288 24.7 / 17.3;
+// a tile 2560 of 520 51.3 / 41.9; 96 channels, 240 of 544 13.2 / 18.2, 360 18.1 / 18.4, 540 23.4 / 19.6, 240 of 4128 51.1 / 48.3; 128 channels, 128 blocks of 4112 33.3 / 44.2, 256 of 4128 45.7 / 45.3, 312 of 8200 95.0 / 75.2, 640 of 288 24.7 / 17.3;
 // one block a tile, 1280 of 516 (64 channels) 37.0 / 37.1, 3200 of 520 183 / 190, 800 of 2049 (fp8) 101 / 159.
 HR_HD int pair_tile_blocks(int d) { return d == 64 ? 512 : 256; }
 struct PairChoice { bool tiles; int pieces; };
