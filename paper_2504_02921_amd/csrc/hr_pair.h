@@ -21,6 +21,15 @@ int rope_apply_check(const hr_rope_cfg* c, const double* freqs, int dtype, int64
 struct RopeShape { int vec, chunks, heads, tokens; };
 RopeShape rope_shape(int head_dim, int rotary_dim, int layout, int esz, bool in_place, int n_heads);
 
+// The channels of a lane's chunk: `n` from `at` on and, where a half layout is turned, as many a half further.  rot_chunks: chunks of rotated channels
+struct RopeChunk { int at, n; };
+HR_HD RopeChunk rope_chunk(int chunk, int rot_chunks, int vec, int layout, int rotary_dim, int head_dim) {
+    const int wide = layout == HR_ROPE_INTERLEAVED ? 2 * vec : vec;
+    if (chunk < rot_chunks) return RopeChunk{chunk * wide, wide};
+    const int at = rotary_dim + (chunk - rot_chunks) * wide;
+    return RopeChunk{at, wide < head_dim - at ? wide : head_dim - at};      // neighbours are taken two at a time: an odd head's last channel stands alone
+}
+
 // ---- tables of a batch of pairs
 // The attention's work list, in int32 units from hr_pair_tables.sched.  "In order": the pairs by document, token behind token.
 // A group is the pairs of one document; its rows for a kv head are (token in order, query head of the group of heads), heads fastest.

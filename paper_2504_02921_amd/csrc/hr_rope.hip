@@ -59,6 +59,9 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_apply_kernel(RopeArgs a)
     using V = Loose<T, W>;
     for (int chunk = chunk0; chunk < a.chunks; chunk += 64) {
         const bool turned = chunk < a.rot_chunks;
+        const RopeChunk own = rope_chunk(chunk, a.rot_chunks, VEC, INTERLEAVED ? HR_ROPE_INTERLEAVED : HR_ROPE_HALF, a.rotary, a.head_dim);
+        const int at = own.at;
+        const bool alone = INTERLEAVED && VEC == 1 && own.n == 1;      // other widths divide what they copy (rope_shape)
         float cs[VEC], sn[VEC];
         if (turned) {
 #pragma unroll
@@ -73,7 +76,6 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_apply_kernel(RopeArgs a)
                 cs[e] = ((quad + 1) & 2 ? -c2 : c2) * a.amplitude;
             }
         }
-        const int at = turned ? (INTERLEAVED ? chunk * 2 * VEC : chunk * VEC) : a.rotary + (chunk - a.rot_chunks) * W;
         for (int h0 = head0; h0 < a.n_heads[1]; h0 += kHeadsAhead * a.heads) {
             V x1[kHeadsAhead], x2[kHeadsAhead];
 #pragma unroll
@@ -82,7 +84,8 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_apply_kernel(RopeArgs a)
                 if (h >= a.n_heads[1]) break;
                 const RopeSide& d = a.side[h >= a.n_heads[0]];
                 const T* p = (const T*)d.in + t * d.in_ts + (h >= a.n_heads[0] ? h - a.n_heads[0] : h) * d.in_hs + at;
-                x1[u] = *(const V*)p;
+                if (alone) x1[u].w[0] = *p;
+                else x1[u] = *(const V*)p;
                 if (!INTERLEAVED && turned) x2[u] = *(const V*)(p + a.rotary / 2);
             }
 #pragma unroll
@@ -106,7 +109,8 @@ __global__ void __launch_bounds__(kRopeWaves * 64) rope_apply_kernel(RopeArgs a)
                     }
                     if (!INTERLEAVED) *(V*)(p + a.rotary / 2) = x2[u];
                 }
-                *(V*)p = x1[u];
+                if (alone) *p = x1[u].w[0];
+                else *(V*)p = x1[u];
             }
         }
     }
