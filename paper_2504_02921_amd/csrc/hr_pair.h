@@ -76,6 +76,15 @@ HR_HD PairChoice pair_choice(int blocks, int tiles, int d, int most) {
     c.pieces = s < 1 ? 1 : s > most ? most : s;
     return c;
 }
+// The launch that joins the pieces: its workgroups, four rows each where a row has few pieces and one by one where it has many; and the rows that there
+// are when the tables say `tokens`.  Tables that were not built say anything
+inline int64_t pair_join_groups(int64_t rows) {
+    const int64_t fours = (rows + 3) / 4, few = rows < kPairSplitWgs ? rows : kPairSplitWgs;
+    return fours > few ? fours : few;
+}
+HR_HD int64_t pair_join_rows(int tokens, int max_tokens, int n_q) {
+    return (int64_t)(tokens < 0 ? 0 : tokens > max_tokens ? max_tokens : tokens) * n_q;
+}
 struct PairWorkspace { size_t ml = 0, o = 0, total = 0; int most = 1; };
 PairWorkspace make_pair_workspace(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);
 

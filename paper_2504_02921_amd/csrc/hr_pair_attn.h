@@ -72,7 +72,7 @@ struct PairItem {
 };
 __device__ __forceinline__ int list_items(const PairAttnArgs& a, bool tiles) {
     const const_int_t hdr = (const_int_t)a.hdr;
-    return (int)min((int64_t)hdr[tiles ? SH_TILES : SH_BLOCKS], tiles ? a.cap_tile : a.cap_blk) * a.n_kv;
+    return (int)min((int64_t)max(hdr[tiles ? SH_TILES : SH_BLOCKS], 0), tiles ? a.cap_tile : a.cap_blk) * a.n_kv;
 }
 __device__ __forceinline__ PairItem list_item(const PairAttnArgs& a, bool tiles, int at) {
     const const_int_t r = (const_int_t)((tiles ? a.rec_tiles : a.rec) + 2 * min((int64_t)at, (tiles ? a.cap_tile : a.cap_blk) - 1));

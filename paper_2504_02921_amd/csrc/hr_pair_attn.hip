@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
     const int blocks = list_items(a, false), tiles = a.blocks_only ? blocks : list_items(a, true);
     const int pieces = pair_choice(blocks, tiles, a.d, a.most_splits).pieces;
     if (pieces == 1) return;                                            // the rows are there
-    const int64_t rows = (int64_t)a.hdr[SH_TOKENS] * a.g * a.n_kv;
+    const int64_t rows = pair_join_rows(a.hdr[SH_TOKENS], a.max_tokens, a.g * a.n_kv);
     constexpr int AHEAD = 8;
     if (pieces <= kJoinAlone) {
         const int64_t row = (int64_t)blockIdx.x * 4 + wave;
@@ -291,8 +291,7 @@ hipError_t f32_by_size(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
 }  // namespace
 
 static hipError_t launch_pair_join(int dtype, const PairAttnArgs& a, int64_t max_tokens, hipStream_t st) {
-    const int64_t rows = max_tokens * a.g * a.n_kv;
-    const unsigned blocks = (unsigned)std::max<int64_t>((rows + 3) / 4, std::min<int64_t>(rows, kPairSplitWgs));
+    const unsigned blocks = (unsigned)pair_join_groups(max_tokens * a.g * a.n_kv);
     if (dtype == HR_F32) pair_join_kernel<float><<<blocks, 256, 0, st>>>(a);
     else pair_join_kernel<bf16_t><<<blocks, 256, 0, st>>>(a);
     return hipGetLastError();
