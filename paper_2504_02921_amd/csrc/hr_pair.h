@@ -76,6 +76,34 @@ HR_HD PairChoice pair_choice(int blocks, int tiles, int d, int most) {
     c.pieces = s < 1 ? 1 : s > most ? most : s;
     return c;
 }
+// What the work list says of an item, from the first five words of its record.  Tables that were not built, or not for this call, are taken for what
+// they can at most be: every index stays inside its array and every loop ends, whatever they hold.
+struct PairItem {
+    int pair, D;                      // a pair of the group, and its document's length
+    int tok, row, rows;               // place of the group's first token, the item's first row, rows of the group
+};
+HR_HD int within(int lo, int v, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+HR_HD PairItem pair_item(int pair, int D, int tok, int row, int rows, int n_pairs, int max_tokens, int pt_stride, int g) {
+    PairItem it;
+    it.pair = within(0, pair, n_pairs - 1);
+    it.D = within(0, D, pt_stride * kPageTokens);
+    it.tok = within(0, tok, max_tokens - 1);
+    it.row = within(0, row, max_tokens * g - 1);
+    it.rows = within(it.row + 1, rows, max_tokens * g);
+    return it;
+}
+// A row's query head within its kv head's group and its token's place in order; rows behind the item's last one repeat that
+struct PairPlace { int head, place; };
+HR_HD PairPlace pair_place(const PairItem& it, int row, int g, int max_tokens) {
+    const int rc = row < it.rows ? row : it.rows - 1, t = rc / g;
+    return PairPlace{rc - t * g, it.tok + t < max_tokens ? it.tok + t : max_tokens - 1};
+}
+// Own keys that a whole query sees, by the caller's prefix and the query's offsets
+HR_HD int pair_prefix(int prefix, int begin, int end, int max_tokens) {
+    const int64_t n = (int64_t)end - begin, all = prefix < n ? prefix : n;
+    return all < 0 ? 0 : (int)(all < max_tokens ? all : max_tokens);
+}
+
 // The launch that joins the pieces: its workgroups, four rows each where a row has few pieces and one by one where it has many; and the rows that there
 // are when the tables say `tokens`.  Tables that were not built say anything
 inline int64_t pair_join_groups(int64_t rows) {

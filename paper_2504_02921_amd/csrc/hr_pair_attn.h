@@ -64,25 +64,13 @@ __device__ __forceinline__ int item_of(int wg, int chunk) {
     return (wg >> (3 + chunk) << (3 + chunk)) + ((wg & 7) << chunk) + (wg >> 3 & ((1 << chunk) - 1));
 }
 
-// What the work list says.  Tables that were not built, or not for this call, are taken for what they can at most be: every index below stays inside
-// its array and every loop ends, whatever they hold.
-struct PairItem {
-    int pair, D;                      // a pair of the group, and its document's length
-    int tok, row, rows;               // place of the group's first token, the item's first row, rows of the group
-};
 __device__ __forceinline__ int list_items(const PairAttnArgs& a, bool tiles) {
     const const_int_t hdr = (const_int_t)a.hdr;
     return (int)min((int64_t)max(hdr[tiles ? SH_TILES : SH_BLOCKS], 0), tiles ? a.cap_tile : a.cap_blk) * a.n_kv;
 }
 __device__ __forceinline__ PairItem list_item(const PairAttnArgs& a, bool tiles, int at) {
     const const_int_t r = (const_int_t)((tiles ? a.rec_tiles : a.rec) + 2 * min((int64_t)at, (tiles ? a.cap_tile : a.cap_blk) - 1));
-    PairItem it;
-    it.pair = min(max(r[0], 0), a.n_pairs - 1);
-    it.D = (int)min((int64_t)max(r[1], 0), (int64_t)a.pt_stride * kPageTokens);
-    it.tok = min(max(r[2], 0), a.max_tokens - 1);
-    it.row = max(r[3], 0);
-    it.rows = min(max(r[4], it.row + 1), a.max_tokens * a.g);
-    return it;
+    return pair_item(r[0], r[1], r[2], r[3], r[4], a.n_pairs, a.max_tokens, a.pt_stride, a.g);
 }
 
 // A lane's row
@@ -98,9 +86,9 @@ struct PairRow {
 __device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, const PairItem& it, int row) {
     PairRow r;
     r.on = row < it.rows;
-    const int rc = min(row, it.rows - 1), t = rc / a.g;
-    r.head = rc - t * a.g;
-    r.place = min(it.tok + t, a.max_tokens - 1);
+    const PairPlace at = pair_place(it, row, a.g, a.max_tokens);
+    r.head = at.head;
+    r.place = at.place;
     const int4 o = a.ord[r.place];    // token row, start, pair, D
     r.token = min(max(o.x, 0), a.max_tokens - 1);
     r.start = min(max(o.y, 0), r.place);
@@ -109,7 +97,7 @@ __device__ __forceinline__ PairRow pair_row(const PairAttnArgs& a, int h, const 
     const int first = a.window > 0 ? r.pos - a.window + 1 : 0;      // the first position the row sees
     r.dlo = min(max(first, 0), it.D);
     int all = 0;
-    if (a.prefix) all = min(max(a.prefix[pair], 0), a.q_cu[pair + 1] - a.q_cu[pair]);
+    if (a.prefix) all = pair_prefix(a.prefix[pair], a.q_cu[pair], a.q_cu[pair + 1], a.max_tokens);
     r.olo = r.start + min(max(first - it.D, 0), i);
     r.ohi = min(r.start + max(i + 1, all), a.max_tokens);
     r.slope = a.slopes ? a.slopes[h * a.g + r.head] * kLog2e : 0.0f;

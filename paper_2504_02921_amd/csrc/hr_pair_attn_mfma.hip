@@ -52,14 +52,15 @@ __device__ __forceinline__ PairSpan pair_span(const PairAttnArgs& a, const PairR
         return s;
     }
     // without a window: the first row's query from its first token, the last row's as far as that row sees
-    const int t0 = min(it.tok + first / a.g, a.max_tokens - 1), t1 = min(it.tok + last / a.g, a.max_tokens - 1);
+    const int t0 = pair_place(it, first, a.g, a.max_tokens).place, t1 = pair_place(it, last, a.g, a.max_tokens).place;
     const const_int_t f = (const_int_t)(a.ord + t0), l = (const_int_t)(a.ord + t1);
     s.dlo = s.dlo_all = 0;
     s.olo = min(max(f[1], 0), t0);
     s.ohi = t1 + 1;
     if (a.prefix) {
-        const int pair = min(max(l[2], 0), a.n_pairs - 1), n = ((const_int_t)a.q_cu)[pair + 1] - ((const_int_t)a.q_cu)[pair];
-        s.ohi = min(max(s.ohi, min(max(l[1], 0), t1) + min(((const_int_t)a.prefix)[pair], n)), a.max_tokens);
+        const int pair = min(max(l[2], 0), a.n_pairs - 1);
+        const const_int_t cu = (const_int_t)a.q_cu + pair;
+        s.ohi = min(max(s.ohi, min(max(l[1], 0), t1) + pair_prefix(((const_int_t)a.prefix)[pair], cu[0], cu[1], a.max_tokens)), a.max_tokens);
     }
     return s;
 }
