@@ -518,7 +518,7 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
 typedef struct hr_attention_args {
     int32_t dtype, layer;
     float scale;            /* finite; 0: 1 / sqrt(head_dim) */
-    float cap;              /* 0 (none) or positive and finite */
+    float cap;              /* 0 (none) or 1e-18 .. 1e18 */
     int32_t window;         /* 0 (none) or the number of positions */
     const void *q, *k, *v;
     void* out;

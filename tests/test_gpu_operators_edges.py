@@ -31,3 +31,41 @@ def test_rope_of_odd_heads_stays_inside_them(kind, layout, d, r):
     wide[..., :d] = x
     rope.apply(dev_i32(pos), wide[..., :d], out=[wide[..., :d]])
     assert T.equal(wide[..., :d], y) and bool((wide[..., d] == 3.0).all())
+
+
+# ---- attention ----------------------------------------------------------------------------------------------------------
+def check_cap(b, cap, **a):
+    """As Batch.check, with a bound that does not grow with the cap.  A capped score is no larger than the score and no farther from its own value than
+    the score is, so the bound of the scores without a cap holds (it has 16 half steps of a score for what is done to it; the cap takes 17 at most, of a
+    sum of magnitudes that has d + 8 and is no smaller than the score); it is taken out of the bound of the log-sum without a cap.  The rest is
+    operators_ref's: weights, sums of as many terms as there are keys, one rounding of the output."""
+    n = b.tokens
+    out, lse = b.run(cap=cap, **a)
+    x = [to64(t)[:n] for t in (b.q, b.k, b.v)]
+    a = dict(a, slopes=None if a.get("slopes") is None else to64(a["slopes"]))
+    ref = lambda v, docs, cap: R.attention(x[0], x[1], v, docs, b.pair_doc, b.q_lens, cap=cap, pool=b.kv, **a)      # noqa: E731
+    want, log, _, _ = ref(x[2], b.docs, cap)
+    _, log0, _, tol0 = ref(x[2], b.docs, 0.0)
+    sizes = ref(np.abs(x[2]), [(k, np.abs(v)) for k, v in b.docs], cap)[0]
+    keys = np.repeat([b.docs[doc][0].shape[0] + m for doc, m in zip(b.pair_doc, b.q_lens)], b.q_lens)[:, None]
+    scores = (tol0 - keys * R.U32 - 4 * R.U32 * (1 + np.abs(log0))) / 2
+    half = b.kv != "f32"
+    tol = (R.UBF if half else R.U32) * np.abs(want) + (2 * scores + 2 * keys * R.U32 + 4 * R.U32 + (R.U16 if half else 0.0))[..., None] * sizes
+    if half:
+        tol += (keys * 2.0 ** -25)[..., None] * max(np.abs(v).max() for v in [x[2]] + [v for _, v in b.docs])
+    tol_log = 2 * scores + keys * R.U32 + 4 * R.U32 * (1 + np.abs(log))
+    err, err_log = np.abs(to64(out)[:n] - want), np.abs(to64(lse)[:n] - log)
+    assert np.all(err <= tol), f"cap {cap}: out, max err / bound {np.max(err / tol):.2f}"
+    assert np.all(err_log <= tol_log), f"cap {cap}: log-sum, max err / bound {np.max(err_log / tol_log):.2f}"
+
+
+@pytest.mark.parametrize("kv,n_q,n_kv,d", [("bf16", 14, 2, 64), ("bf16", 12, 4, 96), ("bf16", 8, 1, 128), ("fp8", 6, 2, 64), ("fp8", 6, 2, 96), ("fp8", 32, 8, 128),
+                                           ("bf16", 5, 1, 80), ("f32", 4, 4, 64)])
+@pytest.mark.parametrize("pairs,doc,query", [(2, 1000, 3), (70, 200, 37)])
+def test_a_cap_does_not_cost_the_score_its_digits(kv, n_q, n_kv, d, pairs, doc, query):
+    """From caps that the scores reach to those that change none of them, in blocks, pieces and tiles."""
+    T = torch()
+    b = Batch(kv, n_q, n_kv, d, np.random.default_rng(pairs).integers(doc // 2, doc + 1, pairs), np.arange(pairs), np.full(pairs, query), seed=5, layers=1, layer=0)
+    for cap in (0.5, 20.0, 1e3, 1e5, 1e8, 1e18):
+        check_cap(b, cap)
+    check_cap(b, 1e6, slopes=T.full((n_q,), 0.01, device=DEV), window=doc // 3, scale=-0.1)
