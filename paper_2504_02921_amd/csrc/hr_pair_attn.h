@@ -180,6 +180,9 @@ __device__ __forceinline__ float pair_softmax(PairSoftmax& sm, floatx16& s) {
     return alpha;
 }
 
+// A row's log-sum: nothing seen is -infinity, a score that is NaN (which no maximum takes in) leaves NaN in the sum
+__device__ __forceinline__ float pair_lse(float m, float sum) { return sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2; }
+
 // Joins a row's pieces: what the results of one with maximum m count for under the common maximum
 __device__ __forceinline__ float piece_factor(float m, float all) { return m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - all); }
 
@@ -244,7 +247,7 @@ __device__ __forceinline__ void pair_join_waves(const PairAttnArgs& a, float* sm
         y.w[2] = from_float<QT>(acc.z * inv);
         y.w[3] = from_float<QT>(acc.w * inv);
         *(W*)out = y;
-        if (c == 0 && a.lse) a.lse[(int64_t)to.x * a.g * a.n_kv + head] = (m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2);
+        if (c == 0 && a.lse) a.lse[(int64_t)to.x * a.g * a.n_kv + head] = pair_lse(m, sum);
     }
 }
 

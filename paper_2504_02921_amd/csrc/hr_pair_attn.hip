@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
             join_store<QT>(a, row, c, acc * inv);
             if (c + 64 < a.d) join_store<QT>(a, row, c + 64, acc2 * inv);
         }
-        if (lane == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (lane == 0 && a.lse) a.lse[row] = pair_lse(m, sum);
         return;
     }
     for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(256) pair_join_kernel(PairAttnArgs a) {
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         const int c = threadIdx.x;
         if (c < a.d) join_store<QT>(a, row, c, (part[0][c] + part[1][c] + part[2][c] + part[3][c]) * inv);
-        if (c == 0 && a.lse) a.lse[row] = m == -INFINITY ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        if (c == 0 && a.lse) a.lse[row] = pair_lse(m, sum);
         __syncthreads();                                                // the next row writes where this one reads
     }
 }

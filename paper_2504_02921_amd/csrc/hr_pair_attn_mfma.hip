@@ -581,7 +581,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             for (int e = 0; e < 4; ++e) y[e] = (bf16_t)(o[mb][r + e] * inv);
             *(W*)(turn + ln * T::TURN + (mb * 32 + 8 * (r >> 2) + 4 * hh) * 2) = y;
         }
-    if (row.on && hh == 0 && a.lse) a.lse[at] = sm.m == -INFINITY ? -INFINITY : (sm.m + __builtin_amdgcn_logf(l)) * kLn2;
+    if (row.on && hh == 0 && a.lse) a.lse[at] = pair_lse(sm.m, l);
     const int64_t out_at = row.on ? row.token * a.o_ts + head * a.o_hs : -1;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");              // LDS accesses of a wavefront are done in order
     constexpr int PIECES = HD / 8;                                      // 16-byte pieces of a row

@@ -69,3 +69,29 @@ def test_a_cap_does_not_cost_the_score_its_digits(kv, n_q, n_kv, d, pairs, doc, 
     for cap in (0.5, 20.0, 1e3, 1e5, 1e8, 1e18):
         check_cap(b, cap)
     check_cap(b, 1e6, slopes=T.full((n_q,), 0.01, device=DEV), window=doc // 3, scale=-0.1)
+
+
+@pytest.mark.parametrize("kv,n_q,n_kv,d", [("bf16", 14, 2, 64), ("fp8", 8, 2, 128), ("bf16", 6, 2, 96), ("bf16", 5, 1, 80), ("f32", 4, 4, 64)])
+@pytest.mark.parametrize("pairs,doc,query", [(3, 60, 5), (1, 6000, 2), (2, 900, 20), (90, 100, 40)])
+def test_a_row_of_nan_has_neither_a_value_nor_a_log_sum(kv, n_q, n_kv, d, pairs, doc, query):
+    """Scores that are all NaN, in blocks, in few and many pieces and in tiles: the row's output and log-sum are NaN, the other rows' are as they were."""
+    T = torch()
+    b = Batch(kv, n_q, n_kv, d, [doc] * pairs, np.arange(pairs), [query] * pairs, seed=11, layers=1, layer=0)
+    out, lse = b.run()
+    q = b.q.clone()
+    q[1, 0], q[-1, n_q - 1, 3] = float("nan"), float("nan")
+    hit = T.zeros((b.tokens, n_q), dtype=T.bool, device=DEV)
+    hit[1, 0] = hit[-1, n_q - 1] = True
+    for own in (True, False):
+        out, lse = b.run(own)
+        bad, bad_lse = b.run(own, q=q)
+        assert bool(T.isnan(bad[hit]).all()) and bool(T.isnan(bad_lse[hit]).all())
+        assert T.equal(bad[~hit], out[~hit]) and T.equal(bad_lse[~hit], lse[~hit])
+    # a key that the rows behind it see beside others
+    k = b.k.clone()
+    k[query - 1, 0] = float("nan")
+    bad, bad_lse = b.run(k=k)
+    out, lse = b.run()
+    g = n_q // n_kv
+    assert bool(T.isnan(bad[query - 1, :g]).all()) and bool(T.isnan(bad_lse[query - 1, :g]).all())
+    assert T.equal(bad[:query - 1], out[:query - 1]) and T.equal(bad_lse[:query - 1], lse[:query - 1]) and T.equal(bad[query:], out[query:])
