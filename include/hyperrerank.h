@@ -509,8 +509,8 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
  *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them),
  *                 or in fp32 where the head size is none of 64, 96 and 128; sums and the softmax are fp32
  *   q, out        device [max_tokens][n_q_heads][head_dim]; k, v: [max_tokens][n_kv_heads][head_dim], both or neither; strides in
- *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written.  out overlaps
- *                 none of the inputs
+ *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written.  out and
+ *                 lse overlap none of the inputs (HR_ERR_INVALID_ARG where they begin where one of those does)
  *   lse           NULL or device fp32 [max_tokens][n_q_heads]: natural logarithm of the row's sum of exp(s)
  *   slopes        NULL or device fp32 [n_q_heads];  prefix_lens: NULL or device int32 [n_pairs] (cut to the query's length)
  * tables come from hr_pair_tables_build with the same pool; n_q_heads is theirs.  HR_ERR_LEN_RANGE if the work list has room for more

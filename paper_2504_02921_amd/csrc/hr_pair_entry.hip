@@ -34,11 +34,13 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
 
 int hr_pair_attention(const hr_pool* pool, const hr_pair_tables* tables, const hr_attention_args* args, void* workspace_dev,
                       size_t workspace_bytes, void* stream) {
-    const int rc = hr::attention_check(pool, tables, args);
+    int rc = hr::attention_check(pool, tables, args);
     if (rc != HR_OK || tables->n_pairs == 0 || tables->max_tokens == 0) return rc;
     const size_t need = hr_pair_attention_workspace_bytes(pool, tables);
     if (need > 0 && (!workspace_dev || (uintptr_t)workspace_dev % hr::kAlign != 0)) return HR_ERR_INVALID_ARG;
     if (workspace_bytes < need) return HR_ERR_WORKSPACE_SMALL;
+    rc = hr::attention_outputs_check(args);
+    if (rc != HR_OK) return rc;
     HR_OP_HIP(hr::launch_pair_attention(pool, tables, args, workspace_dev, (hipStream_t)stream));
     return HR_OK;
 }

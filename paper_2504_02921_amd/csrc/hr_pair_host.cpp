@@ -190,6 +190,15 @@ int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_atten
     return HR_OK;
 }
 
+int attention_outputs_check(const hr_attention_args* a) {
+    // workgroups write their rows while others still read keys and values, and lse is not rows of out
+    for (const void* in : {a->q, a->k, a->v, (const void*)a->lse})
+        if (a->out == in) return HR_ERR_INVALID_ARG;
+    for (const void* in : {a->q, a->k, a->v, (const void*)a->slopes, (const void*)a->prefix_lens})
+        if (a->lse && a->lse == in) return HR_ERR_INVALID_ARG;
+    return HR_OK;
+}
+
 }  // namespace hr
 
 extern "C" {
