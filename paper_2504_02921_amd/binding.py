@@ -531,7 +531,8 @@ class DocList:
 
 class PairTables:
     """Device tables of a batch of n_pairs pairs with room for max_tokens query tokens and pt_stride pages a document (hr_pair_tables).
-    build() fills q_cu, doc_lens, page_table, tok_pos, tok_pair, order and report; n_q_heads is that of the attention that will read them."""
+    build() fills q_cu, doc_lens, page_table, tok_pos, tok_pair, order and report, and comes before an attention; n_q_heads is that of the
+    attention that will read them."""
 
     def __init__(self, pool: KVPool, n_pairs: int, max_tokens: int, pt_stride: int, n_q_heads: int):
         import torch
@@ -546,6 +547,7 @@ class PairTables:
         self.q_cu, self.doc_lens, self.page_table = new(n_pairs + 1), new(n_pairs), new(n_pairs, pt_stride)
         self.tok_pos, self.tok_pair, self.order, self.report = new(max_tokens), new(max_tokens), new(n_pairs), new(4)
         self.sched = new(nbytes // 4)
+        self.built = False
         self.c = hr_pair_tables(n_pairs, max_tokens, pt_stride, n_q_heads, *[t.data_ptr() for t in (
             self.q_cu, self.doc_lens, self.page_table, self.tok_pos, self.tok_pair, self.order, self.report, self.sched)], nbytes)
         self.workspace_bytes = int(lib.hr_pair_attention_workspace_bytes(pool.handle, C.byref(self.c)))
@@ -562,6 +564,7 @@ class PairTables:
         check(lib.hr_pair_tables_build(self.pool.handle, C.byref(docs.c), _ints(pair_doc, n, dev, "PairTables.build: pair_doc"),
                                        _ints(query_lens, n, dev, "PairTables.build: query_lens"), C.byref(self.c), _stream_ptr(stream)),
               "hr_pair_tables_build")
+        self.built = True
         return self
 
 
@@ -580,6 +583,8 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
     code = _act_code(q.dtype)
     if pool is not tables.pool or q.device != dev:
         _refuse(f"pair_attention: the tables' own pool and tensors on {dev} expected, got {q.device}")
+    if not tables.built:
+        _refuse("pair_attention: tables that build() has not filled")
     if scale == 0.0:
         _refuse("pair_attention: scale: None (1 / sqrt(head_dim)) or a number that is not 0")
     layer, window = _int32(layer, "pair_attention: layer"), _int32(window, "pair_attention: window")

@@ -95,3 +95,13 @@ def test_a_row_of_nan_has_neither_a_value_nor_a_log_sum(kv, n_q, n_kv, d, pairs,
     g = n_q // n_kv
     assert bool(T.isnan(bad[query - 1, :g]).all()) and bool(T.isnan(bad_lse[query - 1, :g]).all())
     assert T.equal(bad[:query - 1], out[:query - 1]) and T.equal(bad_lse[:query - 1], lse[:query - 1]) and T.equal(bad[query:], out[query:])
+
+
+def test_tables_that_were_not_built_are_refused():
+    T, H = torch(), hb()
+    b = Batch("bf16", 4, 2, 64, [20], [0], [3])
+    t = H.PairTables(b.pool, 1, 3, 2, n_q_heads=4)
+    with pytest.raises(H.HrError):
+        H.pair_attention(b.pool, 0, t, b.q, b.k, b.v)
+    t.build(b.list, dev_i32([0]), dev_i32([3]))
+    assert T.equal(H.pair_attention(b.pool, b.layer, t, b.q, b.k, b.v), b.run()[0])
