@@ -419,6 +419,15 @@ def _strides(t, rows: int, heads: Optional[int], d: int, like, what: str):
     return shape[1], stride[0], stride[1]
 
 
+def _no_gradients(tensors, what: str) -> None:
+    """These calls have no backward pass: results of tensors that ask for one would look like constants to autograd."""
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            import torch
+            if torch.is_grad_enabled():
+                _refuse(f"{what}: no gradients are computed; call it under torch.no_grad(), or with detached tensors")
+
+
 def _ints(t, n: int, device, what: str):
     import torch
     if t.dtype != torch.int32 or t.device != device or t.numel() < n or not t.is_contiguous():
@@ -478,7 +487,8 @@ class Rope:
     def apply(self, positions, *tensors, out=None, period: int = 0, inverse: bool = False, stream=None):
         """Turns one or two tensors [tokens][heads][head_dim] (bf16 or fp32; views with any token and head stride).  positions: int32
         tensor [tokens] (tokens with a negative one are left out), or an int: token t is at positions + t % period (period 0: + t).
-        out: as many tensors, which may be `tensors` themselves (None: new ones).  Returns the list of outputs."""
+        out: as many tensors, which may be `tensors` themselves (None: new ones).  Returns the list of outputs.  No gradients: tensors that
+        require them are refused outside torch.no_grad()."""
         d = self.cfg.head_dim
         if not 1 <= len(tensors) <= 2:
             _refuse("Rope.apply: one or two tensors")
@@ -490,6 +500,7 @@ class Rope:
             import torch
             with torch.cuda.device(dev):
                 return self.apply(positions, *tensors, out=out, period=period, inverse=inverse, stream=stream)
+        _no_gradients(tensors if out is None else (*tensors, *out), "Rope.apply")
         T = x0.shape[0]
         ptr = None
         if hasattr(positions, "data_ptr"):
@@ -573,7 +584,8 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
     """Attention of the pairs' query tokens over their documents' pages and, with k and v, their own keys (hr_pair_attention).
     q [max_tokens][n_q_heads][d], k and v [max_tokens][n_kv_heads][d]: bf16 (16-bit and fp8 pools) or fp32 (fp32 pools), views with any
     token and head stride; slopes: fp32 [n_q_heads]; prefix_lens: int32 [n_pairs].  Returns out (rows behind the last token are left as they
-    are, in a new tensor unset), with_lse: and the rows' log-sums [max_tokens][n_q_heads]."""
+    are, in a new tensor unset), with_lse: and the rows' log-sums [max_tokens][n_q_heads].  No gradients: tensors that require them are refused
+    outside torch.no_grad()."""
     import torch
     dev, n_q, T = tables.device, tables.n_q_heads, tables.max_tokens
     if _elsewhere(dev):
@@ -583,6 +595,7 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
     code = _act_code(q.dtype)
     if pool is not tables.pool or q.device != dev:
         _refuse(f"pair_attention: the tables' own pool and tensors on {dev} expected, got {q.device}")
+    _no_gradients((q, k, v, out, slopes), "pair_attention")
     if not tables.built:
         _refuse("pair_attention: tables that build() has not filled")
     if scale == 0.0:

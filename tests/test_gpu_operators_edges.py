@@ -105,3 +105,24 @@ def test_tables_that_were_not_built_are_refused():
         H.pair_attention(b.pool, 0, t, b.q, b.k, b.v)
     t.build(b.list, dev_i32([0]), dev_i32([3]))
     assert T.equal(H.pair_attention(b.pool, b.layer, t, b.q, b.k, b.v), b.run()[0])
+
+
+def test_gradients_are_refused_and_not_dropped():
+    T, H = torch(), hb()
+    b = Batch("bf16", 4, 2, 64, [20], [0], [3])
+    rope = H.Rope(64)
+    want, want_q = b.run()[0], rope.apply(0, b.q)[0]
+    for name in ("q", "k", "v"):
+        x = getattr(b, name).clone().requires_grad_()
+        with pytest.raises(H.HrError, match="no_grad"):
+            b.run(**{name: x})
+        with T.no_grad():
+            assert T.equal(b.run(**{name: x})[0], want)
+    x = b.q.clone().requires_grad_()
+    for call in (lambda: rope.apply(0, x), lambda: rope.apply(0, b.q, x), lambda: rope.apply(0, b.q, out=[x]), lambda: b.run(out=x),
+                 lambda: b.run(slopes=T.zeros(4, device=DEV, requires_grad=True))):
+        with pytest.raises(H.HrError, match="no_grad"):
+            call()
+    with T.no_grad():
+        assert T.equal(rope.apply(0, x)[0], want_q)
+    assert T.equal(rope.apply(0, x.detach())[0], want_q)
