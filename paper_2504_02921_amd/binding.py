@@ -419,6 +419,15 @@ def _strides(t, rows: int, heads: Optional[int], d: int, like, what: str):
     return shape[1], stride[0], stride[1]
 
 
+def _used_on(stream, *tensors) -> None:
+    """Tells the allocator that `stream`, if it is not the current one, works with these tensors: their memory is not given out again before it is done,
+    though the caller lets go of them."""
+    if stream is not None and stream.cuda_stream != _stream_ptr():
+        for t in tensors:
+            if t is not None and t.numel():
+                t.record_stream(stream)
+
+
 def _no_gradients(tensors, what: str) -> None:
     """These calls have no backward pass: results of tensors that ask for one would look like constants to autograd."""
     for t in tensors:
@@ -502,9 +511,9 @@ class Rope:
                 return self.apply(positions, *tensors, out=out, period=period, inverse=inverse, stream=stream)
         _no_gradients(tensors if out is None else (*tensors, *out), "Rope.apply")
         T = x0.shape[0]
-        ptr = None
+        ptr = given = None
         if hasattr(positions, "data_ptr"):
-            ptr, positions = _ints(positions, T, dev, "Rope.apply: positions"), 0
+            ptr, given, positions = _ints(positions, T, dev, "Rope.apply: positions"), positions, 0
         else:
             positions, period = _int32(positions, "Rope.apply: positions"), _int32(period, "Rope.apply: period")
         sides = (hr_rope_tensor * len(tensors))()
@@ -525,6 +534,7 @@ class Rope:
         if T > 0:
             check(lib.hr_rope_apply(C.byref(self.cfg), self._freqs, code, T, ptr, positions, period, sides, len(sides),
                                     1 if inverse else 0, _stream_ptr(stream)), "hr_rope_apply")
+            _used_on(stream, given, *tensors, *outs)
         return outs
 
 
@@ -559,8 +569,8 @@ class PairTables:
         self.tok_pos, self.tok_pair, self.order, self.report = new(max_tokens), new(max_tokens), new(n_pairs), new(4)
         self.sched = new(nbytes // 4)
         self.built = False
-        self.c = hr_pair_tables(n_pairs, max_tokens, pt_stride, n_q_heads, *[t.data_ptr() for t in (
-            self.q_cu, self.doc_lens, self.page_table, self.tok_pos, self.tok_pair, self.order, self.report, self.sched)], nbytes)
+        self.tensors = (self.q_cu, self.doc_lens, self.page_table, self.tok_pos, self.tok_pair, self.order, self.report, self.sched)
+        self.c = hr_pair_tables(n_pairs, max_tokens, pt_stride, n_q_heads, *[t.data_ptr() for t in self.tensors], nbytes)
         self.workspace_bytes = int(lib.hr_pair_attention_workspace_bytes(pool.handle, C.byref(self.c)))
 
     def build(self, docs: DocList, pair_doc, query_lens, stream=None) -> "PairTables":
@@ -576,6 +586,7 @@ class PairTables:
                                        _ints(query_lens, n, dev, "PairTables.build: query_lens"), C.byref(self.c), _stream_ptr(stream)),
               "hr_pair_tables_build")
         self.built = True
+        _used_on(stream, pair_doc, query_lens, *docs.tensors, *self.tensors)
         return self
 
 
@@ -624,6 +635,7 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
     if T > 0:
         check(lib.hr_pair_attention(pool.handle, C.byref(tables.c), C.byref(args), None if ws is None else ws.data_ptr(),
                                     tables.workspace_bytes, _stream_ptr(stream)), "hr_pair_attention")
+        _used_on(stream, q, k, v, out, slopes, prefix_lens, pool.mem, *tables.tensors)
     return (out, lse) if with_lse else out
 
 

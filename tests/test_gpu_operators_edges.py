@@ -126,3 +126,41 @@ def test_gradients_are_refused_and_not_dropped():
     with T.no_grad():
         assert T.equal(rope.apply(0, x)[0], want_q)
     assert T.equal(rope.apply(0, x.detach())[0], want_q)
+
+
+def test_inputs_on_another_stream_outlive_the_callers_hold_on_them():
+    """What a call on a busy stream still has to read is not given out again: nothing is written, only asked for."""
+    T, H = torch(), hb()
+    pairs = 300000
+    b = Batch("bf16", 4, 2, 64, [20], [0], [4000])
+    t, side = H.PairTables(b.pool, pairs, 16, 2, n_q_heads=4), T.cuda.Stream()
+    rope = H.Rope(64)
+
+    def build():
+        doc, lens = (T.zeros(pairs, dtype=T.int32, device=DEV) for _ in range(2))
+        call = lambda: t.build(b.list, doc, lens, stream=side)                                      # noqa: E731
+        return call, [doc, lens]
+
+    def turn():
+        x, pos = T.zeros((300000, 2, 64), dtype=T.bfloat16, device=DEV), T.zeros(300000, dtype=T.int32, device=DEV)
+        return (lambda: rope.apply(pos, x, stream=side)), [x, pos]
+
+    def attend():
+        q, k, v = b.q.clone(), b.k.clone(), b.v.clone()
+        return (lambda: b.run(q=q, k=k, v=v, stream=side)), [q, k, v]
+
+    for make in (build, turn, attend):
+        T.cuda.synchronize()
+        call, held = make()
+        T.cuda.synchronize()
+        with T.cuda.stream(side):
+            T.cuda._sleep(50_000_000)
+        result = call()
+        places = {x.data_ptr() for x in held}
+        like = [(x.shape, x.dtype) for x in held]
+        busy = not side.query()
+        del call, held
+        fresh = [T.empty(shape, dtype=dtype, device=DEV) for shape, dtype in like]
+        assert busy and not places & {x.data_ptr() for x in fresh}, make.__name__
+        T.cuda.synchronize()
+        del result
