@@ -482,7 +482,8 @@ class Rope:
             _refuse(f"Rope: layout one of {sorted(ROPE_LAYOUT)}, scaling one of {sorted(ROPE_SCALING)}")
         if amplitude is None:
             amplitude = 0.1 * float(np.log(factor)) + 1.0 if scaling == "ramp" and factor >= 1.0 else 1.0
-        r = head_dim if rotary_dim is None else rotary_dim
+        r = _int32(head_dim if rotary_dim is None else rotary_dim, "Rope: rotary_dim")
+        head_dim = _int32(head_dim, "Rope: head_dim")
         self.cfg = hr_rope_cfg(head_dim, r, ROPE_LAYOUT[layout], ROPE_SCALING[scaling], amplitude, base, factor, original_len, low, high)
         if freqs is None:
             self.freqs = np.zeros(max(r // 2, 1), np.float64)
