@@ -164,3 +164,93 @@ def test_inputs_on_another_stream_outlive_the_callers_hold_on_them():
         assert busy and not places & {x.data_ptr() for x in fresh}, make.__name__
         T.cuda.synchronize()
         del result
+
+
+# ---- tiles ---------------------------------------------------------------------------------------------------------------
+def choice(b):
+    """Whether the device takes tiles for a batch, and into how many pieces it cuts their keys: the rule of pair_choice, on the counts of the built list."""
+    blocks, tiles = (int(x) * b.n_kv for x in b.tables.sched[2:4].tolist())
+    rows = b.tables.max_tokens * b.n_q
+    most = max(1, round(b.tables.workspace_bytes / (rows * (8 + 4 * b.d))))
+    is_tiles = blocks > (512 if b.d == 64 else 256) and 2 * blocks > 3 * tiles
+    return is_tiles, min(max(512 // max(tiles if is_tiles else blocks, 1), 1), most)
+
+
+TILE_SHAPES = [("bf16", 14, 2, 64), ("fp8", 14, 2, 64), ("bf16", 12, 4, 96), ("fp8", 12, 4, 96), ("bf16", 16, 2, 128), ("fp8", 8, 1, 128)]
+
+
+def tile_batch(kv, n_q, n_kv, d, cut, spare=0, seed=21):
+    """Pairs of a long document, of a short one, of none, with queries of no token to many, in no order; or the same behind documents that are not cut."""
+    rng = np.random.default_rng(seed)
+    pairs, rows = 40, 1600 * n_kv * 7 // n_q if d == 64 else 1200 * 8 * n_kv // (n_q * min(n_kv, 2))
+    docs = [2101, 45, 31] if cut else [500, 45, 333]
+    doc = rng.choice([0, 0, 0, 0, 1, 2, -1], pairs) if cut else rng.choice([0, 1, 2, -1], pairs)
+    lens = rng.multinomial(rows, rng.dirichlet(np.ones(pairs) * 3.0))
+    lens[[3, 17]] = [0, 1]
+    b = Batch(kv, n_q, n_kv, d, docs, doc, lens, seed=seed, spare=spare)
+    is_tiles, pieces = choice(b)
+    assert is_tiles and (pieces > 1) == cut, (is_tiles, pieces)
+    return b
+
+
+@pytest.mark.parametrize("kv,n_q,n_kv,d", TILE_SHAPES)
+@pytest.mark.parametrize("cut", [False, True])
+def test_tiles_whole_and_in_pieces(kv, n_q, n_kv, d, cut):
+    T = torch()
+    b = tile_batch(kv, n_q, n_kv, d, cut)
+    pairs = len(b.q_lens)
+    prefix = dev_i32(np.where(np.arange(pairs) % 3 == 0, 0, b.q_lens * (np.arange(pairs) % 4) // 2) - 1)      # none, in the query, past its end
+    slopes = T.full((n_q,), 0.01, device=DEV)
+    b.check(what="plain")
+    b.check(prefix_lens=prefix, what="prefix")
+    b.check(window=300, prefix_lens=prefix, what="prefix and window")
+    b.check(own=False, window=40, what="pieces that see nothing, rows that see nothing")
+    b.check(window=9, what="window inside the queries")
+    b.check(cap=20.0, slopes=slopes, window=450, prefix_lens=prefix, scale=-0.1, what="all")
+
+
+@pytest.mark.parametrize("kv,n_q,n_kv,d", TILE_SHAPES)
+@pytest.mark.parametrize("cut", [False, True])
+def test_tiles_leave_alone_what_is_not_theirs(kv, n_q, n_kv, d, cut):
+    """Values that are not finite where nobody looks, packed rows one element off, outputs between others, rows behind the last token."""
+    T = torch()
+    b = tile_batch(kv, n_q, n_kv, d, cut, spare=5, seed=22)
+    cu = np.concatenate([[0], np.cumsum(b.q_lens)])
+    long = [p for p in range(len(b.q_lens)) if b.q_lens[p] >= 12][:6]
+    prefix = dev_i32(np.minimum(b.q_lens // 3, 4))
+    for a in (dict(), dict(window=200), dict(prefix_lens=prefix, window=100), dict(prefix_lens=prefix)):
+        out, lse = b.run(**a)
+        q, k, v = (t.clone() for t in (b.q, b.k, b.v))
+        for t in (q, k, v):
+            t[b.tokens:] = float("nan")
+        hit = np.zeros(b.tokens, bool)
+        for i, p in enumerate(long):                                        # a key late in a pair's query: the tokens from it on see it
+            at = cu[p] + b.q_lens[p] - 1 - i
+            (v if i % 2 else k)[at] = float("nan") if i < 3 else float("inf")
+            hit[at:cu[p + 1]] = True
+        keep = T.from_numpy(~hit).to(DEV)
+        bad, bad_lse = b.run(q=q, k=k, v=v, **a)
+        assert T.equal(bad[:b.tokens][keep], out[:b.tokens][keep]) and T.equal(bad_lse[:b.tokens][keep], lse[:b.tokens][keep])
+        assert not bool(T.isfinite(bad[:b.tokens][~keep]).all(-1).any())
+        n = b.q.shape[0]
+        flat = T.zeros(n * (n_q + 2 * n_kv) * d + 1, dtype=b.q.dtype, device=DEV)
+        rows = flat[1:].view(n, n_q + 2 * n_kv, d)
+        rows[:, :n_q], rows[:, n_q:n_q + n_kv], rows[:, n_q + n_kv:] = b.q, b.k, b.v
+        rows[b.tokens:] = float("nan")
+        wide = T.full((n_q + 2, n, d + 4), 3.0, dtype=b.q.dtype, device=DEV)
+        into = wide[1:1 + n_q, :, :d].transpose(0, 1)
+        got, got_lse = b.run(q=rows[:, :n_q], k=rows[:, n_q:n_q + n_kv], v=rows[:, n_q + n_kv:], out=into, **a)
+        assert T.equal(got[:b.tokens], out[:b.tokens]) and T.equal(got_lse[:b.tokens], lse[:b.tokens])
+        assert bool((into[b.tokens:] == 3.0).all()) and bool((wide[0] == 3.0).all()) and bool((wide[n_q + 1] == 3.0).all()) and bool((wide[:, :, d:] == 3.0).all())
+
+
+@pytest.mark.parametrize("kv,n_q,n_kv,d", TILE_SHAPES + [("bf16", 5, 1, 80), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("stride", [1, 60])
+def test_a_long_query_without_a_document_attends_to_itself(kv, n_q, n_kv, d, stride):
+    """A prompt's own causal attention; with room for long documents, so that pieces begin among the own keys."""
+    b = Batch(kv, n_q, n_kv, d, [10], [-1, 0, -1], [1400, 33, 90], seed=23, stride=stride)
+    if kv != "f32" and d in (64, 96, 128):                                  # the kernels that know tiles
+        assert choice(b)[0] and (choice(b)[1] > 1) == (stride == 60), choice(b)
+    b.check(what="causal")
+    b.check(window=100, what="window")
+    b.check(prefix_lens=dev_i32([50, 33, 0]), what="prefix")
