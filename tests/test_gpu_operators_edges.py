@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 import operators_ref as R
+from oracle import fp8 as ofp8
 from test_gpu_operators import DEV, Batch, check_rope, dev_i32, dtype_of, hb, to64, torch
 
 pytestmark = pytest.mark.gpu
@@ -254,3 +255,76 @@ def test_a_long_query_without_a_document_attends_to_itself(kv, n_q, n_kv, d, str
     b.check(what="causal")
     b.check(window=100, what="window")
     b.check(prefix_lens=dev_i32([50, 33, 0]), what="prefix")
+
+
+# ---- sizes at their ends --------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("n_pairs", [5, 300, 6000])
+def test_tables_without_a_single_document(n_pairs):
+    H = hb()
+    rng = np.random.default_rng(n_pairs)
+    pool = H.KVPool(1, 2, 16, 1, "bf16", DEV)
+    pair_doc, q_lens = rng.choice([-1, -1, 0, 7], n_pairs), rng.integers(0, 5, n_pairs)
+    none = np.zeros(0, np.int64)
+    t = H.PairTables(pool, n_pairs, int(q_lens.sum()), 0, n_q_heads=14)
+    t.build(H.DocList(dev_i32(none), dev_i32([0]), dev_i32(none)), dev_i32(pair_doc), dev_i32(q_lens))
+    for name, w in R.tables(none, np.zeros(1, np.int64), none, 1, pair_doc, q_lens, int(q_lens.sum()), 0).items():
+        np.testing.assert_array_equal(getattr(t, name).cpu().numpy(), w, err_msg=name)
+
+
+@pytest.mark.parametrize("kv,d", [("bf16", 128), ("fp8", 128), ("bf16", 96), ("bf16", 80), ("f32", 128)])
+@pytest.mark.parametrize("pairs", [3, 90])
+def test_attention_of_pages_and_rows_past_32_bits(kv, d, pairs):
+    """Pages at the end of a pool of more than 4 GiB, rows of q, k, v and out that far apart: the bits of the same call close together."""
+    T, H = torch(), hb()
+    n_q, n_kv, D, query = 8, 8, 70, 12
+    rng = np.random.default_rng(pairs)
+    page = 2 * R.PAGE * d * n_kv * {"bf16": 2, "fp8": 1, "f32": 4}[kv]
+    n_pages = (5 << 30) // page
+    k, v = (rng.standard_normal((1, D, n_kv, d)) for _ in range(2))
+    if kv == "fp8":
+        (kc, ks), (vc, vs) = ofp8.quantize_doc_kv(k), ofp8.quantize_doc_kv(v)
+        given = [T.from_numpy(np.ascontiguousarray(x)).to(DEV) for x in (kc, vc, ks.astype(np.float32), vs.astype(np.float32))]
+    else:
+        given = [T.from_numpy(x).to(dtype_of(kv)).to(DEV) for x in (k, v)]
+    tokens = pairs * query
+    gen = T.Generator().manual_seed(1)
+    rows = [T.randn((tokens, n, d), generator=gen).to(dtype_of(kv)).to(DEV) for n in (n_q, n_kv, n_kv)]
+    results = []
+    for pages in (5, n_pages):
+        pool = H.KVPool(1, n_kv, d, pages, kv, DEV)
+        ids = np.arange(pages - 5, pages, dtype=np.int32)
+        pool.write(D, ids, *given)
+        t = H.PairTables(pool, pairs, tokens, 5, n_q_heads=n_q).build(H.DocList(dev_i32([D]), dev_i32([0, 5]), dev_i32(ids)), dev_i32(np.zeros(pairs)), dev_i32(np.full(pairs, query)))
+        apart = rows
+        if pages == n_pages:
+            step = ((5 << 30) // (4 if kv == "f32" else 2) // tokens + d) // 8 * 8
+            assert step * (tokens - 1) * (4 if kv == "f32" else 2) > 1 << 32 and step >= (n_q + 2 * n_kv) * d
+            room = T.zeros(step * tokens, dtype=rows[0].dtype, device=DEV).view(tokens, step)
+            cut, at = [], 0
+            for x in rows:
+                cut.append(room[:, at:at + x.shape[1] * d].unflatten(1, (x.shape[1], d)))
+                cut[-1].copy_(x)
+                at += x.shape[1] * d
+            apart = cut
+            out = T.zeros_like(room)[:, :n_q * d].unflatten(1, (n_q, d))
+        else:
+            out = T.zeros_like(rows[0])
+        results.append(H.pair_attention(pool, 0, t, *apart, out=out, with_lse=True))
+        T.cuda.synchronize()
+    assert T.equal(results[0][0], results[1][0]) and T.equal(results[0][1], results[1][1]) and bool(T.isfinite(results[0][0]).all())
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_of_rows_past_32_bits(layout):
+    T, H = torch(), hb()
+    tokens, heads, d = (1 << 18) + 3, 64, 128
+    x = T.zeros((tokens, heads, d), dtype=T.bfloat16, device=DEV)
+    assert x.numel() > 1 << 31
+    some = T.randn((5, heads, d), generator=T.Generator().manual_seed(1)).to(T.bfloat16).to(DEV)
+    x[:2], x[-3:] = some[:2], some[2:]
+    rope = H.Rope(d, 10000.0, layout=layout)
+    want, = rope.apply(dev_i32([0, 1, tokens - 3, tokens - 2, tokens - 1]), some)
+    y, = rope.apply(0, x)
+    assert T.equal(y[:2], want[:2]) and T.equal(y[-3:], want[2:])
+    rope.apply(0, x, out=[x])
+    assert T.equal(y, x)
