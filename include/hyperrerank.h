@@ -404,7 +404,7 @@ int hr_rerank_topk_host(const float* scores_dev, const int32_t* seg_offsets, int
  * hr_rerank_score runs the layers of one kind of decoder.  A model with other positions, masks or score functions can still
  * keep its documents in a pool and run its own projections: these calls give it rotary positions (a pool's K is post-RoPE), the
  * tables of a batch of pairs, built on the device, and the attention of the pairs' query tokens over their documents' pages.
- * None of them allocates, waits on the host or keeps anything between calls; all may be recorded into a HIP graph. */
+ * None of them allocates, waits on the host or keeps anything between calls; all may be recorded into a HIP graph.  None has a backward pass. */
 
 /* Rotary positions.  The leading rotary_dim channels of every head are turned in rotary_dim / 2 pairs: pair i of a token at
  * position p by the angle p * freqs[i]:  a' = a cos - b sin, b' = b cos + a sin; the other channels stay as they are.
@@ -492,7 +492,8 @@ size_t hr_pair_tables_sched_bytes(const hr_pool* pool, int32_t n_pairs, int32_t 
 /* Fills the tables from pair_doc_dev (device int32 [n_pairs]: a document, -1 for none) and query_lens_dev (device int32
  * [n_pairs], 0 and more).  Nothing comes back to the host: what is wrong with the contents is mended as the bits above say and
  * noted in report, and no table leads outside the pool, the page list or max_tokens.  Whether pages hold a document (hr_doc_kv_write)
- * is not checked.  HR_ERR_INVALID_ARG on null pointers and bad sizes, HR_ERR_WORKSPACE_SMALL for sched_bytes;
+ * is not checked.  HR_ERR_INVALID_ARG on null pointers and bad sizes, HR_ERR_LEN_RANGE for more than 2^30 pairs or rows of a kv head (max_tokens
+ * times the heads of one) or 2^26 pages a document, HR_ERR_WORKSPACE_SMALL for sched_bytes;
  * n_pairs = 0 is a no-op. */
 int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int32_t* pair_doc_dev, const int32_t* query_lens_dev,
                          const hr_pair_tables* out, void* stream);
@@ -506,14 +507,15 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
  * not seen does not count, whatever it holds.
  * Pairs that share a document share one pass over its pages, whatever their order in the batch.
  *   dtype         of q, k, v and out: HR_BF16 with 16-bit and fp8 pools, HR_F32 with fp32 pools (HR_ERR_MISMATCH otherwise).
- *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them),
- *                 or in fp32 where the head size is none of 64, 96 and 128; sums and the softmax are fp32
+ *                 bf16 values are multiplied as halves (exact for magnitudes in [2^-14, 65504], as hr_doc_kv_write keeps them; smaller
+ *                 ones lose digits, larger ones are infinite), and the weights of V are rounded to half (by 2^-11 of a weight, or
+ *                 2^-25 of the row's largest); in fp32 where the head size is none of 64, 96 and 128.  Maxima, sums and the joins are fp32
  *   q, out        device [max_tokens][n_q_heads][head_dim]; k, v: [max_tokens][n_kv_heads][head_dim], both or neither; strides in
  *                 elements, channels of a head follow each other.  Rows behind the last token are neither read nor written.  out and
  *                 lse overlap none of the inputs (HR_ERR_INVALID_ARG where they begin where one of those does)
  *   lse           NULL or device fp32 [max_tokens][n_q_heads]: natural logarithm of the row's sum of exp(s)
  *   slopes        NULL or device fp32 [n_q_heads];  prefix_lens: NULL or device int32 [n_pairs] (cut to the query's length)
- * tables come from hr_pair_tables_build with the same pool; n_q_heads is theirs.  HR_ERR_LEN_RANGE if the work list has room for more
+ * tables come from hr_pair_tables_build with the same pool, ahead of the call on its stream; n_q_heads is theirs.  HR_ERR_LEN_RANGE if the work list has room for more
  * than some 2^24 blocks of 32 rows (max_tokens x heads of a kv head / 32, and a block for every pair, times the kv heads). */
 typedef struct hr_attention_args {
     int32_t dtype, layer;
@@ -527,7 +529,8 @@ typedef struct hr_attention_args {
     const int32_t* prefix_lens;
     int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, out_token_stride, out_head_stride;
 } hr_attention_args;
-/* Workspace of one call; may be 0.  It is private to the call until `stream` has drained. */
+/* Workspace of one call; may be 0.  It is private to the call until `stream` has drained.  It goes by the tables' room (n_pairs, max_tokens,
+ * pt_stride), and so does the number of pieces that a long document's keys can be cut into where there are few rows: room for many tokens leaves few. */
 size_t hr_pair_attention_workspace_bytes(const hr_pool* pool, const hr_pair_tables* tables);
 int hr_pair_attention(const hr_pool* pool, const hr_pair_tables* tables, const hr_attention_args* args, void* workspace_dev,
                       size_t workspace_bytes, void* stream);

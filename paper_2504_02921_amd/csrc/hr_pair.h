@@ -57,7 +57,7 @@ int tables_build_check(const hr_pool* pool, const hr_doc_list* docs, const int32
 int attention_check(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* a);
 int attention_outputs_check(const hr_attention_args* a);      // ... of a call that has something to write: its outputs are not its inputs
 // Few rows and long documents: an item's keys are cut into up to `most` pieces, each a workgroup's, whose results are joined by a second
-// launch.  How many is decided on the device, which knows the items (pair_splits); `most` bounds grid and workspace.
+// launch.  How many is decided on the device, which knows the items (pair_choice); `most` bounds grid and workspace.
 // Whole / in pieces, with the join: 16 blocks of 304 keys 10.6 / 11.8 us, of 544 12.7 / 12.4, of 1025 18.1 / 12.5, of 2049 28.7 / 12.7.
 constexpr int kPairSplitMost = 128, kPairSplitKeys = 256, kPairSplitLeast = 768;      // keys of a piece, of documents that are cut, at least
 int pair_most_splits(int64_t n_pairs, int64_t max_tokens, int n_q, int n_kv, int d, int64_t pt_stride);

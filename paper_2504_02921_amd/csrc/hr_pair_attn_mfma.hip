@@ -10,7 +10,7 @@
 //              of half pages: half pages straight from memory, fp8 pages by way of a wavefront's registers, which expands them once for all rows.
 //              S of a sub-tile is computed next to the exponentials of the one before.  Bound by what a wavefront issues and, with 128 channels, by
 //              power: 640 x 512 keys x 32 tokens, 64 channels, 81 us, 479 TFLOP/s; 400 x 2048 x 64, 128 channels, 1150 us, 758 TFLOP/s (MFMA 44 % of the
-//              cycles of a clock that falls to 1.3 GHz), the same in fp8 1250 us, 698 TFLOP/s (VALU 65 %, MFMA 33 %, 1.7 GHz).
+//              cycles of a clock that falls to 1.3 GHz), the same in fp8 1250 to 1280 us, 682 to 698 TFLOP/s (VALU 65 %, MFMA 33 %, 1.7 GHz).
 //              Heads of 96 channels have no swizzle in their pages, and their K reads meet in banks: 640 x 512 x 32 155 us, 321 TFLOP/s.
 #include <hip/hip_runtime.h>
 

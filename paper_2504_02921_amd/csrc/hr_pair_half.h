@@ -38,7 +38,9 @@ __device__ __forceinline__ halfx8 to_half8(VecN<bf16_t, 8> x) {
 }
 __device__ __forceinline__ halfx8 bf16x8_to_half(const bf16_t* p) { return to_half8(((const Loose<bf16_t, 8>*)p)->w); }
 
-// the lane's 16 probabilities as the B operands of two products over 16 keys each
+// the lane's 16 probabilities as the B operands of two products over 16 keys each, rounded to half: 2^-11 of a weight (nothing of one below 2^-25, the
+// largest being 1 or more), an eighth of what an output loses in bf16; as fp32 the product would run at the seventh part of the rate.  Their sum is that
+// of the unrounded ones
 __device__ __forceinline__ void pack_p(const floatx16& s, halfx8 (&pf)[2], float f0, float f1) {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {

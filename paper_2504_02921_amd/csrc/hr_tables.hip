@@ -4,8 +4,8 @@
 //   small    one workgroup, a thread a pair, everything that one step hands to the next in LDS: what it costs is the loads that depend on each other
 //            (document, its place in the list, its pages).  20 pairs 6 us on the device, 200 of 4 tokens 18.0 (256, the second way: 20.0).
 //   sorted   one workgroup goes over the pairs in turn (offsets, a stable radix sort by document of up to 8 bits a pass, least first, each wavefront
-//            with a run of its own, groups, row blocks): passes of scans, which are short (a pair is 8 bytes), while a launch of many would wait
-//            at a grid barrier for each.  What is written per pair, token and block goes to the whole chip in a second launch.
+//            with a run of its own, groups, row blocks): passes of scans, which are short (a pair is 8 bytes).  Many workgroups, with a
+//            launch or a grid barrier for each pass, have not been measured.  What is written per pair, token and block goes to the whole chip in a second launch.
 //   counted  many pairs: that workgroup only counts the pairs and tokens of every document, kWindow of them at a time in LDS, which gives groups and
 //            row blocks; the order of the pairs, most of the sort's time, is found by many workgroups (tables_place_kernel).
 // Sorted / counted, in us: 4096 pairs over 1000 documents 33.9 / 34.4, 8192 over 1000 43.6 / 36.7, 25600 over 8192 129 / 65 (counts 30, places 18,
