@@ -515,8 +515,8 @@ int hr_pair_tables_build(const hr_pool* pool, const hr_doc_list* docs, const int
  *                 lse overlap none of the inputs (HR_ERR_INVALID_ARG where they begin where one of those does)
  *   lse           NULL or device fp32 [max_tokens][n_q_heads]: natural logarithm of the row's sum of exp(s)
  *   slopes        NULL or device fp32 [n_q_heads];  prefix_lens: NULL or device int32 [n_pairs] (cut to the query's length)
- * tables come from hr_pair_tables_build with the same pool, ahead of the call on its stream; n_q_heads is theirs.  HR_ERR_LEN_RANGE if the work list has room for more
- * than some 2^24 blocks of 32 rows (max_tokens x heads of a kv head / 32, and a block for every pair, times the kv heads). */
+ * tables come from hr_pair_tables_build with the same pool, ahead of the call on its stream; n_q_heads is theirs.  HR_ERR_LEN_RANGE
+ * if the work list has room for more than some 2^24 blocks of 32 rows (max_tokens x heads of a kv head / 32, and a block for every pair, times the kv heads). */
 typedef struct hr_attention_args {
     int32_t dtype, layer;
     float scale;            /* finite; 0: 1 / sqrt(head_dim) */

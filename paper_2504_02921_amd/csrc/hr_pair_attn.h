@@ -130,7 +130,7 @@ __device__ __forceinline__ void pair_scores(floatx16& s, const PairAttnArgs& a, 
             t = fmaf(u, t, 3.3333333e-1f);
             s[r] = fabsf(x) < 0.5f ? a.cap_log2 * fmaf(-x * u, t, x) : quotient(s[r] * a.cap_in);
         }
-    } else if (a.cap_log2 > kCapSeries * kLog2e) {
+    } else if (a.cap_log2 >= kCapSeries * kLog2e) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             // cap and its reciprocal make one: s (1 - x^2 / 3 + 2 x^4 / 15), of which 2^-22 is left at 1/8; the quotient is 2^-20 of its value off there

@@ -67,7 +67,7 @@ def test_a_cap_does_not_cost_the_score_its_digits(kv, n_q, n_kv, d, pairs, doc, 
     """From caps that the scores reach to those that change none of them, in blocks, pieces and tiles."""
     T = torch()
     b = Batch(kv, n_q, n_kv, d, np.random.default_rng(pairs).integers(doc // 2, doc + 1, pairs), np.arange(pairs), np.full(pairs, query), seed=5, layers=1, layer=0)
-    for cap in (0.5, 20.0, 1e3, 1e5, 1e8, 1e18):
+    for cap in (0.5, 20.0, 64.0, 1e3, 1e5, 1e8, 1e18):
         check_cap(b, cap)
     check_cap(b, 1e6, slopes=T.full((n_q,), 0.01, device=DEV), window=doc // 3, scale=-0.1)
 
@@ -155,7 +155,7 @@ def test_inputs_on_another_stream_outlive_the_callers_hold_on_them():
         call, held = make()
         T.cuda.synchronize()
         with T.cuda.stream(side):
-            T.cuda._sleep(50_000_000)
+            T.cuda._sleep(100_000_000)
         result = call()
         places = {x.data_ptr() for x in held}
         like = [(x.shape, x.dtype) for x in held]
