@@ -45,10 +45,18 @@ struct PairAttnArgs {
     int32_t blocks_only;              // work items are blocks (kernels that know no tiles)
 };
 
-// Scores need more than a positive factor before they are compared: the kernels' EXTRA form
-inline bool pair_extra(const PairAttnArgs& a) { return a.cap_in != 0.0f || a.slopes || a.scale_log2 < 0.0f; }
-
+// What scores need before they are compared, a kernel's form for each: a positive factor alone, or also a cap, a bias or a factor below 0.  The quotient
+// of a cap is off by 2^-23 of it, whatever the score: with wide caps, from kWideCap on, small arguments take the series of tanh, and in the
+// fp32 kernels (EXACT) under any cap.  Below kWideCap the quotient leaves 2^-17 in a score, a 64th of what the weight loses in half.
+// Quotient alone / with the series: 200 documents of 2048 x 64 tokens, 128 channels 742 / 793 us, 640 of 512 x 32, 64 channels 104 / 108
+enum PairScores { PS_FACTOR = 0, PS_EXTRA = 1, PS_WIDE_CAP = 2, PS_EXACT = 3 };
+constexpr float kWideCap = 64.0f;
 constexpr float kLn2 = 0.69314718055994531f, kLog2e = 1.4426950408889634f;
+
+inline PairScores pair_scores_of(const PairAttnArgs& a) {
+    if (a.cap_log2 >= kWideCap * kLog2e) return PS_WIDE_CAP;
+    return a.cap_in != 0.0f || a.slopes || a.scale_log2 < 0.0f ? PS_EXTRA : PS_FACTOR;
+}
 
 __device__ __forceinline__ int rows_min(int v) {          // over the 32 rows of a wavefront
 #pragma unroll
@@ -108,38 +116,36 @@ __device__ __forceinline__ int64_t own_token(const PairAttnArgs& a, int place) {
 
 // The scaled scores of a sub-tile in log2 units: cap, then distance.  first: position (document) or place (own) of its first key as seen from
 // the row, i.e. minus the row's own
-// The quotient is off by 2^-23 of the cap, whatever the score: small arguments take the series of tanh, with EXACT (fp32 operands) under any cap, else
-// under caps from kCapSeries on, below which the quotient leaves 2^-17 in a score, a 64th of what the weight loses in half.
-// Quotient alone / with the series: 200 documents of 2048 x 64 tokens, 128 channels 742 / 793 us, 640 of 512 x 32, 64 channels 104 / 108
-constexpr float kCapSeries = 64.0f;
-template <bool EXACT>
+template <int FORM>
 __device__ __forceinline__ void pair_scores(floatx16& s, const PairAttnArgs& a, const PairRow& row, int first, int hh) {
-    // tanh x = 1 - 2 / (e^2x + 1); 2 log2 e is in cap_in
-    auto quotient = [&](float y) { return fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.0f), a.cap_log2); };
-    constexpr float h = 0.5f * kLn2;                                    // x = h y
-    if (EXACT && a.cap_in != 0.0f) {
+    if (a.cap_in != 0.0f) {
+        // tanh x = 1 - 2 / (e^2x + 1); 2 log2 e is in cap_in
+        auto quotient = [&](float y) { return fmaf(-2.0f * a.cap_log2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y) + 1.0f), a.cap_log2); };
+        constexpr float h = 0.5f * kLn2;                                // x = h y
+        if (FORM == PS_EXACT) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            // x - x^3 / 3 + 2 x^5 / 15 - ..: behind the seventh of these terms 10^-8 of the value is left at 1/2
-            const float x = s[r] * a.cap_in * h, u = x * x;
-            float t = fmaf(u, 1.4558344e-3f, -3.5921280e-3f);
-            t = fmaf(u, t, 8.8632355e-3f);
-            t = fmaf(u, t, -2.1869489e-2f);
-            t = fmaf(u, t, 5.3968254e-2f);
-            t = fmaf(u, t, -1.3333333e-1f);
-            t = fmaf(u, t, 3.3333333e-1f);
-            s[r] = fabsf(x) < 0.5f ? a.cap_log2 * fmaf(-x * u, t, x) : quotient(s[r] * a.cap_in);
+            for (int r = 0; r < 16; ++r) {
+                // x - x^3 / 3 + 2 x^5 / 15 - ..: behind the seventh of these terms 10^-8 of the value is left at 1/2
+                const float x = s[r] * a.cap_in * h, u = x * x;
+                float t = fmaf(u, 1.4558344e-3f, -3.5921280e-3f);
+                t = fmaf(u, t, 8.8632355e-3f);
+                t = fmaf(u, t, -2.1869489e-2f);
+                t = fmaf(u, t, 5.3968254e-2f);
+                t = fmaf(u, t, -1.3333333e-1f);
+                t = fmaf(u, t, 3.3333333e-1f);
+                s[r] = fabsf(x) < 0.5f ? a.cap_log2 * fmaf(-x * u, t, x) : quotient(s[r] * a.cap_in);
+            }
+        } else if (FORM == PS_WIDE_CAP) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                // cap and its reciprocal make one: s (1 - x^2 / 3 + 2 x^4 / 15), of which 2^-22 is left at 1/8; the quotient is 2^-20 of its value off there
+                const float y = s[r] * a.cap_in, u = y * y, t = fmaf(u, fmaf(u, 2.0f * h * h * h * h / 15.0f, -h * h / 3.0f), 1.0f);
+                s[r] = fabsf(y) < 0.125f / h ? s[r] * t : quotient(y);
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = quotient(s[r] * a.cap_in);
         }
-    } else if (a.cap_log2 >= kCapSeries * kLog2e) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            // cap and its reciprocal make one: s (1 - x^2 / 3 + 2 x^4 / 15), of which 2^-22 is left at 1/8; the quotient is 2^-20 of its value off there
-            const float y = s[r] * a.cap_in, u = y * y, t = fmaf(u, fmaf(u, 2.0f * h * h * h * h / 15.0f, -h * h / 3.0f), 1.0f);
-            s[r] = fabsf(y) < 0.125f / h ? s[r] * t : quotient(y);
-        }
-    } else if (a.cap_in != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = quotient(s[r] * a.cap_in);
     }
     if (a.slopes) {
         const float f = (float)(first + 4 * hh);

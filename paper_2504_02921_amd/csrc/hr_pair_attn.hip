@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kWaves * 64) pair_attn_f32_kernel(PairAttnArgs
         const float c0 = a.scale_log2 * ks[0], c1 = a.scale_log2 * ks[1];
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= r < 8 ? c0 : c1;
-        pair_scores<true>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        pair_scores<PS_EXACT>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
         const bool whole = doc && key0 >= dlo_all && key0 + 32 <= D;
         unsigned seen = 0xFFFFu;                                        // of the lane's 16 keys
         if (!whole) {

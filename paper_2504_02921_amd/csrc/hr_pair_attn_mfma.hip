@@ -77,7 +77,7 @@ __device__ __forceinline__ void load_q(const PairAttnArgs& a, const PairRow& row
 }
 
 // ---- few rows
-template <int HD, bool FP8, bool EXTRA>
+template <int HD, bool FP8, int FORM>
 __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, const PairItem& it, int h, int pieces) {
     using G = PairGeo<HD, FP8>;
     using Piece = typename G::Piece;
@@ -167,7 +167,7 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, co
             load_k(kr);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= r < 8 ? c0 : c1;
-            if (EXTRA) pair_scores<false>(s, a, row, (whole0 + j) * 32 - row.pos, hh);
+            if (FORM) pair_scores<FORM>(s, a, row, (whole0 + j) * 32 - row.pos, hh);
             rescale(pair_softmax(sm, s));
             halfx8 pf[2];
             pack_p(s, pf, FP8 ? fp8_scale_mantissa(vs[0]) : 1.0f, FP8 ? fp8_scale_mantissa(vs[1]) : 1.0f);
@@ -224,7 +224,7 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, co
         const float c0 = a.scale_log2 * ks[0], c1 = a.scale_log2 * ks[1];
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= r < 8 ? c0 : c1;
-        if (EXTRA) pair_scores<false>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        if (FORM) pair_scores<FORM>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
         const int lo = (doc ? row.dlo : row.olo) - key0, hi = (doc ? D : row.ohi) - key0;
         hide_keys(s, lo - 4 * hh, hi - 4 * hh);
         rescale(pair_softmax(sm, s));
@@ -239,7 +239,7 @@ __device__ __forceinline__ void pair_rows(const PairAttnArgs& a, float* smem, co
 }
 
 // ---- many rows
-template <int HD, bool FP8, bool EXTRA>
+template <int HD, bool FP8, int FORM>
 __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, const PairItem& it, int h, int pieces) {
     using G = PairGeo<HD, FP8>;
     using T = TileGeo<HD>;
@@ -451,12 +451,12 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         floatx16 s = {};
         float mx = 0.0f;
         Scales c = scales_at(0);
-        // the largest of a lane's raw scores, scaled where they are scaled later; EXTRA: scaled, capped and biased in place
+        // the largest of a lane's raw scores, scaled where they are scaled later; FORM: scaled, capped and biased in place
         auto largest = [&](floatx16& x, int key0, const Scales& c) {
-            if (EXTRA) {
+            if (FORM) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) x[r] *= a.scale_log2 * (r < 8 ? c.k0 : c.k1);
-                pair_scores<false>(x, a, row, key0 - row.pos, hh);
+                pair_scores<FORM>(x, a, row, key0 - row.pos, hh);
             }
             float m0 = x[0], m1 = x[8];
 #pragma unroll
@@ -464,7 +464,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
                 m0 = fmaxf(m0, x[r]);
                 m1 = fmaxf(m1, x[8 + r]);
             }
-            return EXTRA ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
+            return FORM ? fmaxf(m0, m1) : FP8 ? fmaxf(m0 * (a.scale_log2 * c.k0), m1 * (a.scale_log2 * c.k1)) : fmaxf(m0, m1) * a.scale_log2;
         };
         // by = at & 3: known where it is called, so that a slot's place is part of the LDS instructions
         auto step = [&](int at, auto by, Raw& r) {
@@ -474,7 +474,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
             const Scales cn = scales_at(at + 1);
             const float alpha = sm.follow(row_max2(mx)), use = sm.used();
             rescale(alpha);
-            const float c0 = EXTRA ? 1.0f : a.scale_log2 * c.k0, c1 = EXTRA ? 1.0f : a.scale_log2 * c.k1;
+            const float c0 = FORM ? 1.0f : a.scale_log2 * c.k0, c1 = FORM ? 1.0f : a.scale_log2 * c.k1;
             floatx16 sn = {};
 #pragma unroll
             for (int kk = 0; kk < KC; ++kk) sn = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(ks, kk), q[kk], sn, 0, 0, 0);
@@ -540,7 +540,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
         for (int kk = 0; kk < KC; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(k_frag(slot, kk), q[kk], s, 0, 0, 0);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= a.scale_log2 * (r < 8 ? c.k0 : c.k1);
-        if (EXTRA) pair_scores<false>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
+        if (FORM) pair_scores<FORM>(s, a, row, key0 - (doc ? row.pos : row.place), hh);
         const int lo = (doc ? row.dlo : row.olo) - key0, hi = (doc ? D : row.ohi) - key0;
         hide_keys(s, lo - 4 * hh, hi - 4 * hh);
         rescale(pair_softmax(sm, s));
@@ -595,7 +595,7 @@ __device__ __forceinline__ void pair_tile(const PairAttnArgs& a, char* smem, con
     }
 }
 
-template <int HD, bool FP8, bool EXTRA>
+template <int HD, bool FP8, int FORM>
 __global__ void __launch_bounds__(kPairWaves * 64) __attribute__((amdgpu_waves_per_eu(HD == 64 ? 3 : 2, 8))) pair_attn_half_kernel(PairAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // the item's record as either kind is asked for together with the counts that say which kind it is
@@ -605,23 +605,27 @@ __global__ void __launch_bounds__(kPairWaves * 64) __attribute__((amdgpu_waves_p
     const PairChoice ch = pair_choice(blocks, tiles, HD, a.most_splits);
     if (item >= (ch.tiles ? tiles : blocks) || (int)blockIdx.y >= ch.pieces) return;
     const PairItem it = ch.tiles ? tile : block;
-    if (ch.tiles) pair_tile<HD, FP8, EXTRA>(a, smem, it, h, ch.pieces);
-    else pair_rows<HD, FP8, EXTRA>(a, (float*)smem, it, h, ch.pieces);
+    if (ch.tiles) pair_tile<HD, FP8, FORM>(a, smem, it, h, ch.pieces);
+    else pair_rows<HD, FP8, FORM>(a, (float*)smem, it, h, ch.pieces);
 }
 
-template <int HD, bool FP8, bool EXTRA>
+template <int HD, bool FP8, int FORM>
 hipError_t half_launch_as(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
     constexpr size_t lds = std::max<size_t>(TileGeo<HD>::LDS, pair_join_bytes(kPairWaves, HD));
     if (lds > 65536) {
-        const hipError_t e = hipFuncSetAttribute((const void*)pair_attn_half_kernel<HD, FP8, EXTRA>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute((const void*)pair_attn_half_kernel<HD, FP8, FORM>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    pair_attn_half_kernel<HD, FP8, EXTRA><<<grid, kPairWaves * 64, lds, st>>>(a);
+    pair_attn_half_kernel<HD, FP8, FORM><<<grid, kPairWaves * 64, lds, st>>>(a);
     return hipGetLastError();
 }
 template <int HD, bool FP8>
 hipError_t half_launch(const PairAttnArgs& a, dim3 grid, hipStream_t st) {
-    return pair_extra(a) ? half_launch_as<HD, FP8, true>(a, grid, st) : half_launch_as<HD, FP8, false>(a, grid, st);
+    switch (pair_scores_of(a)) {
+        case PS_FACTOR: return half_launch_as<HD, FP8, PS_FACTOR>(a, grid, st);
+        case PS_EXTRA: return half_launch_as<HD, FP8, PS_EXTRA>(a, grid, st);
+        default: return half_launch_as<HD, FP8, PS_WIDE_CAP>(a, grid, st);
+    }
 }
 
 }  // namespace
