@@ -4,8 +4,8 @@
 //   few rows   the item is one block of 32 rows, a wavefront has every fourth sub-tile of 32 keys and a softmax of its own, and they are joined
 //              through LDS in a fixed order.  K and V go from memory straight into operand registers: V pages hold a channel's 8 keys as a lane
 //              wants them, and a K instruction takes 32 bytes of each of 32 rows, whose lines the next ones take the rest of.  Bound by reading:
-//              640 documents of 512 keys, one token, 64 channels, 31 us, 5.4 TB/s; 100 of 2048, 128 channels, fp8, 97 us, 4.3 TB/s (VALU 39 %
-//              busy, MFMA 11 %; a second sub-tile ahead, a third wavefront a SIMD and more pieces each measured slower).
+//              640 documents of 512 keys, one token, 64 channels, 41 us, 4.1 TB/s (31 us again and again, out of the last-level cache); 100 of
+//              2048, 128 channels, fp8, 97 us, 4.3 TB/s (VALU 39 % busy, MFMA 11 %; a second sub-tile ahead, a third wavefront a SIMD and more pieces each measured slower).
 //   many rows  the item is a tile of up to four blocks, one per wavefront, and keys go through LDS in a ring of four sub-tiles of 32, in the arrangement
 //              of half pages: half pages straight from memory, fp8 pages by way of a wavefront's registers, which expands them once for all rows.
 //              S of a sub-tile is computed next to the exponentials of the one before.  Bound by what a wavefront issues and, with 128 channels, by

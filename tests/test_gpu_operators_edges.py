@@ -328,3 +328,40 @@ def test_rope_of_rows_past_32_bits(layout):
     assert T.equal(y[:2], want[:2]) and T.equal(y[-3:], want[2:])
     rope.apply(0, x, out=[x])
     assert T.equal(y, x)
+
+
+def test_calls_on_a_second_stream_of_a_recording():
+    """Tables, rotary positions and attention on a stream that a recording forks to; its positions and keys are temporaries that are let go of."""
+    T, H = torch(), hb()
+    b = Batch("bf16", 14, 2, 64, [900, 40], [0, 1, 0], [5, 9, 1], seed=31)
+    rope = H.Rope(64)
+    doc, lens, rows = dev_i32(b.pair_doc), dev_i32(b.q_lens), [b.q.clone(), b.k.clone(), b.v.clone()]
+    t = H.PairTables(b.pool, 3, b.tokens, 57, n_q_heads=14)
+    side, other, graph = T.cuda.Stream(), T.cuda.Stream(), T.cuda.CUDAGraph()
+
+    def chain(stream):
+        t.build(b.list, doc, lens, stream=stream)
+        q, k = rope.apply(t.tok_pos, rows[0], rows[1], stream=stream)
+        return H.pair_attention(b.pool, b.layer, t, q, k, rows[2], with_lse=True, stream=stream)
+
+    T.cuda.synchronize()
+    with T.cuda.stream(side):
+        chain(None)
+    side.synchronize()
+    with T.cuda.graph(graph):
+        now = T.cuda.current_stream()
+        other.wait_stream(now)
+        out = chain(other)
+        now.wait_stream(other)
+    gen = T.Generator().manual_seed(2)
+    for _ in range(4):
+        for x in rows:
+            x.copy_(T.randn(x.shape, generator=gen).to(x.dtype))
+        q_lens = np.random.default_rng(3).permutation(b.q_lens)
+        lens.copy_(dev_i32(q_lens))
+        graph.replay()
+        T.cuda.synchronize()
+        got = [x.clone() for x in out]
+        want = chain(None)
+        T.cuda.synchronize()
+        assert T.equal(got[0], want[0]) and T.equal(got[1], want[1])
