@@ -81,6 +81,22 @@ class hr_attention_args(C.Structure):
                [(t + s, C.c_int64) for t in ("q", "k", "v", "out") for s in ("_token_stride", "_head_stride")]
 
 
+class hr_block8(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("rows", C.c_int64), ("cols", C.c_int32), ("block_rows", C.c_int32),
+                ("row_stride", C.c_int64), ("scale_stride", C.c_int64)]
+
+
+class hr_norm_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("heads", C.c_int32), ("channels", C.c_int32), ("eps", C.c_float), ("gain_offset", C.c_float), ("tokens", C.c_int64),
+                ("x", C.c_void_p), ("add", C.c_void_p), ("total", C.c_void_p), ("out", C.c_void_p), ("gain", C.c_void_p), ("block8", C.POINTER(hr_block8))] + \
+               [(t + s, C.c_int64) for t in ("x", "add", "total", "out") for s in ("_token_stride", "_head_stride")]
+
+
+class hr_matmul_args(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("gate", C.c_int32), ("bias", C.c_void_p), ("add", C.c_void_p), ("out", C.c_void_p),
+                ("add_stride", C.c_int64), ("out_stride", C.c_int64), ("block8", C.POINTER(hr_block8))]
+
+
 _PP = C.POINTER(C.c_void_p)
 
 
@@ -100,6 +116,7 @@ EXPORTS = [
     "hr_rerank_full_workspace_bytes", "hr_rerank_score_full", "hr_doc_prefill_workspace_bytes", "hr_doc_prefill", "hr_attention_path", "hr_gemm_path",
     "hr_rerank_topk", "hr_rerank_topk_host", "hr_model_range_report", "hr_kv_pool_range_report", "hr_probe_read_bandwidth", "hr_profile_enable", "hr_profile_select", "hr_profile_count", "hr_profile_name", "hr_profile_read",
     "hr_rope_frequencies", "hr_rope_apply", "hr_pair_tables_sched_bytes", "hr_pair_tables_build", "hr_pair_attention_workspace_bytes", "hr_pair_attention",
+    "hr_rms_norm", "hr_block_quantize", "hr_block_matmul",
 ]
 
 
@@ -177,6 +194,9 @@ def _load() -> C.CDLL:
         "hr_pair_tables_build": (C.c_int, [C.c_void_p, C.POINTER(hr_doc_list), C.c_void_p, C.c_void_p, C.POINTER(hr_pair_tables), C.c_void_p]),
         "hr_pair_attention_workspace_bytes": (C.c_size_t, [C.c_void_p, C.POINTER(hr_pair_tables)]),
         "hr_pair_attention": (C.c_int, [C.c_void_p, C.POINTER(hr_pair_tables), C.POINTER(hr_attention_args), C.c_void_p, C.c_size_t, C.c_void_p]),
+        "hr_rms_norm": (C.c_int, [C.POINTER(hr_norm_args), C.c_void_p]),
+        "hr_block_quantize": (C.c_int, [C.c_int, C.c_void_p, C.c_int64, C.POINTER(hr_block8), C.c_void_p]),
+        "hr_block_matmul": (C.c_int, [C.POINTER(hr_block8), C.POINTER(hr_block8), C.POINTER(hr_matmul_args), C.c_void_p]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -638,6 +658,176 @@ def pair_attention(pool: KVPool, layer: int, tables: PairTables, q, k=None, v=No
                                     tables.workspace_bytes, _stream_ptr(stream)), "hr_pair_attention")
         _used_on(stream, q, k, v, out, slopes, prefix_lens, pool.mem, *tables.tensors)
     return (out, lse) if with_lse else out
+
+
+BLOCK_COLS = 128
+GATES = {None: 0, "silu": 1, "gelu": 2}
+
+
+class Block8:
+    """A matrix in 8 bits (hr_block8): E4M3 codes [rows][cols] (float8_e4m3fn or uint8, rows a multiple of 16 bytes apart) and fp32 scales
+    [ceil(rows / block_rows)][ceil(cols / 128)].  block_rows: 1 for activations, 128 for weights."""
+
+    def __init__(self, codes, scales, block_rows: int = 1):
+        import torch
+        dev = codes.device
+        if block_rows not in (1, BLOCK_COLS):
+            _refuse(f"Block8: block_rows 1 or {BLOCK_COLS}, got {block_rows}")
+        if codes.dim() != 2 or codes.dtype not in (torch.float8_e4m3fn, torch.uint8) or codes.shape[1] < 1 or (codes.shape[1] > 1 and codes.numel() and codes.stride(1) != 1):
+            _refuse(f"Block8: codes [rows][cols] in float8_e4m3fn or uint8 with adjacent columns, got {tuple(codes.shape)} {codes.dtype}")
+        rows, cols = codes.shape
+        stride = codes.stride(0) if rows > 1 else -(-cols // 16) * 16
+        if stride % 16 or stride < cols or codes.data_ptr() % 16:
+            _refuse(f"Block8: rows of codes begin at multiples of 16 bytes (Block8.empty makes such), got a stride of {stride} at {codes.data_ptr():#x}")
+        shape = (-(-rows // block_rows), -(-cols // BLOCK_COLS))
+        if tuple(scales.shape) != shape or scales.dtype != torch.float32 or scales.device != dev or (shape[1] > 1 and shape[0] and scales.stride(1) != 1):
+            _refuse(f"Block8: scales {shape} float32 on {dev} with adjacent columns, got {tuple(scales.shape)} {scales.dtype} on {scales.device}")
+        self.codes, self.scales, self.block_rows, self.shape, self.device = codes, scales, block_rows, (rows, cols), dev
+        self.c = hr_block8(codes.data_ptr(), scales.data_ptr(), rows, cols, block_rows, stride, scales.stride(0) if shape[0] > 1 else shape[1])
+
+    @classmethod
+    def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda:0", stream=None) -> "Block8":
+        """One with room for rows x cols, unset.  stream: the one that will write it (None: the current one)."""
+        import torch
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return cls.empty(rows, cols, block_rows, device)
+        rows, cols = _int32(rows, "Block8: rows"), _int32(cols, "Block8: cols")
+        if block_rows not in (1, BLOCK_COLS) or cols < 1:
+            _refuse(f"Block8: block_rows 1 or {BLOCK_COLS} and columns, got {block_rows} and {cols}")
+        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device)
+        scales = torch.empty((-(-rows // block_rows), -(-cols // BLOCK_COLS)), dtype=torch.float32, device=device)
+        return cls(codes if cols % 16 == 0 else codes[:, :cols], scales, block_rows)
+
+
+def _rows_of(t, shape, like, what: str):
+    """(token stride, head stride) of a tensor of `shape`, [tokens][channels] or [tokens][heads][channels], of the type and on the device of `like`."""
+    stride = t.stride()
+    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (shape[-1] > 1 and t.numel() and stride[-1] != 1):
+        _refuse(f"{what}: {tuple(shape)} with adjacent channels, {like.dtype} on {like.device} expected; got {tuple(t.shape)}, strides {stride}, {t.dtype} on {t.device}")
+    return stride[0], stride[1] if len(shape) == 3 else 0
+
+
+def _floats(t, n: int, device, what: str):
+    import torch
+    if t.dtype != torch.float32 or t.device != device or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{what}: {n} contiguous float32 on {device} expected, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _block8_for(given, rows: int, cols: int, device, stream, what: str) -> Block8:
+    """The matrix that a call writes: one of the caller's, or (True) a new one."""
+    if given is True:
+        return Block8.empty(rows, cols, 1, device, stream)
+    if not isinstance(given, Block8) or given.block_rows != 1 or given.shape != (rows, cols) or given.device != device:
+        _refuse(f"{what}: block8: True or a Block8 of ({rows}, {cols}) with block_rows 1 on {device} expected")
+    return given
+
+
+def rms_norm(x, gain=None, add=None, eps: float = 1e-6, gain_offset: float = 0.0, out=True, total=None, block8=None, stream=None):
+    """s = x + add; y = s / sqrt(mean(s^2) + eps) * (gain + gain_offset) over the last dimension (hr_rms_norm).  x: bf16 or fp32, [tokens][channels], or
+    [tokens][heads][channels] whose heads are normed one by one; any token and head stride.  gain: fp32 [channels], None: no factor.
+    out, total, block8: what is written, y, s and y's codes (2 dimensions only): True for a new one, a tensor (a Block8) of the caller's, None for
+    none.  total and out may be x or add.  Returns (out, total, block8), None where nothing was asked for.  No gradients: tensors that require them are
+    refused outside torch.no_grad()."""
+    import torch
+    code, dev, shape = _act_code(x.dtype), x.device, x.shape
+    if code is None or len(shape) not in (2, 3):
+        _refuse(f"rms_norm: [tokens][channels] or [tokens][heads][channels] in float32 or bfloat16, got {tuple(shape)} {x.dtype}")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rms_norm(x, gain, add, eps, gain_offset, out, total, block8, stream)
+    T, C_ = shape[0], shape[-1]
+    heads = shape[1] if len(shape) == 3 else 1
+    out, total = (_new(x, stream) if t is True else None if t is False else t for t in (out, total))
+    _no_gradients((x, gain, add, out, total), "rms_norm")
+    x_t, x_h = _rows_of(x, shape, x, "rms_norm: x")
+    a_t, a_h = (0, 0) if add is None else _rows_of(add, shape, x, "rms_norm: add")
+    s_t, s_h = (0, 0) if total is None else _rows_of(total, shape, x, "rms_norm: total")
+    o_t, o_h = (0, 0) if out is None else _rows_of(out, shape, x, "rms_norm: out")
+    g_p = None if gain is None else _floats(gain, C_, dev, "rms_norm: gain")
+    if block8 is not None and block8 is not False:
+        if len(shape) != 2 or C_ < 1:
+            _refuse("rms_norm: codes are made of [tokens][channels]")
+        block8 = _block8_for(block8, T, C_, dev, stream, "rms_norm")
+    else:
+        block8 = None
+    if heads < 1 or C_ < 1:
+        _refuse(f"rms_norm: heads and channels, got {tuple(shape)}")
+    args = hr_norm_args(code, _int32(heads, "rms_norm: heads"), _int32(C_, "rms_norm: channels"), eps, gain_offset, T, x.data_ptr(), None if add is None else add.data_ptr(),
+                        None if total is None else total.data_ptr(), None if out is None else out.data_ptr(), g_p,
+                        None if block8 is None else C.pointer(block8.c), x_t, x_h, a_t, a_h, s_t, s_h, o_t, o_h)
+    check(lib.hr_rms_norm(C.byref(args), _stream_ptr(stream)), "hr_rms_norm")
+    if stream is not None:
+        _used_on(stream, x, gain, add, out, total, *(() if block8 is None else (block8.codes, block8.scales)))
+    return out, total, block8
+
+
+def block_quantize(x, block_rows: int = 1, out: Optional[Block8] = None, stream=None) -> Block8:
+    """Codes and scales of x [rows][cols], bf16 or fp32, any row stride (hr_block_quantize): block_rows 1 for activations, 128 for weights.  out: a
+    Block8 of the caller's.  No gradients: a tensor that requires them is refused outside torch.no_grad()."""
+    code, dev = _act_code(x.dtype), x.device
+    if code is None or x.dim() != 2 or x.shape[1] < 1:
+        _refuse(f"block_quantize: [rows][cols] in float32 or bfloat16, got {tuple(x.shape)} {x.dtype}")
+    if _elsewhere(dev):
+        import torch
+        with torch.cuda.device(dev):
+            return block_quantize(x, block_rows, out, stream)
+    _no_gradients((x,), "block_quantize")
+    x_t, _ = _rows_of(x, x.shape, x, "block_quantize: x")
+    if out is None:
+        out = Block8.empty(*x.shape, block_rows, dev, stream)
+    elif not isinstance(out, Block8) or out.block_rows != block_rows or out.shape != tuple(x.shape) or out.device != dev:
+        _refuse(f"block_quantize: out: a Block8 of {tuple(x.shape)} with block_rows {block_rows} on {dev} expected")
+    check(lib.hr_block_quantize(code, x.data_ptr(), x_t, C.byref(out.c), _stream_ptr(stream)), "hr_block_quantize")
+    if stream is not None:
+        _used_on(stream, x, out.codes, out.scales)
+    return out
+
+
+def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, bias=None, add=None, out=None, block8=None, stream=None):
+    """a w^T of two matrices in 8 bits, activations and weights, with what follows it in a layer (hr_block_matmul): + bias (fp32 [rows of w]), a gate
+    ("silu" or "gelu": act(first half of the columns) * second half), + add ([rows of a][columns], of out's type).  dtype: of out, float32 or bfloat16
+    (None: out's or add's, else bfloat16); out: a tensor of the caller's, which may be add.  block8 (True, or a Block8 of the caller's): codes and
+    scales of the result instead.  Returns out, or the Block8."""
+    import torch
+    dev = a.device
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return block_matmul(a, w, dtype, gate, bias, add, out, block8, stream)
+    if w.device != dev or gate not in GATES:
+        _refuse(f"block_matmul: weights on {dev}, gate one of {list(GATES)}; got {w.device}, {gate!r}")
+    M, N = a.shape[0], w.shape[0]
+    if gate is not None:
+        if N % (2 * BLOCK_COLS):
+            raise HrError(HR_ERR_MISMATCH, f"block_matmul: halves of a multiple of {BLOCK_COLS} rows, got {N} rows")
+        N //= 2
+    _no_gradients((bias, add, out), "block_matmul")
+    b_p = None if bias is None else _floats(bias, w.shape[0], dev, "block_matmul: bias")
+    if block8 is not None and block8 is not False:
+        if out is not None or add is not None or N < 1:
+            _refuse("block_matmul: codes instead of out, of at least one column, with nothing added")
+        block8 = _block8_for(block8, M, N, dev, stream, "block_matmul")
+        args = hr_matmul_args(HR_F32, GATES[gate], b_p, None, None, 0, 0, C.pointer(block8.c))
+    else:
+        block8 = None
+        if dtype is None:
+            dtype = out.dtype if out is not None else add.dtype if add is not None else torch.bfloat16
+        code = _act_code(dtype)
+        if code is None:
+            _refuse(f"block_matmul: float32 or bfloat16, got {dtype}")
+        if out is None:
+            out = _new(a.codes, stream, (M, N), dtype)
+        shape = torch.Size((M, N))
+        if out.dtype != dtype or out.device != dev:
+            _refuse(f"block_matmul: out: {dtype} on {dev} expected, got {out.dtype} on {out.device}")
+        o_t, _ = _rows_of(out, shape, out, "block_matmul: out")
+        d_t, _ = (0, 0) if add is None else _rows_of(add, shape, out, "block_matmul: add")
+        args = hr_matmul_args(code, GATES[gate], b_p, None if add is None else add.data_ptr(), out.data_ptr(), d_t, o_t, None)
+    check(lib.hr_block_matmul(C.byref(a.c), C.byref(w.c), C.byref(args), _stream_ptr(stream)), "hr_block_matmul")
+    if stream is not None:
+        _used_on(stream, a.codes, a.scales, w.codes, w.scales, bias, add, out, *(() if block8 is None else (block8.codes, block8.scales)))
+    return out if block8 is None else block8
 
 
 _LAYER_KINDS = ("wq", "wk", "wv", "wo", "wg", "wu", "wd", "norm1", "norm2")

@@ -1,0 +1,98 @@
+// Products of 8-bit matrices (hr_block_matmul): what their kernels have in common.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "hr_block8_device.h"
+#include "hr_gemm_tiles.h"
+
+namespace hr {
+
+typedef __attribute__((ext_vector_type(4))) float mm_f4;
+typedef __attribute__((ext_vector_type(2))) _Float16 mm_h2;
+typedef __attribute__((ext_vector_type(8))) _Float16 mm_h8;
+typedef __attribute__((ext_vector_type(4))) int mm_i4;
+
+// Eight codes as halves: every E4M3 value is one
+__device__ __forceinline__ mm_h8 halves(int lo, int hi) {
+    const mm_h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+    const mm_h2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+    return mm_h8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The codes at `at` .. `at` + 15 of a row, those behind its last one as zeros: `left` = columns from `at` to the row's end, of 1 .. 15
+__device__ __forceinline__ mm_i4 first_codes(mm_i4 w, int left) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int keep = left - q * 4;
+        w[q] = keep >= 4 ? w[q] : keep <= 0 ? 0 : w[q] & (int)(0xFFFFFFFFu >> (32 - 8 * keep));
+    }
+    return w;
+}
+
+// A gate's act(z) u.  Both acts are z / (1 + exp(-t)): silu with t = z, gelu with t = 2 sqrt(2 / pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float gated(float z, float u, int gate) {
+    const float t = gate == HR_GATE_SILU ? z : 1.5957691216057308f * fmaf(0.044715f * z * z, z, z);
+    return z / (1.0f + expf(-t)) * u;
+}
+
+// Values n .. n + 3 of y's row m, from c and, with a gate, from what it multiplies
+template <bool GATE>
+__device__ __forceinline__ mm_f4 finish4(const MatmulArgs& a, int n, mm_f4 c, mm_f4 up) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (a.bias) {
+            c[e] += n + e < a.N ? a.bias[n + e] : 0.0f;
+            if (GATE) up[e] += n + e < a.N ? a.bias[a.half + n + e] : 0.0f;
+        }
+        if (GATE) c[e] = gated(c[e], up[e], a.gate);
+    }
+    return c;
+}
+
+// ... + add, into out
+template <typename T>
+__device__ __forceinline__ void store4(const MatmulArgs& a, int64_t m, int n, mm_f4 y) {
+    T* out = (T*)a.out + m * a.out_stride + n;
+    const T* add = (const T*)a.add + m * a.add_stride + n;
+    if (n + 4 <= a.N) {
+        Loose<T, 4> w;
+        if (a.add) {
+            w = *(const Loose<T, 4>*)add;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] += to_float<T>(w.w[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w.w[e] = from_float<T>(y[e]);
+        *(Loose<T, 4>*)out = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < a.N) out[e] = from_float<T>(a.add ? y[e] + to_float<T>(add[e]) : y[e]);
+    }
+}
+
+// ... into codes: 32 lanes have a row's 128 columns from n / 128 * 128 on, and all of them come here.  on: the row is one of y's
+__device__ __forceinline__ void store_block4(const MatmulArgs& a, int64_t m, int n, mm_f4 y, bool on) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = n + e < a.N ? y[e] : 0.0f;
+    float top = max16(finite_top(v));
+    top = fmaxf(top, __shfl_xor(top, 16, 64));
+    const float scale = scale_of(top), by = 1.0f / scale;
+    if (!on || n >= a.N) return;
+    const uint32_t w = codes4(v[0] * by, v[1] * by, v[2] * by, v[3] * by);
+    uint8_t* out = a.codes + m * a.code_stride + n;
+    if (n + 4 <= a.N) {
+        *(uint32_t*)out = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (n + e < a.N) out[e] = (uint8_t)(w >> (8 * e));
+    }
+    if (n % kBlockCols == 0) a.scales[m * a.scale_stride + n / kBlockCols] = scale;
+}
+
+hipError_t launch_block_matmul_few(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st);
+
+}  // namespace hr

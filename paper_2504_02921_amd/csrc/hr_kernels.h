@@ -197,6 +197,8 @@ hipError_t launch_rope_apply(const hr_rope_cfg& c, const double* freqs, int dtyp
 hipError_t launch_pair_tables(const hr_pool* pool, const hr_doc_list* docs, const int32_t* pair_doc, const int32_t* query_lens,
                               const hr_pair_tables* t, hipStream_t st);
 hipError_t launch_pair_attention(const hr_pool* pool, const hr_pair_tables* t, const hr_attention_args* g, void* workspace, hipStream_t st);
+hipError_t launch_rms_norm(const hr_norm_args& n, hipStream_t st);
+hipError_t launch_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block8& out, hipStream_t st);
 // copy whole pages (all kv heads) from the new-KV page buffer to pool pages of one layer:
 // pool page dst_table[i] <- new page src_first[doc(i)] + i  (16-bit pools: same arrangement on both sides)
 hipError_t launch_pages_to_pool(const char* kv_new, char* pool_layer_base, const int32_t* src_page, const int32_t* dst_page,

@@ -1,0 +1,312 @@
+// The norm of a residual stream with its addition, and codes with scales (hr_rms_norm, hr_block_quantize).
+//
+// y = s / sqrt(mean(s^2) + eps) * (gain + offset), s = x + add: one pass over a head whose channels stay in registers between the sum of their squares and
+// what is made of them, so every input is read and every output written once.  What bounds all of it is those bytes.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "hr_block8.h"
+#include "hr_block8_device.h"
+#include "hr_kernels.h"
+
+namespace hr {
+
+namespace {
+
+constexpr int kVec = 8;                      // channels of a lane: 16 lanes have a block of 128
+constexpr int kThreads = 256;
+constexpr int kBlockLanes = kBlockCols / kVec;
+constexpr int64_t kMostGroups = 1 << 20;     // workgroups of a launch; more rows are walked
+
+struct NormSide { const void* p; int64_t ts, hs; };
+struct NormArgs {
+    NormSide x, add, total, out;
+    const float* gain;
+    uint8_t* codes;
+    float* scales;
+    int64_t rows, code_stride, scale_stride;
+    int32_t heads, channels;
+    float eps, offset;
+};
+
+template <typename T>
+__device__ __forceinline__ T* at(const NormSide& s, int64_t token, int head) { return (T*)s.p + token * s.ts + head * s.hs; }
+
+// Channels c .. c + 7, those behind the head's last one as zeros
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int c, int channels, float (&v)[kVec]) {
+    if (c + kVec <= channels) {
+        const Loose<T, kVec> w = *(const Loose<T, kVec>*)(p + c);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = to_float<T>(w.w[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = c + e < channels ? to_float<T>(p[c + e]) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int c, int channels, const float (&v)[kVec]) {
+    if (c + kVec <= channels) {
+        Loose<T, kVec> w;
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) w.w[e] = from_float<T>(v[e]);
+        *(Loose<T, kVec>*)(p + c) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+            if (c + e < channels) p[c + e] = from_float<T>(v[e]);
+    }
+}
+// Codes c .. c + 7 of a row; c is a multiple of 8 and rows begin at multiples of 16
+__device__ __forceinline__ void store_codes8(uint8_t* p, int c, int cols, const float (&v)[kVec], float by) {
+    const uint2 w = {codes4(v[0] * by, v[1] * by, v[2] * by, v[3] * by), codes4(v[4] * by, v[5] * by, v[6] * by, v[7] * by)};
+    if (c + kVec <= cols) {
+        *(uint2*)(p + c) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+            if (c + e < cols) p[c + e] = (uint8_t)((e < 4 ? w.x : w.y) >> (e % 4 * 8));
+    }
+}
+
+// What becomes of eight channels of a head
+template <typename T>
+__device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float r) {
+    float y[kVec];
+    if (a.gain) load8<float>(a.gain, c, a.channels, y);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) y[e] = s[e] * r * (a.gain ? y[e] + a.offset : 1.0f);
+    if (a.codes) {
+        if (c + kVec > a.channels)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (c + e >= a.channels) y[e] = 0.0f;             // an infinite 1 / root makes NaN of them
+        const float scale = scale_of(max16(finite_top(y)));
+        if (on && c < a.channels) {
+            store_codes8(a.codes + token * a.code_stride, c, a.channels, y, 1.0f / scale);
+            if (c % kBlockCols == 0) a.scales[token * a.scale_stride + c / kBlockCols] = scale;
+        }
+    }
+    if (on && c < a.channels) {
+        if (a.total.p) store8<T>(at<T>(a.total, token, head), c, a.channels, s);
+        if (a.out.p) store8<T>(at<T>(a.out, token, head), c, a.channels, y);
+    }
+}
+
+__device__ __forceinline__ float root_of(float squares, const NormArgs& a) {
+    const float m = squares / (float)a.channels + a.eps;
+    return m == 0.0f ? 0.0f : rsqrtf(m);
+}
+
+// LANES lanes have a head, CHUNKS times 8 channels each
+template <typename T, int LANES, int CHUNKS>
+__global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
+    constexpr int UNITS = kThreads / LANES;
+    __shared__ float part[2][kThreads / 64];
+    const int lane = threadIdx.x % LANES, unit = threadIdx.x / LANES;
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * UNITS; first < a.rows; first += (int64_t)gridDim.x * UNITS) {
+        const bool on = first + unit < a.rows;
+        const int64_t row = on ? first + unit : a.rows - 1;
+        int64_t token = row;
+        int head = 0;
+        if (a.heads > 1) {
+            token = a.rows <= 0xFFFFFFFFll ? (int64_t)((uint32_t)row / (uint32_t)a.heads) : row / a.heads;
+            head = (int)(row - token * a.heads);
+        }
+        float s[CHUNKS][kVec], more[CHUNKS][kVec];
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) load8<T>(at<const T>(a.x, token, head), (k * LANES + lane) * kVec, a.channels, s[k]);
+        if (a.add.p) {
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) load8<T>(at<const T>(a.add, token, head), (k * LANES + lane) * kVec, a.channels, more[k]);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                if (a.add.p) s[k][e] += more[k][e];
+                sum = fmaf(s[k][e], s[k][e], sum);
+            }
+        if constexpr (LANES <= 32) {
+            sum = sum16(sum);
+            if constexpr (LANES == 32) sum += __shfl_xor(sum, 16, 64);
+        } else {
+            sum = wave_sum(sum);
+            if constexpr (LANES > 64) {
+                if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = sum;
+                __syncthreads();                    // one a turn: the other half of `part` is written next
+                sum = 0.0f;
+#pragma unroll
+                for (int w = 0; w < kThreads / 64; ++w) sum += part[turn][w];
+                turn ^= 1;
+            }
+        }
+        const float r = root_of(sum, a);
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) finish8<T>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r);
+    }
+}
+
+// Heads of more channels than registers are kept for: read once for the sum and once more, mostly from a cache
+template <typename T>
+__global__ void __launch_bounds__(kThreads) norm_wide_kernel(NormArgs a) {
+    __shared__ float part[2][kThreads / 64];
+    int turn = 0;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const int64_t token = row / a.heads;
+        const int head = (int)(row - token * a.heads);
+        auto load = [&](int c, float (&s)[kVec]) {
+            load8<T>(at<const T>(a.x, token, head), c, a.channels, s);
+            if (!a.add.p) return;
+            float more[kVec];
+            load8<T>(at<const T>(a.add, token, head), c, a.channels, more);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) s[e] += more[e];
+        };
+        float s[kVec], sum = 0.0f;
+        for (int c = threadIdx.x * kVec; c < a.channels; c += kThreads * kVec) {
+            load(c, s);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) sum = fmaf(s[e], s[e], sum);
+        }
+        sum = wave_sum(sum);
+        if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = sum;
+        __syncthreads();
+        sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kThreads / 64; ++w) sum += part[turn][w];
+        turn ^= 1;
+        const float r = root_of(sum, a);
+        const int64_t padded = blocks_of(a.channels) * kBlockCols;        // whole groups of lanes look for a block's largest
+        for (int c = threadIdx.x * kVec; c < padded; c += kThreads * kVec) {
+            load(c, s);
+            finish8<T>(a, token, head, c, true, s, r);
+        }
+    }
+}
+
+template <typename T, int LANES>
+void norm_chunks(int chunks, unsigned groups, const NormArgs& a, hipStream_t st) {
+    switch (chunks) {
+        case 1: norm_kernel<T, LANES, 1><<<groups, kThreads, 0, st>>>(a); break;
+        case 2: if constexpr (LANES >= 64) norm_kernel<T, LANES, 2><<<groups, kThreads, 0, st>>>(a); break;
+        case 4: if constexpr (LANES >= 64) norm_kernel<T, LANES, 4><<<groups, kThreads, 0, st>>>(a); break;
+        default: if constexpr (LANES >= 64) norm_kernel<T, LANES, 8><<<groups, kThreads, 0, st>>>(a);
+    }
+}
+
+template <typename T>
+void norm_launch(const NormArgs& a, hipStream_t st) {
+    const NormShape s = norm_shape(a.channels, a.rows);
+    const int64_t units = kThreads / s.lanes;
+    const unsigned groups = (unsigned)std::min((a.rows + units - 1) / units, kMostGroups);
+    if (s.chunks == 0) norm_wide_kernel<T><<<groups, kThreads, 0, st>>>(a);
+    else if (s.lanes == 16) norm_chunks<T, 16>(s.chunks, groups, a, st);
+    else if (s.lanes == 32) norm_chunks<T, 32>(s.chunks, groups, a, st);
+    else if (s.lanes == 64) norm_chunks<T, 64>(s.chunks, groups, a, st);
+    else norm_chunks<T, 256>(s.chunks, groups, a, st);
+}
+
+struct QuantizeArgs {
+    const void* x;
+    uint8_t* codes;
+    float* scales;
+    int64_t rows, x_stride, code_stride, scale_stride;
+    int32_t cols, blocks;            // blocks of 128 columns
+};
+
+// Rows of activations: 16 lanes have 128 columns of a row
+template <typename T>
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantizeArgs a) {
+    constexpr int UNITS = kThreads / kBlockLanes;
+    const int64_t n = a.rows * a.blocks;
+    for (int64_t first = (int64_t)blockIdx.x * UNITS; first < n; first += (int64_t)gridDim.x * UNITS) {
+        const int64_t u = first + threadIdx.x / kBlockLanes;
+        const bool on = u < n;
+        const int64_t row = n <= 0xFFFFFFFFll ? (int64_t)((uint32_t)(on ? u : 0) / (uint32_t)a.blocks) : (on ? u : 0) / a.blocks;
+        const int b = (int)((on ? u : 0) - row * a.blocks), c = b * kBlockCols + threadIdx.x % kBlockLanes * kVec;
+        float v[kVec];
+        load8<T>((const T*)a.x + row * a.x_stride, c, a.cols, v);
+        const float scale = scale_of(max16(finite_top(v)));
+        if (on && c < a.cols) {
+            store_codes8(a.codes + row * a.code_stride, c, a.cols, v, 1.0f / scale);
+            if (c % kBlockCols == 0) a.scales[row * a.scale_stride + b] = scale;
+        }
+    }
+}
+
+// Weights: a workgroup has a tile of 128 x 128, its lanes 8 columns of every 16th row
+template <typename T>
+__global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(QuantizeArgs a) {
+    constexpr int STEP = kThreads / kBlockLanes, PASSES = kBlockCols / STEP;
+    __shared__ float tops[kThreads / 64];
+    const int64_t tile_row = blockIdx.x / a.blocks, b = blockIdx.x % a.blocks;
+    const int c = (int)b * kBlockCols + threadIdx.x % kBlockLanes * kVec;
+    const int64_t row0 = tile_row * kBlockCols + threadIdx.x / kBlockLanes;
+    float v[PASSES][kVec], top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int64_t row = row0 + p * STEP;
+        load8<T>((const T*)a.x + min(row, a.rows - 1) * a.x_stride, c, a.cols, v[p]);
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) top = fmaxf(top, finite_top(v[p]));
+    top = wave_max(top);
+    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, tops[w]);
+    const float scale = scale_of(top), by = 1.0f / scale;
+    if (c >= a.cols) return;
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int64_t row = row0 + p * STEP;
+        if (row < a.rows) store_codes8(a.codes + row * a.code_stride, c, a.cols, v[p], by);
+    }
+    if (threadIdx.x == 0) a.scales[tile_row * a.scale_stride + b] = scale;
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(const hr_norm_args& n, hipStream_t st) {
+    NormArgs a{};
+    a.x = NormSide{n.x, n.x_token_stride, n.x_head_stride};
+    a.add = NormSide{n.add, n.add_token_stride, n.add_head_stride};
+    a.total = NormSide{n.total, n.total_token_stride, n.total_head_stride};
+    a.out = NormSide{n.out, n.out_token_stride, n.out_head_stride};
+    a.gain = n.gain;
+    if (n.block8) {
+        a.codes = (uint8_t*)n.block8->codes;
+        a.scales = n.block8->scales;
+        a.code_stride = n.block8->row_stride;
+        a.scale_stride = n.block8->scale_stride;
+    }
+    a.rows = n.tokens * n.heads;
+    a.heads = n.heads;
+    a.channels = n.channels;
+    a.eps = n.eps;
+    a.offset = n.gain_offset;
+    if (n.dtype == HR_F32) norm_launch<float>(a, st);
+    else norm_launch<bf16_t>(a, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block8& out, hipStream_t st) {
+    QuantizeArgs a{x, (uint8_t*)out.codes, out.scales, out.rows, x_stride, out.row_stride, out.scale_stride, out.cols, (int32_t)blocks_of(out.cols)};
+    if (out.block_rows == 1) {
+        constexpr int64_t units = kThreads / kBlockLanes;
+        const unsigned groups = (unsigned)std::min((a.rows * a.blocks + units - 1) / units, kMostGroups);
+        if (dtype == HR_F32) quantize_rows_kernel<float><<<groups, kThreads, 0, st>>>(a);
+        else quantize_rows_kernel<bf16_t><<<groups, kThreads, 0, st>>>(a);
+    } else {
+        const unsigned groups = (unsigned)(blocks_of(a.rows) * a.blocks);
+        if (dtype == HR_F32) quantize_tiles_kernel<float><<<groups, kThreads, 0, st>>>(a);
+        else quantize_tiles_kernel<bf16_t><<<groups, kThreads, 0, st>>>(a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace hr
