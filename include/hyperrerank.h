@@ -553,7 +553,7 @@ typedef struct hr_block8 {
     int32_t block_rows;     /* 1 or 128 */
     int64_t row_stride;     /* bytes from row to row, a multiple of 16, at least cols, at most 2^22.  What lies between a row's last code and the next
                              * multiple of 16 may be read (and does not count, whatever it holds) and is not written */
-    int64_t scale_stride;   /* floats from one row of scales to the next, at least ceil(cols / 128) */
+    int64_t scale_stride;   /* floats from one row of scales to the next, at least ceil(cols / 128), at most 2^20 */
 } hr_block8;
 
 /* Root-mean-square norm of every head of every token, after an addition:

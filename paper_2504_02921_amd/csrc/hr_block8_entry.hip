@@ -35,7 +35,7 @@ int hr_block_matmul(const hr_block8* a, const hr_block8* w, const hr_matmul_args
     if (rc != HR_OK || a->rows == 0 || w->rows == 0) return rc;
     const hr::MatmulArgs m = hr::matmul_args(*a, *w, *args);
     const hr::MatmulTile t = hr::matmul_tile(m.M, m.N, m.K, args->dtype, m.gate, m.codes != nullptr);
-    HR_OP_HIP(hr::launch_block_matmul_few(m, args->dtype, t, (hipStream_t)stream));
+    HR_OP_HIP((t.few ? hr::launch_block_matmul_few : hr::launch_block_matmul_tiles)(m, args->dtype, t, (hipStream_t)stream));
     return HR_OK;
 }
 

@@ -10,7 +10,7 @@ namespace hr {
 namespace {
 
 constexpr int64_t kMaxRows = 1 << 30, kMaxStride = (int64_t)1 << 60;
-constexpr int32_t kMaxCols = 1 << 22, kMaxChannels = 65536, kMaxHeads = 65536;
+constexpr int32_t kMaxCols = 1 << 22, kMaxScaleStride = 1 << 20, kMaxChannels = 65536, kMaxHeads = 65536;
 
 bool aligned(const void* p, uintptr_t to) { return (uintptr_t)p % to == 0; }
 
@@ -37,7 +37,7 @@ int block8_check(const hr_block8* b, int block_rows) {
     if (!b || b->block_rows != block_rows || b->rows < 0 || b->cols < 1) return HR_ERR_INVALID_ARG;
     if (b->rows > kMaxRows || b->cols > kMaxCols) return HR_ERR_LEN_RANGE;
     if (b->row_stride % 16 != 0 || b->row_stride < b->cols || b->row_stride > kMaxCols) return HR_ERR_INVALID_ARG;
-    if (b->scale_stride < blocks_of(b->cols) || b->scale_stride > kMaxCols) return HR_ERR_INVALID_ARG;
+    if (b->scale_stride < blocks_of(b->cols) || b->scale_stride > kMaxScaleStride) return HR_ERR_INVALID_ARG;
     if (b->rows == 0) return HR_OK;
     if (!b->codes || !b->scales || !aligned(b->codes, 16) || !aligned(b->scales, 4)) return HR_ERR_INVALID_ARG;
     return HR_OK;
@@ -175,9 +175,15 @@ MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_a
 }
 
 MatmulTile matmul_tile(int64_t M, int N, int K, int dtype, int gate, bool block8) {
-    (void)N; (void)K; (void)dtype;
+    (void)K; (void)dtype;
+    const bool gated = gate != HR_GATE_NONE;
+    if (M > 64) {
+        const bool large = M >= 2048 && N >= 1024;
+        const int bm = large ? 256 : 128, bn = large ? 256 : 128;
+        return MatmulTile{bm, gated ? (block8 && bn < 256 ? 128 : bn / 2) : bn, false};
+    }
     const int bm = M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    return MatmulTile{bm, block8 ? 128 : gate != HR_GATE_NONE ? 16 : 32, true};
+    return MatmulTile{bm, block8 ? 128 : gated ? 16 : 32, true};
 }
 
 }  // namespace hr

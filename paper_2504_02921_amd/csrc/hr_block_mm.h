@@ -94,5 +94,6 @@ __device__ __forceinline__ void store_block4(const MatmulArgs& a, int64_t m, int
 }
 
 hipError_t launch_block_matmul_few(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st);
+hipError_t launch_block_matmul_tiles(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st);
 
 }  // namespace hr

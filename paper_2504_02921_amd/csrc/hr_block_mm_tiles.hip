@@ -1,0 +1,240 @@
+// Products of 8-bit matrices with many rows (hr_block_matmul): tiles of both operands through LDS.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "hr_block_mm.h"
+
+namespace hr {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) int mm_i8;
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+constexpr int kNoLoad = 0x7FF00000;      // a vector offset past every range: nothing is fetched, zero arrives
+
+#ifdef __HIP_DEVICE_COMPILE__            // the host pass does not know the descriptor type
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+#else
+typedef int rsrc_t;
+#endif
+__device__ __forceinline__ rsrc_t make_rsrc(const void* p, int64_t bytes) {
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000);
+#else
+    return 0;
+#endif
+}
+// 16 or 4 bytes a lane, straight to LDS: lane l's behind lane l - 1's from a wave-uniform address on
+__device__ __forceinline__ void load_lds16(rsrc_t r, void* lds, int voff, int soff) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)lds, 16, voff, soff, 0, 0);
+#endif
+}
+__device__ __forceinline__ void load_lds4(rsrc_t r, void* lds, int voff, int soff) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)lds, 4, voff, soff, 0, 0);
+#endif
+}
+
+// BM rows x BN rows of w, WM x WN wavefronts, NS stages.  With a gate a wavefront's rows of w are half gate rows, half the rows that they multiply.
+template <int BM, int BN, int WM, int WN, int NS, bool EIGHT, bool GATE, typename OUT, bool CODES>
+__global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_tile_kernel(MatmulArgs a) {
+    constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;
+    constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
+    constexpr int H = GATE ? 2 : 1, BNY = BN / H, TNY = TN / H;            // columns of y
+    constexpr int RPP = NT / 8, PA = BM / RPP, PB = BN / RPP;              // rows a pass of 16-byte loads brings, passes
+    constexpr int STAGE = (BM + BN) * BK + NT * 4;
+    static_assert(BM % RPP == 0 && BN % RPP == 0 && BM / 64 + H <= NWAVE && (!CODES || BNY % kBlockCols == 0) && TNY <= kBlockCols, "loader shape");
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+
+    const int tiles_m = (int)((a.M + BM - 1) / BM), tiles_n = (a.N + BNY - 1) / BNY;
+    const TileCoord tc = map_tile(blockIdx.x, tiles_m, tiles_n);
+    if (!tc.valid) return;
+    const int64_t m0 = (int64_t)tc.tm * BM;
+    const int n0 = tc.tn * BNY;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave % WN, r = lane & 15, fq = lane >> 4;
+    const int nk = (int)blocks_of(a.K);
+
+    // ---- loads: a wavefront's load brings eight rows of 128 codes
+    const int rows_a = (int)min((int64_t)BM, a.M - m0), rows_w = min(BNY, a.N - n0);
+    const rsrc_t ra = make_rsrc(a.a + m0 * a.a_stride, rows_a * a.a_stride);
+    // which half of w a pass brings goes by the wavefront (a pass has every wavefront's rows) or by the pass
+    constexpr bool BY_WAVE = GATE && RPP % TN == 0;
+    static_assert(!GATE || BY_WAVE || TNY % RPP == 0, "a load lies in one half");
+    const int lrow = lane >> 3, lchunk = (lane & 7) ^ ((wave * 8 + lrow) >> 1 & 7);
+    const int va = lrow * (int)a.a_stride + lchunk * 16, vw = lrow * (int)a.w_stride + lchunk * 16;
+    int pass_a[PA], pass_w[PB];
+    const int64_t first_half = BY_WAVE && wave * 8 % TN >= TNY ? a.half : 0;
+    const rsrc_t rw0 = make_rsrc(a.w + (n0 + first_half) * a.w_stride, rows_w * a.w_stride);
+    const rsrc_t rw1 = make_rsrc(a.w + (n0 + (int64_t)a.half) * a.w_stride, rows_w * a.w_stride);
+#pragma unroll
+    for (int p = 0; p < PA; ++p) {
+        const int row = p * RPP + wave * 8;
+        pass_a[p] = row < rows_a ? row * (int)a.a_stride : 0;              // a pass of rows that there are not: other rows, not stored
+    }
+#pragma unroll
+    for (int p = 0; p < PB; ++p) {
+        const int row = p * RPP + wave * 8, f = GATE ? row / TN * TNY + row % TNY : row;
+        pass_w[p] = f < rows_w ? f * (int)a.w_stride : 0;
+    }
+    // scales: wavefronts 0 .. BM / 64 - 1 bring those of the rows, the next one (two) those of w's blocks
+    const int swave = wave - BM / 64, sblocks = (int)blocks_of(rows_w);
+    rsrc_t rs;
+    int vs = kNoLoad;
+    if (swave < 0) {
+        rs = make_rsrc(a.a_scales + m0 * a.a_scale_stride, rows_a * a.a_scale_stride * 4);
+        if (wave * 64 + lane < rows_a) vs = (wave * 64 + lane) * (int)a.a_scale_stride * 4;
+    } else {
+        rs = make_rsrc(a.w_scales + ((int64_t)n0 + (swave == 1 ? (int64_t)a.half : 0)) / kBlockCols * a.w_scale_stride, sblocks * a.w_scale_stride * 4);
+        if (swave < H && lane < sblocks) vs = lane * (int)a.w_scale_stride * 4;
+    }
+    auto stage = [&](int s) { return smem + s * STAGE; };
+    auto request = [&](int kt, int s) {
+        char* to = stage(s);
+        const bool whole = (kt + 1) * BK <= a.K, some = whole || kt * BK + lchunk * 16 < a.K;
+        const int xa = some && kt < nk ? va : kNoLoad, xw = some && kt < nk ? vw : kNoLoad, at = kt < nk ? kt * BK : 0;
+#pragma unroll
+        for (int p = 0; p < PA; ++p) load_lds16(ra, to + (p * RPP + wave * 8) * BK, xa, pass_a[p] + at);
+#pragma unroll
+        for (int p = 0; p < PB; ++p) load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, xw, pass_w[p] + at);
+        load_lds4(rs, to + (BM + BN) * BK + wave * 256, kt < nk ? vs : kNoLoad, kt < nk ? kt * 4 : 0);
+    };
+    constexpr int LPS = PA + PB + 1;
+    static_assert((NS - 2) * LPS < 64, "the load counter has six bits");
+
+    mm_f4 acc[MI][NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = mm_f4{0.f, 0.f, 0.f, 0.f};
+    const int sw = r >> 1;
+    const int at_a = (wm * TM + r) * BK, at_w = (BM + wn * TN + r) * BK, c0 = (fq ^ sw) * 16, c1 = ((4 + fq) ^ sw) * 16;
+
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) request(s, s);
+    int slot = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        constexpr int V = (NS - 2) * LPS;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();                    // this block has landed, and nobody reads the one before
+        asm volatile("" ::: "memory");
+        const int before = slot == 0 ? NS - 1 : slot - 1;
+        request(kt + NS - 1, before);
+        char* from = stage(slot);
+        if (kt == nk - 1 && a.K % 16 != 0) {             // a chunk that the row ends in
+            for (int row = tid; row < BM + BN; row += NT) {
+                mm_i4* c = (mm_i4*)(from + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
+                *c = first_codes(*c, a.K % 16);
+            }
+            __syncthreads();
+        }
+        const float* scales = (const float*)(from + (BM + BN) * BK);
+        float ws[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h) ws[h] = scales[BM + h * 64 + wn * TNY / kBlockCols];
+        mm_i8 w8[NI];
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+            const mm_i4 lo = *(const mm_i4*)(from + at_w + j * 16 * BK + c0), hi = *(const mm_i4*)(from + at_w + j * 16 * BK + c1);
+            w8[j] = mm_i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        }
+        mm_h8 wh[EIGHT ? 1 : NI][4];
+        if constexpr (!EIGHT) {
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) wh[j][s] = halves(w8[j][2 * s], w8[j][2 * s + 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const float as = scales[wm * TM + i * 16 + r];
+            const mm_i4 lo = *(const mm_i4*)(from + at_a + i * 16 * BK + c0), hi = *(const mm_i4*)(from + at_a + i * 16 * BK + c1);
+            mm_f4 part[NI];
+            if constexpr (EIGHT) {
+                const mm_i8 a8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+                for (int j = 0; j < NI; ++j) part[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8[j], a8, mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const mm_h8 ah = s < 2 ? halves(lo[2 * s % 4], lo[2 * s % 4 + 1]) : halves(hi[2 * s % 4], hi[2 * s % 4 + 1]);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j)
+                        part[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[j][s], ah, s == 0 ? mm_f4{0.f, 0.f, 0.f, 0.f} : part[j], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const float scale = as * ws[GATE && j >= NI / 2 ? 1 : 0];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[j][e], scale, acc[i][j][e]);
+            }
+        }
+        slot = slot + 1 == NS ? 0 : slot + 1;
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing is on its way into LDS
+
+    // ---- the tile's rows, as many at a time as LDS holds
+    constexpr int PITCH = BN + 4, SLABS = MI >= 4 ? 4 : MI, IS = MI / SLABS, SR = WM * IS * 16;       // rows of a slab: IS blocks of every wavefront
+    float* sums = (float*)smem;
+#pragma unroll
+    for (int slab = 0; slab < SLABS; ++slab) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < IS; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) *(mm_f4*)(sums + ((wm * IS + i) * 16 + r) * PITCH + wn * TN + j * 16 + 4 * fq) = acc[slab * IS + i][j];
+        __syncthreads();
+        constexpr int Q = BNY / 4;
+        for (int u = tid; u < SR * Q; u += NT) {
+            const int row = u / Q, col = u % Q * 4;
+            const int64_t m = m0 + row / (IS * 16) * TM + slab * IS * 16 + row % (IS * 16);
+            const int at = GATE ? col / TNY * TN + col % TNY : col;
+            const mm_f4 c = *(const mm_f4*)(sums + row * PITCH + at);
+            const mm_f4 up = GATE ? *(const mm_f4*)(sums + row * PITCH + at + TNY) : c;
+            const mm_f4 y = finish4<GATE>(a, n0 + col, c, up);
+            if constexpr (CODES) store_block4(a, m, n0 + col, y, m < a.M);
+            else if (m < a.M && n0 + col < a.N) store4<OUT>(a, m, n0 + col, y);
+        }
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int NS, bool EIGHT, bool GATE, typename OUT, bool CODES>
+hipError_t launch(const MatmulArgs& a, hipStream_t st) {
+    constexpr size_t stages = (size_t)NS * ((BM + BN) * kBlockCols + WM * WN * 256), slab = (size_t)(BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float);
+    constexpr size_t lds = stages > slab ? stages : slab;
+    const auto kernel = block_mm_tile_kernel<BM, BN, WM, WN, NS, EIGHT, GATE, OUT, CODES>;
+    if (lds > 65536) {
+        const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    constexpr int BNY = GATE ? BN / 2 : BN;
+    const int64_t tiles = (a.M + BM - 1) / BM * ((a.N + BNY - 1) / BNY);
+    kernel<<<(unsigned)((tiles + kXcds - 1) / kXcds * kXcds), WM * WN * 64, lds, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int WM, int WN, int NS, int NSC>
+hipError_t launch_shape(const MatmulArgs& a, int dtype, hipStream_t st) {
+    const bool gate = a.half > 0;
+    if (a.codes) {
+        constexpr int BNC = BN < 256 ? 256 : BN;             // with a gate 128 columns of y take 256 rows of w
+        if (gate) return launch<BM, BNC, BNC == BN ? WM : 2, BNC == BN ? WN : 4, NSC, false, true, float, true>(a, st);
+        if constexpr (BN >= 128) return launch<BM, BN, WM, WN, NS, false, false, float, true>(a, st);
+        else return launch<BM, 128, 2, 4, NSC, false, false, float, true>(a, st);
+    }
+    if (dtype == HR_F32) return gate ? launch<BM, BN, WM, WN, NS, false, true, float, false>(a, st) : launch<BM, BN, WM, WN, NS, false, false, float, false>(a, st);
+    return gate ? launch<BM, BN, WM, WN, NS, true, true, bf16_t, false>(a, st) : launch<BM, BN, WM, WN, NS, true, false, bf16_t, false>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_block_matmul_tiles(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st) {
+    if (t.bm == 256) return launch_shape<256, 256, 2, 4, 2, 2>(a, dtype, st);
+    return launch_shape<128, 128, 2, 2, 2, 3>(a, dtype, st);
+}
+
+}  // namespace hr

@@ -209,7 +209,7 @@ def check_product(a, w, y, kind, bias=None, gate=None, add=None):
         R.check_rounded(to64(y), want, off, unit(kind), "product")
 
 
-SHAPES = [(1, 16, 32), (1, 1, 1), (2, 3, 5), (1, 200, 128), (16, 32, 256), (17, 33, 129), (5, 130, 1000), (33, 96, 300), (64, 128, 130), (65, 100, 896), (70, 257, 2500), (130, 300, 640),
+SHAPES = [(2100, 1100, 140), (2048, 1024, 256), (2049, 1025, 127), (1, 16, 32), (1, 1, 1), (2, 3, 5), (1, 200, 128), (16, 32, 256), (17, 33, 129), (5, 130, 1000), (33, 96, 300), (64, 128, 130), (65, 100, 896), (70, 257, 2500), (130, 300, 640),
           (129, 128, 127), (300, 384, 400), (257, 513, 384), (200, 64, 4864), (1, 640, 4100)]
 
 
