@@ -1,8 +1,8 @@
 // Products of 8-bit matrices with few rows (hr_block_matmul): the weights' bytes are what counts.
 //
 // A workgroup has a tile of y and its wavefronts share the sum over k: wavefront ks takes the 128-column blocks ks, ks + KS, .. of both
-// operands straight into registers, in the order that the matrix instruction wants (a lane has 32 consecutive codes of one row; that a block's columns
-// come in another order than the instruction's own does not matter, it is the same for both).  Codes become halves, which are exact, and
+// operands straight into registers, in the order that the matrix instruction wants (a lane has 16 codes of either half of one row's block; the columns come in
+// another order than the instruction's own, the same for both operands).  Codes become halves, which are exact, and
 // a block's sum of 128 products starts at zero and is added in fp32 with the product of the two scales.  At the end the wavefronts' sums meet in LDS,
 // which also turns them into rows for what follows.
 #include <hip/hip_runtime.h>
@@ -34,13 +34,13 @@ __global__ void __launch_bounds__(KS * CS * 64) block_mm_few_kernel(MatmulArgs a
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int64_t m = min(m0 + 16 * i + r, a.M - 1);
-        pa[i] = a.a + m * a.a_stride + 32 * fq;
+        pa[i] = a.a + m * a.a_stride + 16 * fq;
         sa[i] = a.a_scales + m * a.a_scale_stride;
     }
 #pragma unroll
     for (int h = 0; h < H; ++h) {
 #pragma unroll
-        for (int j = 0; j < NW; ++j) pw[h][j] = a.w + (int64_t)(min(n0 + 16 * (cs * NW + j) + r, a.N - 1) + h * a.half) * a.w_stride + 32 * fq;
+        for (int j = 0; j < NW; ++j) pw[h][j] = a.w + (int64_t)(min(n0 + 16 * (cs * NW + j) + r, a.N - 1) + h * a.half) * a.w_stride + 16 * fq;
         sw[h] = a.w_scales + (int64_t)((n0 + h * a.half) / kBlockCols) * a.w_scale_stride;
     }
 
@@ -56,21 +56,21 @@ __global__ void __launch_bounds__(KS * CS * 64) block_mm_few_kernel(MatmulArgs a
 #pragma unroll
                 for (int h = 0; h < H; ++h)
 #pragma unroll
-                    for (int j = 0; j < NW; ++j) b.w[h][j][c] = *(const mm_i4*)(pw[h][j] + at + 16 * c);
+                    for (int j = 0; j < NW; ++j) b.w[h][j][c] = *(const mm_i4*)(pw[h][j] + at + 64 * c);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) b.a[i][c] = *(const mm_i4*)(pa[i] + at + 16 * c);
+                for (int i = 0; i < MT; ++i) b.a[i][c] = *(const mm_i4*)(pa[i] + at + 64 * c);
             }
         } else {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int left = a.K - (at + 32 * fq + 16 * c);
+                const int left = a.K - (at + 16 * fq + 64 * c);
                 const bool some = left > 0;
 #pragma unroll
                 for (int h = 0; h < H; ++h)
 #pragma unroll
-                    for (int j = 0; j < NW; ++j) b.w[h][j][c] = some ? first_codes(*(const mm_i4*)(pw[h][j] + at + 16 * c), left) : mm_i4{0, 0, 0, 0};
+                    for (int j = 0; j < NW; ++j) b.w[h][j][c] = some ? first_codes(*(const mm_i4*)(pw[h][j] + at + 64 * c), left) : mm_i4{0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < MT; ++i) b.a[i][c] = some ? first_codes(*(const mm_i4*)(pa[i] + at + 16 * c), left) : mm_i4{0, 0, 0, 0};
+                for (int i = 0; i < MT; ++i) b.a[i][c] = some ? first_codes(*(const mm_i4*)(pa[i] + at + 64 * c), left) : mm_i4{0, 0, 0, 0};
             }
         }
 #pragma unroll

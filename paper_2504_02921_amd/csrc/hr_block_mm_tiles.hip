@@ -43,6 +43,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;
     constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     constexpr int H = GATE ? 2 : 1, BNY = BN / H, TNY = TN / H;            // columns of y
+    constexpr bool PIPE = EIGHT && MI >= 4 && NS == 2;
     constexpr int RPP = NT / 8, PA = BM / RPP, PB = BN / RPP;              // rows a pass of 16-byte loads brings, passes
     constexpr int STAGE = (BM + BN) * BK + NT * 4;
     static_assert(BM % RPP == 0 && BN % RPP == 0 && BM / 64 + H <= NWAVE && (!CODES || BNY % kBlockCols == 0) && TNY <= kBlockCols, "loader shape");
@@ -91,17 +92,30 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         if (swave < H && lane < sblocks) vs = lane * (int)a.w_scale_stride * 4;
     }
     auto stage = [&](int s) { return smem + s * STAGE; };
-    auto request = [&](int kt, int s) {
+    constexpr int LPS = PA + PB + 1;                     // loads of a wavefront and block
+    // load q of the LPS of block kt into stage s; a block past the end fetches nothing
+    auto request_one = [&](int q, int kt, int s) {
         char* to = stage(s);
-        const bool whole = (kt + 1) * BK <= a.K, some = whole || kt * BK + lchunk * 16 < a.K;
-        const int xa = some && kt < nk ? va : kNoLoad, xw = some && kt < nk ? vw : kNoLoad, at = kt < nk ? kt * BK : 0;
-#pragma unroll
-        for (int p = 0; p < PA; ++p) load_lds16(ra, to + (p * RPP + wave * 8) * BK, xa, pass_a[p] + at);
-#pragma unroll
-        for (int p = 0; p < PB; ++p) load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, xw, pass_w[p] + at);
-        load_lds4(rs, to + (BM + BN) * BK + wave * 256, kt < nk ? vs : kNoLoad, kt < nk ? kt * 4 : 0);
+        const bool there = kt < nk, some = there && kt * BK + lchunk * 16 < a.K;
+        const int at = there ? kt * BK : 0;
+        if (q < PA) load_lds16(ra, to + (q * RPP + wave * 8) * BK, some ? va : kNoLoad, pass_a[q < PA ? q : 0] + at);
+        else if (q < PA + PB) {
+            const int p = q - PA < PB ? q - PA : 0;
+            load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, some ? vw : kNoLoad, pass_w[p] + at);
+        } else load_lds4(rs, to + (BM + BN) * BK + wave * 256, there ? vs : kNoLoad, there ? kt * 4 : 0);
     };
-    constexpr int LPS = PA + PB + 1;
+    auto request = [&](int kt, int s) {
+#pragma unroll
+        for (int q = 0; q < LPS; ++q) request_one(q, kt, s);
+    };
+    // the chunk that the rows end in, if they end inside one
+    auto mend_end = [&](char* in) {
+        for (int row = tid; row < BM + BN; row += NT) {
+            mm_i4* c = (mm_i4*)(in + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
+            *c = first_codes(*c, a.K % 16);
+        }
+        __syncthreads();
+    };
     static_assert((NS - 2) * LPS < 64, "the load counter has six bits");
 
     mm_f4 acc[MI][NI];
@@ -112,68 +126,140 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     const int sw = r >> 1;
     const int at_a = (wm * TM + r) * BK, at_w = (BM + wn * TN + r) * BK, c0 = (fq ^ sw) * 16, c1 = ((4 + fq) ^ sw) * 16;
 
+    if constexpr (PIPE) {
+        // Two stages.  A block is MI rows of NI instructions; a row's sums are scaled and added while the next row's are computed.  A's fragments are
+        // read two rows ahead and w's replaced behind their last use, so that the block's one barrier, in front of its last row but one, finds
+        // all of the stage read: what is requested behind it has a whole block's time to land.
+        mm_i8 af[2], wf[NI];
+        float as[2], ws[H], sc[2][H];
+        mm_f4 part[2][NI];
+        auto fragment = [&](const char* at) {
+            const mm_i4 lo = *(const mm_i4*)(at + c0), hi = *(const mm_i4*)(at + c1);
+            return mm_i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        };
+        auto read_a = [&](const char* in, int i) {
+            af[i & 1] = fragment(in + at_a + i * 16 * BK);
+            as[i & 1] = ((const float*)(in + (BM + BN) * BK))[wm * TM + i * 16 + r];
+        };
+        auto read_ws = [&](const char* in) {
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s) request(s, s);
-    int slot = 0;
-    for (int kt = 0; kt < nk; ++kt) {
-        constexpr int V = (NS - 2) * LPS;
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
-        __builtin_amdgcn_s_barrier();                    // this block has landed, and nobody reads the one before
-        asm volatile("" ::: "memory");
-        const int before = slot == 0 ? NS - 1 : slot - 1;
-        request(kt + NS - 1, before);
-        char* from = stage(slot);
-        if (kt == nk - 1 && a.K % 16 != 0) {             // a chunk that the row ends in
-            for (int row = tid; row < BM + BN; row += NT) {
-                mm_i4* c = (mm_i4*)(from + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
-                *c = first_codes(*c, a.K % 16);
-            }
-            __syncthreads();
-        }
-        const float* scales = (const float*)(from + (BM + BN) * BK);
-        float ws[H];
-#pragma unroll
-        for (int h = 0; h < H; ++h) ws[h] = scales[BM + h * 64 + wn * TNY / kBlockCols];
-        mm_i8 w8[NI];
+            for (int h = 0; h < H; ++h) ws[h] = ((const float*)(in + (BM + BN) * BK))[BM + h * 64 + wn * TNY / kBlockCols];
+        };
+        request(0, 0);
+        __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
+        __syncthreads();
+        request(1, 1);
+        if (nk == 1 && a.K % 16 != 0) mend_end(stage(0));
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            const mm_i4 lo = *(const mm_i4*)(from + at_w + j * 16 * BK + c0), hi = *(const mm_i4*)(from + at_w + j * 16 * BK + c1);
-            w8[j] = mm_i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        }
-        mm_h8 wh[EIGHT ? 1 : NI][4];
-        if constexpr (!EIGHT) {
-#pragma unroll
-            for (int j = 0; j < NI; ++j)
-#pragma unroll
-                for (int s = 0; s < 4; ++s) wh[j][s] = halves(w8[j][2 * s], w8[j][2 * s + 1]);
+            wf[j] = fragment(stage(0) + at_w + j * 16 * BK);
+            part[1][j] = mm_f4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const float as = scales[wm * TM + i * 16 + r];
-            const mm_i4 lo = *(const mm_i4*)(from + at_a + i * 16 * BK + c0), hi = *(const mm_i4*)(from + at_a + i * 16 * BK + c1);
-            mm_f4 part[NI];
-            if constexpr (EIGHT) {
-                const mm_i8 a8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        for (int h = 0; h < H; ++h) sc[1][h] = 0.0f;
+        read_ws(stage(0));
+        read_a(stage(0), 0);
+        read_a(stage(0), 1);
+        auto block = [&](auto mends, int kt) {           // a branch inside would keep the compiler from the order below
+            char *from = stage(kt & 1), *next = stage((kt & 1) ^ 1);
 #pragma unroll
-                for (int j = 0; j < NI; ++j) part[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8[j], a8, mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    const mm_h8 ah = s < 2 ? halves(lo[2 * s % 4], lo[2 * s % 4 + 1]) : halves(hi[2 * s % 4], hi[2 * s % 4 + 1]);
-#pragma unroll
-                    for (int j = 0; j < NI; ++j)
-                        part[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[j][s], ah, s == 0 ? mm_f4{0.f, 0.f, 0.f, 0.f} : part[j], 0, 0, 0);
+            for (int i = 0; i < MI; ++i) {
+                const int cur = i & 1, old = cur ^ 1, iold = i == 0 ? MI - 1 : i - 1;
+                if (i == MI - 2) {
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    if constexpr (decltype(mends)::value) mend_end(next);
                 }
+#pragma unroll
+                for (int h = 0; h < H; ++h) sc[cur][h] = as[cur] * ws[h];
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    part[cur][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[j], af[cur], mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[iold][j][e] = fmaf(part[old][j][e], sc[old][GATE && j >= NI / 2 ? 1 : 0], acc[iold][j][e]);
+                    if (i == MI - 1) wf[j] = fragment(next + at_w + j * 16 * BK);
+                    if (i >= MI - 2) {
+                        constexpr int SLOTS = 2 * NI, EACH = (LPS + SLOTS - 1) / SLOTS;
+                        const int slot = (i - (MI - 2)) * NI + j;
+#pragma unroll
+                        for (int q = 0; q < EACH; ++q)
+                            if (slot * EACH + q < LPS) request_one(slot * EACH + q, kt + 2, kt & 1);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (i == MI - 1) read_ws(next);
+                read_a(i < MI - 2 ? from : next, i < MI - 2 ? i + 2 : i + 2 - MI);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        };
+        int kt = 0;
+        for (const int plain = a.K % 16 != 0 ? nk - 2 : nk; kt < plain; ++kt) block(std::false_type{}, kt);
+        if (kt < nk - 1) block(std::true_type{}, kt++);
+        if (kt < nk) block(std::false_type{}, kt);
+#pragma unroll
+        for (int j = 0; j < NI; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[MI - 1][j][e] = fmaf(part[1][j][e], sc[1][GATE && j >= NI / 2 ? 1 : 0], acc[MI - 1][j][e]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS - 1; ++s) request(s, s);
+        int slot = 0;
+        for (int kt = 0; kt < nk; ++kt) {
+            constexpr int V = (NS - 2) * LPS;
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();                    // this block has landed, and nobody reads the one before
+            asm volatile("" ::: "memory");
+            const int before = slot == 0 ? NS - 1 : slot - 1;
+            request(kt + NS - 1, before);
+            char* from = stage(slot);
+            if (kt == nk - 1 && a.K % 16 != 0) mend_end(from);
+            const float* scales = (const float*)(from + (BM + BN) * BK);
+            float ws[H];
+#pragma unroll
+            for (int h = 0; h < H; ++h) ws[h] = scales[BM + h * 64 + wn * TNY / kBlockCols];
+            mm_i8 w8[NI];
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
-                const float scale = as * ws[GATE && j >= NI / 2 ? 1 : 0];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[j][e], scale, acc[i][j][e]);
+                const mm_i4 lo = *(const mm_i4*)(from + at_w + j * 16 * BK + c0), hi = *(const mm_i4*)(from + at_w + j * 16 * BK + c1);
+                w8[j] = mm_i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
             }
+            mm_h8 wh[EIGHT ? 1 : NI][4];
+            if constexpr (!EIGHT) {
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) wh[j][s] = halves(w8[j][2 * s], w8[j][2 * s + 1]);
+            }
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const float as = scales[wm * TM + i * 16 + r];
+                const mm_i4 lo = *(const mm_i4*)(from + at_a + i * 16 * BK + c0), hi = *(const mm_i4*)(from + at_a + i * 16 * BK + c1);
+                mm_f4 part[NI];
+                if constexpr (EIGHT) {
+                    const mm_i8 a8 = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) part[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8[j], a8, mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const mm_h8 ah = s < 2 ? halves(lo[2 * s % 4], lo[2 * s % 4 + 1]) : halves(hi[2 * s % 4], hi[2 * s % 4 + 1]);
+#pragma unroll
+                        for (int j = 0; j < NI; ++j)
+                            part[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[j][s], ah, s == 0 ? mm_f4{0.f, 0.f, 0.f, 0.f} : part[j], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    const float scale = as * ws[GATE && j >= NI / 2 ? 1 : 0];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(part[j][e], scale, acc[i][j][e]);
+                }
+            }
+            slot = slot + 1 == NS ? 0 : slot + 1;
         }
-        slot = slot + 1 == NS ? 0 : slot + 1;
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing is on its way into LDS
 
