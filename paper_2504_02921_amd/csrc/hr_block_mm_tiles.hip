@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;
     constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     constexpr int H = GATE ? 2 : 1, BNY = BN / H, TNY = TN / H;            // columns of y
-    constexpr bool PIPE = EIGHT && MI >= 4 && NS == 2;
+    constexpr bool PIPE = MI >= 4 && NS == 2;
     constexpr int RPP = NT / 8, PA = BM / RPP, PB = BN / RPP;              // rows a pass of 16-byte loads brings, passes
     constexpr int STAGE = (BM + BN) * BK + NT * 4;
     static_assert(BM % RPP == 0 && BN % RPP == 0 && BM / 64 + H <= NWAVE && (!CODES || BNY % kBlockCols == 0) && TNY <= kBlockCols, "loader shape");
@@ -127,12 +127,13 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     const int at_a = (wm * TM + r) * BK, at_w = (BM + wn * TN + r) * BK, c0 = (fq ^ sw) * 16, c1 = ((4 + fq) ^ sw) * 16;
 
     if constexpr (PIPE) {
-        // Two stages.  A block is MI rows of NI instructions; a row's sums are scaled and added while the next row's are computed.  A's fragments are
+        // Two stages.  A block is MI rows of NI sums; a row's sums are scaled and added while the next row's are computed.  A's fragments are
         // read two rows ahead and w's replaced behind their last use, so that the block's one barrier, in front of its last row but one, finds
         // all of the stage read: what is requested behind it has a whole block's time to land.
-        mm_i8 af[2], wf[NI];
+        mm_i8 af[2], w8[EIGHT ? NI : 1];
+        mm_h8 wh[EIGHT ? 1 : NI][4];
         float as[2], ws[H], sc[2][H];
-        mm_f4 part[2][NI];
+        mm_f4 part[NI];
         auto fragment = [&](const char* at) {
             const mm_i4 lo = *(const mm_i4*)(at + c0), hi = *(const mm_i4*)(at + c1);
             return mm_i8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
@@ -140,6 +141,14 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         auto read_a = [&](const char* in, int i) {
             af[i & 1] = fragment(in + at_a + i * 16 * BK);
             as[i & 1] = ((const float*)(in + (BM + BN) * BK))[wm * TM + i * 16 + r];
+        };
+        auto read_w = [&](const char* in, int j) {
+            const mm_i8 w = fragment(in + at_w + j * 16 * BK);
+            if constexpr (EIGHT) w8[j] = w;
+            else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) wh[j][s] = halves(w[2 * s], w[2 * s + 1]);
+            }
         };
         auto read_ws = [&](const char* in) {
 #pragma unroll
@@ -152,14 +161,16 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         if (nk == 1 && a.K % 16 != 0) mend_end(stage(0));
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
-            wf[j] = fragment(stage(0) + at_w + j * 16 * BK);
-            part[1][j] = mm_f4{0.f, 0.f, 0.f, 0.f};
+            read_w(stage(0), j);
+            part[j] = mm_f4{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
         for (int h = 0; h < H; ++h) sc[1][h] = 0.0f;
         read_ws(stage(0));
         read_a(stage(0), 0);
         read_a(stage(0), 1);
+        // Two wavefronts share a SIMD: where one goes first, they do not wait for the same unit at the same time
+        if (wave >= NWAVE / 2) __builtin_amdgcn_s_setprio(1);
         auto block = [&](auto mends, int kt) {           // a branch inside would keep the compiler from the order below
             char *from = stage(kt & 1), *next = stage((kt & 1) ^ 1);
 #pragma unroll
@@ -174,34 +185,59 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
                 }
 #pragma unroll
                 for (int h = 0; h < H; ++h) sc[cur][h] = as[cur] * ws[h];
+                auto add_old = [&](int j) {
 #pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    part[cur][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[j], af[cur], mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                    for (int e = 0; e < 4; ++e) acc[iold][j][e] = fmaf(part[j][e], sc[old][GATE && j >= NI / 2 ? 1 : 0], acc[iold][j][e]);
+                };
+                auto ask = [&](int j) {                  // one load behind each of the first instructions behind the barrier
+                    const int slot = (i + 2) % MI * NI + j;
+                    if (slot < LPS) request_one(slot, i >= MI - 2 ? kt + 2 : kt + 1, i >= MI - 2 ? kt & 1 : (kt & 1) ^ 1);
+                };
+                static_assert(LPS <= MI * NI, "a slot for every load");
+                if constexpr (EIGHT) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[iold][j][e] = fmaf(part[old][j][e], sc[old][GATE && j >= NI / 2 ? 1 : 0], acc[iold][j][e]);
-                    if (i == MI - 1) wf[j] = fragment(next + at_w + j * 16 * BK);
-                    if (i >= MI - 2) {
-                        constexpr int SLOTS = 2 * NI, EACH = (LPS + SLOTS - 1) / SLOTS;
-                        const int slot = (i - (MI - 2)) * NI + j;
-#pragma unroll
-                        for (int q = 0; q < EACH; ++q)
-                            if (slot * EACH + q < LPS) request_one(slot * EACH + q, kt + 2, kt & 1);
+                    for (int j = 0; j < NI; ++j) {
+                        add_old(j);
+                        part[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w8[j], af[cur], mm_f4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
+                        if (i == MI - 1) read_w(next, j);
+                        ask(j);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                    __builtin_amdgcn_sched_barrier(0);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const mm_h8 ah = halves(af[cur][2 * s], af[cur][2 * s + 1]);
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) {
+                            if (s == 0) add_old(j);
+                            part[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(wh[j][s], ah, s == 0 ? mm_f4{0.f, 0.f, 0.f, 0.f} : part[j], 0, 0, 0);
+                            if (s == 1) ask(j);
+                        }
+                        if (s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if (i == MI - 1) {
+#pragma unroll
+                        for (int j = 0; j < NI; ++j) {
+                            read_w(next, j);
+                            if (j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+                        }
+                    }
                 }
                 if (i == MI - 1) read_ws(next);
                 read_a(i < MI - 2 ? from : next, i < MI - 2 ? i + 2 : i + 2 - MI);
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
+        // the first loads of block 1 are out; those of a block begin behind the barrier of the one before it
         int kt = 0;
         for (const int plain = a.K % 16 != 0 ? nk - 2 : nk; kt < plain; ++kt) block(std::false_type{}, kt);
         if (kt < nk - 1) block(std::true_type{}, kt++);
         if (kt < nk) block(std::false_type{}, kt);
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int j = 0; j < NI; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[MI - 1][j][e] = fmaf(part[1][j][e], sc[1][GATE && j >= NI / 2 ? 1 : 0], acc[MI - 1][j][e]);
+            for (int e = 0; e < 4; ++e) acc[MI - 1][j][e] = fmaf(part[j][e], sc[1][GATE && j >= NI / 2 ? 1 : 0], acc[MI - 1][j][e]);
     } else {
 #pragma unroll
         for (int s = 0; s < NS - 1; ++s) request(s, s);
