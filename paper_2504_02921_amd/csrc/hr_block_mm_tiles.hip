@@ -37,16 +37,19 @@ __device__ __forceinline__ void load_lds4(rsrc_t r, void* lds, int voff, int sof
 #endif
 }
 
-// BM rows x BN rows of w, WM x WN wavefronts, NS stages.  With a gate a wavefront's rows of w are half gate rows, half the rows that they multiply.
-template <int BM, int BN, int WM, int WN, int NS, bool EIGHT, bool GATE, typename OUT, bool CODES>
-__global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_tile_kernel(MatmulArgs a) {
-    constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;
+// BM rows x BN rows of w by WM x WN wavefronts, KG groups of which take turns along k, each with NS stages.  With a gate a wavefront's rows of w are half
+// gate rows, half the rows that they multiply.
+template <int BM, int BN, int WM, int WN, int NS, int KG, bool EIGHT, bool GATE, typename OUT, bool CODES>
+__global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) block_mm_tile_kernel(MatmulArgs a) {
+    constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;       // of a group
     constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     constexpr int H = GATE ? 2 : 1, BNY = BN / H, TNY = TN / H;            // columns of y
     constexpr bool PIPE = MI >= 4 && NS == 2;
-    constexpr int RPP = NT / 8, PA = BM / RPP, PB = BN / RPP;              // rows a pass of 16-byte loads brings, passes
+    constexpr int RPP = NT / 8, PA = (BM + RPP - 1) / RPP, PB = BN / RPP;  // rows a pass of 16-byte loads brings, passes
+    constexpr bool SHORT = BM < RPP;                                       // the first wavefronts bring all rows of a
+    constexpr int SW = (BM + 63) / 64;                                     // wavefronts that bring the rows' scales
     constexpr int STAGE = (BM + BN) * BK + NT * 4;
-    static_assert(BM % RPP == 0 && BN % RPP == 0 && BM / 64 + H <= NWAVE && (!CODES || BNY % kBlockCols == 0) && TNY <= kBlockCols, "loader shape");
+    static_assert((SHORT ? BM % 8 : BM % RPP) == 0 && BN % RPP == 0 && SW + H <= NWAVE && (!CODES || BNY % kBlockCols == 0) && TNY <= kBlockCols, "loader shape");
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int tiles_m = (int)((a.M + BM - 1) / BM), tiles_n = (a.N + BNY - 1) / BNY;
@@ -54,9 +57,10 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     if (!tc.valid) return;
     const int64_t m0 = (int64_t)tc.tm * BM;
     const int n0 = tc.tn * BNY;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = all / NWAVE, wave = all % NWAVE;
+    const int tid = KG > 1 ? (int)threadIdx.x - group * NT : (int)threadIdx.x;
     const int wm = wave / WN, wn = wave % WN, r = lane & 15, fq = lane >> 4;
-    const int nk = (int)blocks_of(a.K);
+    const int nk = (int)blocks_of(a.K), turns = (nk + KG - 1) / KG;       // blocks of k; block kt is group kt % KG's in turn kt / KG
 
     // ---- loads: a wavefront's load brings eight rows of 128 codes
     const int rows_a = (int)min((int64_t)BM, a.M - m0), rows_w = min(BNY, a.N - n0);
@@ -80,8 +84,8 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         const int row = p * RPP + wave * 8, f = GATE ? row / TN * TNY + row % TNY : row;
         pass_w[p] = f < rows_w ? f * (int)a.w_stride : 0;
     }
-    // scales: wavefronts 0 .. BM / 64 - 1 bring those of the rows, the next one (two) those of w's blocks
-    const int swave = wave - BM / 64, sblocks = (int)blocks_of(rows_w);
+    // scales: the first SW wavefronts bring those of the rows, the next one (two) those of w's blocks
+    const int swave = wave - SW, sblocks = (int)blocks_of(rows_w);
     rsrc_t rs;
     int vs = kNoLoad;
     if (swave < 0) {
@@ -91,26 +95,28 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         rs = make_rsrc(a.w_scales + ((int64_t)n0 + (swave == 1 ? (int64_t)a.half : 0)) / kBlockCols * a.w_scale_stride, sblocks * a.w_scale_stride * 4);
         if (swave < H && lane < sblocks) vs = lane * (int)a.w_scale_stride * 4;
     }
-    auto stage = [&](int s) { return smem + s * STAGE; };
+    auto stage = [&](int s) { return smem + (group * NS + s) * STAGE; };
     constexpr int LPS = PA + PB + 1;                     // loads of a wavefront and block
-    // load q of the LPS of block kt into stage s; a block past the end fetches nothing
-    auto request_one = [&](int q, int kt, int s) {
+    // load q of the LPS of a turn's block into stage s; a block past the end fetches nothing, and its zeros add nothing
+    auto request_one = [&](int q, int turn, int s) {
         char* to = stage(s);
+        const int kt = turn * KG + group;
         const bool there = kt < nk, some = there && kt * BK + lchunk * 16 < a.K;
         const int at = there ? kt * BK : 0;
+        if (SHORT && q == 0 && wave * 8 >= BM) return;   // goes by the wavefront
         if (q < PA) load_lds16(ra, to + (q * RPP + wave * 8) * BK, some ? va : kNoLoad, pass_a[q < PA ? q : 0] + at);
         else if (q < PA + PB) {
             const int p = q - PA < PB ? q - PA : 0;
             load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, some ? vw : kNoLoad, pass_w[p] + at);
         } else load_lds4(rs, to + (BM + BN) * BK + wave * 256, there ? vs : kNoLoad, there ? kt * 4 : 0);
     };
-    auto request = [&](int kt, int s) {
+    auto request = [&](int turn, int s) {
 #pragma unroll
-        for (int q = 0; q < LPS; ++q) request_one(q, kt, s);
+        for (int q = 0; q < LPS; ++q) request_one(q, turn, s);
     };
-    // the chunk that the rows end in, if they end inside one
+    // the chunk that the rows end in, in the last turn, if they end inside one
     auto mend_end = [&](char* in) {
-        for (int row = tid; row < BM + BN; row += NT) {
+        for (int row = tid; row < BM + BN && (nk - 1) % KG == group; row += NT) {
             mm_i4* c = (mm_i4*)(in + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
             *c = first_codes(*c, a.K % 16);
         }
@@ -152,13 +158,13 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         };
         auto read_ws = [&](const char* in) {
 #pragma unroll
-            for (int h = 0; h < H; ++h) ws[h] = ((const float*)(in + (BM + BN) * BK))[BM + h * 64 + wn * TNY / kBlockCols];
+            for (int h = 0; h < H; ++h) ws[h] = ((const float*)(in + (BM + BN) * BK))[SW * 64 + h * 64 + wn * TNY / kBlockCols];
         };
         request(0, 0);
         __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
         __syncthreads();
         request(1, 1);
-        if (nk == 1 && a.K % 16 != 0) mend_end(stage(0));
+        if (turns == 1 && a.K % 16 != 0) mend_end(stage(0));
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             read_w(stage(0), j);
@@ -170,9 +176,9 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
         read_a(stage(0), 0);
         read_a(stage(0), 1);
         // Two wavefronts share a SIMD: where one goes first, they do not wait for the same unit at the same time
-        if (wave >= NWAVE / 2) __builtin_amdgcn_s_setprio(1);
-        auto block = [&](auto mends, int kt) {           // a branch inside would keep the compiler from the order below
-            char *from = stage(kt & 1), *next = stage((kt & 1) ^ 1);
+        if (all >= NWAVE * KG / 2) __builtin_amdgcn_s_setprio(1);
+        auto block = [&](auto mends, int turn) {           // a branch inside would keep the compiler from the order below
+            char *from = stage(turn & 1), *next = stage((turn & 1) ^ 1);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const int cur = i & 1, old = cur ^ 1, iold = i == 0 ? MI - 1 : i - 1;
@@ -191,7 +197,7 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
                 };
                 auto ask = [&](int j) {                  // one load behind each of the first instructions behind the barrier
                     const int slot = (i + 2) % MI * NI + j;
-                    if (slot < LPS) request_one(slot, i >= MI - 2 ? kt + 2 : kt + 1, i >= MI - 2 ? kt & 1 : (kt & 1) ^ 1);
+                    if (slot < LPS) request_one(slot, i >= MI - 2 ? turn + 2 : turn + 1, i >= MI - 2 ? turn & 1 : (turn & 1) ^ 1);
                 };
                 static_assert(LPS <= MI * NI, "a slot for every load");
                 if constexpr (EIGHT) {
@@ -242,20 +248,21 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
 #pragma unroll
         for (int s = 0; s < NS - 1; ++s) request(s, s);
         int slot = 0;
-        for (int kt = 0; kt < nk; ++kt) {
-            constexpr int V = (NS - 2) * LPS;
+        for (int turn = 0; turn < turns; ++turn) {
+            constexpr int V = (NS - 2) * LPS, V1 = (NS - 2) * (LPS - 1);
             asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
+            if (SHORT && wave * 8 >= BM) __builtin_amdgcn_s_waitcnt((V1 & 15) | ((V1 >> 4) << 14) | 0x0070);
+            else __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
             __builtin_amdgcn_s_barrier();                    // this block has landed, and nobody reads the one before
             asm volatile("" ::: "memory");
             const int before = slot == 0 ? NS - 1 : slot - 1;
-            request(kt + NS - 1, before);
+            request(turn + NS - 1, before);
             char* from = stage(slot);
-            if (kt == nk - 1 && a.K % 16 != 0) mend_end(from);
+            if (turn == turns - 1 && a.K % 16 != 0) mend_end(from);
             const float* scales = (const float*)(from + (BM + BN) * BK);
             float ws[H];
 #pragma unroll
-            for (int h = 0; h < H; ++h) ws[h] = scales[BM + h * 64 + wn * TNY / kBlockCols];
+            for (int h = 0; h < H; ++h) ws[h] = scales[SW * 64 + h * 64 + wn * TNY / kBlockCols];
             mm_i8 w8[NI];
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
@@ -308,15 +315,19 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
 #pragma unroll
         for (int i = 0; i < IS; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) *(mm_f4*)(sums + ((wm * IS + i) * 16 + r) * PITCH + wn * TN + j * 16 + 4 * fq) = acc[slab * IS + i][j];
+            for (int j = 0; j < NI; ++j) *(mm_f4*)(sums + ((group * WM + wm) * IS * 16 + i * 16 + r) * PITCH + wn * TN + j * 16 + 4 * fq) = acc[slab * IS + i][j];
         __syncthreads();
         constexpr int Q = BNY / 4;
-        for (int u = tid; u < SR * Q; u += NT) {
+        for (int u = threadIdx.x; u < SR * Q; u += NT * KG) {
             const int row = u / Q, col = u % Q * 4;
             const int64_t m = m0 + row / (IS * 16) * TM + slab * IS * 16 + row % (IS * 16);
             const int at = GATE ? col / TNY * TN + col % TNY : col;
-            const mm_f4 c = *(const mm_f4*)(sums + row * PITCH + at);
-            const mm_f4 up = GATE ? *(const mm_f4*)(sums + row * PITCH + at + TNY) : c;
+            mm_f4 c = *(const mm_f4*)(sums + row * PITCH + at), up = GATE ? *(const mm_f4*)(sums + row * PITCH + at + TNY) : c;
+#pragma unroll
+            for (int g = 1; g < KG; ++g) {
+                c += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at);
+                if (GATE) up += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at + TNY);
+            }
             const mm_f4 y = finish4<GATE>(a, n0 + col, c, up);
             if constexpr (CODES) store_block4(a, m, n0 + col, y, m < a.M);
             else if (m < a.M && n0 + col < a.N) store4<OUT>(a, m, n0 + col, y);
@@ -324,18 +335,20 @@ __global__ void __launch_bounds__(WM * WN * 64, WM * WN == 4 ? 2 : 1) block_mm_t
     }
 }
 
-template <int BM, int BN, int WM, int WN, int NS, bool EIGHT, bool GATE, typename OUT, bool CODES>
+template <int BM, int BN, int WM, int WN, int NS, int KG, bool EIGHT, bool GATE, typename OUT, bool CODES>
 hipError_t launch(const MatmulArgs& a, hipStream_t st) {
-    constexpr size_t stages = (size_t)NS * ((BM + BN) * kBlockCols + WM * WN * 256), slab = (size_t)(BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float);
+    constexpr size_t stages = (size_t)KG * NS * ((BM + BN) * kBlockCols + WM * WN * 256);
+    constexpr size_t slab = (size_t)KG * (BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float);
     constexpr size_t lds = stages > slab ? stages : slab;
-    const auto kernel = block_mm_tile_kernel<BM, BN, WM, WN, NS, EIGHT, GATE, OUT, CODES>;
+    static_assert(lds <= 160 * 1024, "LDS of a CU");
+    const auto kernel = block_mm_tile_kernel<BM, BN, WM, WN, NS, KG, EIGHT, GATE, OUT, CODES>;
     if (lds > 65536) {
         const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
     constexpr int BNY = GATE ? BN / 2 : BN;
     const int64_t tiles = (a.M + BM - 1) / BM * ((a.N + BNY - 1) / BNY);
-    kernel<<<(unsigned)((tiles + kXcds - 1) / kXcds * kXcds), WM * WN * 64, lds, st>>>(a);
+    kernel<<<(unsigned)((tiles + kXcds - 1) / kXcds * kXcds), WM * WN * KG * 64, lds, st>>>(a);
     return hipGetLastError();
 }
 
@@ -344,12 +357,12 @@ hipError_t launch_shape(const MatmulArgs& a, int dtype, hipStream_t st) {
     const bool gate = a.half > 0;
     if (a.codes) {
         constexpr int BNC = BN < 256 ? 256 : BN;             // with a gate 128 columns of y take 256 rows of w
-        if (gate) return launch<BM, BNC, BNC == BN ? WM : 2, BNC == BN ? WN : 4, NSC, false, true, float, true>(a, st);
-        if constexpr (BN >= 128) return launch<BM, BN, WM, WN, NS, false, false, float, true>(a, st);
-        else return launch<BM, 128, 2, 4, NSC, false, false, float, true>(a, st);
+        if (gate) return launch<BM, BNC, BNC == BN ? WM : 2, BNC == BN ? WN : 4, NSC, 1, false, true, float, true>(a, st);
+        if constexpr (BN >= 128) return launch<BM, BN, WM, WN, NS, 1, false, false, float, true>(a, st);
+        else return launch<BM, 128, 2, 4, NSC, 1, false, false, float, true>(a, st);
     }
-    if (dtype == HR_F32) return gate ? launch<BM, BN, WM, WN, NS, false, true, float, false>(a, st) : launch<BM, BN, WM, WN, NS, false, false, float, false>(a, st);
-    return gate ? launch<BM, BN, WM, WN, NS, true, true, bf16_t, false>(a, st) : launch<BM, BN, WM, WN, NS, true, false, bf16_t, false>(a, st);
+    if (dtype == HR_F32) return gate ? launch<BM, BN, WM, WN, NS, 1, false, true, float, false>(a, st) : launch<BM, BN, WM, WN, NS, 1, false, false, float, false>(a, st);
+    return gate ? launch<BM, BN, WM, WN, NS, 1, true, true, bf16_t, false>(a, st) : launch<BM, BN, WM, WN, NS, 1, true, false, bf16_t, false>(a, st);
 }
 
 }  // namespace
