@@ -45,8 +45,16 @@ struct MatmulArgs {
 };
 MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_args& m);
 
-// A product's tile: BM rows x BN columns of y
-struct MatmulTile { int bm, bn; bool few; };
-MatmulTile matmul_tile(int64_t M, int N, int K, int dtype, int gate, bool block8);
+// Tiles of a product: rows x rows of w (with a gate half as many columns of y), _n: n groups of wavefronts that take turns along k
+enum MatmulShape {
+    MM_FEW_16, MM_FEW_32,            // no LDS on the way in: 16 rows x 16 or 32 columns of y
+    MM_16x64_4, MM_32x64_2, MM_64x64, MM_64x64_2, MM_64x128, MM_64x128_2, MM_64x256, MM_128x128, MM_128x256, MM_256x256,
+    MM_16x128_4, MM_32x128_2, MM_16x256, MM_32x256,      // into codes only
+    MM_SHAPES
+};
+struct MatmulPlan { int shape; int64_t rows; int rest; };      // the first `rows` rows, and the shape of what is left
+MatmulPlan matmul_plan(const MatmulArgs& a, int dtype);
+int64_t matmul_tiles(int shape, const MatmulArgs& a, int64_t rows);
+MatmulArgs matmul_rows(const MatmulArgs& a, int dtype, int64_t first, int64_t rows);
 
 }  // namespace hr

@@ -33,9 +33,19 @@ int hr_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block
 int hr_block_matmul(const hr_block8* a, const hr_block8* w, const hr_matmul_args* args, void* stream) {
     const int rc = hr::matmul_check(a, w, args);
     if (rc != HR_OK || a->rows == 0 || w->rows == 0) return rc;
-    const hr::MatmulArgs m = hr::matmul_args(*a, *w, *args);
-    const hr::MatmulTile t = hr::matmul_tile(m.M, m.N, m.K, args->dtype, m.gate, m.codes != nullptr);
-    HR_OP_HIP((t.few ? hr::launch_block_matmul_few : hr::launch_block_matmul_tiles)(m, args->dtype, t, (hipStream_t)stream));
+    hr::MatmulArgs m = hr::matmul_args(*a, *w, *args);
+    const hr::MatmulPlan plan = hr::matmul_plan(m, args->dtype);
+    auto launch = [&](const hr::MatmulArgs& part, int shape) {
+        if (shape <= hr::MM_FEW_32) return hr::launch_block_matmul_few(part, args->dtype, shape, (hipStream_t)stream);
+        if (part.codes) return hr::launch_block_matmul_codes(part, shape, (hipStream_t)stream);
+        return (args->dtype == HR_F32 ? hr::launch_block_matmul_f32 : hr::launch_block_matmul_bf16)(part, shape, (hipStream_t)stream);
+    };
+    if (plan.rows < m.M) {
+        HR_OP_HIP(launch(hr::matmul_rows(m, args->dtype, 0, plan.rows), plan.shape));
+        HR_OP_HIP(launch(hr::matmul_rows(m, args->dtype, plan.rows, m.M - plan.rows), plan.rest));
+    } else {
+        HR_OP_HIP(launch(m, plan.shape));
+    }
     return HR_OK;
 }
 

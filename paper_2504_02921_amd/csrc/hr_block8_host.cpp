@@ -140,8 +140,9 @@ int matmul_check(const hr_block8* a, const hr_block8* w, const hr_matmul_args* m
     for (const void* out : outs)
         for (const void* in : {(const void*)a->codes, (const void*)a->scales, (const void*)w->codes, (const void*)w->scales, (const void*)m->bias})
             if (out && out == in) return HR_ERR_INVALID_ARG;
-    const MatmulTile t = matmul_tile(a->rows, (int)wide, a->cols, m->dtype, m->gate, m->block8 != nullptr);
-    if ((a->rows + t.bm - 1) / t.bm * ((wide + t.bn - 1) / t.bn) > kMaxWorkgroups) return HR_ERR_LEN_RANGE;
+    const MatmulArgs r = matmul_args(*a, *w, *m);
+    const MatmulPlan plan = matmul_plan(r, m->dtype);
+    if (matmul_tiles(plan.shape, r, plan.rows) > kMaxWorkgroups) return HR_ERR_LEN_RANGE;
     return HR_OK;
 }
 
@@ -174,16 +175,103 @@ MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_a
     return r;
 }
 
-MatmulTile matmul_tile(int64_t M, int N, int K, int dtype, int gate, bool block8) {
-    (void)K; (void)dtype;
-    const bool gated = gate != HR_GATE_NONE;
-    if (M > 64) {
-        const bool large = M >= 2048 && N >= 1024;
-        const int bm = large ? 256 : 128, bn = large ? 256 : 128;
-        return MatmulTile{bm, gated ? (block8 && bn < 256 ? 128 : bn / 2) : bn, false};
+namespace {
+
+// What a shape's launch takes in us, by its first round of tiles (one a CU) and by each further one: start + turns * first + rounds * turns * more, a
+// turn being `group` blocks of k.  [0]: 8-bit instruction, [1]: halves; of the kernels without LDS, at 16 rows.  Fitted to products of 896 x 896
+// to 28672 x 4096 and 4096 x 14336 columns x k with 1 to 6000 rows, weights from memory.
+struct Cost { int bm, bn, group; float start[2], first[2], more[2]; };
+constexpr Cost kCost[MM_SHAPES] = {
+    {16, 16, 8, {2.3f, 2.3f}, {1.05f, 1.05f}, {1.10f, 1.10f}},      // MM_FEW_16
+    {16, 32, 8, {3.2f, 3.2f}, {1.50f, 1.50f}, {1.60f, 1.60f}},
+    {16, 64, 4, {4.0f, 4.0f}, {0.55f, 0.72f}, {0.55f, 0.72f}},      // MM_16x64_4
+    {32, 64, 2, {3.0f, 2.9f}, {0.36f, 0.53f}, {0.32f, 0.44f}},
+    {64, 64, 1, {3.2f, 4.0f}, {0.31f, 0.49f}, {0.25f, 0.32f}},
+    {64, 64, 2, {3.6f, 4.4f}, {0.47f, 0.74f}, {0.66f, 0.90f}},
+    {64, 128, 1, {5.0f, 4.9f}, {0.49f, 0.72f}, {0.30f, 0.50f}},
+    {64, 128, 2, {4.4f, 4.9f}, {0.79f, 1.18f}, {0.95f, 1.50f}},
+    {64, 256, 1, {4.4f, 5.5f}, {0.71f, 1.16f}, {0.90f, 1.30f}},
+    {128, 128, 1, {6.0f, 8.7f}, {0.69f, 1.17f}, {0.50f, 0.90f}},
+    {128, 256, 1, {4.4f, 8.5f}, {0.94f, 1.64f}, {1.30f, 2.00f}},
+    {256, 256, 1, {4.0f, 9.6f}, {1.60f, 2.84f}, {2.00f, 3.50f}},
+    {16, 128, 4, {4.1f, 4.1f}, {1.00f, 1.00f}, {1.70f, 1.70f}},      // MM_16x128_4
+    {32, 128, 2, {3.6f, 3.6f}, {0.78f, 0.78f}, {0.96f, 0.96f}},
+    {16, 256, 1, {3.8f, 3.8f}, {0.70f, 0.70f}, {0.90f, 0.90f}},
+    {32, 256, 1, {5.0f, 5.0f}, {0.93f, 0.93f}, {0.95f, 0.95f}},
+};
+constexpr int kCus = 256;
+
+bool covers(int shape, bool codes, bool gate) {
+    const int bn = kCost[shape].bn;
+    if (!codes) return shape < MM_16x128_4 && !(gate && shape == MM_16x64_4);      // whose wavefronts have 16 rows of w
+    return shape > MM_FEW_32 && (gate ? bn >= 2 * kBlockCols : bn == kBlockCols || (bn > kBlockCols && kCost[shape].bm >= 64));
+}
+
+float cost_of(int shape, const MatmulArgs& a, int64_t rows, int mode) {
+    const Cost& c = kCost[shape];
+    const int64_t tiles = matmul_tiles(shape, a, rows), rounds = (tiles + kCus - 1) / kCus, blocks = blocks_of(a.K);
+    const float turns = (float)((blocks + c.group - 1) / c.group);
+    float first = c.first[mode], more = c.more[mode];
+    if (shape <= MM_FEW_32) {
+        if (a.half > 0) {                           // reads two pieces of w
+            first *= 1.4f;
+            more *= 1.5f;
+        }
+        first *= 0.6f + 0.025f * (float)std::min<int64_t>(rows, 16);      // lanes without a row read what others read
     }
-    const int bm = M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    return MatmulTile{bm, block8 ? 128 : gated ? 16 : 32, true};
+    return c.start[mode] + turns * (first + (float)(rounds - 1) * more);
+}
+
+}  // namespace
+
+int64_t matmul_tiles(int shape, const MatmulArgs& a, int64_t rows) {
+    const Cost& c = kCost[shape];
+    const int wide = shape > MM_FEW_32 && a.half > 0 ? c.bn / 2 : c.bn;
+    return (rows + c.bm - 1) / c.bm * ((a.N + wide - 1) / wide);
+}
+
+// The shape that costs least.  Rows that fill whole rounds of the largest tiles may go ahead of the others, which are then tiled for themselves
+MatmulPlan matmul_plan(const MatmulArgs& a, int dtype) {
+    const bool codes = a.codes != nullptr, gate = a.half > 0;
+    const int mode = codes || dtype == HR_F32 ? 1 : 0;
+    auto best = [&](int64_t rows, float& cost) {
+        int shape = -1;
+        for (int s = 0; s < MM_SHAPES; ++s) {
+            if (!covers(s, codes, gate)) continue;
+            const float t = cost_of(s, a, rows, mode);
+            if (shape < 0 || t < cost) {
+                shape = s;
+                cost = t;
+            }
+        }
+        return shape;
+    };
+    float cost = 0.0f, rest_cost = 0.0f;
+    MatmulPlan p{best(a.M, cost), a.M, 0};
+    const Cost& large = kCost[MM_256x256];
+    const int wide = gate ? large.bn / 2 : large.bn;
+    const int64_t columns = (a.N + wide - 1) / wide, rounds = a.M / large.bm * columns / kCus;
+    const int64_t rows = rounds * kCus / columns * large.bm;
+    if (rows > 0 && rows < a.M) {
+        const int rest = best(a.M - rows, rest_cost);
+        if (rest != MM_256x256 && cost_of(MM_256x256, a, rows, mode) + rest_cost < 0.98f * cost) p = MatmulPlan{MM_256x256, rows, rest};
+    }
+    return p;
+}
+
+MatmulArgs matmul_rows(const MatmulArgs& a, int dtype, int64_t first, int64_t rows) {
+    MatmulArgs r = a;
+    const int64_t esz = (int64_t)dtype_size(dtype);
+    r.M = rows;
+    r.a += first * a.a_stride;
+    r.a_scales += first * a.a_scale_stride;
+    if (a.add) r.add = (const char*)a.add + first * a.add_stride * esz;
+    if (a.out) r.out = (char*)a.out + first * a.out_stride * esz;
+    if (a.codes) {
+        r.codes += first * a.code_stride;
+        r.scales += first * a.scale_stride;
+    }
+    return r;
 }
 
 }  // namespace hr

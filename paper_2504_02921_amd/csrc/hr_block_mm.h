@@ -30,10 +30,14 @@ __device__ __forceinline__ mm_i4 first_codes(mm_i4 w, int left) {
     return w;
 }
 
-// A gate's act(z) u.  Both acts are z / (1 + exp(-t)): silu with t = z, gelu with t = 2 sqrt(2 / pi) (z + 0.044715 z^3)
+// A gate's act(z) u.  Both acts are z / (1 + exp(-t)): silu with t = z, gelu with t = 2 sqrt(2 / pi) (z + 0.044715 z^3).  exp(-t) is 2^x with
+// x = -t / ln 2 in two parts, as one would lose |x| 2^-24 of the result; both instructions are good to their last digit.  Beyond +-200 it is infinite or zero
 __device__ __forceinline__ float gated(float z, float u, int gate) {
-    const float t = gate == HR_GATE_SILU ? z : 1.5957691216057308f * fmaf(0.044715f * z * z, z, z);
-    return z / (1.0f + expf(-t)) * u;
+    float t = gate == HR_GATE_SILU ? z : 1.5957691216057308f * fmaf(0.044715f * z * z, z, z);
+    t = fminf(fmaxf(t, -200.0f), 200.0f);
+    const float x = -1.44269504088896341f * t, rest = fmaf(-1.44269504088896341f, t, -x) - 1.9259629911e-8f * t;
+    const float power = __builtin_amdgcn_exp2f(x);
+    return z * __builtin_amdgcn_rcpf(1.0f + (power < __builtin_inff() ? fmaf(power, 0.69314718f * rest, power) : power)) * u;
 }
 
 // Values n .. n + 3 of y's row m, from c and, with a gate, from what it multiplies
@@ -93,7 +97,9 @@ __device__ __forceinline__ void store_block4(const MatmulArgs& a, int64_t m, int
     if (n % kBlockCols == 0) a.scales[m * a.scale_stride + n / kBlockCols] = scale;
 }
 
-hipError_t launch_block_matmul_few(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st);
-hipError_t launch_block_matmul_tiles(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st);
+hipError_t launch_block_matmul_few(const MatmulArgs& a, int dtype, int shape, hipStream_t st);
+hipError_t launch_block_matmul_bf16(const MatmulArgs& a, int shape, hipStream_t st);
+hipError_t launch_block_matmul_f32(const MatmulArgs& a, int shape, hipStream_t st);
+hipError_t launch_block_matmul_codes(const MatmulArgs& a, int shape, hipStream_t st);
 
 }  // namespace hr

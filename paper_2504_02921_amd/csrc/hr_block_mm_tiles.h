@@ -1,4 +1,6 @@
-// Products of 8-bit matrices with many rows (hr_block_matmul): tiles of both operands through LDS.
+// Products of 8-bit matrices through LDS (hr_block_matmul): the kernel, for the files that compile it.
+#pragma once
+
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -67,6 +69,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
     const rsrc_t ra = make_rsrc(a.a + m0 * a.a_stride, rows_a * a.a_stride);
     // which half of w a pass brings goes by the wavefront (a pass has every wavefront's rows) or by the pass
     constexpr bool BY_WAVE = GATE && RPP % TN == 0;
+    static_assert(!GATE || NI % 2 == 0, "whole blocks of 16 of either half");
     static_assert(!GATE || BY_WAVE || TNY % RPP == 0, "a load lies in one half");
     const int lrow = lane >> 3, lchunk = (lane & 7) ^ ((wave * 8 + lrow) >> 1 & 7);
     const int va = lrow * (int)a.a_stride + lchunk * 16, vw = lrow * (int)a.w_stride + lchunk * 16;
@@ -336,7 +339,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 }
 
 template <int BM, int BN, int WM, int WN, int NS, int KG, bool EIGHT, bool GATE, typename OUT, bool CODES>
-hipError_t launch(const MatmulArgs& a, hipStream_t st) {
+hipError_t launch_tile(const MatmulArgs& a, hipStream_t st) {
     constexpr size_t stages = (size_t)KG * NS * ((BM + BN) * kBlockCols + WM * WN * 256);
     constexpr size_t slab = (size_t)KG * (BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float);
     constexpr size_t lds = stages > slab ? stages : slab;
@@ -352,24 +355,6 @@ hipError_t launch(const MatmulArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int NS, int NSC>
-hipError_t launch_shape(const MatmulArgs& a, int dtype, hipStream_t st) {
-    const bool gate = a.half > 0;
-    if (a.codes) {
-        constexpr int BNC = BN < 256 ? 256 : BN;             // with a gate 128 columns of y take 256 rows of w
-        if (gate) return launch<BM, BNC, BNC == BN ? WM : 2, BNC == BN ? WN : 4, NSC, 1, false, true, float, true>(a, st);
-        if constexpr (BN >= 128) return launch<BM, BN, WM, WN, NS, 1, false, false, float, true>(a, st);
-        else return launch<BM, 128, 2, 4, NSC, 1, false, false, float, true>(a, st);
-    }
-    if (dtype == HR_F32) return gate ? launch<BM, BN, WM, WN, NS, 1, false, true, float, false>(a, st) : launch<BM, BN, WM, WN, NS, 1, false, false, float, false>(a, st);
-    return gate ? launch<BM, BN, WM, WN, NS, 1, true, true, bf16_t, false>(a, st) : launch<BM, BN, WM, WN, NS, 1, true, false, bf16_t, false>(a, st);
-}
-
 }  // namespace
-
-hipError_t launch_block_matmul_tiles(const MatmulArgs& a, int dtype, const MatmulTile& t, hipStream_t st) {
-    if (t.bm == 256) return launch_shape<256, 256, 2, 4, 2, 2>(a, dtype, st);
-    return launch_shape<128, 128, 2, 2, 2, 3>(a, dtype, st);
-}
 
 }  // namespace hr

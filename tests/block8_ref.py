@@ -59,61 +59,78 @@ def norm_slack(channels):
 
 
 def act(z, gate):
-    with np.errstate(over="ignore"):
-        return z / (1.0 + np.exp(-z)) if gate == "silu" else z * (0.5 * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (z + 0.044715 * z ** 3))))
+    import torch
+    return z / (1.0 + torch.exp(-z)) if gate == "silu" else z * (0.5 * (1.0 + torch.tanh((2.0 / np.pi) ** 0.5 * (z + 0.044715 * z ** 3))))
 
 
-def product(a, w, bias=None, gate=None, add=None, eight_bit=False):
-    """a, w: (codes, scales).  (y, bound on what y may be off before it is rounded to its type)."""
-    av = ofp8.e4m3_decode(a[0]) * spread(a[1], *a[0].shape, 1)
-    wv = ofp8.e4m3_decode(w[0]) * spread(w[1], *w[0].shape, BLOCK)
-    c, size = av @ wv.T, np.abs(av) @ np.abs(wv).T
+def values64(codes, scales, block_rows):
+    """What codes (uint8) and scales stand for, on the device that has them."""
+    import torch
+    table = torch.from_numpy(ofp8.e4m3_decode(np.arange(256))).to(codes.device)
+    rows, cols = codes.shape
+    return table[codes.long()] * scales.double().repeat_interleave(block_rows, 0)[:rows].repeat_interleave(BLOCK, 1)[:, :cols]
+
+
+def product(av, wv, bias=None, gate=None, add=None, eight_bit=False):
+    """(av wv^T and what follows, bound on what it may be off before it is rounded to its type): torch's elementary operations in 64 bits."""
+    import torch
+    c, size = av @ wv.t().contiguous(), av.abs() @ wv.t().abs().contiguous()
     K = av.shape[1]
     # a block's 128 products one after another, its scale (2 roundings) and addition, a few sums joined at the end
     off = (min(K, BLOCK) + blocks(K) + 3 + 16) * U32 * size
     if eight_bit:
         # the 8-bit instruction adds eight products (of columns 8 i .. 8 i + 7 of a block) at once, cutting each off at 2^-13 of the largest one's power of two
         for k in range(0, K, 8):
-            top = np.zeros_like(c)
+            top = torch.zeros_like(c)
             for e in range(k, min(k + 8, K)):
-                top = np.maximum(top, np.abs(av[:, e, None] * wv[None, :, e]))
+                top = torch.maximum(top, torch.outer(av[:, e].abs(), wv[:, e].abs()))
             off = off + 7 * 2.0 ** -13 * top
     if bias is not None:
-        c = c + np.asarray(bias, np.float64)
-        off = off + U32 * np.abs(c)
+        c = c + bias.double()
+        off = off + U32 * c.abs()
     if gate is not None:
         f = c.shape[1] // 2
         z, u, dz, du = c[:, :f], c[:, f:], off[:, :f], off[:, f:]
         # act's slope is below 1.13; computed, act is off by 8 roundings of z at most (its exponential by its argument's, which weighs less the
         # smaller act is)
         a0 = act(z, gate)
-        da = 1.13 * dz + 8 * U32 * np.abs(z)
-        c, off = a0 * u, da * (np.abs(u) + du) + np.abs(a0) * du + 2 * U32 * np.abs(a0 * u)
+        da = 1.13 * dz + 8 * U32 * z.abs()
+        c, off = a0 * u, da * (u.abs() + du) + a0.abs() * du + 2 * U32 * (a0 * u).abs()
     if add is not None:
-        c = c + np.asarray(add, np.float64)
-        off = off + U32 * np.abs(c)
+        c = c + add.double()
+        off = off + U32 * c.abs()
     return c, off
 
 
 def check_rounded(got, want, off, unit, what=""):
-    bound = off + unit * (np.abs(want) + off)
-    bad = ~(np.abs(got - want) <= bound)
-    bad &= ~(np.isnan(got) & np.isnan(want))
-    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size}, worst error / bound {np.max(np.where(bad, np.abs(got - want) / np.maximum(bound, 1e-300), 0)):.3g} at {np.argwhere(bad)[0]}"
+    """got, want, off: tensors or arrays; got is want to within off, rounded once."""
+    got, want, off = (torch_of(x) for x in (got, want, off))
+    bound = off + unit * (want.abs() + off)
+    err = (got - want).abs()
+    bad = ~(err <= bound) & ~(got.isnan() & want.isnan())
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()}, worst error / bound {float((err / bound.clamp(min=1e-300))[bad].max()):.3g} at {bad.nonzero()[0].tolist()}"
+
+
+def torch_of(x):
+    import torch
+    return torch.from_numpy(np.asarray(x, np.float64)) if not hasattr(x, "data_ptr") else x.double()
 
 
 def check_codes(codes, scales, want, off, what=""):
-    """Codes and scales of values that are `want` to within `off`."""
-    codes, scales = np.asarray(codes), np.asarray(scales, np.float64)
+    """Codes (uint8) and scales of values that are `want` to within `off`."""
+    import torch
+    scales, want, off = (torch_of(x) for x in (scales, want, off))
     rows, cols = want.shape
-    top, far = tops(want, 1), tops(off, 1)
-    low = np.where(top == 0, 1.0, np.maximum(top / TOP, 2.0 ** -126))
+    pad = lambda x: torch.nn.functional.pad(x, (0, -cols % BLOCK)).view(rows, -1, BLOCK)      # noqa: E731
+    top, far = pad(torch.where(want.isfinite(), want.abs(), 0.0)).amax(2), pad(torch.where(off.isfinite(), off, 0.0)).amax(2)
+    low = torch.where(top == 0, 1.0, (top / TOP).clamp(min=2.0 ** -126))
     exact_one = (top == 0) & (far == 0)
-    assert np.all(scales[exact_one] == 1.0), what
-    ok = np.abs(scales - low) <= far / TOP + 2 * U32 * low + 2.0 ** -149
-    assert np.all(ok | exact_one), f"{what}: scales off by {np.max(np.abs(scales - low) / low):.3g}"
-    value = ofp8.e4m3_decode(codes) * spread(scales, rows, cols, 1)
+    assert (scales[exact_one] == 1.0).all(), what
+    ok = (scales - low).abs() <= far / TOP + 2 * U32 * low + 2.0 ** -149
+    assert (ok | exact_one).all(), f"{what}: scales off by {float(((scales - low).abs() / low).max()):.3g}"
+    every = scales.repeat_interleave(BLOCK, 1)[:, :cols]
+    value = values64(codes, scales, 1)
     # a code is off by half a step, of the smallest codes' 2^-9 at least; the fp32 factor and product by two roundings
-    bound = off + U8 * (np.abs(want) + off) * (1 + 4 * U32) + 4 * U32 * np.abs(want) + 2.0 ** -10 * spread(scales, rows, cols, 1)
-    bad = ~(np.abs(value - want) <= bound)
-    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} codes, worst {np.max(np.abs(value - want) / np.maximum(bound, 1e-300)):.3g} at {np.argwhere(bad)[0]}"
+    bound = off + U8 * (want.abs() + off) * (1 + 4 * U32) + 4 * U32 * want.abs() + 2.0 ** -10 * every
+    bad = ~((value - want).abs() <= bound) & ~(value.isnan() & ~want.isfinite())
+    assert not bad.any(), f"{what}: {int(bad.sum())} of {bad.numel()} codes, worst {float(((value - want).abs() / bound)[bad].max()):.3g} at {bad.nonzero()[0].tolist()}"

@@ -1,10 +1,18 @@
 """The operators of a layer's projections in 8 bits on a machine without a GPU: every refusal that the host makes before anything is enqueued."""
 
 import ctypes as C
+import math
+import os
+import random
+import shutil
+import subprocess
 
 import pytest
 
+from block8_shapes import SHAPES
 from paper_2504_02921_amd import binding as hb
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 FAKE = 0x7F0000000000      # never dereferenced on the host
 BAD, LONG, MISMATCH = hb.HR_ERR_INVALID_ARG, hb.HR_ERR_LEN_RANGE, hb.HR_ERR_MISMATCH
@@ -105,3 +113,28 @@ def test_matrices_on_the_host_are_refused_before_the_device_is_asked(what):
         hb.Block8(*((q.codes[:, :32], torch.zeros((4, 2))) if what == "codes" else (q.codes, q.scales.double())))
     with pytest.raises(hb.HrError):
         hb.Block8.empty(1 << 31, 64, device="cpu")
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_every_shape_of_tile_that_a_product_takes_is_tested(tmp_path):
+    """The host's choice of tiles, with AddressSanitizer + UBSan: for sizes of all kinds it ends, and what it takes is among what the GPU tests run."""
+    exe, csrc = str(tmp_path / "shapes"), os.path.join(ROOT, "paper_2504_02921_amd", "csrc")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-I" + os.path.join(ROOT, "include"), "-I" + csrc,
+                        os.path.join(ROOT, "tests", "block8_shapes_driver.cpp"), os.path.join(csrc, "hr_block8_host.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    rng = random.Random(1)
+    size = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi))))      # noqa: E731
+    drawn = [(kind, gate, size(1, 60000), max(size(16, 60000) // 256 * 256, 256) if gate else size(16, 60000), size(32, 32768))
+             for kind in ("bf16", "f32", "block8") for gate in (0, 1) for _ in range(3000)]
+    drawn += [(kind, gate, m, n, k) for kind in ("bf16", "f32", "block8") for gate in (0, 1) for m in (1, 1 << 30) for n in (256, (1 << 30) - 256) for k in (1, 1 << 22)]
+    env = dict(os.environ)
+    env.pop("LD_PRELOAD", None)          # the sanitizer runtime must come first in the link order
+    lines = "".join(f"{int(kind == 'block8')} {int(kind != 'bf16')} {gate} {m} {n} {k}\n" for kind, gate, m, n, k in drawn + SHAPES)
+    r = subprocess.run([exe], input=lines, capture_output=True, text=True, env=env)
+    assert r.returncode == 0, (r.stdout + r.stderr)[-2000:]
+    plans = [tuple(int(x) for x in line.split()) for line in r.stdout.splitlines()]
+    assert len(plans) == len(drawn) + len(SHAPES)
+    taken = {(d[0], d[1], p[0]) for d, p in zip(drawn, plans)}
+    tested = {(d[0], d[1], p[0]) for d, p in zip(SHAPES, plans[len(drawn):])}
+    assert taken <= tested, sorted(taken - tested)
+    assert {d[0] for d, p in zip(SHAPES, plans[len(drawn):]) if p[1] >= 0} == {"bf16", "block8"}

@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 import block8_ref as R
+from block8_shapes import SHAPES
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -33,7 +34,7 @@ def to64(t):
 
 
 def code_bytes(t):
-    return t.contiguous().view(torch().uint8).cpu().numpy()
+    return t.contiguous().view(torch().uint8)
 
 
 def gen(seed):
@@ -54,7 +55,7 @@ def check_norm(x, gain, add, eps, offset, out, total, block8, kind):
     if out is not None:
         R.check_rounded(to64(out), y, off, unit(kind), "out")
     if block8 is not None:
-        R.check_codes(code_bytes(block8.codes), to64(block8.scales), y, off, "codes")
+        R.check_codes(code_bytes(block8.codes).cpu(), to64(block8.scales), y, off, "codes")
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
@@ -147,7 +148,7 @@ def test_codes_are_the_definitions(kind, block_rows, rows, cols):
     q = hb().block_quantize(x, block_rows=block_rows)
     codes, scales = R.quantize(x.float().cpu().numpy(), block_rows)
     np.testing.assert_array_equal(q.scales.cpu().numpy(), scales)
-    got = code_bytes(q.codes)
+    got = code_bytes(q.codes).cpu().numpy()
     np.testing.assert_array_equal(np.where(got == 0x80, 0, got), np.where(codes == 0x80, 0, codes))
 
 
@@ -186,69 +187,65 @@ def test_codes_into_a_matrix_in_hand_and_of_views():
 
 # ---- product ------------------------------------------------------------------------------------------------------------
 def matrix(rows, cols, block_rows, seed, pad=0x7F):
-    """Codes of normal deviates under scales of many sizes, in rows whose padding holds codes that are NaN; and the same on the host."""
+    """Codes of normal deviates under scales of many sizes, in rows whose padding holds codes that are NaN."""
     T = torch()
-    rng = np.random.default_rng([rows, cols, seed])
-    codes = R.ofp8.e4m3_encode(rng.standard_normal((rows, cols)) * 60.0)
-    scales = np.exp(rng.standard_normal((R.blocks_of_rows(rows, block_rows), R.blocks(cols)))).astype(np.float32)
+    g = T.Generator(DEV).manual_seed(1000 * seed + rows + cols)
     held = T.full((rows, R.blocks(cols) * 128 + 16), pad, dtype=T.uint8, device=DEV)
-    held[:, :cols] = T.from_numpy(codes).to(DEV)
-    return hb().Block8(held[:, :cols], T.from_numpy(scales).to(DEV), block_rows), (codes, scales)
-
-
-def eight_bit(m, kind):
-    """Whether the 8-bit instruction may take part: many rows and 16-bit results."""
-    return kind == "bf16"
+    held[:, :cols] = (T.randn((rows, cols), generator=g, device=DEV) * 60.0).to(T.float8_e4m3fn).view(T.uint8)
+    return hb().Block8(held[:, :cols], T.randn((R.blocks_of_rows(rows, block_rows), R.blocks(cols)), generator=g, device=DEV).exp(), block_rows)
 
 
 def check_product(a, w, y, kind, bias=None, gate=None, add=None):
-    want, off = R.product(a, w, None if bias is None else to64(bias), gate, None if add is None else to64(add), eight_bit(a[0].shape[0], kind))
+    want, off = R.product(*(R.values64(x.codes.view(torch().uint8), x.scales, x.block_rows) for x in (a, w)), bias, gate, add, eight_bit=kind == "bf16")
     if kind == "block8":
-        R.check_codes(code_bytes(y.codes), to64(y.scales), want, off, "product")
+        R.check_codes(code_bytes(y.codes), y.scales, want, off, "product")
     else:
-        R.check_rounded(to64(y), want, off, unit(kind), "product")
+        R.check_rounded(y, want, off, unit(kind), "product")
 
 
-SHAPES = [(2100, 1100, 140), (2048, 1024, 256), (2049, 1025, 127), (1, 16, 32), (1, 1, 1), (2, 3, 5), (1, 200, 128), (16, 32, 256), (17, 33, 129), (5, 130, 1000), (33, 96, 300), (64, 128, 130), (65, 100, 896), (70, 257, 2500), (130, 300, 640),
-          (129, 128, 127), (300, 384, 400), (257, 513, 384), (200, 64, 4864), (1, 640, 4100)]
+def run_and_check(kind, m, n, k, gate=None, seed=20):
+    """Without and with what may follow the product."""
+    a, w = matrix(m, k, 1, seed), matrix(n, k, 128, seed + 1)
+    if gate:
+        a.scales.mul_(0.1 / k ** 0.5)                                    # a gate's interesting arguments
+    wide = n // 2 if gate else n
+    bias = draw((n,), 22, "f32", 2.0 if gate else 100.0)
+    if kind == "block8":
+        check_product(a, w, hb().block_matmul(a, w, gate=gate, block8=True), kind, None, gate)
+        return check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, block8=True), kind, bias, gate)
+    check_product(a, w, hb().block_matmul(a, w, dtype=tdt(kind), gate=gate), kind, None, gate)
+    add = draw((m, wide), 23, kind, 2.0 if gate else 100.0)
+    check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, add=add), kind, bias, gate, add)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "block8"])
-@pytest.mark.parametrize("m,n,k", SHAPES)
+@pytest.mark.parametrize("m,n,k", [(1, 16, 32), (1, 1, 1), (2, 3, 5), (1, 200, 128), (16, 32, 256), (17, 33, 129), (5, 130, 1000), (33, 96, 300), (64, 128, 130), (65, 100, 896),
+                                   (70, 257, 2500), (130, 300, 640), (129, 128, 127), (300, 384, 400), (257, 513, 384), (200, 64, 4864), (1, 640, 4100), (700, 1000, 1030)])
 def test_product_is_the_sum_over_blocks(kind, m, n, k):
-    (a, a_host), (w, w_host) = matrix(m, k, 1, 20), matrix(n, k, 128, 21)
-    if kind == "block8":
-        check_product(a_host, w_host, hb().block_matmul(a, w, block8=True), kind)
-        bias = draw((n,), 22, "f32", 100.0)
-        return check_product(a_host, w_host, hb().block_matmul(a, w, bias=bias, block8=True), kind, bias)
-    check_product(a_host, w_host, hb().block_matmul(a, w, dtype=tdt(kind)), kind)
-    bias, add = draw((n,), 22, "f32", 100.0), draw((m, n), 23, kind, 100.0)
-    check_product(a_host, w_host, hb().block_matmul(a, w, bias=bias, add=add), kind, bias, None, add)
+    run_and_check(kind, m, n, k)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "block8"])
 @pytest.mark.parametrize("gate", ["silu", "gelu"])
 @pytest.mark.parametrize("m,n,k", [(1, 256, 128), (3, 512, 100), (20, 256, 1000), (40, 768, 256), (65, 512, 640), (140, 256, 300), (300, 768, 500)])
 def test_gated_product(kind, gate, m, n, k):
-    (a, a_host), (w, w_host) = matrix(m, k, 1, 24), matrix(n, k, 128, 25)
-    a.scales.mul_(0.005)                                                 # a gate's interesting arguments
-    a_host = (a_host[0], a.scales.cpu().numpy())
-    bias = draw((n,), 26, "f32", 2.0)
-    if kind == "block8":
-        return check_product(a_host, w_host, hb().block_matmul(a, w, gate=gate, bias=bias, block8=True), kind, bias, gate)
-    add = draw((m, n // 2), 27, kind)
-    check_product(a_host, w_host, hb().block_matmul(a, w, gate=gate, bias=bias, add=add), kind, bias, gate, add)
-    check_product(a_host, w_host, hb().block_matmul(a, w, dtype=tdt(kind), gate=gate), kind, None, gate)
+    run_and_check(kind, m, n, k, gate)
+
+
+@pytest.mark.parametrize("kind,gated,m,n,k", SHAPES)
+def test_product_of_every_shape_of_tile(kind, gated, m, n, k):
+    run_and_check(kind, m, n, k, "silu" if gated else None)
+    run_and_check(kind, m, n, k - k % 128, "gelu" if gated else None, 25)
 
 
 @pytest.mark.parametrize("m", [3, 40, 300])
 def test_product_onto_the_stream_and_into_views(m):
     T = torch()
-    (a, a_host), (w, w_host) = matrix(m, 500, 1, 28), matrix(200, 500, 128, 29)
+    a, w = matrix(m, 500, 1, 28), matrix(200, 500, 128, 29)
     stream = draw((2 * m, 211), 30, "bf16", 50.0)
     before, x = stream.clone(), stream[::2, 3:203]
     y = hb().block_matmul(a, w, add=x)
-    check_product(a_host, w_host, y, "bf16", None, None, before[::2, 3:203])
+    check_product(a, w, y, "bf16", None, None, before[::2, 3:203])
     assert hb().block_matmul(a, w, add=x, out=x) is x and T.equal(x, y)
     stream[::2, 3:203] = before[::2, 3:203]
     assert T.equal(stream, before)                                       # nothing but those rows and columns
@@ -258,7 +255,7 @@ def test_product_onto_the_stream_and_into_views(m):
 def test_a_code_that_is_nan_stays_in_its_row_or_column(kind):
     T = torch()
     for m in (5, 200):
-        (a, _), (w, _) = matrix(m, 300, 1, 31), matrix(384, 300, 128, 32)
+        a, w = matrix(m, 300, 1, 31), matrix(384, 300, 128, 32)
         run = (lambda: hb().block_matmul(a, w, block8=True).codes.float()) if kind == "block8" else (lambda: hb().block_matmul(a, w, dtype=tdt(kind)).float())
         clean = run()
         assert not clean.isnan().any()
@@ -276,7 +273,7 @@ def test_a_code_that_is_nan_stays_in_its_row_or_column(kind):
 
 def test_product_of_nothing():
     T, H = torch(), hb()
-    (a, _), (w, _) = matrix(4, 64, 1, 33), matrix(256, 64, 128, 34)
+    a, w = matrix(4, 64, 1, 33), matrix(256, 64, 128, 34)
     empty_a, empty_w = H.Block8.empty(0, 64), H.Block8.empty(0, 64, 128)
     assert H.block_matmul(empty_a, w).shape == (0, 256) and H.block_matmul(a, empty_w).shape == (4, 0)
     assert H.block_matmul(empty_a, w, gate="silu", block8=True).shape == (0, 128)
@@ -322,11 +319,10 @@ def test_a_feed_forward_layer_step_by_step_and_recorded(m):
         H.block_matmul(h, down, add=total, out=out)
         H.rms_norm(out, gain, out=last)
 
-    host = lambda b: (code_bytes(b.codes), b.scales.cpu().numpy())      # noqa: E731
     layer()
     check_norm(x, gain, add, 1e-6, 0.0, None, total, q, "bf16")
-    check_product(host(q), host(up), h, "block8", None, "silu")
-    check_product(host(h), host(down), out, "bf16", None, None, total)
+    check_product(q, up, h, "block8", None, "silu")
+    check_product(h, down, out, "bf16", None, None, total)
     check_norm(out, gain, None, 1e-6, 0.0, last, None, None, "bf16")
     graph = T.cuda.CUDAGraph()
     side = T.cuda.Stream()
