@@ -689,15 +689,23 @@ class Block8:
     def empty(cls, rows: int, cols: int, block_rows: int = 1, device="cuda:0", stream=None) -> "Block8":
         """One with room for rows x cols, unset.  stream: the one that will write it (None: the current one)."""
         import torch
-        if stream is not None:
-            with torch.cuda.stream(stream):
-                return cls.empty(rows, cols, block_rows, device)
         rows, cols = _int32(rows, "Block8: rows"), _int32(cols, "Block8: cols")
         if block_rows not in (1, BLOCK_COLS) or cols < 1:
             _refuse(f"Block8: block_rows 1 or {BLOCK_COLS} and columns, got {block_rows} and {cols}")
-        codes = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.float8_e4m3fn, device=device)
-        scales = torch.empty((-(-rows // block_rows), -(-cols // BLOCK_COLS)), dtype=torch.float32, device=device)
-        return cls(codes if cols % 16 == 0 else codes[:, :cols], scales, block_rows)
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return cls.empty(rows, cols, block_rows, device)
+        return cls._made(torch.empty, rows, cols, block_rows, device)
+
+    @classmethod
+    def _made(cls, new, rows: int, cols: int, block_rows: int, device) -> "Block8":
+        import torch
+        pitch, shape = -(-cols // 16) * 16, (-(-rows // block_rows), -(-cols // BLOCK_COLS))
+        codes, scales = new((rows, pitch), dtype=torch.float8_e4m3fn, device=device), new(shape, dtype=torch.float32, device=device)
+        self = cls.__new__(cls)              # nothing that __init__ would find wrong
+        self.c = hr_block8(codes.data_ptr(), scales.data_ptr(), rows, cols, block_rows, pitch, shape[1])
+        self.codes, self.scales, self.block_rows, self.shape, self.device = codes if pitch == cols else codes[:, :cols], scales, block_rows, (rows, cols), scales.device
+        return self
 
 
 def _rows_of(t, shape, like, what: str):
@@ -715,12 +723,12 @@ def _floats(t, n: int, device, what: str):
     return t.data_ptr()
 
 
-def _block8_for(given, rows: int, cols: int, device, stream, what: str) -> Block8:
-    """The matrix that a call writes: one of the caller's, or (True) a new one."""
+def _block8_for(given, rows: int, cols: int, like, stream, what: str) -> Block8:
+    """The matrix that a call writes: one of the caller's, or (True) a new one on the device of `like`."""
     if given is True:
-        return Block8.empty(rows, cols, 1, device, stream)
-    if not isinstance(given, Block8) or given.block_rows != 1 or given.shape != (rows, cols) or given.device != device:
-        _refuse(f"{what}: block8: True or a Block8 of ({rows}, {cols}) with block_rows 1 on {device} expected")
+        return Block8.empty(rows, cols, 1, like.device, stream) if stream is not None else Block8._made(like.new_empty, rows, cols, 1, None)
+    if not isinstance(given, Block8) or given.block_rows != 1 or given.shape != (rows, cols) or given.device != like.device:
+        _refuse(f"{what}: block8: True or a Block8 of ({rows}, {cols}) with block_rows 1 on {like.device} expected")
     return given
 
 
@@ -739,7 +747,10 @@ def rms_norm(x, gain=None, add=None, eps: float = 1e-6, gain_offset: float = 0.0
             return rms_norm(x, gain, add, eps, gain_offset, out, total, block8, stream)
     T, C_ = shape[0], shape[-1]
     heads = shape[1] if len(shape) == 3 else 1
-    out, total = (_new(x, stream) if t is True else None if t is False else t for t in (out, total))
+    if heads < 1 or C_ < 1:
+        _refuse(f"rms_norm: heads and channels, got {tuple(shape)}")
+    out = _new(x, stream) if out is True else None if out is False else out
+    total = _new(x, stream) if total is True else None if total is False else total
     _no_gradients((x, gain, add, out, total), "rms_norm")
     x_t, x_h = _rows_of(x, shape, x, "rms_norm: x")
     a_t, a_h = (0, 0) if add is None else _rows_of(add, shape, x, "rms_norm: add")
@@ -747,14 +758,14 @@ def rms_norm(x, gain=None, add=None, eps: float = 1e-6, gain_offset: float = 0.0
     o_t, o_h = (0, 0) if out is None else _rows_of(out, shape, x, "rms_norm: out")
     g_p = None if gain is None else _floats(gain, C_, dev, "rms_norm: gain")
     if block8 is not None and block8 is not False:
-        if len(shape) != 2 or C_ < 1:
+        if len(shape) != 2:
             _refuse("rms_norm: codes are made of [tokens][channels]")
-        block8 = _block8_for(block8, T, C_, dev, stream, "rms_norm")
+        block8 = _block8_for(block8, T, C_, x, stream, "rms_norm")
     else:
         block8 = None
-    if heads < 1 or C_ < 1:
-        _refuse(f"rms_norm: heads and channels, got {tuple(shape)}")
-    args = hr_norm_args(code, _int32(heads, "rms_norm: heads"), _int32(C_, "rms_norm: channels"), eps, gain_offset, T, x.data_ptr(), None if add is None else add.data_ptr(),
+    if heads >= 1 << 31 or C_ >= 1 << 31:
+        _refuse(f"rms_norm: heads and channels below 2^31, got {tuple(shape)}")
+    args = hr_norm_args(code, heads, C_, eps, gain_offset, T, x.data_ptr(), None if add is None else add.data_ptr(),
                         None if total is None else total.data_ptr(), None if out is None else out.data_ptr(), g_p,
                         None if block8 is None else C.pointer(block8.c), x_t, x_h, a_t, a_h, s_t, s_h, o_t, o_h)
     check(lib.hr_rms_norm(C.byref(args), _stream_ptr(stream)), "hr_rms_norm")
@@ -776,7 +787,9 @@ def block_quantize(x, block_rows: int = 1, out: Optional[Block8] = None, stream=
     _no_gradients((x,), "block_quantize")
     x_t, _ = _rows_of(x, x.shape, x, "block_quantize: x")
     if out is None:
-        out = Block8.empty(*x.shape, block_rows, dev, stream)
+        if block_rows not in (1, BLOCK_COLS):
+            _refuse(f"block_quantize: block_rows 1 or {BLOCK_COLS}, got {block_rows}")
+        out = Block8.empty(*x.shape, block_rows, dev, stream) if stream is not None else Block8._made(x.new_empty, *x.shape, block_rows, None)
     elif not isinstance(out, Block8) or out.block_rows != block_rows or out.shape != tuple(x.shape) or out.device != dev:
         _refuse(f"block_quantize: out: a Block8 of {tuple(x.shape)} with block_rows {block_rows} on {dev} expected")
     check(lib.hr_block_quantize(code, x.data_ptr(), x_t, C.byref(out.c), _stream_ptr(stream)), "hr_block_quantize")
@@ -807,7 +820,7 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
     if block8 is not None and block8 is not False:
         if out is not None or add is not None or N < 1:
             _refuse("block_matmul: codes instead of out, of at least one column, with nothing added")
-        block8 = _block8_for(block8, M, N, dev, stream, "block_matmul")
+        block8 = _block8_for(block8, M, N, a.scales, stream, "block_matmul")
         args = hr_matmul_args(HR_F32, GATES[gate], b_p, None, None, 0, 0, C.pointer(block8.c))
     else:
         block8 = None
@@ -817,7 +830,7 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
         if code is None:
             _refuse(f"block_matmul: float32 or bfloat16, got {dtype}")
         if out is None:
-            out = _new(a.codes, stream, (M, N), dtype)
+            out = a.scales.new_empty((M, N), dtype=dtype) if stream is None else _new(a.scales, stream, (M, N), dtype)
         shape = torch.Size((M, N))
         if out.dtype != dtype or out.device != dev:
             _refuse(f"block_matmul: out: {dtype} on {dev} expected, got {out.dtype} on {out.device}")

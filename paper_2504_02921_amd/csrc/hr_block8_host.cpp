@@ -44,18 +44,14 @@ int block8_check(const hr_block8* b, int block_rows) {
 }
 
 NormShape norm_shape(int channels, int64_t rows) {
-    NormShape s{256, 0};
-    auto fits = [&](int lanes, int most) {
-        const int chunks = (channels + lanes * 8 - 1) / (lanes * 8);
-        if (chunks > most) return false;
-        s.lanes = lanes;
-        s.chunks = chunks <= 1 ? 1 : chunks <= 2 ? 2 : chunks <= 4 ? 4 : 8;
-        return true;
-    };
-    if (fits(16, 1) || fits(32, 1)) return s;
-    if (rows >= 1024 ? fits(64, 8) : fits(64, 1)) return s;
-    if (fits(256, 8)) return s;
-    return s;
+    if (channels <= 128) return {16, 1};
+    if (channels <= 256) return {32, 1};
+    if (channels <= 512) return {64, 1};
+    if (channels <= 1024 && rows >= 1024) return {64, 2};
+    if (channels <= 2048) return {256, 1};
+    if (channels <= 4096) return {256, 2};
+    if (channels <= 8192) return {512, 2};
+    return {1024, channels <= 16384 ? 2 : 0};
 }
 
 int norm_check(const hr_norm_args* a) {

@@ -15,7 +15,7 @@ namespace hr {
 namespace {
 
 constexpr int kVec = 8;                      // channels of a lane: 16 lanes have a block of 128
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWideThreads = 1024;
 constexpr int kBlockLanes = kBlockCols / kVec;
 constexpr int64_t kMostGroups = 1 << 20;     // workgroups of a launch; more rows are walked
 
@@ -101,9 +101,9 @@ __device__ __forceinline__ float root_of(float squares, const NormArgs& a) {
 
 // LANES lanes have a head, CHUNKS times 8 channels each
 template <typename T, int LANES, int CHUNKS>
-__global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
-    constexpr int UNITS = kThreads / LANES;
-    __shared__ float part[2][kThreads / 64];
+__global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kernel(NormArgs a) {
+    constexpr int UNITS = LANES > kThreads ? 1 : kThreads / LANES, WAVES = LANES / 64;
+    __shared__ float part[2][LANES > 64 ? WAVES : 1];
     const int lane = threadIdx.x % LANES, unit = threadIdx.x / LANES;
     int turn = 0;
     for (int64_t first = (int64_t)blockIdx.x * UNITS; first < a.rows; first += (int64_t)gridDim.x * UNITS) {
@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
                 __syncthreads();                    // one a turn: the other half of `part` is written next
                 sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < kThreads / 64; ++w) sum += part[turn][w];
+                for (int w = 0; w < WAVES; ++w) sum += part[turn][w];
                 turn ^= 1;
             }
         }
@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(NormArgs a) {
 
 // Heads of more channels than registers are kept for: read once for the sum and once more, mostly from a cache
 template <typename T>
-__global__ void __launch_bounds__(kThreads) norm_wide_kernel(NormArgs a) {
-    __shared__ float part[2][kThreads / 64];
+__global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
+    __shared__ float part[2][kWideThreads / 64];
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const int64_t token = row / a.heads;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kThreads) norm_wide_kernel(NormArgs a) {
             for (int e = 0; e < kVec; ++e) s[e] += more[e];
         };
         float s[kVec], sum = 0.0f;
-        for (int c = threadIdx.x * kVec; c < a.channels; c += kThreads * kVec) {
+        for (int c = threadIdx.x * kVec; c < a.channels; c += kWideThreads * kVec) {
             load(c, s);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) sum = fmaf(s[e], s[e], sum);
@@ -177,37 +177,36 @@ __global__ void __launch_bounds__(kThreads) norm_wide_kernel(NormArgs a) {
         __syncthreads();
         sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kThreads / 64; ++w) sum += part[turn][w];
+        for (int w = 0; w < kWideThreads / 64; ++w) sum += part[turn][w];
         turn ^= 1;
         const float r = root_of(sum, a);
         const int64_t padded = blocks_of(a.channels) * kBlockCols;        // whole groups of lanes look for a block's largest
-        for (int c = threadIdx.x * kVec; c < padded; c += kThreads * kVec) {
+        for (int c = threadIdx.x * kVec; c < padded; c += kWideThreads * kVec) {
             load(c, s);
             finish8<T>(a, token, head, c, true, s, r);
         }
     }
 }
 
-template <typename T, int LANES>
-void norm_chunks(int chunks, unsigned groups, const NormArgs& a, hipStream_t st) {
-    switch (chunks) {
-        case 1: norm_kernel<T, LANES, 1><<<groups, kThreads, 0, st>>>(a); break;
-        case 2: if constexpr (LANES >= 64) norm_kernel<T, LANES, 2><<<groups, kThreads, 0, st>>>(a); break;
-        case 4: if constexpr (LANES >= 64) norm_kernel<T, LANES, 4><<<groups, kThreads, 0, st>>>(a); break;
-        default: if constexpr (LANES >= 64) norm_kernel<T, LANES, 8><<<groups, kThreads, 0, st>>>(a);
-    }
+template <typename T, int LANES, int CHUNKS>
+void norm_go(const NormArgs& a, hipStream_t st) {
+    constexpr int64_t units = LANES > kThreads ? 1 : kThreads / LANES;
+    norm_kernel<T, LANES, CHUNKS><<<(unsigned)std::min((a.rows + units - 1) / units, kMostGroups), LANES > kThreads ? LANES : kThreads, 0, st>>>(a);
 }
 
 template <typename T>
 void norm_launch(const NormArgs& a, hipStream_t st) {
     const NormShape s = norm_shape(a.channels, a.rows);
-    const int64_t units = kThreads / s.lanes;
-    const unsigned groups = (unsigned)std::min((a.rows + units - 1) / units, kMostGroups);
-    if (s.chunks == 0) norm_wide_kernel<T><<<groups, kThreads, 0, st>>>(a);
-    else if (s.lanes == 16) norm_chunks<T, 16>(s.chunks, groups, a, st);
-    else if (s.lanes == 32) norm_chunks<T, 32>(s.chunks, groups, a, st);
-    else if (s.lanes == 64) norm_chunks<T, 64>(s.chunks, groups, a, st);
-    else norm_chunks<T, 256>(s.chunks, groups, a, st);
+    switch (s.lanes) {
+        case 16: norm_go<T, 16, 1>(a, st); break;
+        case 32: norm_go<T, 32, 1>(a, st); break;
+        case 64: s.chunks == 1 ? norm_go<T, 64, 1>(a, st) : norm_go<T, 64, 2>(a, st); break;
+        case 256: s.chunks == 1 ? norm_go<T, 256, 1>(a, st) : norm_go<T, 256, 2>(a, st); break;
+        case 512: norm_go<T, 512, 2>(a, st); break;
+        default:
+            if (s.chunks) norm_go<T, 1024, 2>(a, st);
+            else norm_wide_kernel<T><<<(unsigned)std::min(a.rows, kMostGroups), kWideThreads, 0, st>>>(a);
+    }
 }
 
 struct QuantizeArgs {

@@ -52,10 +52,10 @@ def norm(x, add, gain, eps, offset):
 
 
 def norm_slack(channels):
-    """How far y may be off, relative to it, before it is rounded to its type: s is off by one rounding (and its square by two); a lane adds at most
-    8 ceil(channels / 2048) + 64 squares one after another, and ten more additions join the lanes; the mean, eps, the root (2 of its steps), 1 / root (half of
+    """How far y may be off, relative to it, before it is rounded to its type: s is off by one rounding (and its square by two); a lane adds 16 squares one
+    after another, or 8 ceil(channels / 8192) of more than 16384 channels, and 6 + 16 more additions join the lanes; the mean, eps, the root (2 of its steps), 1 / root (half of
     what the sum is off), gain + offset and the two products.  In 64 bits gain + offset is exact, in 32 off by a rounding of the sum."""
-    return ((8 * -(-channels // 2048) + 64 + 10 + 2 + 2) / 2 + 2 + 4) * U32
+    return ((max(16, 8 * -(-channels // 8192)) + 22 + 2 + 2) / 2 + 2 + 4) * U32
 
 
 def act(z, gate):
