@@ -173,27 +173,29 @@ MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_a
 
 namespace {
 
-// What a shape's launch takes in us, by its first round of tiles (one a CU) and by each further one: start + turns * first + rounds * turns * more, a
-// turn being `group` blocks of k.  [0]: 8-bit instruction, [1]: halves; of the kernels without LDS, at 16 rows.  Fitted to products of 896 x 896
-// to 28672 x 4096 and 4096 x 14336 columns x k with 1 to 6000 rows, weights from memory.
-struct Cost { int bm, bn, group; float start[2], first[2], more[2]; };
+// What a shape's launch takes in us: start + turns * first with a tile a CU at most, turns being its blocks of k by its groups along k; where a CU holds
+// two workgroups, start + turns * pair with up to two; and turns * more + again for each further round of as many (the last of two may be half a round).
+// By results: bf16, fp32, codes without and with a gate.  Fitted to 3643 launches of 1 to 6000 rows with weights of 896 x 896 to 28672 x 4096 and
+// 4096 x 14336, operands from memory: what it picks takes 0.6 % more than the fastest shape on average, 21 % at most.  The kernels without LDS: at 16 rows.
+struct Times { float start, first, pair, more, again; };
+struct Cost { int bm, bn, groups, held; Times t[4]; };
 constexpr Cost kCost[MM_SHAPES] = {
-    {16, 16, 8, {2.3f, 2.3f}, {1.05f, 1.05f}, {1.10f, 1.10f}},      // MM_FEW_16
-    {16, 32, 8, {3.2f, 3.2f}, {1.50f, 1.50f}, {1.60f, 1.60f}},
-    {16, 64, 4, {4.0f, 4.0f}, {0.55f, 0.72f}, {0.55f, 0.72f}},      // MM_16x64_4
-    {32, 64, 2, {3.0f, 2.9f}, {0.36f, 0.53f}, {0.32f, 0.44f}},
-    {64, 64, 1, {3.2f, 4.0f}, {0.31f, 0.49f}, {0.25f, 0.32f}},
-    {64, 64, 2, {3.6f, 4.4f}, {0.47f, 0.74f}, {0.66f, 0.90f}},
-    {64, 128, 1, {5.0f, 4.9f}, {0.49f, 0.72f}, {0.30f, 0.50f}},
-    {64, 128, 2, {4.4f, 4.9f}, {0.79f, 1.18f}, {0.95f, 1.50f}},
-    {64, 256, 1, {4.4f, 5.5f}, {0.71f, 1.16f}, {0.90f, 1.30f}},
-    {128, 128, 1, {6.0f, 8.7f}, {0.69f, 1.17f}, {0.50f, 0.90f}},
-    {128, 256, 1, {4.4f, 8.5f}, {0.94f, 1.64f}, {1.30f, 2.00f}},
-    {256, 256, 1, {4.0f, 9.6f}, {1.60f, 2.84f}, {2.00f, 3.50f}},
-    {16, 128, 4, {4.1f, 4.1f}, {1.00f, 1.00f}, {1.70f, 1.70f}},      // MM_16x128_4
-    {32, 128, 2, {3.6f, 3.6f}, {0.78f, 0.78f}, {0.96f, 0.96f}},
-    {16, 256, 1, {3.8f, 3.8f}, {0.70f, 0.70f}, {0.90f, 0.90f}},
-    {32, 256, 1, {5.0f, 5.0f}, {0.93f, 0.93f}, {0.95f, 0.95f}},
+    {16, 16, 8, 1, {{2.3f, 1.05f, 0.0f, 1.10f, 0.0f}, {2.3f, 1.05f, 0.0f, 1.10f, 0.0f}, {}, {}}},      // MM_FEW_16
+    {16, 32, 8, 1, {{3.2f, 1.50f, 0.0f, 1.60f, 0.0f}, {3.2f, 1.50f, 0.0f, 1.60f, 0.0f}, {}, {}}},
+    {16, 64, 4, 1, {{3.9f, 0.58f, 0.00f, 0.80f, 2.6f}, {3.9f, 0.75f, 0.00f, 0.91f, 2.9f}, {}, {}}},      // MM_16x64_4
+    {32, 64, 2, 2, {{3.1f, 0.35f, 0.74f, 0.59f, 2.3f}, {3.2f, 0.53f, 1.05f, 0.81f, 2.8f}, {}, {}}},      // MM_32x64_2
+    {64, 64, 1, 2, {{3.5f, 0.32f, 0.50f, 0.47f, 2.7f}, {3.6f, 0.48f, 0.79f, 0.68f, 2.7f}, {}, {}}},      // MM_64x64
+    {64, 64, 2, 1, {{3.4f, 0.50f, 0.00f, 0.54f, 2.6f}, {3.4f, 0.78f, 0.00f, 0.77f, 2.8f}, {}, {}}},      // MM_64x64_2
+    {64, 128, 1, 2, {{4.7f, 0.51f, 0.75f, 0.73f, 3.7f}, {5.1f, 0.71f, 1.23f, 1.17f, 3.5f}, {7.7f, 0.72f, 1.23f, 1.15f, 5.0f}, {}}},      // MM_64x128
+    {64, 128, 2, 1, {{4.1f, 0.82f, 0.00f, 0.81f, 3.1f}, {4.5f, 1.23f, 0.00f, 1.24f, 3.1f}, {5.1f, 1.24f, 0.00f, 1.23f, 4.2f}, {}}},      // MM_64x128_2
+    {64, 256, 1, 1, {{4.4f, 0.74f, 0.00f, 0.74f, 3.2f}, {5.3f, 1.17f, 0.00f, 1.21f, 3.4f}, {6.7f, 1.16f, 0.00f, 1.19f, 5.2f}, {6.4f, 1.17f, 0.00f, 1.22f, 4.5f}}},      // MM_64x256
+    {128, 128, 1, 2, {{6.5f, 0.69f, 1.12f, 1.27f, 4.9f}, {9.0f, 1.15f, 1.85f, 2.07f, 5.8f}, {12.5f, 1.14f, 1.86f, 2.04f, 9.9f}, {}}},      // MM_128x128
+    {128, 256, 1, 1, {{6.9f, 0.87f, 0.00f, 1.18f, 4.3f}, {8.8f, 1.64f, 0.00f, 1.91f, 5.2f}, {12.3f, 1.67f, 0.00f, 1.88f, 9.4f}, {10.8f, 1.62f, 0.00f, 1.88f, 8.4f}}},      // MM_128x256
+    {256, 256, 1, 1, {{12.1f, 1.35f, 0.00f, 1.76f, 9.0f}, {12.6f, 2.85f, 0.00f, 3.24f, 9.6f}, {20.4f, 2.83f, 0.00f, 3.21f, 17.6f}, {17.8f, 2.84f, 0.00f, 3.23f, 15.5f}}},      // MM_256x256
+    {16, 128, 4, 1, {{}, {}, {4.0f, 1.12f, 0.00f, 1.25f, 2.8f}, {}}},      // MM_16x128_4
+    {32, 128, 2, 1, {{}, {}, {3.9f, 0.80f, 0.00f, 0.80f, 3.0f}, {}}},      // MM_32x128_2
+    {16, 256, 1, 1, {{}, {}, {}, {3.6f, 0.68f, 0.00f, 0.65f, 3.2f}}},      // MM_16x256
+    {32, 256, 1, 1, {{}, {}, {}, {4.6f, 0.83f, 0.00f, 0.85f, 3.9f}}},      // MM_32x256
 };
 constexpr int kCus = 256;
 
@@ -203,11 +205,12 @@ bool covers(int shape, bool codes, bool gate) {
     return shape > MM_FEW_32 && (gate ? bn >= 2 * kBlockCols : bn == kBlockCols || (bn > kBlockCols && kCost[shape].bm >= 64));
 }
 
-float cost_of(int shape, const MatmulArgs& a, int64_t rows, int mode) {
+float cost_of(int shape, const MatmulArgs& a, int64_t rows, int results) {
     const Cost& c = kCost[shape];
+    const Times& t = c.t[results];
     const int64_t tiles = matmul_tiles(shape, a, rows), rounds = (tiles + kCus - 1) / kCus, blocks = blocks_of(a.K);
-    const float turns = (float)((blocks + c.group - 1) / c.group);
-    float first = c.first[mode], more = c.more[mode];
+    const float turns = (float)((blocks + c.groups - 1) / c.groups), further = std::max((float)(rounds - c.held) / (float)c.held, 0.0f);
+    float first = rounds > 1 && c.held > 1 ? t.pair : t.first, more = t.more;
     if (shape <= MM_FEW_32) {
         if (a.half > 0) {                           // reads two pieces of w
             first *= 1.4f;
@@ -215,7 +218,7 @@ float cost_of(int shape, const MatmulArgs& a, int64_t rows, int mode) {
         }
         first *= 0.6f + 0.025f * (float)std::min<int64_t>(rows, 16);      // lanes without a row read what others read
     }
-    return c.start[mode] + turns * (first + (float)(rounds - 1) * more);
+    return t.start + turns * first + further * (turns * more + t.again);
 }
 
 }  // namespace
@@ -229,12 +232,12 @@ int64_t matmul_tiles(int shape, const MatmulArgs& a, int64_t rows) {
 // The shape that costs least.  Rows that fill whole rounds of the largest tiles may go ahead of the others, which are then tiled for themselves
 MatmulPlan matmul_plan(const MatmulArgs& a, int dtype) {
     const bool codes = a.codes != nullptr, gate = a.half > 0;
-    const int mode = codes || dtype == HR_F32 ? 1 : 0;
+    const int results = codes ? (gate ? 3 : 2) : dtype == HR_F32 ? 1 : 0;
     auto best = [&](int64_t rows, float& cost) {
         int shape = -1;
         for (int s = 0; s < MM_SHAPES; ++s) {
             if (!covers(s, codes, gate)) continue;
-            const float t = cost_of(s, a, rows, mode);
+            const float t = cost_of(s, a, rows, results);
             if (shape < 0 || t < cost) {
                 shape = s;
                 cost = t;
@@ -250,7 +253,7 @@ MatmulPlan matmul_plan(const MatmulArgs& a, int dtype) {
     const int64_t rows = rounds * kCus / columns * large.bm;
     if (rows > 0 && rows < a.M) {
         const int rest = best(a.M - rows, rest_cost);
-        if (rest != MM_256x256 && cost_of(MM_256x256, a, rows, mode) + rest_cost < 0.98f * cost) p = MatmulPlan{MM_256x256, rows, rest};
+        if (rest != MM_256x256 && cost_of(MM_256x256, a, rows, results) + rest_cost < 0.98f * cost) p = MatmulPlan{MM_256x256, rows, rest};
     }
     return p;
 }

@@ -8,6 +8,8 @@
 
 namespace hr {
 
+constexpr int kCus = 256;
+
 typedef __attribute__((ext_vector_type(4))) float mm_f4;
 typedef __attribute__((ext_vector_type(2))) _Float16 mm_h2;
 typedef __attribute__((ext_vector_type(8))) _Float16 mm_h8;
@@ -73,6 +75,79 @@ __device__ __forceinline__ void store4(const MatmulArgs& a, int64_t m, int n, mm
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (n + e < a.N) out[e] = from_float<T>(a.add ? y[e] + to_float<T>(add[e]) : y[e]);
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store8(const MatmulArgs& a, int64_t m, int n, mm_f4 lo, mm_f4 hi) {
+    if (n + 8 <= a.N) {
+        T* out = (T*)a.out + m * a.out_stride + n;
+        const T* add = (const T*)a.add + m * a.add_stride + n;
+        Loose<T, 8> w;
+        if (a.add) {
+            w = *(const Loose<T, 8>*)add;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                lo[e] += to_float<T>(w.w[e]);
+                hi[e] += to_float<T>(w.w[4 + e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            w.w[e] = from_float<T>(lo[e]);
+            w.w[4 + e] = from_float<T>(hi[e]);
+        }
+        *(Loose<T, 8>*)out = w;
+    } else {
+        if (n < a.N) store4<T>(a, m, n, lo);
+        if (n + 4 < a.N) store4<T>(a, m, n + 4, hi);
+    }
+}
+
+// Largest value over the lanes l, l ^ 16, l ^ 32 and l ^ 48, in each of them
+__device__ __forceinline__ float max_over_fq(float v) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
+// A row's codes in NY blocks of 16 columns from n0 on, of which a lane has columns 4 fq .. 4 fq + 3 in w[block]: swapped among the four lanes of a row until
+// a lane has what NY of them had of one block
+template <int NY>
+__device__ __forceinline__ void store_codes(const MatmulArgs& a, int64_t m, int n0, int fq, uint32_t (&w)[NY]) {
+    static_assert(NY == 1 || NY == 2 || NY == 4, "blocks of a wavefront");
+    int n = n0 + 4 * fq;
+    if constexpr (NY == 4) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const auto x = __builtin_amdgcn_permlane32_swap(w[j], w[j + 2], false, false);
+            w[j] = x[0];
+            w[j + 2] = x[1];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            const auto x = __builtin_amdgcn_permlane16_swap(w[j], w[j + 1], false, false);
+            w[j] = x[0];
+            w[j + 1] = x[1];
+        }
+        n = n0 + 16 * fq;
+    } else if constexpr (NY == 2) {
+        const auto x = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+        w[0] = x[0];
+        w[1] = x[1];
+        n = n0 + (fq & 1) * 16 + (fq >> 1) * 8;
+    }
+    if (m >= a.M) return;
+    uint8_t* out = a.codes + m * a.code_stride + n;
+    if (n + 4 * NY <= a.N) {
+        if constexpr (NY == 4) *(uint4*)out = uint4{w[0], w[1], w[2], w[3]};
+        else if constexpr (NY == 2) *(uint2*)out = uint2{w[0], w[1]};
+        else *(uint32_t*)out = w[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4 * NY; ++e)
+            if (n + e < a.N) out[e] = (uint8_t)(w[e / 4] >> (e % 4 * 8));
     }
 }
 

@@ -55,67 +55,81 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
     extern __shared__ __attribute__((aligned(16))) char smem[];
 
     const int tiles_m = (int)((a.M + BM - 1) / BM), tiles_n = (a.N + BNY - 1) / BNY;
-    const TileCoord tc = map_tile(blockIdx.x, tiles_m, tiles_n);
+    unsigned pid = blockIdx.x;
+    TileCoord tc = map_tile((int)pid, tiles_m, tiles_n);
     if (!tc.valid) return;
-    const int64_t m0 = (int64_t)tc.tm * BM;
-    const int n0 = tc.tn * BNY;
     const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = all / NWAVE, wave = all % NWAVE;
     const int tid = KG > 1 ? (int)threadIdx.x - group * NT : (int)threadIdx.x;
     const int wm = wave / WN, wn = wave % WN, r = lane & 15, fq = lane >> 4;
     const int nk = (int)blocks_of(a.K), turns = (nk + KG - 1) / KG;       // blocks of k; block kt is group kt % KG's in turn kt / KG
 
     // ---- loads: a wavefront's load brings eight rows of 128 codes
-    const int rows_a = (int)min((int64_t)BM, a.M - m0), rows_w = min(BNY, a.N - n0);
-    const rsrc_t ra = make_rsrc(a.a + m0 * a.a_stride, rows_a * a.a_stride);
     // which half of w a pass brings goes by the wavefront (a pass has every wavefront's rows) or by the pass
     constexpr bool BY_WAVE = GATE && RPP % TN == 0;
     static_assert(!GATE || NI % 2 == 0, "whole blocks of 16 of either half");
     static_assert(!GATE || BY_WAVE || TNY % RPP == 0, "a load lies in one half");
-    const int lrow = lane >> 3, lchunk = (lane & 7) ^ ((wave * 8 + lrow) >> 1 & 7);
-    const int va = lrow * (int)a.a_stride + lchunk * 16, vw = lrow * (int)a.w_stride + lchunk * 16;
-    int pass_a[PA], pass_w[PB];
+    // A lane's place in its wavefront's loads: of a and w, kNoLoad behind the last column, and of the scales.  Beside the largest tile's halves there is no
+    // register to keep them in (a reload from memory would stand in front of every block's first loads): they are computed when they are used
+    constexpr bool CROWDED = PIPE && !EIGHT && MI * NI >= 32;
+    auto places = [&](int kt, int& xa, int& xw) {
+        int l = lane;
+        if constexpr (CROWDED) asm volatile("" : "+v"(l));
+        const int lrow = l >> 3, column = ((l & 7) ^ ((wave * 8 + lrow) >> 1 & 7)) * 16;
+        const int left = kt < nk ? a.K - kt * BK : 0, in_a = lrow * (int)a.a_stride + column, in_w = lrow * (int)a.w_stride + column;
+        xa = column < left ? in_a : kNoLoad;
+        xw = column < left ? in_w : kNoLoad;
+    };
+    const int swave = wave - SW, scale_row = swave < 0 ? wave * 64 : 0, scale_step = (int)(swave < 0 ? a.a_scale_stride : a.w_scale_stride) * 4;
+    auto scale_place = [&](int kt) {
+        int l = lane;
+        if constexpr (CROWDED) asm volatile("" : "+v"(l));
+        return (scale_row + l) * scale_step | (kt < nk ? 0 : kNoLoad);
+    };
     const int64_t first_half = BY_WAVE && wave * 8 % TN >= TNY ? a.half : 0;
-    const rsrc_t rw0 = make_rsrc(a.w + (n0 + first_half) * a.w_stride, rows_w * a.w_stride);
-    const rsrc_t rw1 = make_rsrc(a.w + (n0 + (int64_t)a.half) * a.w_stride, rows_w * a.w_stride);
+    int64_t m0;
+    int n0, pass_a[PA], pass_w[PB];
+    rsrc_t ra, rw0, rw1, rs;
+    auto set_tile = [&](const TileCoord& t) {
+        m0 = (int64_t)t.tm * BM;
+        n0 = t.tn * BNY;
+        const int rows_a = (int)min((int64_t)BM, a.M - m0), rows_w = min(BNY, a.N - n0);
+        ra = make_rsrc(a.a + m0 * a.a_stride, rows_a * a.a_stride);
+        rw0 = make_rsrc(a.w + (n0 + first_half) * a.w_stride, rows_w * a.w_stride);
+        rw1 = make_rsrc(a.w + (n0 + (int64_t)a.half) * a.w_stride, rows_w * a.w_stride);
 #pragma unroll
-    for (int p = 0; p < PA; ++p) {
-        const int row = p * RPP + wave * 8;
-        pass_a[p] = row < rows_a ? row * (int)a.a_stride : 0;              // a pass of rows that there are not: other rows, not stored
-    }
+        for (int p = 0; p < PA; ++p) {
+            const int row = p * RPP + wave * 8;
+            pass_a[p] = row < rows_a ? row * (int)a.a_stride : 0;          // a pass of rows that there are not: other rows, not stored
+        }
 #pragma unroll
-    for (int p = 0; p < PB; ++p) {
-        const int row = p * RPP + wave * 8, f = GATE ? row / TN * TNY + row % TNY : row;
-        pass_w[p] = f < rows_w ? f * (int)a.w_stride : 0;
-    }
-    // scales: the first SW wavefronts bring those of the rows, the next one (two) those of w's blocks
-    const int swave = wave - SW, sblocks = (int)blocks_of(rows_w);
-    rsrc_t rs;
-    int vs = kNoLoad;
-    if (swave < 0) {
-        rs = make_rsrc(a.a_scales + m0 * a.a_scale_stride, rows_a * a.a_scale_stride * 4);
-        if (wave * 64 + lane < rows_a) vs = (wave * 64 + lane) * (int)a.a_scale_stride * 4;
-    } else {
-        rs = make_rsrc(a.w_scales + ((int64_t)n0 + (swave == 1 ? (int64_t)a.half : 0)) / kBlockCols * a.w_scale_stride, sblocks * a.w_scale_stride * 4);
-        if (swave < H && lane < sblocks) vs = lane * (int)a.w_scale_stride * 4;
-    }
+        for (int p = 0; p < PB; ++p) {
+            const int row = p * RPP + wave * 8, f = GATE ? row / TN * TNY + row % TNY : row;
+            pass_w[p] = f < rows_w ? f * (int)a.w_stride : 0;
+        }
+        // scales: the first SW wavefronts bring those of the rows, the next one (two) those of w's blocks, the others none
+        const int sblocks = swave < H ? (int)blocks_of(rows_w) : 0;
+        rs = swave < 0 ? make_rsrc(a.a_scales + m0 * a.a_scale_stride, rows_a * a.a_scale_stride * 4)
+                       : make_rsrc(a.w_scales + ((int64_t)n0 + (swave == 1 ? (int64_t)a.half : 0)) / kBlockCols * a.w_scale_stride, sblocks * a.w_scale_stride * 4);
+    };
+    set_tile(tc);
     auto stage = [&](int s) { return smem + (group * NS + s) * STAGE; };
     constexpr int LPS = PA + PB + 1;                     // loads of a wavefront and block
     // load q of the LPS of a turn's block into stage s; a block past the end fetches nothing, and its zeros add nothing
-    auto request_one = [&](int q, int turn, int s) {
+    auto request_one = [&](int q, int turn, int s, int xa, int xw) {
         char* to = stage(s);
-        const int kt = turn * KG + group;
-        const bool there = kt < nk, some = there && kt * BK + lchunk * 16 < a.K;
-        const int at = there ? kt * BK : 0;
+        const int kt = turn * KG + group, at = kt < nk ? kt * BK : 0;
         if (SHORT && q == 0 && wave * 8 >= BM) return;   // goes by the wavefront
-        if (q < PA) load_lds16(ra, to + (q * RPP + wave * 8) * BK, some ? va : kNoLoad, pass_a[q < PA ? q : 0] + at);
+        if (q < PA) load_lds16(ra, to + (q * RPP + wave * 8) * BK, xa, pass_a[q < PA ? q : 0] + at);
         else if (q < PA + PB) {
             const int p = q - PA < PB ? q - PA : 0;
-            load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, some ? vw : kNoLoad, pass_w[p] + at);
-        } else load_lds4(rs, to + (BM + BN) * BK + wave * 256, there ? vs : kNoLoad, there ? kt * 4 : 0);
+            load_lds16(GATE && !BY_WAVE && p * RPP % TN >= TNY ? rw1 : rw0, to + (BM + p * RPP + wave * 8) * BK, xw, pass_w[p] + at);
+        } else load_lds4(rs, to + (BM + BN) * BK + wave * 256, scale_place(kt), kt < nk ? kt * 4 : 0);
     };
     auto request = [&](int turn, int s) {
+        int xa, xw;
+        places(turn * KG + group, xa, xw);
 #pragma unroll
-        for (int q = 0; q < LPS; ++q) request_one(q, turn, s);
+        for (int q = 0; q < LPS; ++q) request_one(q, turn, s, xa, xw);
     };
     // the chunk that the rows end in, in the last turn, if they end inside one
     auto mend_end = [&](char* in) {
@@ -125,16 +139,29 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
         }
         __syncthreads();
     };
+    // ... of what a wavefront's own loads brought, which have landed
+    auto mend_own = [&](char* in) {
+        for (int p = lane >> 3; p < PA + PB; p += 8) {
+            const int row = (p < PA ? p * RPP : BM + (p - PA) * RPP) + wave * 8 + (lane & 7);
+            mm_i4* c = (mm_i4*)(in + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
+            *c = first_codes(*c, a.K % 16);
+        }
+    };
     static_assert((NS - 2) * LPS < 64, "the load counter has six bits");
 
     mm_f4 acc[MI][NI];
+    const int sw = r >> 1;
+    const int at_a = (wm * TM + r) * BK, at_w = (BM + wn * TN + r) * BK, c0 = (fq ^ sw) * 16, c1 = ((4 + fq) ^ sw) * 16;
+
+    // A workgroup of the large tiles takes one after another and requests the first block of the next before it stores what it has (a tile's
+    // start waits for memory for 2 to 3 us)
+    constexpr bool PERSIST = PIPE && KG == 1;
+    if constexpr (PERSIST) request(0, 0);
+    for (;;) {                                           // one pass unless PERSIST
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = mm_f4{0.f, 0.f, 0.f, 0.f};
-    const int sw = r >> 1;
-    const int at_a = (wm * TM + r) * BK, at_w = (BM + wn * TN + r) * BK, c0 = (fq ^ sw) * 16, c1 = ((4 + fq) ^ sw) * 16;
-
     if constexpr (PIPE) {
         // Two stages.  A block is MI rows of NI sums; a row's sums are scaled and added while the next row's are computed.  A's fragments are
         // read two rows ahead and w's replaced behind their last use, so that the block's one barrier, in front of its last row but one, finds
@@ -163,11 +190,11 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 #pragma unroll
             for (int h = 0; h < H; ++h) ws[h] = ((const float*)(in + (BM + BN) * BK))[SW * 64 + h * 64 + wn * TNY / kBlockCols];
         };
-        request(0, 0);
+        if constexpr (!PERSIST) request(0, 0);
         __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
+        if (turns == 1 && a.K % 16 != 0) mend_own(stage(0));
         __syncthreads();
         request(1, 1);
-        if (turns == 1 && a.K % 16 != 0) mend_end(stage(0));
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             read_w(stage(0), j);
@@ -180,7 +207,12 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
         read_a(stage(0), 1);
         // Two wavefronts share a SIMD: where one goes first, they do not wait for the same unit at the same time
         if (all >= NWAVE * KG / 2) __builtin_amdgcn_s_setprio(1);
-        auto block = [&](auto mends, int turn) {           // a branch inside would keep the compiler from the order below
+        for (int turn = 0; turn < turns; ++turn) {       // no branch further down: it would keep the compiler from the order there
+            if (turn == turns - 2 && a.K % 16 != 0) {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+                mend_own(stage((turn & 1) ^ 1));
+            }
+            int xa = kNoLoad, xw = kNoLoad;
             char *from = stage(turn & 1), *next = stage((turn & 1) ^ 1);
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
@@ -190,7 +222,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
                     __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
-                    if constexpr (decltype(mends)::value) mend_end(next);
+                    places((turn + 2) * KG + group, xa, xw);
                 }
 #pragma unroll
                 for (int h = 0; h < H; ++h) sc[cur][h] = as[cur] * ws[h];
@@ -200,9 +232,9 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
                 };
                 auto ask = [&](int j) {                  // one load behind each of the first instructions behind the barrier
                     const int slot = (i + 2) % MI * NI + j;
-                    if (slot < LPS) request_one(slot, i >= MI - 2 ? turn + 2 : turn + 1, i >= MI - 2 ? turn & 1 : (turn & 1) ^ 1);
+                    if (slot < LPS) request_one(slot, i >= MI - 2 ? turn + 2 : turn + 1, i >= MI - 2 ? turn & 1 : (turn & 1) ^ 1, xa, xw);
                 };
-                static_assert(LPS <= MI * NI, "a slot for every load");
+                static_assert(PA + PB <= 2 * NI, "codes are requested in the two rows behind the barrier, scales there or behind them");
                 if constexpr (EIGHT) {
 #pragma unroll
                     for (int j = 0; j < NI; ++j) {
@@ -228,7 +260,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 #pragma unroll
                         for (int j = 0; j < NI; ++j) {
                             read_w(next, j);
-                            if (j % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                     }
                 }
@@ -236,12 +268,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
                 read_a(i < MI - 2 ? from : next, i < MI - 2 ? i + 2 : i + 2 - MI);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        };
-        // the first loads of block 1 are out; those of a block begin behind the barrier of the one before it
-        int kt = 0;
-        for (const int plain = a.K % 16 != 0 ? nk - 2 : nk; kt < plain; ++kt) block(std::false_type{}, kt);
-        if (kt < nk - 1) block(std::true_type{}, kt++);
-        if (kt < nk) block(std::false_type{}, kt);
+        }
         __builtin_amdgcn_s_setprio(0);
 #pragma unroll
         for (int j = 0; j < NI; ++j)
@@ -307,42 +334,158 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
             slot = slot + 1 == NS ? 0 : slot + 1;
         }
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);                  // nothing is on its way into LDS
-
-    // ---- the tile's rows, as many at a time as LDS holds
-    constexpr int PITCH = BN + 4, SLABS = MI >= 4 ? 4 : MI, IS = MI / SLABS, SR = WM * IS * 16;       // rows of a slab: IS blocks of every wavefront
-    float* sums = (float*)smem;
-#pragma unroll
-    for (int slab = 0; slab < SLABS; ++slab) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < IS; ++i)
-#pragma unroll
-            for (int j = 0; j < NI; ++j) *(mm_f4*)(sums + ((group * WM + wm) * IS * 16 + i * 16 + r) * PITCH + wn * TN + j * 16 + 4 * fq) = acc[slab * IS + i][j];
-        __syncthreads();
-        constexpr int Q = BNY / 4;
-        for (int u = threadIdx.x; u < SR * Q; u += NT * KG) {
-            const int row = u / Q, col = u % Q * 4;
-            const int64_t m = m0 + row / (IS * 16) * TM + slab * IS * 16 + row % (IS * 16);
-            const int at = GATE ? col / TNY * TN + col % TNY : col;
-            mm_f4 c = *(const mm_f4*)(sums + row * PITCH + at), up = GATE ? *(const mm_f4*)(sums + row * PITCH + at + TNY) : c;
-#pragma unroll
-            for (int g = 1; g < KG; ++g) {
-                c += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at);
-                if (GATE) up += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at + TNY);
-            }
-            const mm_f4 y = finish4<GATE>(a, n0 + col, c, up);
-            if constexpr (CODES) store_block4(a, m, n0 + col, y, m < a.M);
-            else if (m < a.M && n0 + col < a.N) store4<OUT>(a, m, n0 + col, y);
+    const int64_t tile_m0 = m0;
+    const int tile_n0 = n0;
+    bool another = false;
+    if constexpr (PERSIST) {
+        pid += gridDim.x;
+        if (pid / kXcds < (unsigned)(tiles_m * tiles_n)) tc = map_tile((int)pid, tiles_m, tiles_n);
+        else tc.valid = false;
+        another = tc.valid;
+        // into stage 0, where nobody reads any more what counts: the last block's fragments were read in front of its barrier
+        if (another) {
+            set_tile(tc);
+            request(0, 0);
         }
+    }
+    if constexpr (KG > 1) {
+        // the groups' sums meet in LDS, as many rows at a time as it holds, and leave it in rows
+        constexpr int PITCH = BN + 4, SLABS = MI >= 4 ? 4 : MI, IS = MI / SLABS, SR = WM * IS * 16;       // rows of a slab: IS blocks of every wavefront
+        float* sums = (float*)smem;
+        __builtin_amdgcn_s_waitcnt(0x0F70);              // nothing is on its way into LDS
+#pragma unroll
+        for (int slab = 0; slab < SLABS; ++slab) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < IS; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    *(mm_f4*)(sums + ((group * WM + wm) * IS * 16 + i * 16 + r) * PITCH + wn * TN + j * 16 + 4 * fq) = acc[slab * IS + i][j];
+            __syncthreads();
+            constexpr int Q = BNY / 4;
+            for (int u = threadIdx.x; u < SR * Q; u += NT * KG) {
+                const int row = u / Q, col = u % Q * 4;
+                const int64_t m = tile_m0 + row / (IS * 16) * TM + slab * IS * 16 + row % (IS * 16);
+                const int at = GATE ? col / TNY * TN + col % TNY : col;
+                mm_f4 c = *(const mm_f4*)(sums + row * PITCH + at), up = GATE ? *(const mm_f4*)(sums + row * PITCH + at + TNY) : c;
+#pragma unroll
+                for (int g = 1; g < KG; ++g) {
+                    c += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at);
+                    if (GATE) up += *(const mm_f4*)(sums + (g * SR + row) * PITCH + at + TNY);
+                }
+                const mm_f4 y = finish4<GATE>(a, tile_n0 + col, c, up);
+                if constexpr (CODES) store_block4(a, m, tile_n0 + col, y, m < a.M);
+                else if (m < a.M && tile_n0 + col < a.N) store4<OUT>(a, m, tile_n0 + col, y);
+            }
+        }
+    } else {
+        // From registers: a lane has four columns of a row in each block of 16 x 16
+        constexpr int NY = NI / H;
+        const int64_t row0 = tile_m0 + wm * TM + r;
+        const int col0 = tile_n0 + wn * TNY;
+        float bias[H][NY][4];
+        if (a.bias) {
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < NY; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int n = col0 + j * 16 + 4 * fq + e;
+                        bias[h][j][e] = n < a.N ? a.bias[n + h * a.half] : 0.0f;
+                    }
+        }
+        auto finish = [&](int i) {
+            if (a.bias) {
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] += bias[j / NY][j % NY][e];
+            }
+            if constexpr (GATE) {
+#pragma unroll
+                for (int j = 0; j < NY; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = gated(acc[i][j][e], acc[i][NY + j][e], a.gate);
+            }
+        };
+        if constexpr (CODES) {
+            // a row's largest value over its 128 columns: over a wavefront's by lane swaps, then over the wavefronts that share the block through LDS,
+            // in stage 1
+            constexpr int SHARE = kBlockCols / TNY;
+            float* tops = (float*)(smem + (PERSIST ? STAGE : 0));            // [BM][WN]
+            if constexpr (PERSIST) {
+                if (another) __builtin_amdgcn_s_waitcnt((LPS & 15) | ((LPS >> 4) << 14) | 0x0F70);      // all but the next tile's block have arrived
+                else __builtin_amdgcn_s_waitcnt(0x0F70);
+            } else {
+                __builtin_amdgcn_s_waitcnt(0x0F70);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                finish(i);
+                float v[NY * 4];
+#pragma unroll
+                for (int q = 0; q < NY * 4; ++q) {
+                    if (col0 + q / 4 * 16 + 4 * fq + q % 4 >= a.N) acc[i][q / 4][q % 4] = 0.0f;
+                    v[q] = acc[i][q / 4][q % 4];
+                }
+                const float top = max_over_fq(finite_top(v));
+                if (fq == 0) tops[(wm * TM + i * 16 + r) * WN + wn] = top;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                float top = 0.0f;
+#pragma unroll
+                for (int q = 0; q < SHARE; ++q) top = fmaxf(top, tops[(wm * TM + i * 16 + r) * WN + wn / SHARE * SHARE + q]);
+                const float scale = scale_of(top), by = 1.0f / scale;
+                const int64_t m = row0 + i * 16;
+                if (wn % SHARE == 0 && fq == 0 && m < a.M && col0 < a.N) a.scales[m * a.scale_stride + col0 / kBlockCols] = scale;
+                uint32_t w[NY];
+#pragma unroll
+                for (int j = 0; j < NY; ++j) w[j] = codes4(acc[i][j][0] * by, acc[i][j][1] * by, acc[i][j][2] * by, acc[i][j][3] * by);
+                store_codes<NY>(a, m, col0, fq, w);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                finish(i);
+                const int64_t m = row0 + i * 16;
+                if constexpr (sizeof(OUT) == 2 && NY % 2 == 0) {
+                    // of two blocks side by side a lane takes eight neighbouring columns of one
+#pragma unroll
+                    for (int j = 0; j < NY; j += 2) {
+                        mm_f4 lo, hi;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][j][e]), __float_as_uint(acc[i][j + 1][e]), false, false);
+                            lo[e] = __uint_as_float(x[0]);
+                            hi[e] = __uint_as_float(x[1]);
+                        }
+                        const int n = col0 + (j + (fq & 1)) * 16 + (fq >> 1) * 8;
+                        if (m < a.M) store8<OUT>(a, m, n, lo, hi);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NY; ++j) {
+                        const int n = col0 + j * 16 + 4 * fq;
+                        if (m < a.M && n < a.N) store4<OUT>(a, m, n, acc[i][j]);
+                    }
+                }
+            }
+        }
+    }
+    if (!another) break;
     }
 }
 
 template <int BM, int BN, int WM, int WN, int NS, int KG, bool EIGHT, bool GATE, typename OUT, bool CODES>
 hipError_t launch_tile(const MatmulArgs& a, hipStream_t st) {
     constexpr size_t stages = (size_t)KG * NS * ((BM + BN) * kBlockCols + WM * WN * 256);
-    constexpr size_t slab = (size_t)KG * (BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float);
+    constexpr size_t slab = KG > 1 ? (size_t)KG * (BM >= 64 * WM ? BM / 4 : WM * 16) * (BN + 4) * sizeof(float) : 0;
     constexpr size_t lds = stages > slab ? stages : slab;
+    constexpr bool persist = BM / WM >= 64 && NS == 2 && KG == 1;
     static_assert(lds <= 160 * 1024, "LDS of a CU");
     const auto kernel = block_mm_tile_kernel<BM, BN, WM, WN, NS, KG, EIGHT, GATE, OUT, CODES>;
     if (lds > 65536) {
@@ -351,7 +494,8 @@ hipError_t launch_tile(const MatmulArgs& a, hipStream_t st) {
     }
     constexpr int BNY = GATE ? BN / 2 : BN;
     const int64_t tiles = (a.M + BM - 1) / BM * ((a.N + BNY - 1) / BNY);
-    kernel<<<(unsigned)((tiles + kXcds - 1) / kXcds * kXcds), WM * WN * KG * 64, lds, st>>>(a);
+    const int64_t groups = (tiles + kXcds - 1) / kXcds * kXcds, held = kCus * (WM * WN == 4 ? 2 : 1);
+    kernel<<<(unsigned)(persist && groups > held ? held : groups), WM * WN * KG * 64, lds, st>>>(a);
     return hipGetLastError();
 }
 
