@@ -591,8 +591,8 @@ int hr_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block
  * and out = y + add, rounded once; or block8 = codes and scales of y.
  * a: activations (block_rows 1), w: weights (block_rows 128) with as many columns.  Sums over k and over blocks are fp32.  What the matrix
  * instructions round inside a sum over k: with fp32 out and with block8 (whose scales are fp32) nothing but the fp32 sum (codes are multiplied
- * as halves, exactly); with bf16 out and many rows the 8-bit instruction's own sum of eight products, which keeps 14 bits of the largest of the
- * eight (1.4e-5 of a row's rms over normal deviates, a hundredth of what out's rounding takes).
+ * as halves, exactly); with bf16 out and many rows, or where fast is set, the 8-bit instruction's own sum of eight products, which keeps 14 bits of the
+ * largest of the eight (1.4e-5 of a row's rms over normal deviates, a hundredth of what out's rounding takes) at up to 1.8 times the speed.
  * out may be add (then with the same stride).  HR_ERR_INVALID_ARG on null pointers, bad matrices, strides and overlaps (out, add, the codes and
  * scales of block8 and those of a and w begin at places of their own); HR_ERR_MISMATCH if a and w differ in columns, block8 from y's shape or a gate's half is no multiple
  * of 128; HR_ERR_LEN_RANGE beyond 2^24 - 512 workgroups; no rows of a or of w: a no-op. */
@@ -600,6 +600,7 @@ typedef enum hr_gate { HR_GATE_NONE = 0, HR_GATE_SILU = 1, HR_GATE_GELU = 2 } hr
 typedef struct hr_matmul_args {
     int32_t dtype;            /* of out and add: HR_F32 or HR_BF16 */
     int32_t gate;             /* hr_gate */
+    int32_t fast;             /* 0; not 0: the 8-bit instruction for every kind of result (see above) */
     const float* bias;        /* NULL or device [w->rows] */
     const void* add;          /* NULL or device [a->rows][columns of y]; not with block8 */
     void* out;                /* device, likewise; NULL with block8 */

@@ -93,7 +93,7 @@ class hr_norm_args(C.Structure):
 
 
 class hr_matmul_args(C.Structure):
-    _fields_ = [("dtype", C.c_int32), ("gate", C.c_int32), ("bias", C.c_void_p), ("add", C.c_void_p), ("out", C.c_void_p),
+    _fields_ = [("dtype", C.c_int32), ("gate", C.c_int32), ("fast", C.c_int32), ("bias", C.c_void_p), ("add", C.c_void_p), ("out", C.c_void_p),
                 ("add_stride", C.c_int64), ("out_stride", C.c_int64), ("block8", C.POINTER(hr_block8))]
 
 
@@ -798,16 +798,18 @@ def block_quantize(x, block_rows: int = 1, out: Optional[Block8] = None, stream=
     return out
 
 
-def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, bias=None, add=None, out=None, block8=None, stream=None):
+def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, bias=None, add=None, out=None, block8=None, fast: bool = False,
+                 stream=None):
     """a w^T of two matrices in 8 bits, activations and weights, with what follows it in a layer (hr_block_matmul): + bias (fp32 [rows of w]), a gate
     ("silu" or "gelu": act(first half of the columns) * second half), + add ([rows of a][columns], of out's type).  dtype: of out, float32 or bfloat16
     (None: out's or add's, else bfloat16); out: a tensor of the caller's, which may be add.  block8 (True, or a Block8 of the caller's): codes and
-    scales of the result instead.  Returns out, or the Block8."""
+    scales of the result instead.  fast: the 8-bit instruction for fp32 results and codes too, whose sums are else exact
+    to fp32.  Returns out, or the Block8."""
     import torch
     dev = a.device
     if _elsewhere(dev):
         with torch.cuda.device(dev):
-            return block_matmul(a, w, dtype, gate, bias, add, out, block8, stream)
+            return block_matmul(a, w, dtype, gate, bias, add, out, block8, fast, stream)
     if w.device != dev or gate not in GATES:
         _refuse(f"block_matmul: weights on {dev}, gate one of {list(GATES)}; got {w.device}, {gate!r}")
     M, N = a.shape[0], w.shape[0]
@@ -821,7 +823,7 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
         if out is not None or add is not None or N < 1:
             _refuse("block_matmul: codes instead of out, of at least one column, with nothing added")
         block8 = _block8_for(block8, M, N, a.scales, stream, "block_matmul")
-        args = hr_matmul_args(HR_F32, GATES[gate], b_p, None, None, 0, 0, C.pointer(block8.c))
+        args = hr_matmul_args(HR_F32, GATES[gate], 1 if fast else 0, b_p, None, None, 0, 0, C.pointer(block8.c))
     else:
         block8 = None
         if dtype is None:
@@ -836,7 +838,7 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
             _refuse(f"block_matmul: out: {dtype} on {dev} expected, got {out.dtype} on {out.device}")
         o_t, _ = _rows_of(out, shape, out, "block_matmul: out")
         d_t, _ = (0, 0) if add is None else _rows_of(add, shape, out, "block_matmul: add")
-        args = hr_matmul_args(code, GATES[gate], b_p, None if add is None else add.data_ptr(), out.data_ptr(), d_t, o_t, None)
+        args = hr_matmul_args(code, GATES[gate], 1 if fast else 0, b_p, None if add is None else add.data_ptr(), out.data_ptr(), d_t, o_t, None)
     check(lib.hr_block_matmul(C.byref(a.c), C.byref(w.c), C.byref(args), _stream_ptr(stream)), "hr_block_matmul")
     if stream is not None:
         _used_on(stream, a.codes, a.scales, w.codes, w.scales, bias, add, out, *(() if block8 is None else (block8.codes, block8.scales)))

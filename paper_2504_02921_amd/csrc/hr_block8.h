@@ -36,6 +36,7 @@ struct MatmulArgs {
     int32_t N, K;              // N: columns of y (half of w's rows with a gate)
     int32_t half;              // rows of w from a gate's row to the row it multiplies; 0: no gate
     int32_t gate;
+    bool eight;                // the 8-bit instruction
     const float* bias;
     const void* add;
     void* out;
@@ -54,7 +55,7 @@ enum MatmulShape {
     MM_SHAPES
 };
 struct MatmulPlan { int shape; int64_t rows; int rest; };      // the first `rows` rows, and the shape of what is left
-MatmulPlan matmul_plan(const MatmulArgs& a, int dtype);
+MatmulPlan matmul_plan(const MatmulArgs& a);
 int64_t matmul_tiles(int shape, const MatmulArgs& a, int64_t rows);
 MatmulArgs matmul_rows(const MatmulArgs& a, int dtype, int64_t first, int64_t rows);
 

@@ -34,11 +34,12 @@ int hr_block_matmul(const hr_block8* a, const hr_block8* w, const hr_matmul_args
     const int rc = hr::matmul_check(a, w, args);
     if (rc != HR_OK || a->rows == 0 || w->rows == 0) return rc;
     hr::MatmulArgs m = hr::matmul_args(*a, *w, *args);
-    const hr::MatmulPlan plan = hr::matmul_plan(m, args->dtype);
+    const hr::MatmulPlan plan = hr::matmul_plan(m);
     auto launch = [&](const hr::MatmulArgs& part, int shape) {
         if (shape <= hr::MM_FEW_32) return hr::launch_block_matmul_few(part, args->dtype, shape, (hipStream_t)stream);
-        if (part.codes) return hr::launch_block_matmul_codes(part, shape, (hipStream_t)stream);
-        return (args->dtype == HR_F32 ? hr::launch_block_matmul_f32 : hr::launch_block_matmul_bf16)(part, shape, (hipStream_t)stream);
+        if (part.codes) return (part.eight ? hr::launch_block_matmul_codes_fast : hr::launch_block_matmul_codes)(part, shape, (hipStream_t)stream);
+        if (args->dtype == HR_BF16) return hr::launch_block_matmul_bf16(part, shape, (hipStream_t)stream);
+        return (part.eight ? hr::launch_block_matmul_f32_fast : hr::launch_block_matmul_f32)(part, shape, (hipStream_t)stream);
     };
     if (plan.rows < m.M) {
         HR_OP_HIP(launch(hr::matmul_rows(m, args->dtype, 0, plan.rows), plan.shape));

@@ -1,0 +1,8 @@
+// Products of 8-bit matrices: fp32 results, 8-bit instruction.
+#include "hr_block_mm_tiles.h"
+
+namespace hr {
+
+hipError_t launch_block_matmul_f32_fast(const MatmulArgs& a, int shape, hipStream_t st) { return launch_out_shape<true, float>(a, shape, st); }
+
+}  // namespace hr

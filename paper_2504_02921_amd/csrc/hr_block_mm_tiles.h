@@ -499,6 +499,61 @@ hipError_t launch_tile(const MatmulArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// DEPTH: stages; TURNS: groups along k
+template <bool EIGHT, typename OUT, int BM, int BN, int WM, int WN, int DEPTH, int TURNS>
+hipError_t launch_out(const MatmulArgs& a, hipStream_t st) {
+    if constexpr (BN / WN < 32) {                    // a wavefront has no 16 columns of either half
+        if (a.half > 0) return hipErrorInvalidValue;
+    } else {
+        if (a.half > 0) return launch_tile<BM, BN, WM, WN, DEPTH, TURNS, EIGHT, true, OUT, false>(a, st);
+    }
+    return launch_tile<BM, BN, WM, WN, DEPTH, TURNS, EIGHT, false, OUT, false>(a, st);
+}
+template <bool EIGHT, typename OUT>
+hipError_t launch_out_shape(const MatmulArgs& a, int shape, hipStream_t st) {
+    switch (shape) {
+        case MM_16x64_4: return launch_out<EIGHT, OUT, 16, 64, 1, 4, 3, 4>(a, st);
+        case MM_32x64_2: return launch_out<EIGHT, OUT, 32, 64, 2, 2, 3, 2>(a, st);
+        case MM_64x64: return launch_out<EIGHT, OUT, 64, 64, 2, 2, 4, 1>(a, st);
+        case MM_64x64_2: return launch_out<EIGHT, OUT, 64, 64, 2, 2, 4, 2>(a, st);
+        case MM_64x128: return launch_out<EIGHT, OUT, 64, 128, 2, 2, 3, 1>(a, st);
+        case MM_64x128_2: return launch_out<EIGHT, OUT, 64, 128, 2, 2, 3, 2>(a, st);
+        case MM_64x256: return launch_out<EIGHT, OUT, 64, 256, 2, 4, 3, 1>(a, st);
+        case MM_128x128: return launch_out<EIGHT, OUT, 128, 128, 2, 2, 2, 1>(a, st);
+        case MM_128x256: return launch_out<EIGHT, OUT, 128, 256, 2, 4, 2, 1>(a, st);
+        case MM_256x256: return launch_out<EIGHT, OUT, 256, 256, 2, 4, 2, 1>(a, st);
+        default: return hipErrorInvalidValue;
+    }
+}
+
+// Into codes: tiles with whole blocks of 128 columns of y
+template <bool EIGHT, int BM, int BN, int WM, int WN, int DEPTH, int TURNS>
+hipError_t launch_codes(const MatmulArgs& a, hipStream_t st) {
+    if constexpr (BN >= 2 * kBlockCols) {
+        if (a.half > 0) return launch_tile<BM, BN, WM, WN, DEPTH, TURNS, EIGHT, true, float, true>(a, st);
+    }
+    if constexpr (BN == kBlockCols || BM >= 64) {
+        if (a.half == 0) return launch_tile<BM, BN, WM, WN, DEPTH, TURNS, EIGHT, false, float, true>(a, st);
+    }
+    return hipErrorInvalidValue;
+}
+template <bool EIGHT>
+hipError_t launch_codes_shape(const MatmulArgs& a, int shape, hipStream_t st) {
+    switch (shape) {
+        case MM_16x128_4: return launch_codes<EIGHT, 16, 128, 1, 4, 2, 4>(a, st);
+        case MM_32x128_2: return launch_codes<EIGHT, 32, 128, 1, 4, 3, 2>(a, st);
+        case MM_16x256: return launch_codes<EIGHT, 16, 256, 1, 8, 4, 1>(a, st);
+        case MM_32x256: return launch_codes<EIGHT, 32, 256, 1, 8, 4, 1>(a, st);
+        case MM_64x128: return launch_codes<EIGHT, 64, 128, 2, 2, 3, 1>(a, st);
+        case MM_64x128_2: return launch_codes<EIGHT, 64, 128, 2, 2, 3, 2>(a, st);
+        case MM_64x256: return launch_codes<EIGHT, 64, 256, 2, 4, 3, 1>(a, st);
+        case MM_128x128: return launch_codes<EIGHT, 128, 128, 2, 2, 2, 1>(a, st);
+        case MM_128x256: return launch_codes<EIGHT, 128, 256, 2, 4, 2, 1>(a, st);
+        case MM_256x256: return launch_codes<EIGHT, 256, 256, 2, 4, 2, 1>(a, st);
+        default: return hipErrorInvalidValue;
+    }
+}
+
 }  // namespace
 
 }  // namespace hr

@@ -16,6 +16,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 FAKE = 0x7F0000000000      # never dereferenced on the host
 BAD, LONG, MISMATCH = hb.HR_ERR_INVALID_ARG, hb.HR_ERR_LEN_RANGE, hb.HR_ERR_MISMATCH
+KINDS = ("bf16", "f32", "f32 fast", "block8", "block8 fast")
 NAN, INF = float("nan"), float("inf")
 
 
@@ -73,7 +74,7 @@ def test_codes_that_are_refused():
 # ---- product
 def product(a=None, w=None, out8=None, **more):
     a, w = a or block8(4, 100), w or block8(256, 100, 128, at=2)
-    m = hb.hr_matmul_args(hb.HR_BF16, 0, None, None, FAKE + 64, 256, 256, None)
+    m = hb.hr_matmul_args(hb.HR_BF16, 0, 0, None, None, FAKE + 64, 256, 256, None)
     if out8 is not None:
         m.block8, m.out = C.pointer(out8), None
     for k, v in more.items():
@@ -125,11 +126,11 @@ def test_every_shape_of_tile_that_a_product_takes_is_tested(tmp_path):
     rng = random.Random(1)
     size = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi))))      # noqa: E731
     drawn = [(kind, gate, size(1, 60000), max(size(16, 60000) // 256 * 256, 256) if gate else size(16, 60000), size(32, 32768))
-             for kind in ("bf16", "f32", "block8") for gate in (0, 1) for _ in range(3000)]
-    drawn += [(kind, gate, m, n, k) for kind in ("bf16", "f32", "block8") for gate in (0, 1) for m in (1, 1 << 30) for n in (256, (1 << 30) - 256) for k in (1, 1 << 22)]
+             for kind in KINDS for gate in (0, 1) for _ in range(3000)]
+    drawn += [(kind, gate, m, n, k) for kind in KINDS for gate in (0, 1) for m in (1, 1 << 30) for n in (256, (1 << 30) - 256) for k in (1, 1 << 22)]
     env = dict(os.environ)
     env.pop("LD_PRELOAD", None)          # the sanitizer runtime must come first in the link order
-    lines = "".join(f"{int(kind == 'block8')} {int(kind != 'bf16')} {gate} {m} {n} {k}\n" for kind, gate, m, n, k in drawn + SHAPES)
+    lines = "".join(f"{int(kind.startswith('block8'))} {int(kind == 'bf16' or kind.endswith('fast'))} {gate} {m} {n} {k}\n" for kind, gate, m, n, k in drawn + SHAPES)
     r = subprocess.run([exe], input=lines, capture_output=True, text=True, env=env)
     assert r.returncode == 0, (r.stdout + r.stderr)[-2000:]
     plans = [tuple(int(x) for x in line.split()) for line in r.stdout.splitlines()]
@@ -137,4 +138,4 @@ def test_every_shape_of_tile_that_a_product_takes_is_tested(tmp_path):
     taken = {(d[0], d[1], p[0]) for d, p in zip(drawn, plans)}
     tested = {(d[0], d[1], p[0]) for d, p in zip(SHAPES, plans[len(drawn):])}
     assert taken <= tested, sorted(taken - tested)
-    assert {d[0] for d, p in zip(SHAPES, plans[len(drawn):]) if p[1] >= 0} == {"bf16", "block8"}
+    assert {d[0] for d, p in zip(SHAPES, plans[len(drawn):]) if p[1] >= 0} == set(KINDS)

@@ -22,11 +22,11 @@ def torch():
 
 
 def tdt(kind):
-    return torch().float32 if kind == "f32" else torch().bfloat16
+    return torch().float32 if kind.startswith("f32") else torch().bfloat16
 
 
 def unit(kind):
-    return R.U32 if kind == "f32" else R.UBF
+    return R.U32 if kind.startswith("f32") else R.UBF
 
 
 def to64(t):
@@ -196,8 +196,8 @@ def matrix(rows, cols, block_rows, seed, pad=0x7F):
 
 
 def check_product(a, w, y, kind, bias=None, gate=None, add=None):
-    want, off = R.product(*(R.values64(x.codes.view(torch().uint8), x.scales, x.block_rows) for x in (a, w)), bias, gate, add, eight_bit=kind == "bf16")
-    if kind == "block8":
+    want, off = R.product(*(R.values64(x.codes.view(torch().uint8), x.scales, x.block_rows) for x in (a, w)), bias, gate, add, eight_bit=kind == "bf16" or kind.endswith("fast"))
+    if kind.startswith("block8"):
         R.check_codes(code_bytes(y.codes), y.scales, want, off, "product")
     else:
         R.check_rounded(y, want, off, unit(kind), "product")
@@ -208,14 +208,14 @@ def run_and_check(kind, m, n, k, gate=None, seed=20):
     a, w = matrix(m, k, 1, seed), matrix(n, k, 128, seed + 1)
     if gate:
         a.scales.mul_(0.1 / k ** 0.5)                                    # a gate's interesting arguments
-    wide = n // 2 if gate else n
+    wide, fast = n // 2 if gate else n, kind.endswith("fast")
     bias = draw((n,), 22, "f32", 2.0 if gate else 100.0)
-    if kind == "block8":
-        check_product(a, w, hb().block_matmul(a, w, gate=gate, block8=True), kind, None, gate)
-        return check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, block8=True), kind, bias, gate)
-    check_product(a, w, hb().block_matmul(a, w, dtype=tdt(kind), gate=gate), kind, None, gate)
+    if kind.startswith("block8"):
+        check_product(a, w, hb().block_matmul(a, w, gate=gate, block8=True, fast=fast), kind, None, gate)
+        return check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, block8=True, fast=fast), kind, bias, gate)
+    check_product(a, w, hb().block_matmul(a, w, dtype=tdt(kind), gate=gate, fast=fast), kind, None, gate)
     add = draw((m, wide), 23, kind, 2.0 if gate else 100.0)
-    check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, add=add), kind, bias, gate, add)
+    check_product(a, w, hb().block_matmul(a, w, gate=gate, bias=bias, add=add, fast=fast), kind, bias, gate, add)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "block8"])
