@@ -46,7 +46,9 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
     constexpr int NWAVE = WM * WN, NT = NWAVE * 64, BK = kBlockCols;       // of a group
     constexpr int TM = BM / WM, TN = BN / WN, MI = TM / 16, NI = TN / 16;
     constexpr int H = GATE ? 2 : 1, BNY = BN / H, TNY = TN / H;            // columns of y
-    constexpr bool PIPE = MI >= 4 && NS == 2;
+    // The next block's fragments are read under this one's last instructions.  With halves, two rows a wavefront and others that have the same rows of w it
+    // lost: 64 x 64 and 64 x 128 tiles 7 to 9 % slower (8-bit instruction: up to 30 % faster)
+    constexpr bool PIPE = MI % 2 == 0 && (EIGHT || MI >= 4 || WM == 1);
     constexpr int RPP = NT / 8, PA = (BM + RPP - 1) / RPP, PB = BN / RPP;  // rows a pass of 16-byte loads brings, passes
     constexpr bool SHORT = BM < RPP;                                       // the first wavefronts bring all rows of a
     constexpr int SW = (BM + 63) / 64;                                     // wavefronts that bring the rows' scales
@@ -139,15 +141,32 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
         }
         __syncthreads();
     };
+    // All but the loads of BLOCKS blocks have landed (of which a wavefront that brings no rows of a has one less each)
+    auto landed = [&](auto blocks) {
+        constexpr int V = decltype(blocks)::value * LPS, V1 = decltype(blocks)::value * (LPS - 1);
+        static_assert(V < 64, "the load counter has six bits");
+        asm volatile("" ::: "memory");
+        if (SHORT && wave * 8 >= BM) __builtin_amdgcn_s_waitcnt((V1 & 15) | ((V1 >> 4) << 14) | 0x0F70);
+        else __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0F70);
+        asm volatile("" ::: "memory");
+    };
+    // Everybody is here, and what they wrote to LDS too
+    auto meet = [&]() {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xC07F);              // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    using std::integral_constant;
     // ... of what a wavefront's own loads brought, which have landed
     auto mend_own = [&](char* in) {
-        for (int p = lane >> 3; p < PA + PB; p += 8) {
+        for (int p = lane >> 3; p < PA + PB && (nk - 1) % KG == group; p += 8) {
+            if (SHORT && p == 0 && wave * 8 >= BM) continue;         // others' rows
             const int row = (p < PA ? p * RPP : BM + (p - PA) * RPP) + wave * 8 + (lane & 7);
             mm_i4* c = (mm_i4*)(in + row * BK + ((a.K % BK / 16) ^ (row >> 1 & 7)) * 16);
             *c = first_codes(*c, a.K % 16);
         }
     };
-    static_assert((NS - 2) * LPS < 64, "the load counter has six bits");
 
     mm_f4 acc[MI][NI];
     const int sw = r >> 1;
@@ -155,7 +174,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 
     // A workgroup of the large tiles takes one after another and requests the first block of the next before it stores what it has (a tile's
     // start waits for memory for 2 to 3 us)
-    constexpr bool PERSIST = PIPE && KG == 1;
+    constexpr bool PERSIST = PIPE && KG == 1 && MI >= 4 && NS == 2;
     if constexpr (PERSIST) request(0, 0);
     for (;;) {                                           // one pass unless PERSIST
 #pragma unroll
@@ -163,7 +182,7 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = mm_f4{0.f, 0.f, 0.f, 0.f};
     if constexpr (PIPE) {
-        // Two stages.  A block is MI rows of NI sums; a row's sums are scaled and added while the next row's are computed.  A's fragments are
+        // A block is MI rows of NI sums; a row's sums are scaled and added while the next row's are computed.  A's fragments are
         // read two rows ahead and w's replaced behind their last use, so that the block's one barrier, in front of its last row but one, finds
         // all of the stage read: what is requested behind it has a whole block's time to land.
         mm_i8 af[2], w8[EIGHT ? NI : 1];
@@ -190,11 +209,16 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 #pragma unroll
             for (int h = 0; h < H; ++h) ws[h] = ((const float*)(in + (BM + BN) * BK))[SW * 64 + h * 64 + wn * TNY / kBlockCols];
         };
-        if constexpr (!PERSIST) request(0, 0);
-        __builtin_amdgcn_s_waitcnt(0x0F70);              // vmcnt(0)
+        if constexpr (PERSIST) {
+            landed(integral_constant<int, 0>{});
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS; ++s) request(s, s);
+            landed(integral_constant<int, NS - 1>{});
+        }
         if (turns == 1 && a.K % 16 != 0) mend_own(stage(0));
-        __syncthreads();
-        request(1, 1);
+        meet();
+        if constexpr (PERSIST) request(1, 1);
 #pragma unroll
         for (int j = 0; j < NI; ++j) {
             read_w(stage(0), j);
@@ -207,22 +231,23 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
         read_a(stage(0), 1);
         // Two wavefronts share a SIMD: where one goes first, they do not wait for the same unit at the same time
         if (all >= NWAVE * KG / 2) __builtin_amdgcn_s_setprio(1);
+        int slot = 0;
         for (int turn = 0; turn < turns; ++turn) {       // no branch further down: it would keep the compiler from the order there
             if (turn == turns - 2 && a.K % 16 != 0) {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
-                mend_own(stage((turn & 1) ^ 1));
+                landed(integral_constant<int, 0>{});
+                mend_own(stage(slot + 1 == NS ? 0 : slot + 1));
             }
             int xa = kNoLoad, xw = kNoLoad;
-            char *from = stage(turn & 1), *next = stage((turn & 1) ^ 1);
+            const int here = slot, ahead = slot + 1 == NS ? 0 : slot + 1, behind = slot == 0 ? NS - 1 : slot - 1;
+            char *from = stage(here), *next = stage(ahead);
+            slot = ahead;
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 const int cur = i & 1, old = cur ^ 1, iold = i == 0 ? MI - 1 : i - 1;
                 if (i == MI - 2) {
-                    asm volatile("" ::: "memory");
-                    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    places((turn + 2) * KG + group, xa, xw);
+                    landed(integral_constant<int, NS - 2>{});      // the next block; those behind it may be on their way
+                    meet();
+                    places((turn + NS) * KG + group, xa, xw);
                 }
 #pragma unroll
                 for (int h = 0; h < H; ++h) sc[cur][h] = as[cur] * ws[h];
@@ -230,11 +255,15 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[iold][j][e] = fmaf(part[j][e], sc[old][GATE && j >= NI / 2 ? 1 : 0], acc[iold][j][e]);
                 };
-                auto ask = [&](int j) {                  // one load behind each of the first instructions behind the barrier
-                    const int slot = (i + 2) % MI * NI + j;
-                    if (slot < LPS) request_one(slot, i >= MI - 2 ? turn + 2 : turn + 1, i >= MI - 2 ? turn & 1 : (turn & 1) ^ 1, xa, xw);
+                auto ask = [&](int j) {                  // a load behind each of the first instructions behind the barrier
+                    constexpr int EACH = MI > 2 ? 1 : (LPS + 2 * NI - 1) / (2 * NI);
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e) {
+                        const int q = ((i + 2) % MI * NI + j) * EACH + e;
+                        if (q < LPS) request_one(q, i >= MI - 2 ? turn + NS : turn + NS - 1, i >= MI - 2 ? here : behind, xa, xw);
+                    }
                 };
-                static_assert(PA + PB <= 2 * NI, "codes are requested in the two rows behind the barrier, scales there or behind them");
+                static_assert(MI == 2 || PA + PB <= 2 * NI, "codes are requested in the two rows behind the barrier, scales there or behind them");
                 if constexpr (EIGHT) {
 #pragma unroll
                     for (int j = 0; j < NI; ++j) {
@@ -279,12 +308,8 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
         for (int s = 0; s < NS - 1; ++s) request(s, s);
         int slot = 0;
         for (int turn = 0; turn < turns; ++turn) {
-            constexpr int V = (NS - 2) * LPS, V1 = (NS - 2) * (LPS - 1);
-            asm volatile("" ::: "memory");
-            if (SHORT && wave * 8 >= BM) __builtin_amdgcn_s_waitcnt((V1 & 15) | ((V1 >> 4) << 14) | 0x0070);
-            else __builtin_amdgcn_s_waitcnt((V & 15) | ((V >> 4) << 14) | 0x0070);       // vmcnt(V) lgkmcnt(0)
-            __builtin_amdgcn_s_barrier();                    // this block has landed, and nobody reads the one before
-            asm volatile("" ::: "memory");
+            landed(integral_constant<int, NS - 2>{});
+            meet();                                      // this block has landed, and nobody reads the one before
             const int before = slot == 0 ? NS - 1 : slot - 1;
             request(turn + NS - 1, before);
             char* from = stage(slot);
@@ -415,12 +440,12 @@ __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) 
             constexpr int SHARE = kBlockCols / TNY;
             float* tops = (float*)(smem + (PERSIST ? STAGE : 0));            // [BM][WN]
             if constexpr (PERSIST) {
-                if (another) __builtin_amdgcn_s_waitcnt((LPS & 15) | ((LPS >> 4) << 14) | 0x0F70);      // all but the next tile's block have arrived
-                else __builtin_amdgcn_s_waitcnt(0x0F70);
+                if (another) landed(integral_constant<int, 1>{});      // all but the next tile's block
+                else landed(integral_constant<int, 0>{});
             } else {
-                __builtin_amdgcn_s_waitcnt(0x0F70);
+                landed(integral_constant<int, 0>{});
             }
-            __syncthreads();
+            meet();
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
                 finish(i);
@@ -520,7 +545,8 @@ hipError_t launch_out_shape(const MatmulArgs& a, int shape, hipStream_t st) {
         case MM_64x128_2: return launch_out<EIGHT, OUT, 64, 128, 2, 2, 3, 2>(a, st);
         case MM_64x256: return launch_out<EIGHT, OUT, 64, 256, 2, 4, 3, 1>(a, st);
         case MM_128x128: return launch_out<EIGHT, OUT, 128, 128, 2, 2, 2, 1>(a, st);
-        case MM_128x256: return launch_out<EIGHT, OUT, 128, 256, 2, 4, 2, 1>(a, st);
+        case MM_128x128_2: return launch_out<EIGHT, OUT, 128, 128, 2, 2, 2, 2>(a, st);
+        case MM_128x256: return launch_out<EIGHT, OUT, 128, 256, 2, 4, 3, 1>(a, st);
         case MM_256x256: return launch_out<EIGHT, OUT, 256, 256, 2, 4, 2, 1>(a, st);
         default: return hipErrorInvalidValue;
     }
@@ -548,7 +574,8 @@ hipError_t launch_codes_shape(const MatmulArgs& a, int shape, hipStream_t st) {
         case MM_64x128_2: return launch_codes<EIGHT, 64, 128, 2, 2, 3, 2>(a, st);
         case MM_64x256: return launch_codes<EIGHT, 64, 256, 2, 4, 3, 1>(a, st);
         case MM_128x128: return launch_codes<EIGHT, 128, 128, 2, 2, 2, 1>(a, st);
-        case MM_128x256: return launch_codes<EIGHT, 128, 256, 2, 4, 2, 1>(a, st);
+        case MM_128x128_2: return launch_codes<EIGHT, 128, 128, 2, 2, 2, 2>(a, st);
+        case MM_128x256: return launch_codes<EIGHT, 128, 256, 2, 4, 3, 1>(a, st);
         case MM_256x256: return launch_codes<EIGHT, 256, 256, 2, 4, 2, 1>(a, st);
         default: return hipErrorInvalidValue;
     }
