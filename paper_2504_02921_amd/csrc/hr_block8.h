@@ -15,9 +15,8 @@ constexpr int64_t kMaxWorkgroups = (1 << 24) - 512;                    // of a l
 HR_HD int64_t blocks_of(int64_t n) { return (n + kBlockCols - 1) / kBlockCols; }
 
 // ---- norm
-// How a head's channels are spread: `lanes` lanes have a head (16, 32 or 64 of a wavefront, or a workgroup's 256, 512 or 1024), `chunks` times 8 channels
-// each; chunks = 0: more channels than that holds, read twice.  Rows of few channels fill wavefronts, a wavefront with more than two chunks waits for its
-// loads: bf16, sums and codes written, 12800 x 896 by wavefronts / workgroups 19.6 / 27.5 us, 12800 x 2048 61 / 50, 12800 x 4096 223 / 81; 65 x 896 4.6 / 3.6.
+// How a head's channels are spread: `lanes` lanes have a head (16, 32 or 64 of a wavefront, or a workgroup's 128 to 1024), `chunks` times 8 channels each;
+// chunks = 0: more channels than that holds, read twice.
 struct NormShape { int lanes, chunks; };
 NormShape norm_shape(int channels, int64_t rows);
 int norm_check(const hr_norm_args* a);

@@ -33,64 +33,69 @@ struct NormArgs {
 template <typename T>
 __device__ __forceinline__ T* at(const NormSide& s, int64_t token, int head) { return (T*)s.p + token * s.ts + head * s.hs; }
 
-// Channels c .. c + 7, those behind the head's last one as zeros
-template <typename T>
+// Channels c .. c + 7, those behind the head's last one as zeros.  WHOLE: the number of channels is a multiple of 8
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void load8(const T* p, int c, int channels, float (&v)[kVec]) {
     if (c + kVec <= channels) {
         const Loose<T, kVec> w = *(const Loose<T, kVec>*)(p + c);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] = to_float<T>(w.w[e]);
+    } else if (WHOLE || c >= channels) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = 0.0f;
     } else {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] = c + e < channels ? to_float<T>(p[c + e]) : 0.0f;
     }
 }
-template <typename T>
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void store8(T* p, int c, int channels, const float (&v)[kVec]) {
     if (c + kVec <= channels) {
         Loose<T, kVec> w;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) w.w[e] = from_float<T>(v[e]);
         *(Loose<T, kVec>*)(p + c) = w;
-    } else {
+    } else if (!WHOLE) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
             if (c + e < channels) p[c + e] = from_float<T>(v[e]);
     }
 }
 // Codes c .. c + 7 of a row; c is a multiple of 8 and rows begin at multiples of 16
+template <bool WHOLE>
 __device__ __forceinline__ void store_codes8(uint8_t* p, int c, int cols, const float (&v)[kVec], float by) {
     const uint2 w = {codes4(v[0] * by, v[1] * by, v[2] * by, v[3] * by), codes4(v[4] * by, v[5] * by, v[6] * by, v[7] * by)};
     if (c + kVec <= cols) {
         *(uint2*)(p + c) = w;
-    } else {
+    } else if (!WHOLE) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e)
             if (c + e < cols) p[c + e] = (uint8_t)((e < 4 ? w.x : w.y) >> (e % 4 * 8));
     }
 }
 
-// What becomes of eight channels of a head
-template <typename T>
+// What becomes of eight channels of a head; 16 lanes in a row come here together for a block of 128
+template <typename T, bool WHOLE>
 __device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float r) {
+    if (c / kBlockCols * kBlockCols >= a.channels) return;
     float y[kVec];
-    if (a.gain) load8<float>(a.gain, c, a.channels, y);
+    if (a.gain) load8<float, WHOLE>(a.gain, c, a.channels, y);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) y[e] = s[e] * r * (a.gain ? y[e] + a.offset : 1.0f);
     if (a.codes) {
         if (c + kVec > a.channels)
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (c + e >= a.channels) y[e] = 0.0f;             // an infinite 1 / root makes NaN of them
+                if (WHOLE || c + e >= a.channels) y[e] = 0.0f;    // an infinite 1 / root makes NaN of them
         const float scale = scale_of(max16(finite_top(y)));
         if (on && c < a.channels) {
-            store_codes8(a.codes + token * a.code_stride, c, a.channels, y, 1.0f / scale);
+            store_codes8<WHOLE>(a.codes + token * a.code_stride, c, a.channels, y, 1.0f / scale);
             if (c % kBlockCols == 0) a.scales[token * a.scale_stride + c / kBlockCols] = scale;
         }
     }
     if (on && c < a.channels) {
-        if (a.total.p) store8<T>(at<T>(a.total, token, head), c, a.channels, s);
-        if (a.out.p) store8<T>(at<T>(a.out, token, head), c, a.channels, y);
+        if (a.total.p) store8<T, WHOLE>(at<T>(a.total, token, head), c, a.channels, s);
+        if (a.out.p) store8<T, WHOLE>(at<T>(a.out, token, head), c, a.channels, y);
     }
 }
 
@@ -99,11 +104,12 @@ __device__ __forceinline__ float root_of(float squares, const NormArgs& a) {
     return m == 0.0f ? 0.0f : rsqrtf(m);
 }
 
-// LANES lanes have a head, CHUNKS times 8 channels each
-template <typename T, int LANES, int CHUNKS>
-__global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kernel(NormArgs a) {
+// LANES lanes have a head, CHUNKS times 8 channels each.  Two workgroups of 1024 lanes share a compute unit if a lane has 64 registers, and one loads while
+// the other stores: bf16 is held to that (8000 x 14336 with sums and codes 191 to 166 us, 4 rows 5.0 to 5.7); fp32 would spill (284 to 374 us)
+template <typename T, bool WHOLE, int LANES, int CHUNKS>
+__global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads, sizeof(T) == 2 && LANES == 1024 && CHUNKS == 2 ? 8 : 1) norm_kernel(NormArgs a) {
     constexpr int UNITS = LANES > kThreads ? 1 : kThreads / LANES, WAVES = LANES / 64;
-    __shared__ float part[2][LANES > 64 ? WAVES : 1];
+    __shared__ float part[2][UNITS][LANES > 64 ? WAVES : 1];
     const int lane = threadIdx.x % LANES, unit = threadIdx.x / LANES;
     int turn = 0;
     for (int64_t first = (int64_t)blockIdx.x * UNITS; first < a.rows; first += (int64_t)gridDim.x * UNITS) {
@@ -117,10 +123,10 @@ __global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kern
         }
         float s[CHUNKS][kVec], more[CHUNKS][kVec];
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) load8<T>(at<const T>(a.x, token, head), (k * LANES + lane) * kVec, a.channels, s[k]);
+        for (int k = 0; k < CHUNKS; ++k) load8<T, WHOLE>(at<const T>(a.x, token, head), (k * LANES + lane) * kVec, a.channels, s[k]);
         if (a.add.p) {
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) load8<T>(at<const T>(a.add, token, head), (k * LANES + lane) * kVec, a.channels, more[k]);
+            for (int k = 0; k < CHUNKS; ++k) load8<T, WHOLE>(at<const T>(a.add, token, head), (k * LANES + lane) * kVec, a.channels, more[k]);
         }
         float sum = 0.0f;
 #pragma unroll
@@ -136,17 +142,17 @@ __global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kern
         } else {
             sum = wave_sum(sum);
             if constexpr (LANES > 64) {
-                if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = sum;
+                if (lane % 64 == 0) part[turn][unit][lane / 64] = sum;
                 __syncthreads();                    // one a turn: the other half of `part` is written next
                 sum = 0.0f;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) sum += part[turn][w];
+                for (int w = 0; w < WAVES; ++w) sum += part[turn][unit][w];
                 turn ^= 1;
             }
         }
         const float r = root_of(sum, a);
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) finish8<T>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r);
+        for (int k = 0; k < CHUNKS; ++k) finish8<T, WHOLE>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r);
     }
 }
 
@@ -159,10 +165,10 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
         const int64_t token = row / a.heads;
         const int head = (int)(row - token * a.heads);
         auto load = [&](int c, float (&s)[kVec]) {
-            load8<T>(at<const T>(a.x, token, head), c, a.channels, s);
+            load8<T, false>(at<const T>(a.x, token, head), c, a.channels, s);
             if (!a.add.p) return;
             float more[kVec];
-            load8<T>(at<const T>(a.add, token, head), c, a.channels, more);
+            load8<T, false>(at<const T>(a.add, token, head), c, a.channels, more);
 #pragma unroll
             for (int e = 0; e < kVec; ++e) s[e] += more[e];
         };
@@ -183,7 +189,7 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
         const int64_t padded = blocks_of(a.channels) * kBlockCols;        // whole groups of lanes look for a block's largest
         for (int c = threadIdx.x * kVec; c < padded; c += kWideThreads * kVec) {
             load(c, s);
-            finish8<T>(a, token, head, c, true, s, r);
+            finish8<T, false>(a, token, head, c, true, s, r);
         }
     }
 }
@@ -191,7 +197,9 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
 template <typename T, int LANES, int CHUNKS>
 void norm_go(const NormArgs& a, hipStream_t st) {
     constexpr int64_t units = LANES > kThreads ? 1 : kThreads / LANES;
-    norm_kernel<T, LANES, CHUNKS><<<(unsigned)std::min((a.rows + units - 1) / units, kMostGroups), LANES > kThreads ? LANES : kThreads, 0, st>>>(a);
+    const unsigned groups = (unsigned)std::min((a.rows + units - 1) / units, kMostGroups);
+    if (a.channels % kVec == 0) norm_kernel<T, true, LANES, CHUNKS><<<groups, LANES > kThreads ? LANES : kThreads, 0, st>>>(a);
+    else norm_kernel<T, false, LANES, CHUNKS><<<groups, LANES > kThreads ? LANES : kThreads, 0, st>>>(a);
 }
 
 template <typename T>
@@ -200,11 +208,13 @@ void norm_launch(const NormArgs& a, hipStream_t st) {
     switch (s.lanes) {
         case 16: norm_go<T, 16, 1>(a, st); break;
         case 32: norm_go<T, 32, 1>(a, st); break;
-        case 64: s.chunks == 1 ? norm_go<T, 64, 1>(a, st) : norm_go<T, 64, 2>(a, st); break;
-        case 256: s.chunks == 1 ? norm_go<T, 256, 1>(a, st) : norm_go<T, 256, 2>(a, st); break;
-        case 512: norm_go<T, 512, 2>(a, st); break;
+        case 64: norm_go<T, 64, 1>(a, st); break;
+        case 128: norm_go<T, 128, 1>(a, st); break;
+        case 256: norm_go<T, 256, 1>(a, st); break;
+        case 512: s.chunks == 1 ? norm_go<T, 512, 1>(a, st) : norm_go<T, 512, 2>(a, st); break;
         default:
-            if (s.chunks) norm_go<T, 1024, 2>(a, st);
+            if (s.chunks == 1) norm_go<T, 1024, 1>(a, st);
+            else if (s.chunks) norm_go<T, 1024, 2>(a, st);
             else norm_wide_kernel<T><<<(unsigned)std::min(a.rows, kMostGroups), kWideThreads, 0, st>>>(a);
     }
 }
@@ -228,10 +238,10 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantizeArgs a)
         const int64_t row = n <= 0xFFFFFFFFll ? (int64_t)((uint32_t)(on ? u : 0) / (uint32_t)a.blocks) : (on ? u : 0) / a.blocks;
         const int b = (int)((on ? u : 0) - row * a.blocks), c = b * kBlockCols + threadIdx.x % kBlockLanes * kVec;
         float v[kVec];
-        load8<T>((const T*)a.x + row * a.x_stride, c, a.cols, v);
+        load8<T, false>((const T*)a.x + row * a.x_stride, c, a.cols, v);
         const float scale = scale_of(max16(finite_top(v)));
         if (on && c < a.cols) {
-            store_codes8(a.codes + row * a.code_stride, c, a.cols, v, 1.0f / scale);
+            store_codes8<false>(a.codes + row * a.code_stride, c, a.cols, v, 1.0f / scale);
             if (c % kBlockCols == 0) a.scales[row * a.scale_stride + b] = scale;
         }
     }
@@ -249,7 +259,7 @@ __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(QuantizeArgs a
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int64_t row = row0 + p * STEP;
-        load8<T>((const T*)a.x + min(row, a.rows - 1) * a.x_stride, c, a.cols, v[p]);
+        load8<T, false>((const T*)a.x + min(row, a.rows - 1) * a.x_stride, c, a.cols, v[p]);
     }
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) top = fmaxf(top, finite_top(v[p]));
@@ -263,7 +273,7 @@ __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(QuantizeArgs a
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int64_t row = row0 + p * STEP;
-        if (row < a.rows) store_codes8(a.codes + row * a.code_stride, c, a.cols, v[p], by);
+        if (row < a.rows) store_codes8<false>(a.codes + row * a.code_stride, c, a.cols, v[p], by);
     }
     if (threadIdx.x == 0) a.scales[tile_row * a.scale_stride + b] = scale;
 }

@@ -74,6 +74,15 @@ def test_norm_is_the_formula(kind, tokens, channels):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("channels", [120, 136, 250, 264, 504, 520, 1016, 1032, 2040, 2056, 4095, 4104, 8191, 8200, 16383, 16392])
+def test_norm_by_every_number_of_lanes(kind, channels):
+    """On both sides of each number of channels behind which more lanes, more chunks or a second reading take over, with few rows and many."""
+    for tokens in (3, 255, 257):
+        x, add, gain = draw((tokens, channels), 21, kind, 3.0), draw((tokens, channels), 22, kind), draw((channels,), 23)
+        check_norm(x, gain, add, 1e-5, 0.0, *hb().rms_norm(x, gain, add=add, eps=1e-5, total=True, block8=True), kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("tokens,heads,channels", [(1, 1, 64), (5, 14, 64), (3, 32, 128), (2, 5, 80), (7, 3, 96), (4, 2, 256), (1, 2, 300), (50, 32, 600)])
 def test_norm_of_heads_in_rows_of_a_projection(kind, tokens, heads, channels):
     rows = draw((tokens, (heads + 2) * channels + 3), 4, kind)
