@@ -595,7 +595,7 @@ int hr_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block
  * largest of the eight (1.4e-5 of a row's rms over normal deviates, a hundredth of what out's rounding takes) at up to 1.8 times the speed.
  * out may be add (then with the same stride).  HR_ERR_INVALID_ARG on null pointers, bad matrices, strides and overlaps (out, add, the codes and
  * scales of block8 and those of a and w begin at places of their own); HR_ERR_MISMATCH if a and w differ in columns, block8 from y's shape or a gate's half is no multiple
- * of 128; HR_ERR_LEN_RANGE beyond 2^24 - 512 workgroups; no rows of a or of w: a no-op. */
+ * of 128; HR_ERR_LEN_RANGE beyond 2^22 - 512 tiles (the smallest, for a few rows, have 16 x 16 values); no rows of a or of w: a no-op. */
 typedef enum hr_gate { HR_GATE_NONE = 0, HR_GATE_SILU = 1, HR_GATE_GELU = 2 } hr_gate;
 typedef struct hr_matmul_args {
     int32_t dtype;            /* of out and add: HR_F32 or HR_BF16 */

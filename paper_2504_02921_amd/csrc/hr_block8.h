@@ -11,7 +11,8 @@ namespace hr {
 
 constexpr int kBlockCols = HR_BLOCK_COLS;
 constexpr float kE4m3Top = 448.0f, kLeastScale = 1.17549435e-38f;      // 2^-126: its reciprocal is finite
-constexpr int64_t kMaxWorkgroups = (1 << 24) - 512;                    // of a launch
+// Of a launch, whose lanes are counted in 32 bits: workgroups of 256 lanes, and of up to 1024
+constexpr int64_t kMaxWorkgroups = (1 << 24) - 512, kMaxWideWorkgroups = (1 << 22) - 512;
 HR_HD int64_t blocks_of(int64_t n) { return (n + kBlockCols - 1) / kBlockCols; }
 
 // ---- norm

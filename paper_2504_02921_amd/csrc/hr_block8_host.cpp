@@ -138,7 +138,7 @@ int matmul_check(const hr_block8* a, const hr_block8* w, const hr_matmul_args* m
             if (out && out == in) return HR_ERR_INVALID_ARG;
     const MatmulArgs r = matmul_args(*a, *w, *m);
     const MatmulPlan plan = matmul_plan(r);
-    if (matmul_tiles(plan.shape, r, plan.rows) > kMaxWorkgroups) return HR_ERR_LEN_RANGE;
+    if (matmul_tiles(plan.shape, r, plan.rows) > kMaxWideWorkgroups) return HR_ERR_LEN_RANGE;
     return HR_OK;
 }
 

@@ -100,6 +100,13 @@ def test_products_that_are_refused():
     assert product(block8(0, 100), out8=block8(0, 256, at=3)) == hb.HR_OK
 
 
+def test_products_of_more_tiles_than_a_launch_has_are_refused():
+    """A launch counts its lanes in 32 bits: 2^22 workgroups, of 1024 lanes where they are widest, are too many."""
+    assert product(block8(1, 100), block8(1 << 30, 100, 128, at=2), out_stride=1 << 30) == LONG
+    assert product(block8(1 << 30, 100), block8(256 * 256, 100, 128, at=2), out_stride=1 << 16) == LONG
+    assert product(block8(0, 100), block8(1 << 30, 100, 128, at=2), out_stride=1 << 30) == hb.HR_OK
+
+
 @pytest.mark.parametrize("what", ["codes", "scales"])
 def test_matrices_on_the_host_are_refused_before_the_device_is_asked(what):
     import torch

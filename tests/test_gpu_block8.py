@@ -352,6 +352,115 @@ def test_a_feed_forward_layer_step_by_step_and_recorded(m):
         assert all(T.equal(a, b) for a, b in zip(want, (total, out, last, h.scales)))
 
 
+# ---- places far apart ---------------------------------------------------------------------------------------------------
+def same(a, b):
+    if isinstance(a, hb().Block8):
+        return torch().equal(code_bytes(a.codes), code_bytes(b.codes)) and torch().equal(a.scales, b.scales)
+    return torch().equal(a, b)
+
+
+def apart(rows, cols, block_rows=1, like=None, stride=1 << 22):
+    """A matrix whose rows are `stride` bytes apart, with the codes of `like`."""
+    T = torch()
+    codes = T.empty((rows - 1) * stride + R.blocks(cols) * 128, dtype=T.uint8, device=DEV).as_strided((rows, cols), (stride, 1))
+    if like is not None:
+        codes.copy_(code_bytes(like.codes))
+    scales = T.empty((R.blocks_of_rows(rows, block_rows), R.blocks(cols)), device=DEV) if like is None else like.scales
+    return hb().Block8(codes, scales, block_rows)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_heads_past_four_gib(kind):
+    T = torch()
+    place = lambda: T.empty((1 << 32) + (1 << 30) + 300, dtype=tdt(kind), device=DEV).as_strided((3, 2, 300), (1 << 31, 1 << 30, 1))      # noqa: E731
+    x, add, gain = draw((3, 2, 300), 70, kind), draw((3, 2, 300), 71, kind), draw((300,), 72)
+    far = [place() for _ in range(3)]
+    far[0].copy_(x)
+    out, total, _ = hb().rms_norm(x, gain, add=add, total=True)
+    hb().rms_norm(far[0], gain, add=add, total=far[1], out=far[2])
+    assert T.equal(far[1], total) and T.equal(far[2], out)
+
+
+def test_codes_past_four_gib():
+    x = draw((1100, 300), 73)
+    q = apart(1100, 300)
+    assert same(hb().rms_norm(x, out=None, block8=q)[2], hb().rms_norm(x, out=None, block8=True)[2])
+    assert same(hb().block_quantize(x, out=q), hb().block_quantize(x))
+    q = apart(1100, 300, 128)
+    assert same(hb().block_quantize(x, 128, out=q), hb().block_quantize(x, 128))
+    rows = torch().empty((1099 << 21) + 300, device=DEV).as_strided((1100, 300), (1 << 21, 1))
+    rows.copy_(x)
+    assert same(hb().block_quantize(rows), hb().block_quantize(x))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "block8"])
+@pytest.mark.parametrize("m,n,stride", [(20, 1152, 1 << 22), (1100, 1152, 1 << 22), (16640, 4096, 1 << 19)])
+def test_products_past_four_gib(kind, m, n, stride):
+    T, k = torch(), 300
+    a, w = matrix(m, k, 1, 74), matrix(n, k, 128, 75)
+    fa, fw = apart(m, k, 1, a, stride if m > 1000 else 1 << 22), apart(n, k, 128, w)
+    if kind == "block8":
+        assert same(hb().block_matmul(fa, fw, block8=apart(m, n, stride=stride)), hb().block_matmul(a, w, block8=True))
+        return
+    out = T.empty((m - 1) * (stride >> 1) + n, dtype=tdt(kind), device=DEV).as_strided((m, n), (stride >> 1, 1))
+    add = draw((m, n), 76, kind)
+    assert same(hb().block_matmul(fa, fw, add=add, out=out), hb().block_matmul(a, w, add=add))
+
+
+# ---- several at once ----------------------------------------------------------------------------------------------------
+def test_layers_from_two_threads_on_streams_of_their_own():
+    """Nothing is kept between calls, so calls of several host threads at once give the bits of the same calls alone."""
+    import threading
+    T, H = torch(), hb()
+    up, down = H.block_quantize(draw((512, 700), 80), 128), H.block_quantize(draw((700, 256), 81), 128)
+    xs = [draw((m, 700), 82 + m, "bf16") for m in (3, 290)]
+
+    def layer(x):
+        _, total, q = H.rms_norm(x, out=None, total=True, block8=True)
+        return H.block_matmul(H.block_matmul(q, up, gate="gelu", block8=True), down, add=total)
+
+    want = [layer(x) for x in xs]
+    T.cuda.synchronize()
+    got = [[], []]
+
+    def work(i):
+        with T.cuda.stream(T.cuda.Stream()):
+            got[i] = [layer(xs[i]) for _ in range(20)]
+            T.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert all(len(g) == 20 and all(T.equal(y, want[i]) for y in g) for i, g in enumerate(got))
+
+
+def test_two_branches_of_one_recording():
+    """Two products on two streams of one recording, each with a second launch for its last rows, replayed on other values."""
+    T, H = torch(), hb()
+    m, n, k = 16640, 4096, 300
+    a, w = matrix(m, k, 1, 84), [matrix(n, k, 128, s) for s in (85, 86)]
+    outs = [T.empty((m, n), dtype=T.bfloat16, device=DEV) for _ in w]
+    for i in range(2):
+        H.block_matmul(a, w[i], out=outs[i])
+    T.cuda.synchronize()
+    graph, side = T.cuda.CUDAGraph(), T.cuda.Stream()
+    with T.cuda.graph(graph):
+        side.wait_stream(T.cuda.current_stream())
+        H.block_matmul(a, w[0], out=outs[0])
+        with T.cuda.stream(side):
+            H.block_matmul(a, w[1], out=outs[1])
+        T.cuda.current_stream().wait_stream(side)
+    for seed in (87, 88):
+        fresh = matrix(m, k, 1, seed)
+        a.codes.copy_(fresh.codes)
+        a.scales.copy_(fresh.scales)
+        want = [H.block_matmul(fresh, x) for x in w]
+        [o.zero_() for o in outs]
+        graph.replay()
+        T.cuda.synchronize()
+        assert all(T.equal(x, y) for x, y in zip(want, outs))
+
+
 # ---- refusals of the binding --------------------------------------------------------------------------------------------
 def test_wrong_tensors_are_refused():
     T, H = torch(), hb()
