@@ -1,13 +1,14 @@
 """End-to-end walk through the library on one GPU: prefill a few documents into a paged pool, score every (query,
-document) pair with only the query tokens run through the layers, pick each query's best candidates, run one layer's
-rotary positions and attention over the same pool, move a document to pinned host memory and back (16-bit records, then 4-bit ones).  Random weights and token ids; run as `python -m paper_2504_02921_amd.demo`."""
+document) pair with only the query tokens run through the layers, pick each query's best candidates, run one layer operator by operator
+(norms, projections in 8 bits, rotary positions, attention over the same pool), move a document to pinned host memory and back (16-bit records, then 4-bit ones).  Random weights and token ids; run as `python -m paper_2504_02921_amd.demo`."""
 
 import numpy as np
 
 
 def layer_of_the_callers(pool, cfg, docs, doc_pages, query_lens, window: int = 64):
-    """One layer as a caller runs it whose model hr_rerank_score does not cover: rotary positions, tables built on the device, attention with a
-    window over the documents' pages (layer 0).  Every document gets one query.  Returns the largest difference from plain torch operations."""
+    """One layer as a caller runs it whose model hr_rerank_score does not cover: norms, projections in 8 bits, rotary positions, tables built on the device,
+    attention with a window over the documents' pages (layer 0), a gated feed-forward.  Every document gets one query.  Returns the attention's largest
+    difference from plain torch operations, and the projections' distance from fp32 ones with the weights as they were, relative to what those give."""
     import torch
 
     from . import binding as hb
@@ -19,9 +20,26 @@ def layer_of_the_callers(pool, cfg, docs, doc_pages, query_lens, window: int = 6
     tables = hb.PairTables(pool, n, tokens, max(n_pages), n_q_heads=cfg.n_q_heads)
     tables.build(listed, i32(np.arange(n)), i32(query_lens))
     gen = torch.Generator(device=dev).manual_seed(0)
-    q, k, v = (torch.randn((tokens, heads, cfg.head_dim), generator=gen, device=dev, dtype=torch.bfloat16) for heads in (cfg.n_q_heads, cfg.n_kv_heads, cfg.n_kv_heads))
+    normal = lambda *shape: torch.randn(shape, generator=gen, device=dev)                  # noqa: E731
+    heads = cfg.n_q_heads * cfg.head_dim
+    plain = [normal(rows, cols) * cols ** -0.5 for rows, cols in ((cfg.qkv_out, cfg.hidden), (cfg.hidden, heads), (2 * cfg.ffn, cfg.hidden), (cfg.hidden, cfg.ffn))]
+    qkv_w, out_w, up_w, down_w = (hb.block_quantize(w, hb.BLOCK_COLS) for w in plain)
+    gains = 1 + 0.1 * normal(2, cfg.hidden)
+    x = normal(tokens, cfg.hidden).bfloat16()
+
+    rows = hb.block_matmul(hb.rms_norm(x, gains[0], eps=cfg.rms_eps, out=None, block8=True)[2], qkv_w)
+    q, k, v = (part.unflatten(1, (-1, cfg.head_dim)) for part in rows.split([heads, cfg.n_kv_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim], 1))
     q, k = hb.Rope(cfg.head_dim, cfg.rope_base).apply(tables.tok_pos, q, k)
     out = hb.pair_attention(pool, 0, tables, q, k, v, window=window)
+    x2 = hb.block_matmul(hb.block_quantize(out.flatten(1)), out_w, add=x)
+    up = hb.block_matmul(hb.rms_norm(x2, gains[1], eps=cfg.rms_eps, out=None, block8=True)[2], up_w, gate="silu", block8=True)
+    y = hb.block_matmul(up, down_w, add=x2)
+
+    normed = lambda s, gain: s * (s.square().mean(-1, keepdim=True) + cfg.rms_eps).rsqrt() * gain      # noqa: E731
+    s = x.float() + out.flatten(1).float() @ plain[1].t()
+    gate, lin = (normed(s, gains[1]) @ plain[2].t()).chunk(2, 1)
+    s = s + (gate * torch.sigmoid(gate) * lin) @ plain[3].t()
+    away = max(float((a.float() - b).norm() / b.norm()) for a, b in ((rows, normed(x.float(), gains[0]) @ plain[0].t()), (y, s)))
 
     gap, t0 = 0.0, 0
     for doc, pages, m in zip(docs, doc_pages, query_lens):
@@ -32,7 +50,7 @@ def layer_of_the_callers(pool, cfg, docs, doc_pages, query_lens, window: int = 6
         s = s.masked_fill((behind < 0) | (behind >= window), float("-inf"))
         gap = max(gap, float((torch.einsum("hij,jhd->ihd", s.softmax(-1), values) - out[t0:t0 + m].float()).abs().max()))
         t0 += m
-    return gap
+    return gap, away
 
 
 def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int = 24, top_k: int = 2, verbose: bool = True):
@@ -71,7 +89,7 @@ def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int
     torch.cuda.synchronize()
     gap = float((scores - full).abs().max())
 
-    layer_gap = layer_of_the_callers(pool, cfg, docs, doc_pages, [query_len] * n_docs)
+    layer_gap, layer_away = layer_of_the_callers(pool, cfg, docs, doc_pages, [query_len] * n_docs)
 
     # host tier: evict document 0 to pinned host memory, free its pages, bring it back at other pages
     rec = torch.empty(pages_per_doc * pool.page_record_bytes, dtype=torch.uint8, pin_memory=True)
@@ -103,7 +121,8 @@ def main(n_queries: int = 3, n_docs: int = 6, doc_len: int = 200, query_len: int
             print(f"query {q}: best documents {best[q].tolist()}  scores {[round(float(scores[q * n_docs + int(d)]), 4) for d in best[q]]}")
         print(f"max |reuse - full recompute| = {gap:.2e}; scores after the host-tier round trip identical: {same}; "
               f"after a round trip of one document in 4 bits they move by at most {change4:.2e}")
-        print(f"a layer of the caller's own (rotary positions, windowed attention over the pool) differs from plain operations by at most {layer_gap:.2e}")
+        print(f"a layer of the caller's own: windowed attention over the pool differs from plain operations by at most {layer_gap:.2e}, projections in 8 bits "
+              f"from fp32 ones by {100 * layer_away:.1f} %")
     model.close()
     pool.close()
     return scores.cpu().numpy(), best.cpu().numpy(), gap, same

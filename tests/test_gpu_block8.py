@@ -461,6 +461,26 @@ def test_two_branches_of_one_recording():
         assert all(T.equal(x, y) for x, y in zip(want, outs))
 
 
+def test_the_demos_layer_runs():
+    """Norms, projections, rotary positions and attention in one layer, over a pool with documents of several lengths.  Rounding both operands of a
+    product to E4M3 moves it by 2^-5 of itself or so (half a step of 2^-4, uniform over it: 2^-4 / 3^0.5 each at most); the gated branch multiplies two such."""
+    from paper_2504_02921_amd import demo, workloads
+    import numpy
+    T, cfg, rng = torch(), workloads.ModelCfg("layer", 1, 256, 4, 2, 64, 384, 500, 1e6, 1e-6, dtype="bf16"), numpy.random.default_rng(3)
+    docs = [rng.integers(0, cfg.vocab, n).astype(numpy.int32) for n in (40, 130)]
+    pool = hb().KVPool(1, cfg.n_kv_heads, cfg.head_dim, 16, "bf16", DEV)
+    model = hb().Model(cfg, workloads.SeededWeights(cfg, seed=1, std=0.05), DEV)
+    try:
+        pages = [pool.alloc(-(-len(d) // hb().PAGE_TOKENS)) for d in docs]
+        model.doc_prefill(pool, docs, pages)
+        gap, away = demo.layer_of_the_callers(pool, cfg, docs, pages, [5, 9])
+        T.cuda.synchronize()
+        assert numpy.isfinite(gap) and 0 < away < 0.25
+    finally:
+        model.close()
+        pool.close()
+
+
 # ---- refusals of the binding --------------------------------------------------------------------------------------------
 def test_wrong_tensors_are_refused():
     T, H = torch(), hb()
