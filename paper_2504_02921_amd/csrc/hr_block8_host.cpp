@@ -43,10 +43,10 @@ int block8_check(const hr_block8* b, int block_rows) {
     return HR_OK;
 }
 
-// Lanes of a head and, for each, chunks of 8 channels (0: as many as there are, read twice).  One chunk wherever a workgroup has the lanes: with two, the
-// loads wait for each other's registers (8000 x 4096 bf16 with sums and codes by 512 lanes 49 us, by 256 lanes of two chunks 52; 4 rows 3.3 and 4.2).  Of
-// 1024 lanes only two workgroups fit a compute unit, so rows that fill the chip take 512 lanes of two chunks instead (8000 x 8192 95 us for 110, 65 rows
-// 4.6 for 4.1).
+// Lanes of a head and, for each, chunks of 8 channels (0: as many as there are, read twice).  One chunk wherever a workgroup of 512 has the lanes (bf16, sums
+// and codes: 8000 x 4096 by 512 lanes 45 us, by 256 lanes of two chunks 46, by 1024 74; 4 rows 3.2, 3.5, 3.4).  Of 1024 lanes only two workgroups fit a compute
+// unit, so rows that fill the chip take 512 lanes of two chunks (8000 x 8192 84 us for 110, fp32 65 x 5003 5.0 for 4.4), and 1024 of two where that is needed
+// (8000 x 14336 149 us, by 512 lanes of four chunks 149, fp32 286 and 304).
 NormShape norm_shape(int channels, int64_t rows) {
     for (int lanes : {16, 32, 64, 128, 256, 512})
         if (channels <= lanes * 8) return {lanes, 1};

@@ -1,7 +1,12 @@
 // The norm of a residual stream with its addition, and codes with scales (hr_rms_norm, hr_block_quantize).
 //
 // y = s / sqrt(mean(s^2) + eps) * (gain + offset), s = x + add: one pass over a head whose channels stay in registers between the sum of their squares and
-// what is made of them, so every input is read and every output written once.  What bounds all of it is those bytes.
+// what is made of them, so every input is read and every output written once.  A block of 128 channels has its scale from 16 lanes of a row (three lane
+// swaps away), and its codes leave in 8 bytes a lane.  All values and sums are fp32; out and total are rounded once each.
+//
+// What bounds it is those bytes, if everything is requested before anything is waited for and addresses are scalar: bf16, sums and codes written, 12800 x 4096
+// 70 us (5.3 TB/s; a copy of 4 GiB reaches 4.8 read and written), 12800 x 896 15.4 (5.2), 25600 x 32 heads of 128 76 (5.5), fp32 3000 x 4096 39 (5.0); of
+// 65 x 896 (3.0 us) the launch and one way to memory and back.  bf16 rows that begin at odd elements: 8000 x 5003 93 us (3.0).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -33,20 +38,24 @@ struct NormArgs {
 template <typename T>
 __device__ __forceinline__ T* at(const NormSide& s, int64_t token, int head) { return (T*)s.p + token * s.ts + head * s.hs; }
 
-// Channels c .. c + 7, those behind the head's last one as zeros.  WHOLE: the number of channels is a multiple of 8
+// Channels c .. c + 7 as they lie there.  WHOLE: the number of channels is a multiple of 8; a lane behind the last one has others then, which must not count,
+// else those behind the last one are zeros
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void load8(const T* p, int c, int channels, float (&v)[kVec]) {
+__device__ __forceinline__ Loose<T, kVec> load8(const T* p, int c, int channels) {
+    if constexpr (WHOLE) return *(const Loose<T, kVec>*)(p + (c < channels ? c : 0));
+    Loose<T, kVec> w;
     if (c + kVec <= channels) {
-        const Loose<T, kVec> w = *(const Loose<T, kVec>*)(p + c);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = to_float<T>(w.w[e]);
-    } else if (WHOLE || c >= channels) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = 0.0f;
+        w = *(const Loose<T, kVec>*)(p + c);
     } else {
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = c + e < channels ? to_float<T>(p[c + e]) : 0.0f;
+        for (int e = 0; e < kVec; ++e) w.w[e] = c + e < channels ? p[c + e] : (T)0.0f;
     }
+    return w;
+}
+template <typename T>
+__device__ __forceinline__ void values8(const Loose<T, kVec>& w, float (&v)[kVec]) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = to_float<T>(w.w[e]);
 }
 template <typename T, bool WHOLE>
 __device__ __forceinline__ void store8(T* p, int c, int channels, const float (&v)[kVec]) {
@@ -76,24 +85,28 @@ __device__ __forceinline__ void store_codes8(uint8_t* p, int c, int cols, const 
 
 // What becomes of eight channels of a head; 16 lanes in a row come here together for a block of 128
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float r) {
+__device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float r, const Loose<float, kVec>& gain) {
     if (c / kBlockCols * kBlockCols >= a.channels) return;
+    const bool any = c < a.channels;
     float y[kVec];
-    if (a.gain) load8<float, WHOLE>(a.gain, c, a.channels, y);
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) y[e] = s[e] * r * (a.gain ? y[e] + a.offset : 1.0f);
+    for (int e = 0; e < kVec; ++e) y[e] = s[e] * r;
+    if (a.gain) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) y[e] *= gain.w[e] + a.offset;
+    }
     if (a.codes) {
-        if (c + kVec > a.channels)
+        if (!WHOLE && c + kVec > a.channels)
 #pragma unroll
             for (int e = 0; e < kVec; ++e)
-                if (WHOLE || c + e >= a.channels) y[e] = 0.0f;    // an infinite 1 / root makes NaN of them
-        const float scale = scale_of(max16(finite_top(y)));
-        if (on && c < a.channels) {
+                if (c + e >= a.channels) y[e] = 0.0f;             // an infinite 1 / root makes NaN of them
+        const float scale = scale_of(max16(any ? finite_top(y) : 0.0f));
+        if (on && any) {
             store_codes8<WHOLE>(a.codes + token * a.code_stride, c, a.channels, y, 1.0f / scale);
             if (c % kBlockCols == 0) a.scales[token * a.scale_stride + c / kBlockCols] = scale;
         }
     }
-    if (on && c < a.channels) {
+    if (on && any) {
         if (a.total.p) store8<T, WHOLE>(at<T>(a.total, token, head), c, a.channels, s);
         if (a.out.p) store8<T, WHOLE>(at<T>(a.out, token, head), c, a.channels, y);
     }
@@ -104,10 +117,9 @@ __device__ __forceinline__ float root_of(float squares, const NormArgs& a) {
     return m == 0.0f ? 0.0f : rsqrtf(m);
 }
 
-// LANES lanes have a head, CHUNKS times 8 channels each.  Two workgroups of 1024 lanes share a compute unit if a lane has 64 registers, and one loads while
-// the other stores: bf16 is held to that (8000 x 14336 with sums and codes 191 to 166 us, 4 rows 5.0 to 5.7); fp32 would spill (284 to 374 us)
+// LANES lanes have a head, CHUNKS times 8 channels each
 template <typename T, bool WHOLE, int LANES, int CHUNKS>
-__global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads, sizeof(T) == 2 && LANES == 1024 && CHUNKS == 2 ? 8 : 1) norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kernel(NormArgs a) {
     constexpr int UNITS = LANES > kThreads ? 1 : kThreads / LANES, WAVES = LANES / 64;
     __shared__ float part[2][UNITS][LANES > 64 ? WAVES : 1];
     const int lane = threadIdx.x % LANES, unit = threadIdx.x / LANES;
@@ -121,21 +133,37 @@ __global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads, sizeof(T)
             token = a.rows <= 0xFFFFFFFFll ? (int64_t)((uint32_t)row / (uint32_t)a.heads) : row / a.heads;
             head = (int)(row - token * a.heads);
         }
-        float s[CHUNKS][kVec], more[CHUNKS][kVec];
+        if constexpr (LANES >= 64) {                     // the same in a wavefront's lanes: scalar addresses (tokens are at most 2^30)
+            token = __builtin_amdgcn_readfirstlane((int)token);
+            head = __builtin_amdgcn_readfirstlane(head);
+        }
+        // everything is requested before anything is waited for
+        Loose<T, kVec> x[CHUNKS], add[CHUNKS];
+        Loose<float, kVec> gain[CHUNKS];
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) load8<T, WHOLE>(at<const T>(a.x, token, head), (k * LANES + lane) * kVec, a.channels, s[k]);
+        for (int k = 0; k < CHUNKS; ++k) x[k] = load8<T, WHOLE>(at<const T>(a.x, token, head), (k * LANES + lane) * kVec, a.channels);
         if (a.add.p) {
 #pragma unroll
-            for (int k = 0; k < CHUNKS; ++k) load8<T, WHOLE>(at<const T>(a.add, token, head), (k * LANES + lane) * kVec, a.channels, more[k]);
+            for (int k = 0; k < CHUNKS; ++k) add[k] = load8<T, WHOLE>(at<const T>(a.add, token, head), (k * LANES + lane) * kVec, a.channels);
+        }
+        if (CHUNKS == 1 && a.gain) gain[0] = load8<float, WHOLE>(a.gain, lane * kVec, a.channels);
+        float s[CHUNKS][kVec];
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) values8<T>(x[k], s[k]);
+        if (a.add.p) {
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k)
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) s[k][e] += to_float<T>(add[k].w[e]);
         }
         float sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k)
+        for (int k = 0; k < CHUNKS; ++k) {
+            float part = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) {
-                if (a.add.p) s[k][e] += more[k][e];
-                sum = fmaf(s[k][e], s[k][e], sum);
-            }
+            for (int e = 0; e < kVec; ++e) part = fmaf(s[k][e], s[k][e], part);
+            sum += !WHOLE || (k * LANES + lane) * kVec < a.channels ? part : 0.0f;
+        }
         if constexpr (LANES <= 32) {
             sum = sum16(sum);
             if constexpr (LANES == 32) sum += __shfl_xor(sum, 16, 64);
@@ -152,7 +180,10 @@ __global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads, sizeof(T)
         }
         const float r = root_of(sum, a);
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) finish8<T, WHOLE>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r);
+        for (int k = 0; k < CHUNKS; ++k) {
+            if (CHUNKS > 1 && a.gain) gain[k] = load8<float, WHOLE>(a.gain, (k * LANES + lane) * kVec, a.channels);
+            finish8<T, WHOLE>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r, gain[k]);
+        }
     }
 }
 
@@ -165,12 +196,11 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
         const int64_t token = row / a.heads;
         const int head = (int)(row - token * a.heads);
         auto load = [&](int c, float (&s)[kVec]) {
-            load8<T, false>(at<const T>(a.x, token, head), c, a.channels, s);
+            values8<T>(load8<T, false>(at<const T>(a.x, token, head), c, a.channels), s);
             if (!a.add.p) return;
-            float more[kVec];
-            load8<T, false>(at<const T>(a.add, token, head), c, a.channels, more);
+            const Loose<T, kVec> add = load8<T, false>(at<const T>(a.add, token, head), c, a.channels);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) s[e] += more[e];
+            for (int e = 0; e < kVec; ++e) s[e] += to_float<T>(add.w[e]);
         };
         float s[kVec], sum = 0.0f;
         for (int c = threadIdx.x * kVec; c < a.channels; c += kWideThreads * kVec) {
@@ -189,7 +219,9 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
         const int64_t padded = blocks_of(a.channels) * kBlockCols;        // whole groups of lanes look for a block's largest
         for (int c = threadIdx.x * kVec; c < padded; c += kWideThreads * kVec) {
             load(c, s);
-            finish8<T, false>(a, token, head, c, true, s, r);
+            Loose<float, kVec> gain;
+            if (a.gain) gain = load8<float, false>(a.gain, c, a.channels);
+            finish8<T, false>(a, token, head, c, true, s, r, gain);
         }
     }
 }
@@ -227,8 +259,8 @@ struct QuantizeArgs {
     int32_t cols, blocks;            // blocks of 128 columns
 };
 
-// Rows of activations: 16 lanes have 128 columns of a row
-template <typename T>
+// Rows of activations: 16 lanes have 128 columns of a row.  12800 x 4096 bf16: 32 us (4.9 TB/s)
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantizeArgs a) {
     constexpr int UNITS = kThreads / kBlockLanes;
     const int64_t n = a.rows * a.blocks;
@@ -238,32 +270,34 @@ __global__ void __launch_bounds__(kThreads) quantize_rows_kernel(QuantizeArgs a)
         const int64_t row = n <= 0xFFFFFFFFll ? (int64_t)((uint32_t)(on ? u : 0) / (uint32_t)a.blocks) : (on ? u : 0) / a.blocks;
         const int b = (int)((on ? u : 0) - row * a.blocks), c = b * kBlockCols + threadIdx.x % kBlockLanes * kVec;
         float v[kVec];
-        load8<T, false>((const T*)a.x + row * a.x_stride, c, a.cols, v);
-        const float scale = scale_of(max16(finite_top(v)));
+        values8<T>(load8<T, WHOLE>((const T*)a.x + row * a.x_stride, c, a.cols), v);
+        const float scale = scale_of(max16(!WHOLE || c < a.cols ? finite_top(v) : 0.0f));
         if (on && c < a.cols) {
-            store_codes8<false>(a.codes + row * a.code_stride, c, a.cols, v, 1.0f / scale);
+            store_codes8<WHOLE>(a.codes + row * a.code_stride, c, a.cols, v, 1.0f / scale);
             if (c % kBlockCols == 0) a.scales[row * a.scale_stride + b] = scale;
         }
     }
 }
 
-// Weights: a workgroup has a tile of 128 x 128, its lanes 8 columns of every 16th row
-template <typename T>
+// Weights: a workgroup has a tile of 128 x 128, its lanes 8 columns of every 16th row, all eight of them under way at once and kept in registers until the
+// tile's largest is known.  28672 x 4096 bf16: 63 us (5.6 TB/s)
+template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(QuantizeArgs a) {
     constexpr int STEP = kThreads / kBlockLanes, PASSES = kBlockCols / STEP;
     __shared__ float tops[kThreads / 64];
     const int64_t tile_row = blockIdx.x / a.blocks, b = blockIdx.x % a.blocks;
     const int c = (int)b * kBlockCols + threadIdx.x % kBlockLanes * kVec;
     const int64_t row0 = tile_row * kBlockCols + threadIdx.x / kBlockLanes;
+    Loose<T, kVec> x[PASSES];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) x[p] = load8<T, WHOLE>((const T*)a.x + min(row0 + p * STEP, a.rows - 1) * a.x_stride, c, a.cols);
     float v[PASSES][kVec], top = 0.0f;
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
-        const int64_t row = row0 + p * STEP;
-        load8<T, false>((const T*)a.x + min(row, a.rows - 1) * a.x_stride, c, a.cols, v[p]);
+        values8<T>(x[p], v[p]);
+        top = fmaxf(top, finite_top(v[p]));
     }
-#pragma unroll
-    for (int p = 0; p < PASSES; ++p) top = fmaxf(top, finite_top(v[p]));
-    top = wave_max(top);
+    top = wave_max(!WHOLE || c < a.cols ? top : 0.0f);
     if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
     __syncthreads();
 #pragma unroll
@@ -273,9 +307,18 @@ __global__ void __launch_bounds__(kThreads) quantize_tiles_kernel(QuantizeArgs a
 #pragma unroll
     for (int p = 0; p < PASSES; ++p) {
         const int64_t row = row0 + p * STEP;
-        if (row < a.rows) store_codes8<false>(a.codes + row * a.code_stride, c, a.cols, v[p], by);
+        if (row < a.rows) store_codes8<WHOLE>(a.codes + row * a.code_stride, c, a.cols, v[p], by);
     }
     if (threadIdx.x == 0) a.scales[tile_row * a.scale_stride + b] = scale;
+}
+
+template <typename T>
+void quantize_launch(const QuantizeArgs& a, int block_rows, hipStream_t st) {
+    constexpr int64_t units = kThreads / kBlockLanes;
+    const unsigned groups = (unsigned)(block_rows == 1 ? std::min((a.rows * a.blocks + units - 1) / units, kMostGroups) : blocks_of(a.rows) * a.blocks);
+    const auto kernel = block_rows == 1 ? (a.cols % kVec == 0 ? quantize_rows_kernel<T, true> : quantize_rows_kernel<T, false>)
+                                        : (a.cols % kVec == 0 ? quantize_tiles_kernel<T, true> : quantize_tiles_kernel<T, false>);
+    kernel<<<groups, kThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -305,16 +348,8 @@ hipError_t launch_rms_norm(const hr_norm_args& n, hipStream_t st) {
 
 hipError_t launch_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block8& out, hipStream_t st) {
     QuantizeArgs a{x, (uint8_t*)out.codes, out.scales, out.rows, x_stride, out.row_stride, out.scale_stride, out.cols, (int32_t)blocks_of(out.cols)};
-    if (out.block_rows == 1) {
-        constexpr int64_t units = kThreads / kBlockLanes;
-        const unsigned groups = (unsigned)std::min((a.rows * a.blocks + units - 1) / units, kMostGroups);
-        if (dtype == HR_F32) quantize_rows_kernel<float><<<groups, kThreads, 0, st>>>(a);
-        else quantize_rows_kernel<bf16_t><<<groups, kThreads, 0, st>>>(a);
-    } else {
-        const unsigned groups = (unsigned)(blocks_of(a.rows) * a.blocks);
-        if (dtype == HR_F32) quantize_tiles_kernel<float><<<groups, kThreads, 0, st>>>(a);
-        else quantize_tiles_kernel<bf16_t><<<groups, kThreads, 0, st>>>(a);
-    }
+    if (dtype == HR_F32) quantize_launch<float>(a, out.block_rows, st);
+    else quantize_launch<bf16_t>(a, out.block_rows, st);
     return hipGetLastError();
 }
 
