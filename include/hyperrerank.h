@@ -589,7 +589,8 @@ int hr_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block
  *   HR_GATE_SILU   y[m][f] = silu(c[m][f]) c[m][F + f] with F = w->rows / 2 (a multiple of 128): the weights' first half is the gate
  *   HR_GATE_GELU   the same with gelu(z) = z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
  * and out = y + add, rounded once; or block8 = codes and scales of y.
- * a: activations (block_rows 1), w: weights (block_rows 128) with as many columns.  Sums over k and over blocks are fp32.  What the matrix
+ * a: activations (block_rows 1), w: weights (block_rows 128) with as many columns.  Sums over k and over blocks are fp32, and so is a.scale w.scale, which is
+ * formed first: scales whose product passes 3.4e38 give infinities and NaN.  What the matrix
  * instructions round inside a sum over k: with fp32 out and with block8 (whose scales are fp32) nothing but the fp32 sum (codes are multiplied
  * as halves, exactly); with bf16 out and many rows, or where fast is set, the 8-bit instruction's own sum of eight products, which keeps 14 bits of the
  * largest of the eight (1.4e-5 of a row's rms over normal deviates, a hundredth of what out's rounding takes) at up to 1.8 times the speed.

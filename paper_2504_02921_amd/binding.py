@@ -666,7 +666,10 @@ GATES = {None: 0, "silu": 1, "gelu": 2}
 
 class Block8:
     """A matrix in 8 bits (hr_block8): E4M3 codes [rows][cols] (float8_e4m3fn or uint8, rows a multiple of 16 bytes apart) and fp32 scales
-    [ceil(rows / block_rows)][ceil(cols / 128)].  block_rows: 1 for activations, 128 for weights."""
+    [ceil(rows / block_rows)][ceil(cols / 128)].  block_rows: 1 for activations, 128 for weights.  Its tensors can be written, not replaced."""
+
+    codes = property(lambda self: self._codes)
+    scales = property(lambda self: self._scales)
 
     def __init__(self, codes, scales, block_rows: int = 1):
         import torch
@@ -682,7 +685,7 @@ class Block8:
         shape = (-(-rows // block_rows), -(-cols // BLOCK_COLS))
         if tuple(scales.shape) != shape or scales.dtype != torch.float32 or scales.device != dev or (shape[1] > 1 and shape[0] and scales.stride(1) != 1):
             _refuse(f"Block8: scales {shape} float32 on {dev} with adjacent columns, got {tuple(scales.shape)} {scales.dtype} on {scales.device}")
-        self.codes, self.scales, self.block_rows, self.shape, self.device = codes, scales, block_rows, (rows, cols), dev
+        self._codes, self._scales, self.block_rows, self.shape, self.device = codes, scales, block_rows, (rows, cols), dev
         self.c = hr_block8(codes.data_ptr(), scales.data_ptr(), rows, cols, block_rows, stride, scales.stride(0) if shape[0] > 1 else shape[1])
 
     @classmethod
@@ -704,7 +707,7 @@ class Block8:
         codes, scales = new((rows, pitch), dtype=torch.float8_e4m3fn, device=device), new(shape, dtype=torch.float32, device=device)
         self = cls.__new__(cls)              # nothing that __init__ would find wrong
         self.c = hr_block8(codes.data_ptr(), scales.data_ptr(), rows, cols, block_rows, pitch, shape[1])
-        self.codes, self.scales, self.block_rows, self.shape, self.device = codes if pitch == cols else codes[:, :cols], scales, block_rows, (rows, cols), scales.device
+        self._codes, self._scales, self.block_rows, self.shape, self.device = codes if pitch == cols else codes[:, :cols], scales, block_rows, (rows, cols), scales.device
         return self
 
 
@@ -806,6 +809,8 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
     scales of the result instead.  fast: the 8-bit instruction for fp32 results and codes too, whose sums are else exact
     to fp32.  Returns out, or the Block8."""
     import torch
+    if not (isinstance(a, Block8) and isinstance(w, Block8)):
+        _refuse(f"block_matmul: two Block8 expected, got {type(a).__name__} and {type(w).__name__}")
     dev = a.device
     if _elsewhere(dev):
         with torch.cuda.device(dev):
@@ -817,7 +822,7 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
         if N % (2 * BLOCK_COLS):
             raise HrError(HR_ERR_MISMATCH, f"block_matmul: halves of a multiple of {BLOCK_COLS} rows, got {N} rows")
         N //= 2
-    _no_gradients((bias, add, out), "block_matmul")
+    _no_gradients((a.scales, w.scales, bias, add, out), "block_matmul")
     b_p = None if bias is None else _floats(bias, w.shape[0], dev, "block_matmul: bias")
     if block8 is not None and block8 is not False:
         if out is not None or add is not None or N < 1:

@@ -123,6 +123,20 @@ def test_matrices_on_the_host_are_refused_before_the_device_is_asked(what):
         hb.Block8.empty(1 << 31, 64, device="cpu")
 
 
+def test_a_matrix_keeps_its_tensors():
+    """Calls take the places that the matrix began with, so its tensors cannot be replaced under it."""
+    import torch
+    q = hb.Block8(torch.zeros((4, 64), dtype=torch.uint8), torch.ones((4, 1)))
+    for name in ("codes", "scales"):
+        with pytest.raises(AttributeError):
+            setattr(q, name, getattr(q, name).clone())
+    assert q.c.codes == q.codes.data_ptr() and q.c.scales == q.scales.data_ptr()
+    w = hb.Block8(torch.zeros((128, 64), dtype=torch.uint8), torch.ones((1, 1)), 128)
+    for pair in ((q.codes, w), (q, w.codes), (None, w)):
+        with pytest.raises(hb.HrError):
+            hb.block_matmul(*pair)
+
+
 @pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
 def test_every_shape_of_tile_that_a_product_takes_is_tested(tmp_path):
     """The host's choice of tiles, with AddressSanitizer + UBSan: for sizes of all kinds it ends, and what it takes is among what the GPU tests run."""

@@ -525,5 +525,6 @@ def test_wrong_tensors_are_refused():
     refused(lambda: H.block_matmul(a, w, add=x, block8=True))
     refused(lambda: H.block_matmul(a, w, block8=H.Block8.empty(4, 128)))
     refused(lambda: H.block_matmul(a, w, bias=T.zeros(256, device=DEV).requires_grad_()))
+    refused(lambda: H.block_matmul(H.Block8(a.codes, a.scales.clone().requires_grad_()), w))
     with T.no_grad():
         H.rms_norm(x.float().requires_grad_(), draw((64,), 61).requires_grad_())
