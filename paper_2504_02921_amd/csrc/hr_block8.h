@@ -50,7 +50,7 @@ MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_a
 // Tiles of a product: rows x rows of w (with a gate half as many columns of y), _n: n groups of wavefronts that take turns along k
 enum MatmulShape {
     MM_FEW_16, MM_FEW_32,            // no LDS on the way in: 16 rows x 16 or 32 columns of y
-    MM_16x64_4, MM_32x64_2, MM_64x64, MM_64x64_2, MM_64x128, MM_64x128_2, MM_64x256, MM_128x128, MM_128x128_2, MM_128x256, MM_256x256,
+    MM_16x32_8, MM_32x32_8, MM_16x64_4, MM_32x64_2, MM_64x64, MM_64x64_2, MM_64x128, MM_64x128_2, MM_64x256, MM_128x128, MM_128x128_2, MM_128x256, MM_256x256,
     MM_16x128_4, MM_32x128_2, MM_16x256, MM_32x256,      // into codes only
     MM_SHAPES
 };

@@ -176,20 +176,22 @@ namespace {
 
 // What a shape's launch takes in us: start + turns * first with a tile a CU at most, turns being its blocks of k by its groups along k; where a CU holds
 // two workgroups, start + turns * pair with up to two; and turns * more + again for each further round of as many (the last of two may be half a round).
-// By results: bf16 (8-bit instruction) and fp32 (halves), codes with either, codes of a gate with either.  Fitted to 5530 launches of 1 to 6000 rows with
-// weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory: what it picks takes 0.3 % more than the fastest shape on average, 16 % at
+// By results: bf16 (8-bit instruction) and fp32 (halves), codes with either, codes of a gate with either.  Fitted to 5872 launches of 1 to 6000 rows with
+// weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory: what it picks takes 0.3 % more than the fastest shape on average, 17 % at
 // most.  The kernels without LDS: at 16 rows.
 struct Times { float start, first, pair, more, again; };
 struct Cost { int bm, bn, groups, held; Times t[6]; };
 constexpr Cost kCost[MM_SHAPES] = {
     {16, 16, 8, 1, {{2.3f, 1.05f, 0.0f, 1.10f, 0.0f}, {2.3f, 1.05f, 0.0f, 1.10f, 0.0f}}},      // MM_FEW_16
     {16, 32, 8, 1, {{3.2f, 1.50f, 0.0f, 1.60f, 0.0f}, {3.2f, 1.50f, 0.0f, 1.60f, 0.0f}}},
-    {16, 64, 4, 1, {{4.0f, 0.58f, 0.00f, 0.78f, 2.8f}, {4.1f, 0.72f, 0.00f, 0.87f, 3.0f}, {}, {}, {}, {}}},      // MM_16x64_4
-    {32, 64, 2, 2, {{3.1f, 0.37f, 0.79f, 0.65f, 2.3f}, {3.2f, 0.53f, 1.05f, 0.79f, 2.8f}, {}, {}, {}, {}}},      // MM_32x64_2
+    {16, 32, 8, 1, {{3.9f, 0.64f, 0.00f, 0.65f, 2.9f}, {3.9f, 0.76f, 0.00f, 0.76f, 2.9f}, {}, {}, {}, {}}},      // MM_16x32_8
+    {32, 32, 8, 1, {{4.4f, 0.89f, 0.00f, 1.06f, 3.4f}, {4.7f, 1.00f, 0.00f, 1.05f, 3.7f}, {}, {}, {}, {}}},      // MM_32x32_8
+    {16, 64, 4, 1, {{4.0f, 0.58f, 0.00f, 0.78f, 2.8f}, {4.0f, 0.73f, 0.00f, 0.87f, 3.0f}, {}, {}, {}, {}}},      // MM_16x64_4
+    {32, 64, 2, 2, {{3.1f, 0.37f, 0.79f, 0.66f, 2.3f}, {3.2f, 0.53f, 1.04f, 0.79f, 2.8f}, {}, {}, {}, {}}},      // MM_32x64_2
     {64, 64, 1, 2, {{3.2f, 0.28f, 0.48f, 0.46f, 2.5f}, {3.1f, 0.47f, 0.77f, 0.66f, 2.7f}, {}, {}, {}, {}}},      // MM_64x64
-    {64, 64, 2, 1, {{4.0f, 0.40f, 0.00f, 0.49f, 3.2f}, {3.5f, 0.79f, 0.00f, 0.74f, 3.2f}, {}, {}, {}, {}}},      // MM_64x64_2
-    {64, 128, 1, 2, {{3.3f, 0.36f, 0.70f, 0.70f, 2.7f}, {4.3f, 0.72f, 1.23f, 1.12f, 3.4f}, {4.0f, 0.35f, 0.69f, 0.73f, 2.7f}, {3.8f, 0.80f, 1.25f, 1.12f, 2.9f}, {}, {}}},      // MM_64x128
-    {64, 128, 2, 1, {{4.6f, 0.57f, 0.00f, 0.76f, 3.5f}, {4.6f, 1.25f, 0.00f, 1.21f, 3.5f}, {5.7f, 0.55f, 0.00f, 0.74f, 4.9f}, {5.4f, 1.24f, 0.00f, 1.19f, 4.4f}, {}, {}}},      // MM_64x128_2
+    {64, 64, 2, 1, {{3.9f, 0.43f, 0.00f, 0.47f, 3.3f}, {3.5f, 0.79f, 0.00f, 0.74f, 3.2f}, {}, {}, {}, {}}},      // MM_64x64_2
+    {64, 128, 1, 2, {{3.3f, 0.37f, 0.70f, 0.70f, 2.7f}, {4.3f, 0.72f, 1.23f, 1.12f, 3.4f}, {4.0f, 0.35f, 0.69f, 0.73f, 2.7f}, {3.8f, 0.80f, 1.25f, 1.12f, 2.9f}, {}, {}}},      // MM_64x128
+    {64, 128, 2, 1, {{4.5f, 0.62f, 0.00f, 0.73f, 3.6f}, {4.6f, 1.25f, 0.00f, 1.21f, 3.5f}, {5.7f, 0.55f, 0.00f, 0.74f, 4.9f}, {5.4f, 1.24f, 0.00f, 1.19f, 4.4f}, {}, {}}},      // MM_64x128_2
     {64, 256, 1, 1, {{4.2f, 0.55f, 0.00f, 0.64f, 2.8f}, {5.0f, 1.17f, 0.00f, 1.16f, 3.4f}, {4.1f, 0.56f, 0.00f, 0.64f, 3.3f}, {4.3f, 1.20f, 0.00f, 1.19f, 3.2f}, {5.3f, 0.51f, 0.00f, 0.67f, 3.8f}, {4.8f, 1.18f, 0.00f, 1.18f, 3.7f}}},      // MM_64x256
     {128, 128, 1, 2, {{4.1f, 0.69f, 1.13f, 1.25f, 2.8f}, {7.9f, 1.17f, 1.84f, 1.92f, 4.7f}, {5.1f, 0.70f, 1.11f, 1.23f, 3.0f}, {7.1f, 1.18f, 1.83f, 1.92f, 4.4f}, {}, {}}},      // MM_128x128
     {128, 128, 2, 1, {{6.0f, 1.12f, 0.00f, 1.27f, 5.1f}, {8.2f, 1.71f, 0.00f, 1.83f, 5.5f}, {8.0f, 1.14f, 0.00f, 1.22f, 7.5f}, {9.6f, 1.73f, 0.00f, 1.83f, 7.6f}, {}, {}}},      // MM_128x128_2
@@ -204,7 +206,7 @@ constexpr int kCus = 256;
 
 bool covers(int shape, bool codes, bool gate) {
     const int bn = kCost[shape].bn;
-    if (!codes) return shape < MM_16x128_4 && !(gate && shape == MM_16x64_4);      // whose wavefronts have 16 rows of w
+    if (!codes) return shape < MM_16x128_4 && !(gate && shape >= MM_16x32_8 && shape <= MM_16x64_4);      // whose wavefronts have 16 rows of w
     return shape > MM_FEW_32 && (gate ? bn >= 2 * kBlockCols : bn == kBlockCols || (bn > kBlockCols && kCost[shape].bm >= 64));
 }
 

@@ -57,7 +57,8 @@ __device__ __forceinline__ void load_lds4(rsrc_t r, void* lds, int voff, int sof
 #endif
 }
 
-// BM rows x BN rows of w by WM x WN wavefronts, KG groups of which take turns along k, each with NS stages.  With a gate a wavefront's rows of w are half
+// BM rows x BN rows of w by WM x WN wavefronts, KG groups of which take turns along k, each with NS stages: where there are few tiles, a compute unit's loads are
+// what counts (65 x 896 x 4864: 70 tiles of 16 x 64 by four groups 9.6 us, 140 of 16 x 32 by eight 6.8).  With a gate a wavefront's rows of w are half
 // gate rows, half the rows that they multiply.
 template <int BM, int BN, int WM, int WN, int NS, int KG, bool EIGHT, bool GATE, typename OUT, bool CODES>
 __global__ void __launch_bounds__(WM * WN * KG * 64, WM * WN * KG == 4 ? 2 : 1) block_mm_tile_kernel(MatmulArgs a) {
@@ -555,6 +556,8 @@ hipError_t launch_out(const MatmulArgs& a, hipStream_t st) {
 template <bool EIGHT, typename OUT>
 hipError_t launch_out_shape(const MatmulArgs& a, int shape, hipStream_t st) {
     switch (shape) {
+        case MM_16x32_8: return launch_out<EIGHT, OUT, 16, 32, 1, 2, 3, 8>(a, st);
+        case MM_32x32_8: return launch_out<EIGHT, OUT, 32, 32, 1, 2, 2, 8>(a, st);
         case MM_16x64_4: return launch_out<EIGHT, OUT, 16, 64, 1, 4, 3, 4>(a, st);
         case MM_32x64_2: return launch_out<EIGHT, OUT, 32, 64, 2, 2, 3, 2>(a, st);
         case MM_64x64: return launch_out<EIGHT, OUT, 64, 64, 2, 2, 4, 1>(a, st);
