@@ -407,6 +407,26 @@ def test_products_past_four_gib(kind, m, n, stride):
     assert same(hb().block_matmul(fa, fw, add=add, out=out), hb().block_matmul(a, w, add=add))
 
 
+def test_more_rows_than_a_launch_has_workgroups():
+    """1 100 000 rows, a thousand over and over: workgroups walk rows, and every row is the same as alone."""
+    T, n, times = torch(), 1000, 1100
+    few = draw((n, 2056), 77, "bf16")
+    x = few.repeat(times, 1)
+    gain = draw((2056,), 78)
+    out, _, q = hb().rms_norm(x, gain, block8=True)
+    want, _, wq = hb().rms_norm(few, gain, block8=True)
+    whole = lambda t: t.view(times, n, -1)                               # noqa: E731
+    assert (whole(out) == want).all()
+    assert (whole(code_bytes(q.codes)) == code_bytes(wq.codes)).all() and (whole(q.scales) == wq.scales).all()
+    del out
+    q, wq = hb().block_quantize(x, out=q), hb().block_quantize(few)
+    assert (whole(code_bytes(q.codes)) == code_bytes(wq.codes)).all() and (whole(q.scales) == wq.scales).all()
+    w = matrix(100, 2056, 128, 79)
+    y = hb().block_matmul(q, w)
+    for at in (0, 777, times - 1):
+        check_product(wq, w, y[at * n:(at + 1) * n], "bf16")
+
+
 # ---- several at once ----------------------------------------------------------------------------------------------------
 def test_layers_from_two_threads_on_streams_of_their_own():
     """Nothing is kept between calls, so calls of several host threads at once give the bits of the same calls alone."""
@@ -432,6 +452,30 @@ def test_layers_from_two_threads_on_streams_of_their_own():
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert all(len(g) == 20 and all(T.equal(y, want[i]) for y in g) for i, g in enumerate(got))
+
+
+def test_matrices_that_are_let_go_stay_until_their_stream_is_done():
+    """A call on another stream keeps what it reads: memory that the caller lets go while it waits there is not given to anybody else."""
+    T, H = torch(), hb()
+    x, up, busy = draw((300, 900), 90, "bf16"), H.block_quantize(draw((512, 900), 91), 128), T.randn((4096, 4096), device=DEV)
+    want = H.block_matmul(H.block_quantize(x), up)
+    T.cuda.synchronize()
+    side = T.cuda.Stream()
+    with T.cuda.stream(side):
+        for _ in range(20):
+            T.mm(busy, busy)
+    side.wait_stream(T.cuda.current_stream())
+    held = x.clone()
+    q = H.block_quantize(held)
+    side.wait_stream(T.cuda.current_stream())
+    total = H.rms_norm(held, out=False, total=True, stream=side)[1]
+    y = H.block_matmul(q, up, stream=side)
+    places = {held.data_ptr(), q.codes.data_ptr()}
+    del held, q
+    fresh = [T.zeros_like(x), H.Block8.empty(300, 900)]
+    assert not places & {fresh[0].data_ptr(), fresh[1].codes.data_ptr()}
+    T.cuda.synchronize()
+    assert T.equal(total, x) and T.equal(y, want)
 
 
 def test_two_branches_of_one_recording():
