@@ -714,7 +714,7 @@ class Block8:
 def _rows_of(t, shape, like, what: str):
     """(token stride, head stride) of a tensor of `shape`, [tokens][channels] or [tokens][heads][channels], of the type and on the device of `like`."""
     stride = t.stride()
-    if t.shape != shape or t.dtype != like.dtype or t.device != like.device or (shape[-1] > 1 and t.numel() and stride[-1] != 1):
+    if t.shape != shape or (t is not like and (t.dtype != like.dtype or t.device != like.device)) or (shape[-1] > 1 and stride[-1] != 1 and t.numel()):
         _refuse(f"{what}: {tuple(shape)} with adjacent channels, {like.dtype} on {like.device} expected; got {tuple(t.shape)}, strides {stride}, {t.dtype} on {t.device}")
     return stride[0], stride[1] if len(shape) == 3 else 0
 
@@ -752,13 +752,18 @@ def rms_norm(x, gain=None, add=None, eps: float = 1e-6, gain_offset: float = 0.0
     heads = shape[1] if len(shape) == 3 else 1
     if heads < 1 or C_ < 1:
         _refuse(f"rms_norm: heads and channels, got {tuple(shape)}")
-    out = _new(x, stream) if out is True else None if out is False else out
-    total = _new(x, stream) if total is True else None if total is False else total
-    _no_gradients((x, gain, add, out, total), "rms_norm")
+    out, total = None if out is False else out, None if total is False else total
+    _no_gradients((x, gain, add, None if out is True else out, None if total is True else total), "rms_norm")
     x_t, x_h = _rows_of(x, shape, x, "rms_norm: x")
     a_t, a_h = (0, 0) if add is None else _rows_of(add, shape, x, "rms_norm: add")
-    s_t, s_h = (0, 0) if total is None else _rows_of(total, shape, x, "rms_norm: total")
-    o_t, o_h = (0, 0) if out is None else _rows_of(out, shape, x, "rms_norm: out")
+    if total is True:
+        total, s_t, s_h = _new(x, stream), heads * C_, C_
+    else:
+        s_t, s_h = (0, 0) if total is None else _rows_of(total, shape, x, "rms_norm: total")
+    if out is True:
+        out, o_t, o_h = _new(x, stream), heads * C_, C_
+    else:
+        o_t, o_h = (0, 0) if out is None else _rows_of(out, shape, x, "rms_norm: out")
     g_p = None if gain is None else _floats(gain, C_, dev, "rms_norm: gain")
     if block8 is not None and block8 is not False:
         if len(shape) != 2:
@@ -837,12 +842,12 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
         if code is None:
             _refuse(f"block_matmul: float32 or bfloat16, got {dtype}")
         if out is None:
-            out = a.scales.new_empty((M, N), dtype=dtype) if stream is None else _new(a.scales, stream, (M, N), dtype)
-        shape = torch.Size((M, N))
-        if out.dtype != dtype or out.device != dev:
-            _refuse(f"block_matmul: out: {dtype} on {dev} expected, got {out.dtype} on {out.device}")
-        o_t, _ = _rows_of(out, shape, out, "block_matmul: out")
-        d_t, _ = (0, 0) if add is None else _rows_of(add, shape, out, "block_matmul: add")
+            out, o_t = a.scales.new_empty((M, N), dtype=dtype) if stream is None else _new(a.scales, stream, (M, N), dtype), N
+        else:
+            if out.dtype != dtype or out.device != dev:
+                _refuse(f"block_matmul: out: {dtype} on {dev} expected, got {out.dtype} on {out.device}")
+            o_t, _ = _rows_of(out, torch.Size((M, N)), out, "block_matmul: out")
+        d_t, _ = (0, 0) if add is None else _rows_of(add, torch.Size((M, N)), out, "block_matmul: add")
         args = hr_matmul_args(code, GATES[gate], 1 if fast else 0, b_p, None if add is None else add.data_ptr(), out.data_ptr(), d_t, o_t, None)
     check(lib.hr_block_matmul(C.byref(a.c), C.byref(w.c), C.byref(args), _stream_ptr(stream)), "hr_block_matmul")
     if stream is not None:

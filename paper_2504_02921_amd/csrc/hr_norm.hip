@@ -1,7 +1,7 @@
 // The norm of a residual stream with its addition, and codes with scales (hr_rms_norm, hr_block_quantize).
 //
 // y = s / sqrt(mean(s^2) + eps) * (gain + offset), s = x + add: one pass over a head whose channels stay in registers between the sum of their squares and
-// what is made of them, so every input is read and every output written once.  A block of 128 channels has its scale from 16 lanes of a row (three lane
+// what is made of them, so every input is read and every output written once.  A block of 128 channels has its scale from 16 lanes of a row (four lane
 // swaps away), and its codes leave in 8 bytes a lane.  All values and sums are fp32; out and total are rounded once each.
 //
 // What bounds it is those bytes, if everything is requested before anything is waited for and addresses are scalar: bf16, sums and codes written, 12800 x 4096
