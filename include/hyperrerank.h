@@ -590,10 +590,12 @@ int hr_block_quantize(int dtype, const void* x, int64_t x_stride, const hr_block
  *   HR_GATE_GELU   the same with gelu(z) = z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))
  * and out = y + add, rounded once; or block8 = codes and scales of y.
  * a: activations (block_rows 1), w: weights (block_rows 128) with as many columns.  Sums over k and over blocks are fp32, and so is a.scale w.scale, which is
- * formed first: scales whose product passes 3.4e38 give infinities and NaN.  What the matrix
- * instructions round inside a sum over k: with fp32 out and with block8 (whose scales are fp32) nothing but the fp32 sum (codes are multiplied
- * as halves, exactly); with bf16 out and many rows, or where fast is set, the 8-bit instruction's own sum of eight products, which keeps 14 bits of the
- * largest of the eight (1.4e-5 of a row's rms over normal deviates, a hundredth of what out's rounding takes) at up to 1.8 times the speed.
+ * formed first: scales whose product passes 3.4e38 give infinities and NaN.  Codes are multiplied as halves, exactly, so that nothing but fp32 additions
+ * rounds a sum, whatever the result's type.
+ * fast: products may be summed by the 8-bit instruction, at up to 1.8 times the speed, where the tile that M, N and K lead to has it (most have; those
+ * for a few rows may not, so that a row alone and the same row in a batch can differ by what it rounds).  It adds the products of columns 8 i .. 8 i + 7 of a block at
+ * once, each cut off at 2^-13 of the power of two of the largest of them: 7 * 2^-13 of that product at most for every eight columns.  Over normal deviates that is
+ * 1.4e-5 of a row's rms; where large terms cancel it can be more than what is left, in bf16 too.
  * out may be add (then with the same stride).  HR_ERR_INVALID_ARG on null pointers, bad matrices, strides and overlaps (out, add, the codes and
  * scales of block8 and those of a and w begin at places of their own); HR_ERR_MISMATCH if a and w differ in columns, block8 from y's shape or a gate's half is no multiple
  * of 128; HR_ERR_LEN_RANGE beyond 2^22 - 512 tiles (the smallest, for a few rows, have 16 x 16 values); no rows of a or of w: a no-op. */
@@ -601,7 +603,7 @@ typedef enum hr_gate { HR_GATE_NONE = 0, HR_GATE_SILU = 1, HR_GATE_GELU = 2 } hr
 typedef struct hr_matmul_args {
     int32_t dtype;            /* of out and add: HR_F32 or HR_BF16 */
     int32_t gate;             /* hr_gate */
-    int32_t fast;             /* 0; not 0: the 8-bit instruction for every kind of result (see above) */
+    int32_t fast;             /* 0: fp32 sums; not 0: sums by the 8-bit instruction (see above) */
     const float* bias;        /* NULL or device [w->rows] */
     const void* add;          /* NULL or device [a->rows][columns of y]; not with block8 */
     void* out;                /* device, likewise; NULL with block8 */

@@ -811,8 +811,8 @@ def block_matmul(a: Block8, w: Block8, dtype=None, gate: Optional[str] = None, b
     """a w^T of two matrices in 8 bits, activations and weights, with what follows it in a layer (hr_block_matmul): + bias (fp32 [rows of w]), a gate
     ("silu" or "gelu": act(first half of the columns) * second half), + add ([rows of a][columns], of out's type).  dtype: of out, float32 or bfloat16
     (None: out's or add's, else bfloat16); out: a tensor of the caller's, which may be add.  block8 (True, or a Block8 of the caller's): codes and
-    scales of the result instead.  fast: the 8-bit instruction for fp32 results and codes too, whose sums are else exact
-    to fp32.  Returns out, or the Block8."""
+    scales of the result instead.  fast: sums by the 8-bit instruction where the sizes lead to a tile that has it, which cuts what it adds off at 2^-13 of the
+    largest of eight products; else they are fp32 sums of exact products.  Returns out, or the Block8."""
     import torch
     if not (isinstance(a, Block8) and isinstance(w, Block8)):
         _refuse(f"block_matmul: two Block8 expected, got {type(a).__name__} and {type(w).__name__}")

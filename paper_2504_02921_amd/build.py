@@ -14,8 +14,8 @@ LIB = os.path.join(HERE, "libhyperrerank.so")
 
 SOURCES = ["hr_host.cpp", "hr_engine.hip", "hr_kernels_generic.hip", "hr_f32.hip", "hr_gemm_mfma.hip", "hr_attn_mfma.hip", "hr_attn_rows.hip",
            "hr_pair_host.cpp", "hr_pair_entry.hip", "hr_rope.hip", "hr_tables.hip", "hr_pair_attn.hip", "hr_pair_attn_mfma.hip",
-           "hr_block8_host.cpp", "hr_block8_entry.hip", "hr_norm.hip", "hr_block_mm_few.hip", "hr_block_mm_bf16.hip", "hr_block_mm_f32.hip",
-           "hr_block_mm_f32_fast.hip", "hr_block_mm_codes.hip", "hr_block_mm_codes_fast.hip"]
+           "hr_block8_host.cpp", "hr_block8_entry.hip", "hr_norm.hip", "hr_block_mm_few.hip", "hr_block_mm_bf16.hip", "hr_block_mm_bf16_fast.hip",
+           "hr_block_mm_f32.hip", "hr_block_mm_f32_fast.hip", "hr_block_mm_codes.hip", "hr_block_mm_codes_fast.hip"]
 
 # packed-fp32 instruction selection is switched off for all device code.  Kernarg preload: a kernel's first parameters are in scalar registers when
 # a wavefront starts, where a fetch of them is a trip to memory in every launch

@@ -38,7 +38,7 @@ int hr_block_matmul(const hr_block8* a, const hr_block8* w, const hr_matmul_args
     auto launch = [&](const hr::MatmulArgs& part, int shape) {
         if (shape <= hr::MM_FEW_32) return hr::launch_block_matmul_few(part, args->dtype, shape, (hipStream_t)stream);
         if (part.codes) return (part.eight ? hr::launch_block_matmul_codes_fast : hr::launch_block_matmul_codes)(part, shape, (hipStream_t)stream);
-        if (args->dtype == HR_BF16) return hr::launch_block_matmul_bf16(part, shape, (hipStream_t)stream);
+        if (args->dtype == HR_BF16) return (part.eight ? hr::launch_block_matmul_bf16_fast : hr::launch_block_matmul_bf16)(part, shape, (hipStream_t)stream);
         return (part.eight ? hr::launch_block_matmul_f32_fast : hr::launch_block_matmul_f32)(part, shape, (hipStream_t)stream);
     };
     if (plan.rows < m.M) {

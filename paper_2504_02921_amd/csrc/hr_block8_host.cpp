@@ -157,7 +157,7 @@ MatmulArgs matmul_args(const hr_block8& a, const hr_block8& w, const hr_matmul_a
     r.half = m.gate != HR_GATE_NONE ? (int32_t)(w.rows / 2) : 0;
     r.N = r.half > 0 ? r.half : (int32_t)w.rows;
     r.gate = m.gate;
-    r.eight = m.fast != 0 || (!m.block8 && m.dtype == HR_BF16);
+    r.eight = m.fast != 0;
     r.bias = m.bias;
     r.add = m.add;
     r.out = m.out;
@@ -176,7 +176,7 @@ namespace {
 
 // What a shape's launch takes in us: start + turns * first with a tile a CU at most, turns being its blocks of k by its groups along k; where a CU holds
 // two workgroups, start + turns * pair with up to two; and turns * more + again for each further round of as many (the last of two may be half a round).
-// By results: bf16 (8-bit instruction) and fp32 (halves), codes with either, codes of a gate with either.  Fitted to 5872 launches of 1 to 6000 rows with
+// By results: out with the 8-bit instruction (fitted into bf16) and with halves (into fp32), codes with either, codes of a gate with either.  Fitted to 5872 launches of 1 to 6000 rows with
 // weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory: what it picks takes 0.3 % more than the fastest shape on average, 17 % at
 // most.  The kernels without LDS: at 16 rows.
 struct Times { float start, first, pair, more, again; };

@@ -174,6 +174,7 @@ __device__ __forceinline__ void store_block4(const MatmulArgs& a, int64_t m, int
 
 hipError_t launch_block_matmul_few(const MatmulArgs& a, int dtype, int shape, hipStream_t st);
 hipError_t launch_block_matmul_bf16(const MatmulArgs& a, int shape, hipStream_t st);
+hipError_t launch_block_matmul_bf16_fast(const MatmulArgs& a, int shape, hipStream_t st);
 hipError_t launch_block_matmul_f32(const MatmulArgs& a, int shape, hipStream_t st);
 hipError_t launch_block_matmul_f32_fast(const MatmulArgs& a, int shape, hipStream_t st);
 hipError_t launch_block_matmul_codes(const MatmulArgs& a, int shape, hipStream_t st);

@@ -1,0 +1,42 @@
+"""What a product's arguments lead to on the host: the instruction that sums, the tiles."""
+
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2504_02921_amd import binding as hb
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+pytestmark = pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+
+
+@pytest.fixture(scope="module")
+def plans(tmp_path_factory):
+    """(kind, gate, rows, rows of w, columns) of many products -> (8-bit instruction, shape, its rows, shape of the rest, tiles, tiles of the rest, shapes) of each."""
+    exe, csrc = str(tmp_path_factory.mktemp("plans") / "plans"), os.path.join(ROOT, "paper_2504_02921_amd", "csrc")
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-I" + os.path.join(ROOT, "include"), "-I" + csrc,
+                        os.path.join(ROOT, "tests", "block8_plan_driver.cpp"), os.path.join(csrc, "hr_block8_host.cpp"), "-o", exe], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    env = dict(os.environ)
+    env.pop("LD_PRELOAD", None)          # the sanitizer runtime must come first in the link order
+
+    def run(products):
+        lines = "".join(f"{int(kind.startswith('block8'))} {hb.HR_BF16 if kind.startswith('bf16') else hb.HR_F32} {int(kind.endswith('fast'))} {gate} {m} {n} {k}\n"
+                        for kind, gate, m, n, k in products)
+        r = subprocess.run([exe], input=lines, capture_output=True, text=True, env=env)
+        assert r.returncode == 0, (r.stdout + r.stderr)[-2000:]
+        got = [tuple(int(x) for x in line.split()) for line in r.stdout.splitlines()]
+        assert len(got) == len(products)
+        return got
+    return run
+
+
+def test_only_callers_that_ask_for_speed_get_the_8_bit_sums(plans):
+    sizes = [(gate, m, n, k) for gate in (0, 1, 2) for m in (1, 20, 300, 12800) for n in (256, 6144) for k in (128, 4100)]
+    for kind in ("bf16", "f32", "block8"):
+        assert all(p[0] == 0 for p in plans([(kind, *s) for s in sizes])), kind
+        assert all(p[0] == 1 for p in plans([(kind + " fast", *s) for s in sizes])), kind
+    # bf16 results take the tiles of fp32 ones
+    assert plans([("bf16", *s) for s in sizes]) == plans([("f32", *s) for s in sizes])
