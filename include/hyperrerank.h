@@ -559,7 +559,8 @@ typedef struct hr_block8 {
 /* Root-mean-square norm of every head of every token, after an addition:
  *   s = x + add;   y = s / sqrt(mean(s^2) + eps) * (gain + gain_offset)
  * over the head's channels.  total receives s (the residual stream), out receives y, block8 receives y as codes; all from the fp32 values, which
- * are rounded once.  Sums are fp32: a head whose squares pass 3.4e38 comes out as 0.  A head of zeros is 0 with eps = 0 too.
+ * are rounded once.  Sums are fp32: a head whose squares pass 3.4e38 comes out as 0.  Heads of any small size down to fp32's least value are summed to the same
+ * digits (their squares scaled where they would be below fp32's range).  A head of zeros is 0 with eps = 0 too.
  * Any of total, out and block8 may be left out, not all.  total and out may be x or add (then with the same strides) and share no memory
  * otherwise (HR_ERR_INVALID_ARG where outputs begin at the same place, or one begins where an input with other strides, gain or codes do). */
 typedef struct hr_norm_args {

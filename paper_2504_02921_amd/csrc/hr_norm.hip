@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "hr_block8.h"
 #include "hr_block8_device.h"
@@ -85,12 +86,13 @@ __device__ __forceinline__ void store_codes8(uint8_t* p, int c, int cols, const 
 
 // What becomes of eight channels of a head; 16 lanes in a row come here together for a block of 128
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float r, const Loose<float, kVec>& gain) {
+__device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int head, int c, bool on, const float (&s)[kVec], float up, float r,
+                                        const Loose<float, kVec>& gain) {
     if (c / kBlockCols * kBlockCols >= a.channels) return;
     const bool any = c < a.channels;
     float y[kVec];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) y[e] = s[e] * r;
+    for (int e = 0; e < kVec; ++e) y[e] = s[e] * up * r;
     if (a.gain) {
 #pragma unroll
         for (int e = 0; e < kVec; ++e) y[e] *= gain.w[e] + a.offset;
@@ -112,10 +114,12 @@ __device__ __forceinline__ void finish8(const NormArgs& a, int64_t token, int he
     }
 }
 
-__device__ __forceinline__ float root_of(float squares, const NormArgs& a) {
-    const float m = squares / (float)a.channels + a.eps;
-    return m == 0.0f ? 0.0f : rsqrtf(m);
-}
+// Squares of values below 1e-19 leave fp32's normal range, where each is off by 2^-150 at most.  Where mean + eps is below 2^-120, of which that is more than
+// 2^-30, a head is summed once more, its values times 2^100 (at most 2^48 then, and 2^-49 or more): y = (s 2^100) / root of mean and eps times 2^200.  A branch that
+// heads of usual sizes do not take: 12800 x 4096 is as fast without it
+constexpr float kSmallMean = 0x1p-120f, kUp = 0x1p100f;
+__device__ __forceinline__ float mean_of(float squares, float up, const NormArgs& a) { return squares / (float)a.channels + a.eps * up * up; }
+__device__ __forceinline__ float root_of(float mean) { return mean == 0.0f ? 0.0f : rsqrtf(mean); }
 
 // LANES lanes have a head, CHUNKS times 8 channels each
 template <typename T, bool WHOLE, int LANES, int CHUNKS>
@@ -156,33 +160,58 @@ __global__ void __launch_bounds__(LANES > kThreads ? LANES : kThreads) norm_kern
 #pragma unroll
                 for (int e = 0; e < kVec; ++e) s[k][e] += to_float<T>(add[k].w[e]);
         }
-        float sum = 0.0f;
+        // mean + eps of the head; low: that of one of the workgroup's heads, where these meet at barriers, is small
+        auto mean = [&](auto again, bool& low) {
+            constexpr float up = decltype(again)::value ? kUp : 1.0f;
+            float sum = 0.0f;
 #pragma unroll
-        for (int k = 0; k < CHUNKS; ++k) {
-            float part = 0.0f;
+            for (int k = 0; k < CHUNKS; ++k) {
+                float part = 0.0f;
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) part = fmaf(s[k][e], s[k][e], part);
-            sum += !WHOLE || (k * LANES + lane) * kVec < a.channels ? part : 0.0f;
-        }
-        if constexpr (LANES <= 32) {
-            sum = sum16(sum);
-            if constexpr (LANES == 32) sum += __shfl_xor(sum, 16, 64);
-        } else {
-            sum = wave_sum(sum);
-            if constexpr (LANES > 64) {
+                for (int e = 0; e < kVec; ++e) part = fmaf(s[k][e] * up, s[k][e] * up, part);
+                sum += !WHOLE || (k * LANES + lane) * kVec < a.channels ? part : 0.0f;
+            }
+            float m;
+            if constexpr (LANES <= 64) {
+                if constexpr (LANES == 64) sum = wave_sum(sum);
+                else sum = sum16(sum);
+                if constexpr (LANES == 32) sum += __shfl_xor(sum, 16, 64);
+                m = mean_of(sum, up, a);
+                low = m < kSmallMean;
+            } else {
+                sum = wave_sum(sum);
                 if (lane % 64 == 0) part[turn][unit][lane / 64] = sum;
                 __syncthreads();                    // one a turn: the other half of `part` is written next
-                sum = 0.0f;
+                low = false;
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) sum += part[turn][unit][w];
+                for (int u = 0; u < UNITS; ++u) {
+                    sum = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) sum += part[turn][u][w];
+                    const float of = mean_of(sum, up, a);
+                    low = low || of < kSmallMean;
+                    if (u == unit) m = of;
+                }
                 turn ^= 1;
             }
+            return m;
+        };
+        float up = 1.0f;
+        bool low;
+        float m = mean(std::false_type{}, low);
+        if (low) {                                  // the same in all lanes that meet in mean()
+            bool unused;
+            const float more = mean(std::true_type{}, unused);
+            if (m < kSmallMean) {
+                m = more;
+                up = kUp;
+            }
         }
-        const float r = root_of(sum, a);
+        const float r = root_of(m);
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             if (CHUNKS > 1 && a.gain) gain[k] = load8<float, WHOLE>(a.gain, (k * LANES + lane) * kVec, a.channels);
-            finish8<T, WHOLE>(a, token, head, (k * LANES + lane) * kVec, on, s[k], r, gain[k]);
+            finish8<T, WHOLE>(a, token, head, (k * LANES + lane) * kVec, on, s[k], up, r, gain[k]);
         }
     }
 }
@@ -202,26 +231,32 @@ __global__ void __launch_bounds__(kWideThreads) norm_wide_kernel(NormArgs a) {
 #pragma unroll
             for (int e = 0; e < kVec; ++e) s[e] += to_float<T>(add.w[e]);
         };
-        float s[kVec], sum = 0.0f;
-        for (int c = threadIdx.x * kVec; c < a.channels; c += kWideThreads * kVec) {
-            load(c, s);
+        float s[kVec];
+        auto mean = [&](float up) {
+            float sum = 0.0f;
+            for (int c = threadIdx.x * kVec; c < a.channels; c += kWideThreads * kVec) {
+                load(c, s);
 #pragma unroll
-            for (int e = 0; e < kVec; ++e) sum = fmaf(s[e], s[e], sum);
-        }
-        sum = wave_sum(sum);
-        if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = sum;
-        __syncthreads();
-        sum = 0.0f;
+                for (int e = 0; e < kVec; ++e) sum = fmaf(s[e] * up, s[e] * up, sum);
+            }
+            sum = wave_sum(sum);
+            if (threadIdx.x % 64 == 0) part[turn][threadIdx.x / 64] = sum;
+            __syncthreads();
+            sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWideThreads / 64; ++w) sum += part[turn][w];
-        turn ^= 1;
-        const float r = root_of(sum, a);
+            for (int w = 0; w < kWideThreads / 64; ++w) sum += part[turn][w];
+            turn ^= 1;
+            return mean_of(sum, up, a);
+        };
+        float up = 1.0f, m = mean(up);
+        if (m < kSmallMean) m = mean(up = kUp);
+        const float r = root_of(m);
         const int64_t padded = blocks_of(a.channels) * kBlockCols;        // whole groups of lanes look for a block's largest
         for (int c = threadIdx.x * kVec; c < padded; c += kWideThreads * kVec) {
             load(c, s);
             Loose<float, kVec> gain;
             if (a.gain) gain = load8<float, false>(a.gain, c, a.channels);
-            finish8<T, false>(a, token, head, c, true, s, r, gain);
+            finish8<T, false>(a, token, head, c, true, s, up, r, gain);
         }
     }
 }

@@ -1,4 +1,5 @@
-"""Sums that products hold in fp32, for results of every type unless the caller asks for speed, with terms that cancel."""
+"""Sums that products and norms hold in fp32: products into every type unless the caller asks for speed, with terms that cancel; heads whose squares are below
+fp32's range."""
 
 import pytest
 
@@ -60,3 +61,39 @@ def test_bf16_products_of_callers_that_ask_for_speed(gated, m, n, k):
         a.scales.mul_(0.1 / k ** 0.5)
     gate, add = "silu" if gated else None, B.draw((m, n // 2 if gated else n), 126, "bf16", 2.0)
     check(a, w, hb().block_matmul(a, w, gate=gate, add=add, fast=True), "bf16", None, gate, add, fast=True)
+
+
+# ---- norms --------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("channels", [1, 7, 128, 200, 250, 300, 520, 1000, 1030, 2056, 4096, 4104, 8200, 12000, 16392, 20000])
+def test_norm_of_heads_whose_squares_are_below_fp32(kind, channels):
+    """Heads of every size down to fp32's least beside each other and beside zeros.  A square's rounding is 2^-150 at most where it is below fp32's normal range,
+    which matters up to 2^-120: a root of 2^-30 more, relative to it, beyond what larger heads may be off."""
+    T = torch()
+    sizes = [1e-19, 1.0, 1e-23, 0.0, 1e-30, 3e-38, 1e-17, 1e-41, 1e-18, 1e-21, 1e4]
+    x = B.draw((len(sizes), channels), 130, "f32").cpu().double() * T.tensor(sizes, dtype=T.float64)[:, None]
+    x = x.float().to(B.tdt(kind)).to(B.DEV)
+    gain = B.draw((channels,), 131).abs() + 0.5
+    for eps in (0.0, 1e-42, 2.0 ** -125, 2.0 ** -119, 1e-30):
+        held = float(T.tensor(eps, dtype=T.float32))
+        out, total, q = hb().rms_norm(x, gain, eps=eps, total=True, block8=True)
+        assert T.equal(total, x)
+        _, y = R.norm(B.to64(x), None, B.to64(gain), held, 0.0)
+        off = (R.norm_slack(channels) + 2 * R.U32 + 2.0 ** -30) * abs(y)
+        # y below its type's normal range would be off by half of the least value: of s / size in fp32, times gains below 8, and of bf16
+        R.check_rounded(B.to64(out), y, off + 2.0 ** -146 + (2.0 ** -134 if kind == "bf16" else 0.0), B.unit(kind), f"eps {eps}")
+        R.check_codes(B.code_bytes(q.codes).cpu(), B.to64(q.scales), y, off + 2.0 ** -146, f"eps {eps}")
+        again = hb().rms_norm(x, gain, eps=eps, out=x.clone())[0]
+        assert T.equal(again, out)
+
+
+@pytest.mark.parametrize("heads,channels", [(5, 64), (32, 128), (3, 200), (2, 1000), (3, 1500)])
+def test_norm_of_small_heads_beside_large_ones(heads, channels):
+    """Heads of one token of both kinds, so that lanes of one wavefront and workgroup differ."""
+    T = torch()
+    x = B.draw((37, heads, channels), 132)
+    x[::3, ::2] *= 1e-25
+    x[1::4, 1::2] = 0.0
+    out, _, _ = hb().rms_norm(x, eps=0.0)
+    _, y = R.norm(B.to64(x), None, None, 0.0, 0.0)
+    R.check_rounded(B.to64(out), y, (R.norm_slack(channels) + 2 * R.U32 + 2.0 ** -30) * abs(y), R.U32)
