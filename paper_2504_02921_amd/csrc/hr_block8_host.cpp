@@ -234,7 +234,8 @@ int64_t matmul_tiles(int shape, const MatmulArgs& a, int64_t rows) {
     return (rows + c.bm - 1) / c.bm * ((a.N + wide - 1) / wide);
 }
 
-// The shape that costs least.  Rows that fill whole rounds of the largest tiles may go ahead of the others, which are then tiled for themselves
+// The shape that costs least.  Rows that fill whole rounds of the largest tiles may go ahead of the others, which are then tiled for themselves where a launch can have
+// that many tiles (matmul_check counts those of the first launch)
 MatmulPlan matmul_plan(const MatmulArgs& a) {
     const bool codes = a.codes != nullptr, gate = a.half > 0;
     const int results = (codes ? (gate ? 4 : 2) : 0) + (a.eight ? 0 : 1);
@@ -258,7 +259,8 @@ MatmulPlan matmul_plan(const MatmulArgs& a) {
     const int64_t rows = rounds * kCus / columns * large.bm;
     if (rows > 0 && rows < a.M) {
         const int rest = best(a.M - rows, rest_cost);
-        if (rest != MM_256x256 && cost_of(MM_256x256, a, rows, results) + rest_cost < 0.98f * cost) p = MatmulPlan{MM_256x256, rows, rest};
+        if (rest != MM_256x256 && matmul_tiles(rest, a, a.M - rows) <= kMaxWideWorkgroups && cost_of(MM_256x256, a, rows, results) + rest_cost < 0.98f * cost)
+            p = MatmulPlan{MM_256x256, rows, rest};
     }
     return p;
 }

@@ -1,6 +1,8 @@
 """What a product's arguments lead to on the host: the instruction that sums, the tiles."""
 
+import math
 import os
+import random
 import shutil
 import subprocess
 
@@ -40,3 +42,16 @@ def test_only_callers_that_ask_for_speed_get_the_8_bit_sums(plans):
         assert all(p[0] == 1 for p in plans([(kind + " fast", *s) for s in sizes])), kind
     # bf16 results take the tiles of fp32 ones
     assert plans([("bf16", *s) for s in sizes]) == plans([("f32", *s) for s in sizes])
+
+
+def test_neither_launch_of_a_product_has_more_tiles_than_a_launch_can(plans):
+    """Rows behind the largest tiles are a second launch, with tiles of its own: a product whose first launch is accepted has no second one of too many."""
+    most = (1 << 22) - 512
+    sizes = [("bf16 fast", 0, 513, 181444029, 64), ("f32", 0, 513, 186746523, 1398), ("bf16", 0, 257, 372375436, 1834), ("f32 fast", 1, 518, 184733696, 15),
+             ("f32", 0, 257, 836829046, 3934685), ("bf16 fast", 1, 513, 179889408, 6)]
+    rng = random.Random(4)
+    for _ in range(20000):
+        gate, n = rng.choice((0, 1)), int(math.exp(rng.uniform(math.log(1 << 20), math.log(1 << 30))))
+        sizes.append((rng.choice(("bf16", "f32", "f32 fast")), gate, rng.choice((257, 300, 513, 521, 1000, 3000)), max(n // 256 * 256, 256) if gate else n, rng.choice((16, 128, 700, 4000))))
+    for size, (_, shape, rows, rest, tiles, rest_tiles, _) in zip(sizes, plans(sizes)):
+        assert tiles > most or rest_tiles <= most, (size, shape, rows, rest, tiles, rest_tiles)
