@@ -8,6 +8,8 @@ import subprocess
 
 import pytest
 
+from block8_edges import EDGES
+from block8_shapes import SHAPES
 from paper_2504_02921_amd import binding as hb
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -55,3 +57,36 @@ def test_neither_launch_of_a_product_has_more_tiles_than_a_launch_can(plans):
         sizes.append((rng.choice(("bf16", "f32", "f32 fast")), gate, rng.choice((257, 300, 513, 521, 1000, 3000)), max(n // 256 * 256, 256) if gate else n, rng.choice((16, 128, 700, 4000))))
     for size, (_, shape, rows, rest, tiles, rest_tiles, _) in zip(sizes, plans(sizes)):
         assert tiles > most or rest_tiles <= most, (size, shape, rows, rest, tiles, rest_tiles)
+
+
+# Shapes in the host's order: groups along k, and workgroups at once where they take several tiles (else 0)
+GROUPS = [8, 8, 8, 8, 4, 2, 1, 2, 1, 2, 1, 1, 2, 1, 1, 4, 2, 1, 1]
+AT_ONCE = [0] * 11 + [512, 0, 0, 256] + [0] * 4
+FEW = 2          # the first shapes have one kernel for both instructions
+
+
+def classes(size, plan):
+    """What the loop over k of a product's launches goes by: (kind, gate, shape, one, two, an odd (3) or even (4) number of turns, a second tile of a workgroup)."""
+    kind, gate, k = size[0], size[1], size[4]
+    _, shape, _, rest, tiles, rest_tiles, shapes = plan
+    assert shapes == len(GROUPS) == len(AT_ONCE)
+    for s, n in ((shape, tiles), (rest, rest_tiles)):
+        if s >= 0:
+            turns = -(-(-(-k // 128)) // GROUPS[s])
+            yield "f32" if s < FEW else kind.replace("bf16", "f32"), gate, s, turns if turns < 3 else 3 + (turns % 2 == 0), 0 < AT_ONCE[s] < n
+
+
+def test_every_way_through_the_loop_over_k_that_a_product_takes_is_tested(plans):
+    """With columns that end inside 16, whose last codes are set to zero in LDS: the sizes that the GPU tests run have every class that sizes of all kinds do."""
+    rng = random.Random(6)
+    size = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi))))      # noqa: E731
+    drawn = []
+    for kind in ("f32", "f32 fast", "block8", "block8 fast"):
+        for gate in (0, 1):
+            for _ in range(5000):
+                n, k = size(16, 30000), size(1, 5000)
+                drawn.append((kind, gate, size(1, 30000), max(n // 256 * 256, 256) if gate else n, k + (k % 16 == 0)))
+    sizes = [s for s in SHAPES + EDGES if s[4] % 16]
+    taken = {c for s, p in zip(drawn, plans(drawn)) for c in classes(s, p)}
+    tested = {c for s, p in zip(sizes, plans(sizes)) for c in classes(s, p)}
+    assert taken <= tested, sorted(taken - tested)
