@@ -543,7 +543,8 @@ int hr_pair_attention(const hr_pool* pool, const hr_pair_tables* tables, const h
 /* A matrix in 8 bits: E4M3 codes and fp32 scales, value = decode(code) * scale.  One scale for 128 consecutive columns (the last block has what
  * is left) of block_rows rows: 1 for activations, 128 for weights.
  * Codes made here: scale = amax / 448 over the block's finite values, at least 2^-126 (1 if amax = 0); code = the E4M3 value nearest to
- * x * (1 / scale), ties to the even code; a value that is not finite becomes a code NaN (0x7f or 0xff). */
+ * x * (1 / scale), ties to the even code (x / scale gives its neighbour now and then, where that lies within 2^-23 of a tie); a value that is not finite becomes
+ * a code NaN (0x7f or 0xff). */
 #define HR_BLOCK_COLS 128
 typedef struct hr_block8 {
     void* codes;            /* device, 16-byte aligned */

@@ -177,8 +177,9 @@ namespace {
 // What a shape's launch takes in us: start + turns * first with a tile a CU at most, turns being its blocks of k by its groups along k; where a CU holds
 // two workgroups, start + turns * pair with up to two; and turns * more + again for each further round of as many (the last of two may be half a round).
 // By results: out with the 8-bit instruction (fitted into bf16) and with halves (into fp32), codes with either, codes of a gate with either.  Fitted to 5872 launches of 1 to 6000 rows with
-// weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory: what it picks takes 0.3 % more than the fastest shape on average, 17 % at
-// most.  The kernels without LDS: at 16 rows.
+// weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory, gates among them for codes only.  Over 21480 launches of other sizes, gated ones of
+// every kind among them, what it picks takes 1.2 % more than the fastest shape in the mean and 30 % at most, with the 8-bit instruction 39 %, gated 78 % (17 to 250 rows, few
+// columns).  The kernels without LDS: at 16 rows, with a gate by factors that were not fitted.
 struct Times { float start, first, pair, more, again; };
 struct Cost { int bm, bn, groups, held; Times t[6]; };
 constexpr Cost kCost[MM_SHAPES] = {

@@ -9,7 +9,7 @@
 // y[m][n] = sum over blocks b of a.scale[m][b] w.scale[n / 128][b] sum over k in b of a[m][k] w[n][k].  A row of y reads all of w once, so its bytes at the
 // memory's rate are what a call cannot do without; 16 x 16 or 16 x 32 tiles are the most workgroups that still read whole lines of w, and eight
 // wavefronts with two blocks each under way ask for up to 64 KB a compute unit at once.  1 x 4096 x 4096 (17 MB): 5.7 us, 2.9 TB/s, of which 2.3 to 3.2 are the
-// launch, the first answer from memory and the join; 1 x 4096 x 14336 (59 MB) 11.8 us, 5.0 TB/s.  Rows share w's lines in the L2s only: from a dozen rows on, and
+// launch, the first answer from memory and the join; 1 x 4096 x 14336 (59 MB) 11.8 us, 5.0 TB/s.  Rows share w's lines in the L2s only: from a dozen or two rows on, and
 // for weights of more than 256 tiles, the tiles through LDS are faster.
 #include <hip/hip_runtime.h>
 

@@ -7,9 +7,9 @@
 // 8-bit instruction or halves: of random normal codes the 8-bit instruction reaches 3.4 PFLOP/s from registers with the fused multiply-adds (4.1 without),
 // halves 1.97.  But it adds groups of eight neighbouring products after cutting each at 2^-13 of the group's largest, which moves a sum by 1.4e-5 of the row's rms; sums of halves
 // are off by 1e-8.  Behind bf16's rounding of a typical value that is little, but where large terms cancel it is more than what is left.  So every kind of result
-// takes halves, unless the caller asks for speed (12800 x 4096 x 14336 into bf16 1180 us, with the 8-bit instruction 700).
+// takes halves, unless the caller asks for speed (12800 x 4096 x 14336 into bf16 1180 to 1240 us, with the 8-bit instruction 700 to 730).
 //
-// What bounds it: 8192 x 8192 x 8192 into bf16 by the 8-bit instruction takes 467 us (2.35 PFLOP/s; a library product of the same codes with a single scale 371), with the matrix pipe 65 %
+// What bounds it: 8192 x 8192 x 8192 into bf16 by the 8-bit instruction takes 467 us (2.35 PFLOP/s; on another card 493; a library product of the same codes with a single scale 371), with the matrix pipe 65 %
 // busy at 1.69 GHz; the same without any load in the loop is 70 % at 1.79.  The clock is what power allows: the products themselves draw most of it (zeros run
 // 1.3 times as fast as normal deviates), the fused multiply-adds of the blocks' scales the next part.  Halves: 820 us into bf16 (1.34 PFLOP/s), 843 into
 // fp32 (a library product of matrices in half 734).

@@ -5,8 +5,8 @@
 // swaps away), and its codes leave in 8 bytes a lane.  All values and sums are fp32; out and total are rounded once each.
 //
 // What bounds it is those bytes, if everything is requested before anything is waited for and addresses are scalar: bf16, sums and codes written, 12800 x 4096
-// 70 us (5.3 TB/s; a copy of 4 GiB reaches 4.8 read and written), 12800 x 896 15.4 (5.2), 25600 x 32 heads of 128 76 (5.5), fp32 3000 x 4096 39 (5.0); of
-// 65 x 896 (3.0 us) the launch and one way to memory and back.  bf16 rows that begin at odd elements: 8000 x 5003 93 us (3.0).
+// 69 us (5.3 TB/s; a copy of 4 GiB reaches 4.8 read and written), 12800 x 896 15.4 (5.2), 25600 x 32 heads of 128 77 (5.5), fp32 3000 x 4096 39 (5.0); of
+// 65 x 896 (3.1 us) the launch and one way to memory and back.  bf16 rows that begin at odd elements: 8000 x 5003 93 us (3.0).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
