@@ -179,7 +179,7 @@ namespace {
 // By results: out with the 8-bit instruction (fitted into bf16) and with halves (into fp32), codes with either, codes of a gate with either.  Fitted to 5872 launches of 1 to 6000 rows with
 // weights of 896 x 896 to 28672 x 4096 and 4096 x 14336, operands from memory, gates among them for codes only.  Over 21480 launches of other sizes, gated ones of
 // every kind among them, what it picks takes 1.2 % more than the fastest shape in the mean and 30 % at most, with the 8-bit instruction 39 %, gated 78 % (17 to 250 rows, few
-// columns).  The kernels without LDS: at 16 rows, with a gate by factors that were not fitted.
+// columns).  The kernels without LDS: at 16 rows, with a gate by factors set by hand.
 struct Times { float start, first, pair, more, again; };
 struct Cost { int bm, bn, groups, held; Times t[6]; };
 constexpr Cost kCost[MM_SHAPES] = {
